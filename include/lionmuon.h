@@ -409,6 +409,151 @@ lm_status lm_profile_enable(lm_state* s, int on);
  * and, if reset != 0, clear them.  Errors: LM_ERR_INVALID_ARG, LM_ERR_CUDA. */
 lm_status lm_profile_read(lm_state* s, lm_profile* out, int reset);
 
+/* ---------------------------------------------------------------------------
+ * Training-step operators next to the optimizer: what produces the gradients
+ * lm_step takes.  The paper leaves the model to its user; these calls have no
+ * counterpart in it.
+ *
+ * They are stateless: everything a call reads or writes is in its arguments,
+ * it allocates nothing, never synchronises, and may be captured into a CUDA
+ * graph.  Matrices may have any row pitch and any element alignment (the
+ * 16-byte rule of the optimizer's tensors does not apply; aligned rows are
+ * faster); pointers to host memory or to another device's memory are refused
+ * with LM_ERR_INVALID_ARG.  An output must not overlap an input or another
+ * output except where a call says so.  rows == 0 or cols == 0 is accepted
+ * (sums over nothing are zero).  All sums, softmax statistics and norms are
+ * held in fp32; a result is rounded once, to its own type.
+ * ------------------------------------------------------------------------- */
+
+/* rows x cols elements, row r starting ld elements after row r - 1
+ * (ld >= cols; ld is not read when rows <= 1). */
+typedef struct {
+  void* data;
+  int64_t rows;
+  int64_t cols;
+  int64_t ld;
+  lm_dtype dtype;
+} lm_matrix;
+
+/* Log probabilities of given tokens.  For each row z of logits (N x V):
+ *   lse = log sum_j exp z_j,   log p_j = z_j - lse
+ *   logp = log p_y for the row's target y, 0 for a negative target (no
+ *          target), NaN for a target >= V
+ *   entropy = - sum_j p_j log p_j
+ *   top_index, top_logp (N x top_k, dense): the top_k most likely tokens, most
+ *          likely first, equal logits in index order, and their log p
+ * -inf masks a token: p = 0, nothing is added to the entropy, and it is never
+ * an alternative (places left over hold index -1 and -inf).  A row whose
+ * logits are all -inf has lse = -inf, logp = -inf (0 without a target),
+ * entropy = 0 and a zero gradient.  A row that holds NaN or +inf has NaN in
+ * every floating output and -1 in its indices.
+ *
+ * Gradient, for weights g of the loss sum_rows (g_logp logp + g_entropy entropy
+ * + g_lse lse):
+ *   dlogits_j = p_j (g_lse - g_logp - g_entropy (log p_j + entropy)) + g_logp [j = y]
+ * where g_logp counts as 0 in a row without a target, and p_j = 0 gives 0.
+ * dlogits has the shape and dtype of logits and may be logits itself (same
+ * data and ld). */
+typedef struct {
+  lm_matrix logits;
+  const int64_t* targets;   /* N, device; NULL only when neither logp nor g_logp is given */
+  int top_k;                /* 0 .. 32, at most V */
+  float* logp;              /* N floats each, device, or NULL */
+  float* entropy;
+  float* lse;
+  float* top_logp;          /* N x top_k, NULL iff top_k == 0 */
+  int64_t* top_index;
+  const float* g_logp;      /* N floats each, device, or NULL for zero */
+  const float* g_entropy;
+  const float* g_lse;
+  lm_matrix dlogits;        /* data NULL: no gradient */
+} lm_token_logprob_args;
+
+/* Forward (logp, entropy, lse, top alternatives: those that are not NULL) and,
+ * when dlogits.data is not NULL, the gradient in the same call: a loss whose
+ * weights g are known beforehand, such as a mean cross entropy, needs no
+ * second call.  Errors: LM_ERR_INVALID_ARG, LM_ERR_DTYPE, LM_ERR_ALIGN (a
+ * pointer is not aligned to its element), LM_ERR_UNSUPPORTED, LM_ERR_CUDA. */
+lm_status lm_token_logprob(const lm_token_logprob_args* a, void* cuda_stream);
+
+/* The gradient alone, for weights known only after the forward call: lse, and
+ * entropy where g_entropy is not NULL, are read, as lm_token_logprob wrote
+ * them; logp, top_logp, top_index and top_k are ignored.  Errors as above. */
+lm_status lm_token_logprob_grad(const lm_token_logprob_args* a, void* cuda_stream);
+
+/* 8-bit checkpoint of a rows x cols matrix: one byte an element (row pitch
+ * ld_codes bytes, a multiple of 16, codes 16-byte aligned) and one scale for
+ * each row's group of LM_CODE_GROUP channels (the last group may be short).
+ * scales is laid out group by group: the scale of row r, group k is
+ * scales[k * ld_scales + r], ld_scales >= rows.
+ * A scale is the least power of two s with max |x| <= limit * s over its group
+ * (limit 127 for LM_CODE_I8, 448 for LM_CODE_E4M3), at least 2^-126 (2^-117);
+ * a code is x / s rounded to nearest even, and stands for code * s.  Scales
+ * are powers of two so that code * s is a bf16 number: the tensor cores take
+ * a checkpoint without a second rounding.  A group that holds a NaN or an
+ * infinity has scale NaN and reads back as NaN.  A code that would stand for 2^128
+ * is lowered to the one below it (63 under a scale of 2^122, 240 under 2^120). */
+#define LM_CODE_GROUP 128
+typedef enum { LM_CODE_I8 = 0, LM_CODE_E4M3 = 1 } lm_code_format;
+typedef struct {
+  void* codes;
+  float* scales;
+  int64_t rows;
+  int64_t cols;
+  int64_t ld_codes;
+  int64_t ld_scales;
+  lm_code_format format;
+} lm_checkpoint8;
+
+/* c <- x, and x <- c (x in bf16 or fp32; a checkpoint's values are bf16
+ * numbers, so both are exact).  Errors: LM_ERR_INVALID_ARG, LM_ERR_DTYPE,
+ * LM_ERR_ALIGN, LM_ERR_UNSUPPORTED, LM_ERR_CUDA. */
+lm_status lm_checkpoint8_pack(const lm_matrix* x, const lm_checkpoint8* c, void* cuda_stream);
+lm_status lm_checkpoint8_unpack(const lm_checkpoint8* c, const lm_matrix* x, void* cuda_stream);
+
+/* Root-mean-square norm of T x C rows, with the residual's addition:
+ *   h = x + residual (x where residual is NULL)
+ *   rstd = 1 / sqrt(mean_c h^2 + eps),   y = h rstd weight
+ * h and y have the dtype of x and may be NULL (h only with residual); h may be
+ * x or residual itself.  weight: C elements (1 x C or C x 1, bf16 or fp32),
+ * NULL for ones.  rstd: T floats or NULL.  kept: NULL, or a T x C checkpoint
+ * that receives y in 8 bits (from y before its rounding to x's dtype).  The
+ * norm is taken of h before its rounding.  eps >= 0, finite.
+ * Errors: LM_ERR_INVALID_ARG, LM_ERR_DTYPE, LM_ERR_ALIGN, LM_ERR_UNSUPPORTED,
+ * LM_ERR_CUDA. */
+lm_status lm_rmsnorm(const lm_matrix* x, const lm_matrix* residual, const lm_tensor* weight, double eps,
+                     const lm_matrix* h, const lm_matrix* y, float* rstd, const lm_checkpoint8* kept,
+                     void* cuda_stream);
+
+/* Its gradient.  With xh = h rstd:
+ *   dx = dh + rstd (weight dy - xh mean_c(weight dy xh)),   dweight = sum_rows dy xh
+ * h comes either from the stored matrix h or from its 8-bit checkpoint h8
+ * (exactly one of them is not NULL); dx is the gradient of x and of residual
+ * alike.  dh: the gradient that reaches h past the norm, or NULL.  dx (dtype of
+ * dy; may be dy or dh itself) and dweight (C elements, bf16 or fp32) may be
+ * NULL, not both.  dweight is summed in a fixed order: the same inputs give
+ * the same bits.  workspace: lm_rmsnorm_grad_workspace(T, C) bytes of device
+ * memory, 16-byte aligned, free again when the work is done (not read when
+ * dweight is NULL).
+ * Errors: LM_ERR_INVALID_ARG (also a workspace that is too small),
+ * LM_ERR_DTYPE, LM_ERR_ALIGN, LM_ERR_UNSUPPORTED, LM_ERR_CUDA. */
+size_t lm_rmsnorm_grad_workspace(int64_t rows, int64_t cols);
+lm_status lm_rmsnorm_grad(const lm_matrix* dy, const lm_matrix* h, const lm_checkpoint8* h8, const float* rstd,
+                          const lm_tensor* weight, const lm_matrix* dh, const lm_matrix* dx, const lm_tensor* dweight,
+                          void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Weight gradient of a linear layer y = x W^T whose input was kept in 8 bits:
+ *   dw (+)= dy^T x      dw: out x in, dy: T x out, x: T x in
+ * dw is bf16 or fp32, dy bf16 or fp32 (independently); accumulate != 0 adds to
+ * dw, else dw is overwritten.  The sum over tokens is taken in a fixed order.
+ * workspace: lm_linear_wgrad8_workspace(...) bytes of device memory, 256-byte
+ * aligned.
+ * Errors: LM_ERR_INVALID_ARG (also a workspace that is too small),
+ * LM_ERR_DTYPE, LM_ERR_ALIGN, LM_ERR_UNSUPPORTED, LM_ERR_CUDA. */
+size_t lm_linear_wgrad8_workspace(const lm_matrix* dy, const lm_checkpoint8* x, const lm_matrix* dw);
+lm_status lm_linear_wgrad8(const lm_matrix* dy, const lm_checkpoint8* x, const lm_matrix* dw, int accumulate,
+                           void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

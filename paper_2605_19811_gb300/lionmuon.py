@@ -31,7 +31,10 @@ EXPORTED = ("lm_config_default", "lm_create", "lm_step", "lm_set_lr", "lm_msign_
             "lm_kernel_launch_count", "lm_profile_enable", "lm_profile_read",
             "lm_msign_ns_noalloc", "lm_probe_bounded_wait", "lm_msign_ns_coeffs",
             "lm_set_adamw_lr", "lm_get_second_moment", "lm_set_second_moment", "lm_get_selection",
-            "lm_msign_ns_noalloc_status", "lm_shard_owners", "lm_config_size")
+            "lm_msign_ns_noalloc_status", "lm_shard_owners", "lm_config_size",
+            "lm_token_logprob", "lm_token_logprob_grad", "lm_checkpoint8_pack", "lm_checkpoint8_unpack",
+            "lm_rmsnorm", "lm_rmsnorm_grad", "lm_rmsnorm_grad_workspace",
+            "lm_linear_wgrad8", "lm_linear_wgrad8_workspace")
 
 KERNEL_FAMILIES = ("lion", "momentum_norm", "ns_gram", "ns_poly", "ns_apply", "finalize", "other", "adamw",
                    "srank")
@@ -61,6 +64,24 @@ class LmConfig(ctypes.Structure):
 
 class LmProfile(ctypes.Structure):
     _fields_ = [("ms", ctypes.c_double * 9), ("launches", ctypes.c_uint64 * 9)]
+
+
+class LmMatrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("ld", ctypes.c_int64), ("dtype", ctypes.c_int)]
+
+
+class LmCheckpoint8(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64), ("ld_codes", ctypes.c_int64), ("ld_scales", ctypes.c_int64),
+                ("format", ctypes.c_int)]
+
+
+class LmTokenLogprobArgs(ctypes.Structure):
+    _fields_ = [("logits", LmMatrix), ("targets", ctypes.c_void_p), ("top_k", ctypes.c_int),
+                ("logp", ctypes.c_void_p), ("entropy", ctypes.c_void_p), ("lse", ctypes.c_void_p),
+                ("top_logp", ctypes.c_void_p), ("top_index", ctypes.c_void_p), ("g_logp", ctypes.c_void_p),
+                ("g_entropy", ctypes.c_void_p), ("g_lse", ctypes.c_void_p), ("dlogits", LmMatrix)]
 
 
 class LionMuonError(RuntimeError):
@@ -142,6 +163,26 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.lm_profile_enable.restype = c_int
     lib.lm_profile_read.argtypes = [c_void_p, P(LmProfile), c_int]
     lib.lm_profile_read.restype = c_int
+    for fn in ("lm_token_logprob", "lm_token_logprob_grad"):
+        getattr(lib, fn).argtypes = [P(LmTokenLogprobArgs), c_void_p]
+        getattr(lib, fn).restype = c_int
+    lib.lm_checkpoint8_pack.argtypes = [P(LmMatrix), P(LmCheckpoint8), c_void_p]
+    lib.lm_checkpoint8_pack.restype = c_int
+    lib.lm_checkpoint8_unpack.argtypes = [P(LmCheckpoint8), P(LmMatrix), c_void_p]
+    lib.lm_checkpoint8_unpack.restype = c_int
+    lib.lm_rmsnorm.argtypes = [P(LmMatrix), P(LmMatrix), P(LmTensor), c_double, P(LmMatrix), P(LmMatrix),
+                               c_void_p, P(LmCheckpoint8), c_void_p]
+    lib.lm_rmsnorm.restype = c_int
+    lib.lm_rmsnorm_grad_workspace.argtypes = [c_int64, c_int64]
+    lib.lm_rmsnorm_grad_workspace.restype = ctypes.c_size_t
+    lib.lm_rmsnorm_grad.argtypes = [P(LmMatrix), P(LmMatrix), P(LmCheckpoint8), c_void_p, P(LmTensor), P(LmMatrix),
+                                    P(LmMatrix), P(LmTensor), c_void_p, ctypes.c_size_t, c_void_p]
+    lib.lm_rmsnorm_grad.restype = c_int
+    lib.lm_linear_wgrad8_workspace.argtypes = [P(LmMatrix), P(LmCheckpoint8), P(LmMatrix)]
+    lib.lm_linear_wgrad8_workspace.restype = ctypes.c_size_t
+    lib.lm_linear_wgrad8.argtypes = [P(LmMatrix), P(LmCheckpoint8), P(LmMatrix), c_int, c_void_p, ctypes.c_size_t,
+                                     c_void_p]
+    lib.lm_linear_wgrad8.restype = c_int
     if path is None:
         _LIB = lib
     return lib
