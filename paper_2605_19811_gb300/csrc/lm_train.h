@@ -80,7 +80,7 @@ struct WgradParams {
   int32_t accumulate;
   void* workspace;
 };
-size_t wgrad8_workspace(int64_t tokens, int64_t out, int64_t in);
+size_t wgrad8_workspace(const Mat& dy, int dydt, int64_t tokens, int64_t out, int64_t in);
 cudaError_t launch_wgrad8(const WgradParams& p, cudaStream_t st);
 
 }  // namespace lm

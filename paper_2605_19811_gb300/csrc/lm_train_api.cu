@@ -340,7 +340,7 @@ lm_status lm_rmsnorm_grad(const lm_matrix* dy, const lm_matrix* h, const lm_chec
 size_t lm_linear_wgrad8_workspace(const lm_matrix* dy, const lm_checkpoint8* x, const lm_matrix* dw) {
   if (dy == nullptr || x == nullptr || dw == nullptr) return 0;
   if (dy->rows < 0 || dy->cols <= 0 || x->cols <= 0) return 0;
-  return wgrad8_workspace(dy->rows, dy->cols, x->cols);
+  return wgrad8_workspace(mat(dy), (int)dy->dtype, dy->rows, dy->cols, x->cols);
 }
 
 lm_status lm_linear_wgrad8(const lm_matrix* dy, const lm_checkpoint8* x, const lm_matrix* dw, int accumulate,
