@@ -145,26 +145,14 @@ struct Items {
 __device__ __forceinline__ void tma_load_dy(void* dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2) {
   tma_load_3d(dst, map, bar, c0, c1, c2);
 }
-// Bounded wait on a barrier that threads of either CTA arrive on; false where
-// it gave up.  Without a call: a call would spill the sums that the epilogue
-// holds in registers.
-__device__ __forceinline__ bool probe(uint64_t* bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(smem_u32(bar)), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
+// Bounded wait; false where it gave up.  Without a call: a call would spill the
+// sums that the epilogue holds in registers.
 __device__ __forceinline__ bool await(uint64_t* bar, uint32_t parity, volatile int* abort_flag, uint64_t limit_ns) {
   // the clock is read every 256 probes (each may already sleep a while), at
   // every probe under a limit below a millisecond
   const uint32_t every = limit_ns < 1000000ull ? 0u : 255u;
   uint64_t t0 = 0;
-  for (uint32_t i = 0; !probe(bar, parity); ++i) {
+  for (uint32_t i = 0; !mbar_try_wait(bar, parity); ++i) {
     if ((i & every) != every) continue;
     if (*abort_flag) return false;
     const uint64_t now = globaltimer();
@@ -172,6 +160,16 @@ __device__ __forceinline__ bool await(uint64_t* bar, uint32_t parity, volatile i
     else if (now - t0 > limit_ns) return false;
   }
   return true;
+}
+
+// Arrive on a barrier of CTA 0.  What the arrival announces is in the arriving
+// CTA's own SM: operand bytes in its shared memory, which the arriving threads
+// have fenced towards the tensor core (fence.proxy.async) before, or TMEM
+// columns read to the end (tcgen05.wait::ld).  Nothing in global memory hangs
+// on it, so the arrival needs no fence of cluster scope; with one
+// (.release.cluster) it took 1300 cycles, against 512 of a token block's MMA.
+__device__ __forceinline__ void arrive_cta0(uint64_t* bar) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(peer_addr(bar, 0)) : "memory");
 }
 
 // Four codes (one word) to four bf16 values times the scale (twice in s2).
@@ -493,7 +491,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad8_
       __syncwarp();
       if (lane == 0) {
         mbar_arrive(&code_empty[stage]);
-        mbar_arrive_cluster(peer_addr(&full_b[stage], 0));
+        arrive_cta0(&full_b[stage]);
       }
       stage += kTeams;
       if (stage >= kStages) {
@@ -552,7 +550,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad8_
             }
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(peer_addr(&accempty[ab], 0));
+          if (lane == 0) arrive_cta0(&accempty[ab]);
           ab ^= 1;
           if (ab == 0) aph ^= 1u;
         }
@@ -582,7 +580,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad8_
           if (ok && b == 3) {
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(peer_addr(&accempty[ab], 0));
+            if (lane == 0) arrive_cta0(&accempty[ab]);
           }
           put_block(p, it, tm, tn, r0, c_tile + 32 * b, v, stg, lane);
         }
@@ -618,16 +616,27 @@ __global__ void __launch_bounds__(256) wgrad8_join_kernel(const __grid_constant_
   if (share_begin(s, k) <= u0 && share_begin(s, k + 1) >= u1) return;   // one pair wrote it whole
   int tm, tn;
   tile_place(s, s.waves * kPairs + t, tm, tn);
+  int last = k;   // the last sharer of the tile
+  while (last + 1 < s.sharers && share_begin(s, last + 1) < u1) ++last;
   const int rows = min(kTileM, p.out - tm * kTileM), cols = min(kTileN, p.in - tn * kTileN);
-  for (int r = blockIdx.y * 8 + (threadIdx.x >> 5); r < rows; r += gridDim.y * 8)
-    for (int c = threadIdx.x & 31; c < cols; c += 32) {
-      float sum = 0.f;
-      for (int j = k; j < s.sharers && share_begin(s, j) < u1; ++j) {
-        const int slot = 2 * j + (share_begin(s, j) / s.nkb == t ? 0 : 1);
-        sum += p.parts[(size_t)slot * (kTileM * kTileN) + (size_t)r * kTileN + c];
-      }
-      put_dw(p, (int64_t)(tm * kTileM + r) * p.dw.ld + tn * kTileN + c, sum);
-    }
+  // the first part may be its pair's second item; every later one is a first
+  const float* part0 = p.parts + (size_t)(2 * k + (share_begin(s, k) / s.nkb == t ? 0 : 1)) * (kTileM * kTileN);
+  const int r = blockIdx.y * 4 + (threadIdx.x >> 6), c = 4 * (threadIdx.x & 63);
+  if (r >= rows || c >= cols) return;
+  const size_t at = (size_t)r * kTileN + c;
+  float4 sum = *reinterpret_cast<const float4*>(part0 + at);
+#pragma unroll 4
+  for (int j = k + 1; j <= last; ++j) {
+    const float4 v = *reinterpret_cast<const float4*>(p.parts + (size_t)(2 * j) * (kTileM * kTileN) + at);
+    sum.x += v.x;
+    sum.y += v.y;
+    sum.z += v.z;
+    sum.w += v.w;
+  }
+  const float out[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (c + e < cols) put_dw(p, (int64_t)(tm * kTileM + r) * p.dw.ld + tn * kTileN + c + e, out[e]);
 }
 
 // dW of no tokens.
@@ -784,7 +793,7 @@ cudaError_t launch_wgrad8(const WgradParams& w, cudaStream_t st) {
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess || !has_parts(p.sch)) return e;
   count_launch();
-  wgrad8_join_kernel<<<dim3(p.sch.rest, 16), 256, 0, st>>>(p);
+  wgrad8_join_kernel<<<dim3(p.sch.rest, kTileM / 4), 256, 0, st>>>(p);
   return cudaGetLastError();
 }
 
