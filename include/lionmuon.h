@@ -545,9 +545,14 @@ lm_status lm_rmsnorm_grad(const lm_matrix* dy, const lm_matrix* h, const lm_chec
 /* Weight gradient of a linear layer y = x W^T whose input was kept in 8 bits:
  *   dw (+)= dy^T x      dw: out x in, dy: T x out, x: T x in
  * dw is bf16 or fp32, dy bf16 or fp32 (independently); accumulate != 0 adds to
- * dw, else dw is overwritten.  The sum over tokens is taken in a fixed order.
- * workspace: lm_linear_wgrad8_workspace(...) bytes of device memory, 256-byte
- * aligned.
+ * dw, else dw is overwritten.  Products are exact and the sum over tokens is
+ * taken in a fixed order: the same inputs give the same bits.
+ * workspace: lm_linear_wgrad8_workspace(...) bytes of device memory for the
+ * same arguments, 256-byte aligned, free again when the work is done (x in
+ * bf16, dy where it is fp32 or its rows are not 16-byte aligned, and partial
+ * sums of at most 40 MB).
+ * Should a device-side wait give up (LM_WAIT_LIMIT_NS), what was not computed
+ * is NaN in dw.
  * Errors: LM_ERR_INVALID_ARG (also a workspace that is too small),
  * LM_ERR_DTYPE, LM_ERR_ALIGN, LM_ERR_UNSUPPORTED, LM_ERR_CUDA. */
 size_t lm_linear_wgrad8_workspace(const lm_matrix* dy, const lm_checkpoint8* x, const lm_matrix* dw);

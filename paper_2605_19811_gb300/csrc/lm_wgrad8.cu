@@ -3,25 +3,24 @@
 // (lm_linear_wgrad8 in lionmuon.h) on the tensor cores: tcgen05.mma on CTA
 // pairs, one 256 x 256 tile of dW per pair, a sum over tokens 64 at a time.
 //
-// A code times its power-of-two scale is a bf16 number, so X enters the
-// product exactly; dY does too, as itself (bf16) or as three bf16 pieces
-// (fp32: 8 + 8 + 8 significant bits, summed as three times as many tokens).
-// Every product is then exact and only the sums are rounded.
+// A code times its power-of-two scale is a bf16 number, so a first kernel
+// writes X as bf16 into the workspace without a rounding; dY is taken as it is
+// (bf16), or laid out as three bf16 planes whose sum is the fp32 value (8 + 8 +
+// 8 significant bits, summed as three times as many tokens).  Every product is
+// then exact and only the sums are rounded.
+// (The codes made bf16 inside the product's kernel, by warps of their own,
+// cost more: the conversion shares the shared memory's bandwidth with the MMA,
+// 440 ns instead of 350 for a pair's 64 tokens.)
 //
 // Both operands lie token by token in memory, so both are MN-major: rows of
 // 64 channels (128 bytes, 128-byte swizzle), one row a token.  CTA r of the
-// pair holds output channels 128 r .. of the tile (A, from dY by TMA) and input
-// channels 128 r .. (B): exactly one scale group, so one scale a token.  The
-// codes come by TMA and the scales by cp.async into a ring of their own; eight
-// converter warps make B from them: code -> bf16 by integer operations on
-// pairs, times the scale, 16-byte stores into the swizzled stage.
+// pair holds output channels 128 r .. of the tile (A, from dY) and input
+// channels 128 r .. (B, from X), both by TMA.
 //
-// CTA roles (20 warps, one CTA per SM):
-//   warp 0       TMA producer of A (one lane); both CTAs' copies signal CTA 0
-//   warp 1       TMEM allocation; MMA issuer (CTA 0, one lane)
-//   warp 2       codes (TMA) and scales (cp.async) of B
-//   warps 4-11   converters of B
-//   warps 12-19  epilogue: one TMEM lane quadrant and half of the columns each
+// CTA roles (12 warps, one CTA per SM):
+//   warp 0      TMA producer (one lane); both CTAs' copies signal CTA 0
+//   warp 1      TMEM allocation; MMA issuer (CTA 0, one lane)
+//   warps 4-11  epilogue: one TMEM lane quadrant and half of the columns each
 //
 // Accumulation: the tensor cores lose up to a unit of the last place of the
 // accumulator at each addition (16 tokens).  For a bf16 result that is far
@@ -55,25 +54,18 @@ using tcs::kCleanupWaitNs;
 constexpr int kTileM = 256, kTileN = 256, kBlockK = 64;
 constexpr int kHalf = 128;
 constexpr int kABytes = kHalf * kBlockK * 2, kBBytes = kHalf * kBlockK * 2;
-constexpr int kStages = 5;
-constexpr int kStageBytes = kABytes + kBBytes;
-constexpr int kCodeBytes = kBlockK * kHalf;            // a token block's codes of one CTA
-constexpr int kCodeStage = kCodeBytes + kBlockK * 4;   // and their scales
-constexpr int kConvWarps = 8, kEpiWarps = 8;
-constexpr int kTeams = 2, kTeamWarps = kConvWarps / kTeams;   // converter teams take token blocks in turn
-constexpr int kCodeWarp = 2;
-constexpr int kFirstConv = 4, kFirstEpi = kFirstConv + kConvWarps;
+constexpr int kStages = 6, kStageBytes = kABytes + kBBytes;
+constexpr int kFirstEpi = 4, kEpiWarps = 8;            // whole warpgroups: a warp reads the TMEM lanes of its number mod 4
 constexpr int kThreads = 32 * (kFirstEpi + kEpiWarps);
 constexpr int kChunk = 8;                              // token blocks summed in one accumulator (fp32 results)
 constexpr int kPairs = 76;                             // CTA pairs of the GPU (152 SMs)
 constexpr int kTmemCols = 512;
-constexpr size_t kTransBytes = 32 * 17 * 4;            // an epilogue warp's transpose tile
-constexpr size_t kCodeOffset = (size_t)kStages * kStageBytes;
-constexpr size_t kTransOffset = kCodeOffset + (size_t)kStages * kCodeStage;
-constexpr size_t kBarOffset = kTransOffset + kEpiWarps * kTransBytes;
+constexpr int kTransBytes = 32 * 20 * 4;               // an epilogue warp's transpose tile: 32 rows x 16 columns, 80-byte rows
+constexpr size_t kTransOffset = (size_t)kStages * kStageBytes;
+constexpr size_t kBarOffset = kTransOffset + (size_t)kEpiWarps * kTransBytes;
 constexpr size_t kSmemBytes = 1024 + kBarOffset + 512;
-constexpr size_t kPartBytes = (size_t)kTileM * kTileN * 4;
 static_assert(kSmemBytes <= 232448, "shared memory of one SM");
+constexpr size_t kPartBytes = (size_t)kTileM * kTileN * 4;
 
 // How the work falls to the pairs.
 struct Schedule {
@@ -85,14 +77,13 @@ struct Schedule {
   int32_t sharers;      // pairs that share them; 0: none left over
 };
 struct KernelParams {
-  CUtensorMap dy, codes;
+  CUtensorMap dy, x;
   Schedule sch;
-  int64_t tokens;
   int32_t out, in;
-  Codes x;
   Mat dw;
   int32_t dwdt;
   int32_t accumulate;
+  int32_t vec;          // dW takes four elements at a time
   float* parts;
   uint64_t wait_ns;
 };
@@ -142,9 +133,6 @@ struct Items {
   }
 };
 
-__device__ __forceinline__ void tma_load_dy(void* dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2) {
-  tma_load_3d(dst, map, bar, c0, c1, c2);
-}
 // Bounded wait; false where it gave up.  Without a call: a call would spill the
 // sums that the epilogue holds in registers.
 __device__ __forceinline__ bool await(uint64_t* bar, uint32_t parity, volatile int* abort_flag, uint64_t limit_ns) {
@@ -160,6 +148,17 @@ __device__ __forceinline__ bool await(uint64_t* bar, uint32_t parity, volatile i
     else if (now - t0 > limit_ns) return false;
   }
   return true;
+}
+
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32"
+      " {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
 }
 
 // Arrive on a barrier of CTA 0.  What the arrival announces is in the arriving
@@ -198,18 +197,6 @@ __device__ __forceinline__ uint2 convert4(uint32_t w, uint32_t s2) {
   return make_uint2(r[0], r[1]);
 }
 
-// 128 codes x 64 tokens into this CTA's shared memory.
-__device__ __forceinline__ void tma_load_codes(void* dst, const CUtensorMap* map, uint64_t* bar, int c0, int c1) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(c0), "r"(c1)
-      : "memory");
-}
-// One scale into shared memory, zero where there is none.
-__device__ __forceinline__ void copy_scale(float* dst, const float* src, bool in) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(in ? 4 : 0) : "memory");
-}
-
 __device__ __forceinline__ void put_dw(const KernelParams& p, int64_t at, float v) {
   if (p.dwdt == LM_F32) {
     float* d = static_cast<float*>(p.dw.data) + at;
@@ -220,46 +207,66 @@ __device__ __forceinline__ void put_dw(const KernelParams& p, int64_t at, float 
   }
 }
 
+// Four elements of a row of dW, `left` of them inside.
+__device__ __forceinline__ void put_dw4(const KernelParams& p, int64_t at, float4 v, int left) {
+  if (!p.vec || left < 4) {
+    const float e[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (k < left) put_dw(p, at + k, e[k]);
+  } else if (p.dwdt == LM_F32) {
+    float4* d = reinterpret_cast<float4*>(static_cast<float*>(p.dw.data) + at);
+    if (p.accumulate) {
+      const float4 o = *d;
+      v = make_float4(o.x + v.x, o.y + v.y, o.z + v.z, o.w + v.w);
+    }
+    *d = v;
+  } else {
+    uint2* d = reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.dw.data) + at);
+    if (p.accumulate) {
+      const uint2 o = *d;
+      v = make_float4(bf_lo(o.x) + v.x, bf_hi(o.x) + v.y, bf_lo(o.y) + v.z, bf_hi(o.y) + v.w);
+    }
+    *d = make_uint2(pack_bf2(v.x, v.y), pack_bf2(v.z, v.w));
+  }
+}
+
 // 32 rows (one a lane) x 32 columns of a tile, row r0 / column c0 of the tile:
-// through the warp's transpose tile, 16 columns at a time, then two rows a
-// step, a column a lane.
+// through the warp's transpose tile, 16 columns at a time, then eight rows a
+// step, four columns a lane.
 __device__ __forceinline__ void put_block(const KernelParams& p, const Item& it, int tm, int tn, int r0, int c0,
                                           const float (&v)[32], float* stg, int lane) {
   const int row0 = tm * kTileM + r0, rows = min(32, p.out - row0);
+  const int q = 4 * (lane & 3), r8 = lane >> 2;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) stg[lane * 17 + e] = v[16 * h + e];
+    for (int e = 0; e < 16; e += 4)
+      *reinterpret_cast<float4*>(stg + lane * 20 + e) = make_float4(v[16 * h + e], v[16 * h + e + 1], v[16 * h + e + 2], v[16 * h + e + 3]);
     __syncwarp();
-    const int c = c0 + 16 * h + (lane & 15), col = tn * kTileN + c;
-    if (col < p.in) {
-      float* part = it.slot >= 0 ? p.parts + (size_t)it.slot * (kTileM * kTileN) + (size_t)r0 * kTileN + c : nullptr;
-      for (int r = lane >> 4; r < rows; r += 2) {
-        const float x = stg[r * 17 + (lane & 15)];
-        if (part != nullptr) part[(size_t)r * kTileN] = x;
-        else put_dw(p, (int64_t)(row0 + r) * p.dw.ld + col, x);
+    const int c = c0 + 16 * h + q, left = p.in - (tn * kTileN + c);
+    if (left > 0) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int r = r8 + 8 * k;
+        const float4 x = *reinterpret_cast<const float4*>(stg + r * 20 + q);
+        if (r >= rows) continue;
+        if (it.slot >= 0) *reinterpret_cast<float4*>(p.parts + (size_t)it.slot * (kTileM * kTileN) + (size_t)(r0 + r) * kTileN + c) = x;
+        else put_dw4(p, (int64_t)(row0 + r) * p.dw.ld + tn * kTileN + c, x, left);
       }
     }
     __syncwarp();
   }
 }
 
-// Before the register split is taken back: a warp that asked for its registers
-// back earlier could take what an epilogue warp still waits for, and neither
-// would go on.
-__device__ __forceinline__ void all_roles_done() { asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory"); }
-
 // kLong: sums of fp32 results, cut every kChunk token blocks.
-template <int kFormat, bool kLong>
+template <bool kLong>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad8_kernel(const __grid_constant__ KernelParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint64_t* full_a = reinterpret_cast<uint64_t*>(smem + kBarOffset);
-  uint64_t* full_b = full_a + kStages;
-  uint64_t* empty = full_b + kStages;
-  uint64_t* code_full = empty + kStages;
-  uint64_t* code_empty = code_full + kStages;
-  uint64_t* accfull = code_empty + kStages;
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + kBarOffset);
+  uint64_t* empty = full + kStages;
+  uint64_t* accfull = empty + kStages;
   uint64_t* accempty = accfull + 2;
   uint64_t* done = accempty + 2;
   ProducerLog<kStages>* log = reinterpret_cast<ProducerLog<kStages>*>(done + 1);
@@ -274,11 +281,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad8_
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(&full_a[s], 1);
-      mbar_init(&full_b[s], 2 * kTeamWarps);
+      mbar_init(&full[s], 1);
       mbar_init(&empty[s], 1);
-      mbar_init(&code_full[s], 1 + 32);
-      mbar_init(&code_empty[s], kTeamWarps);
       armed[s] = -1;
     }
     for (int b = 0; b < 2; ++b) {
@@ -300,11 +304,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad8_
   const uint32_t tmem_base = *tmem_slot;
   const uint64_t wait_ns = p.wait_ns;
 
-  if (warp < kFirstConv) {
-    // Registers: 640 threads x 96 at launch = 128 x 32 + 256 x 64 + 256 x 160 after the split.
-    if (kLong) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
-    if (warp == 0 && lane == 0) {
-      // ------------------------------ producer of A ------------------------------
+  if (warp == 0) {
+    // -------------------------------- producer ---------------------------------
+    if (lane == 0) {
       int stage = 0;
       uint32_t ph = 0;
       bool ok = true;
@@ -313,7 +315,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad8_
       while (ok && items.next(sch, it)) {
         int tm, tn;
         tile_place(sch, it.tile, tm, tn);
-        const int row = tm * kTileM + (int)rank * kHalf;
+        const int row = tm * kTileM + (int)rank * kHalf, col = tn * kTileN + (int)rank * kHalf;
         int plane = it.kb0 / sch.nkb_plane, tb = it.kb0 - plane * sch.nkb_plane;
         for (int kb = it.kb0; kb < it.kb1; ++kb) {
           if (!await(&empty[stage], ph ^ 1u, abort_flag, wait_ns)) {
@@ -321,15 +323,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad8_
             break;
           }
           uint8_t* sa = smem + (size_t)stage * kStageBytes;
-          const uint32_t fb = peer_addr(&full_a[stage], 0);
+          uint8_t* sb = sa + kABytes;
+          const uint32_t fb = peer_addr(&full[stage], 0);
           if (rank == 0) {
-            mbar_arrive_expect_tx(&full_a[stage], 2u * kABytes);
+            mbar_arrive_expect_tx(&full[stage], 2u * kStageBytes);
             armed[stage] = (int)ph;
           }
-          log->bytes[stage] = kABytes;
+          log->bytes[stage] = kStageBytes;
           log->n += 1u;
-          tma_load_dy(sa, &p.dy, fb, row, tb * kBlockK, plane);
-          tma_load_dy(sa + kABytes / 2, &p.dy, fb, row + 64, tb * kBlockK, plane);
+          tma_load_3d(sa, &p.dy, fb, row, tb * kBlockK, plane);
+          tma_load_3d(sa + kABytes / 2, &p.dy, fb, row + 64, tb * kBlockK, plane);
+          tma_load_3d(sb, &p.x, fb, col, tb * kBlockK, 0);
+          tma_load_3d(sb + kBBytes / 2, &p.x, fb, col + 64, tb * kBlockK, 0);
           if (++tb == sch.nkb_plane) {
             tb = 0;
             ++plane;
@@ -341,8 +346,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad8_
         }
       }
       if (!ok) *abort_flag = 1;
-    } else if (warp == 1 && lane == 0 && rank == 0) {
-      // -------------------------------- MMA issuer -------------------------------
+    }
+  } else if (warp == 1) {
+    // -------------------------------- MMA issuer -------------------------------
+    if (lane == 0 && rank == 0) {
       const uint32_t idesc = make_idesc(kTileM, kTileN, true, true);
       int stage = 0, ab = 0;
       uint32_t ph = 0, aph = 0;
@@ -359,7 +366,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad8_
           tc_fence_after();
           const uint32_t d = tmem_base + (uint32_t)(ab * kTileN);
           for (int kb = kc; kb < ke; ++kb) {
-            if (!await(&full_a[stage], ph, abort_flag, wait_ns) || !await(&full_b[stage], ph, abort_flag, wait_ns)) {
+            if (!await(&full[stage], ph, abort_flag, wait_ns)) {
               ok = false;
               break;
             }
@@ -387,126 +394,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad8_
       volatile int never = 0;
       await(done, 0, &never, kCleanupWaitNs);
     }
-    if (warp == kCodeWarp) {
-      // ------------------------- codes and scales of B ---------------------------
-      // By TMA and cp.async, into a ring of their own: the converters then have no
-      // load in flight when they fence their stores (the fence would wait for it).
-      int stage = 0, issued = 0;   // issued: token blocks, counted up to kStages
-      uint32_t ph = 0;
-      bool ok = true;
-      Items items(sch, pair);
-      Item it;
-      while (ok && items.next(sch, it)) {
-        int tm, tn;
-        tile_place(sch, it.tile, tm, tn);
-        const int col = tn * kTileN + (int)rank * kHalf;
-        const float* cs = p.x.scales + (int64_t)(col / LM_CODE_GROUP) * p.x.ld_scales;
-        int tb = it.kb0 % sch.nkb_plane;
-        for (int kb = it.kb0; kb < it.kb1; ++kb) {
-          if (!await(&code_empty[stage], ph ^ 1u, abort_flag, wait_ns)) {
-            ok = false;
-            break;
-          }
-          uint8_t* c = smem + kCodeOffset + (size_t)stage * kCodeStage;
-          if (lane == 0) {
-            mbar_arrive_expect_tx(&code_full[stage], kCodeBytes);
-            tma_load_codes(c, &p.codes, &code_full[stage], col, tb * kBlockK);
-          }
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const int64_t t = (int64_t)tb * kBlockK + 32 * j + lane;
-            const bool in = col < p.in && t < p.tokens;
-            copy_scale(reinterpret_cast<float*>(c + kCodeBytes) + 32 * j + lane, in ? cs + t : p.x.scales, in);
-          }
-          asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&code_full[stage])) : "memory");
-          if (issued < kStages) ++issued;
-          if (++tb == sch.nkb_plane) tb = 0;
-          if (++stage == kStages) {
-            stage = 0;
-            ph ^= 1u;
-          }
-        }
-      }
-      asm volatile("cp.async.wait_all;" ::: "memory");
-      if (!ok) {
-        // nothing may be in flight into a CTA that leaves: wait (bounded) for the
-        // newest phase of every stage that was used
-        *abort_flag = 1;
-        volatile int never = 0;
-        for (int s = 0; s < kStages && s < issued; ++s) await(&code_full[s], s < stage ? ph : ph ^ 1u, &never, kCleanupWaitNs);
-      }
-    }
-    __syncwarp();
-    if (kLong) {
-      all_roles_done();
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
-    }
-  } else if (warp < kFirstEpi) {
-    // ------------------------------ converters of B ------------------------------
-    // Two teams of four warps take the token blocks in turn.  Warp w of a team
-    // makes tokens 16 w .. 16 w + 15 of a block: lane l reads 16 codes (columns
-    // 16 (l % 8) ..) of tokens l / 8 + 4 j.  The two atoms of 64 columns store
-    // their halves in opposite order, so that the eight lanes of a 16-byte store
-    // phase touch all banks.
-    if (kLong) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-    const int team = (warp - kFirstConv) / kTeamWarps;
-    const int tok = 16 * ((warp - kFirstConv) % kTeamWarps) + (lane >> 3);
-    const int atom = (lane & 7) >> 2, chunk = 2 * (lane & 3);
-    uint32_t off[2][2];   // of tokens j = 0 and 1; j = 2 and 3 lie 8 rows further
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int k = tok + 4 * j, c = chunk + (h ^ atom);
-        off[j][h] = (uint32_t)(kABytes + atom * (kBBytes / 2) + k * 128 + ((c ^ (k & 7)) << 4));
-      }
-    int64_t blocks = (int64_t)sch.waves * sch.nkb;   // token blocks of this pair
-    if (pair < sch.sharers) blocks += share_begin(sch, pair + 1) - share_begin(sch, pair);
-    int stage = team;
-    uint32_t ph = 0;
-    for (int64_t n = team; n < blocks; n += kTeams) {
-      if (!await(&code_full[stage], ph, abort_flag, wait_ns) || !await(&empty[stage], ph ^ 1u, abort_flag, wait_ns)) {
-        *abort_flag = 1;
-        break;
-      }
-      const uint8_t* code = smem + kCodeOffset + (size_t)stage * kCodeStage;
-      uint8_t* st = smem + (size_t)stage * kStageBytes;
-      uint4 q[4];
-      uint32_t s2[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        q[j] = *reinterpret_cast<const uint4*>(code + (tok + 4 * j) * kHalf + 16 * (lane & 7));
-        const uint32_t sb = *reinterpret_cast<const uint32_t*>(code + kCodeBytes + 4 * (tok + 4 * j));
-        s2[j] = __byte_perm(sb, sb, 0x3232);
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint2 w0 = convert4<kFormat>(q[j].x, s2[j]), w1 = convert4<kFormat>(q[j].y, s2[j]);
-        const uint2 w2 = convert4<kFormat>(q[j].z, s2[j]), w3 = convert4<kFormat>(q[j].w, s2[j]);
-        const uint4 lo = make_uint4(w0.x, w0.y, w1.x, w1.y), hi = make_uint4(w2.x, w2.y, w3.x, w3.y);
-        *reinterpret_cast<uint4*>(st + off[j & 1][0] + (j >> 1) * 1024) = atom == 0 ? lo : hi;
-        *reinterpret_cast<uint4*>(st + off[j & 1][1] + (j >> 1) * 1024) = atom == 0 ? hi : lo;
-      }
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(&code_empty[stage]);
-        arrive_cta0(&full_b[stage]);
-      }
-      stage += kTeams;
-      if (stage >= kStages) {
-        stage -= kStages;
-        ph ^= 1u;
-      }
-    }
-    __syncwarp();
-    if (kLong) {
-      all_roles_done();
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
-    }
-  } else {
+  } else if (warp >= kFirstEpi) {
     // --------------------------------- epilogue ----------------------------------
-    if (kLong) asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
     const int q = warp & 3, half = (warp - kFirstEpi) >> 2;
     float* stg = reinterpret_cast<float*>(smem + kTransOffset + (size_t)(warp - kFirstEpi) * kTransBytes);
     const int r0 = (int)rank * kHalf + q * 32;      // the warp's first row of the tile
@@ -521,14 +410,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad8_
       int tm, tn;
       tile_place(sch, it.tile, tm, tn);
       const int c_tile = half * 128;
-      if (kLong) {
+      if constexpr (kLong) {
         float acc[4][32];
 #pragma unroll
         for (int b = 0; b < 4; ++b)
 #pragma unroll
           for (int e = 0; e < 32; ++e) acc[b][e] = 0.f;
         for (int kc = it.kb0; kc < it.kb1; kc += kChunk) {
-          if (ok && !await(&accfull[ab], aph, abort_flag, wait_ns)) ok = false;
+          // one answer for the warp: the TMEM loads below are taken by all lanes or none
+          ok = ok && __all_sync(0xFFFFFFFFu, await(&accfull[ab], aph, abort_flag, wait_ns));
           if (!ok) {
             *abort_flag = 1;
             break;
@@ -537,16 +427,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad8_
 #pragma unroll
           for (int b = 0; b < 4; ++b)
 #pragma unroll
-            for (int o = 0; o < 4; ++o) {
-              uint32_t r[8];
-              asm volatile(
-                  "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\t"
-                  "tcgen05.wait::ld.sync.aligned;"
-                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-                  : "r"(tmem_base + (uint32_t)(ab * kTileN + c_tile + 32 * b + 8 * o) + lanes)
-                  : "memory");
+            for (int o = 0; o < 32; o += 16) {
+              uint32_t r[16];
+              tmem_ld16(tmem_base + (uint32_t)(ab * kTileN + c_tile + 32 * b + o) + lanes, r);
 #pragma unroll
-              for (int e = 0; e < 8; ++e) acc[b][8 * o + e] += __uint_as_float(r[e]);
+              for (int e = 0; e < 16; ++e) acc[b][o + e] += __uint_as_float(r[e]);
             }
           tc_fence_before();
           __syncwarp();
@@ -561,11 +446,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad8_
           put_block(p, it, tm, tn, r0, c_tile + 32 * b, acc[b], stg, lane);
         }
       } else {
-        if (ok && !await(&accfull[ab], aph, abort_flag, wait_ns)) {
-          ok = false;
-          *abort_flag = 1;
-        }
+        ok = ok && __all_sync(0xFFFFFFFFu, await(&accfull[ab], aph, abort_flag, wait_ns));
         if (ok) tc_fence_after();
+        else *abort_flag = 1;
         for (int b = 0; b < 4; ++b) {
           float v[32];
           if (ok) {
@@ -588,15 +471,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad8_
         if (ab == 0) aph ^= 1u;
       }
     }
-    __syncwarp();
-    if (kLong) {
-      all_roles_done();
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
-    }
   }
 
   __syncwarp();
-  pair_finish<kStages>(*log, abort_flag, full_a, armed, rank);
+  pair_finish<kStages>(*log, abort_flag, full, armed, rank);
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc(tmem_base, kTmemCols);
@@ -633,10 +511,7 @@ __global__ void __launch_bounds__(256) wgrad8_join_kernel(const __grid_constant_
     sum.z += v.z;
     sum.w += v.w;
   }
-  const float out[4] = {sum.x, sum.y, sum.z, sum.w};
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (c + e < cols) put_dw(p, (int64_t)(tm * kTileM + r) * p.dw.ld + tn * kTileN + c + e, out[e]);
+  put_dw4(p, (int64_t)(tm * kTileM + r) * p.dw.ld + tn * kTileN + c, sum, cols - c);
 }
 
 // dW of no tokens.
@@ -648,16 +523,48 @@ __global__ void __launch_bounds__(256) wgrad8_zero_kernel(Mat dw, int dwdt, int 
     }
 }
 
-// dY as the TMA wants it: rows of a 16-byte pitch, bf16; fp32 values as three
-// planes whose sum is exactly the value (each takes the next 8 significant
-// bits by truncation, so that no piece rounds up to infinity; a non-finite
-// value keeps its first piece and has NaN or infinity in the others).
-template <typename T>
-__global__ void __launch_bounds__(256) wgrad8_layout_kernel(Mat dy, int64_t tokens, int out, __nv_bfloat16* dst, int64_t ld) {
+// The operands as the TMA takes them.  Blocks below x_blocks: X = code * scale
+// as bf16, 16 codes a thread and step.  The others: dY in rows of a 16-byte
+// pitch where its own are not; fp32 values as three planes whose sum is
+// exactly the value (each takes the next 8 significant bits by truncation, so
+// that no piece rounds up to infinity; a non-finite value keeps its first
+// piece and has NaN in the second).
+template <int kFormat, typename T>
+__global__ void __launch_bounds__(256) wgrad8_operands_kernel(Codes x, __nv_bfloat16* xdst, int64_t ldx, unsigned x_blocks, Mat dy, int64_t tokens,
+                                                              int out, __nv_bfloat16* dst, int64_t ld) {
+  if (blockIdx.x < x_blocks) {
+    const int64_t per = ldx / 16, all = tokens * per, step = (int64_t)x_blocks * 256;
+    for (int64_t i0 = (int64_t)blockIdx.x * 256 + threadIdx.x; i0 < all; i0 += 4 * step) {
+      uint4 q[4];
+      uint32_t s[4];
+      int64_t t[4];
+      int c[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int64_t i = i0 + k * step;
+        if (i >= all) break;
+        t[k] = i / per;
+        c[k] = (int)(i - t[k] * per) * 16;
+        q[k] = __ldcs(reinterpret_cast<const uint4*>(x.data + t[k] * x.ld + c[k]));
+        s[k] = __float_as_uint(__ldg(x.scales + (int64_t)(c[k] / LM_CODE_GROUP) * x.ld_scales + t[k]));
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (i0 + k * step >= all) break;
+        const uint32_t s2 = __byte_perm(s[k], s[k], 0x3232);
+        const uint2 w0 = convert4<kFormat>(q[k].x, s2), w1 = convert4<kFormat>(q[k].y, s2);
+        const uint2 w2 = convert4<kFormat>(q[k].z, s2), w3 = convert4<kFormat>(q[k].w, s2);
+        uint4* d = reinterpret_cast<uint4*>(xdst + t[k] * ldx + c[k]);
+        d[0] = make_uint4(w0.x, w0.y, w1.x, w1.y);
+        d[1] = make_uint4(w2.x, w2.y, w3.x, w3.y);
+      }
+    }
+    return;
+  }
   const int64_t plane = tokens * ld;
-  for (int64_t t = blockIdx.y; t < tokens; t += gridDim.y) {
+  for (int64_t t = blockIdx.x - x_blocks; t < tokens; t += gridDim.x - x_blocks) {
     const T* src = static_cast<const T*>(dy.data) + t * dy.ld;
-    for (int c = blockIdx.x * 256 + threadIdx.x; c < out; c += gridDim.x * 256) {
+    for (int c = threadIdx.x; c < out; c += 256) {
       __nv_bfloat16* d = dst + t * ld + c;
       if constexpr (sizeof(T) == 2) {
         *d = src[c];
@@ -706,17 +613,43 @@ bool has_parts(const Schedule& s) { return s.rest > 0 && s.sharers > s.rest; }
 struct Layout {
   bool copy;          // dY is laid out anew in the workspace
   int planes;
-  int64_t ld;         // of the copy
-  size_t parts, total;
+  int64_t ld, ldx;    // of the copies of dY and X
+  size_t parts, dy, total;   // bytes: parts, then dY, then X
 };
-Layout make_layout(const Schedule& s, int64_t tokens, int64_t out, int dydt, const Mat& dy) {
+Layout make_layout(const Schedule& s, int64_t tokens, int64_t out, int64_t in, int dydt, const Mat& dy) {
+  auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   Layout l{};
   l.planes = dydt == LM_F32 ? 3 : 1;
   l.copy = dydt == LM_F32 || reinterpret_cast<uintptr_t>(dy.data) % 16 != 0 || (tokens > 1 && dy.ld % 8 != 0) || (tokens == 1 && out % 8 != 0);
   l.ld = (out + 7) / 8 * 8;
+  l.ldx = (in + 15) / 16 * 16;
   l.parts = has_parts(s) ? 2 * (size_t)s.sharers * kPartBytes : 0;
-  l.total = l.parts + (l.copy ? (size_t)l.planes * tokens * l.ld * 2 : 0);
+  l.dy = l.copy ? up((size_t)l.planes * tokens * l.ld * 2) : 0;
+  l.total = l.parts + l.dy + up((size_t)tokens * l.ldx * 2);
   return l;
+}
+
+// A 3-D map (columns, rows, planes) of boxes of 64 columns x 64 tokens, bf16, 128-byte swizzle.
+CUresult encode_operand(PFN_cuTensorMapEncodeTiled_v12000 enc, CUtensorMap* m, void* base, int64_t cols, int64_t rows, int64_t ld, int planes) {
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
+  const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * 2 * (cuuint64_t)rows};
+  const cuuint32_t box[3] = {64, kBlockK, 1}, estr[3] = {1, 1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
+template <bool kLong>
+cudaError_t start(const KernelParams& p, int pairs, cudaStream_t st) {
+  const int dev = device_slot();
+  static bool ready[kMaxDevices];
+  if (dev < 0 || !ready[dev]) {
+    const cudaError_t e = cudaFuncSetAttribute(wgrad8_kernel<kLong>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
+    if (e != cudaSuccess) return e;
+    if (dev >= 0) ready[dev] = true;
+  }
+  count_launch();
+  wgrad8_kernel<kLong><<<2 * pairs, kThreads, kSmemBytes, st>>>(p);
+  return cudaGetLastError();
 }
 
 }  // namespace
@@ -724,7 +657,7 @@ Layout make_layout(const Schedule& s, int64_t tokens, int64_t out, int dydt, con
 size_t wgrad8_workspace(const Mat& dy, int dydt, int64_t tokens, int64_t out, int64_t in) {
   if (tokens <= 0) return 0;
   const Schedule s = make_schedule(tokens, out, in, dydt == LM_F32 ? 3 : 1);
-  return make_layout(s, tokens, out, dydt, dy).total;
+  return make_layout(s, tokens, out, in, dydt, dy).total;
 }
 
 cudaError_t launch_wgrad8(const WgradParams& w, cudaStream_t st) {
@@ -736,61 +669,42 @@ cudaError_t launch_wgrad8(const WgradParams& w, cudaStream_t st) {
   const int planes = w.dydt == LM_F32 ? 3 : 1;
   KernelParams p{};
   p.sch = make_schedule(w.tokens, w.out, w.in, planes);
-  p.tokens = w.tokens;
   p.out = w.out;
   p.in = w.in;
-  p.x = w.x;
   p.dw = w.dw;
   p.dwdt = w.dwdt;
   p.accumulate = w.accumulate;
+  const uintptr_t four = w.dwdt == LM_F32 ? 16 : 8;   // bytes of four elements
+  p.vec = reinterpret_cast<uintptr_t>(w.dw.data) % four == 0 && (w.out == 1 || w.dw.ld % 4 == 0);
   p.wait_ns = env_wait_limit_ns();
-  const Layout l = make_layout(p.sch, w.tokens, w.out, w.dydt, w.dy);
+  const Layout l = make_layout(p.sch, w.tokens, w.out, w.in, w.dydt, w.dy);
   p.parts = static_cast<float*>(w.workspace);
   void* dy = w.dy.data;
   int64_t ld = w.dy.ld;
   if (l.copy) {
     dy = static_cast<uint8_t*>(w.workspace) + l.parts;
     ld = l.ld;
-    const dim3 grid((unsigned)((w.out + 255) / 256), (unsigned)(w.tokens < 8192 ? w.tokens : 8192));
+  }
+  __nv_bfloat16* x = reinterpret_cast<__nv_bfloat16*>(static_cast<uint8_t*>(w.workspace) + l.parts + l.dy);
+  {
+    const int64_t steps = (w.tokens * (l.ldx / 16) + 1023) / 1024;   // four a thread
+    const unsigned x_blocks = (unsigned)(steps < 152 * 8 ? steps : 152 * 8);
+    const unsigned dy_blocks = l.copy ? (unsigned)(w.tokens < 152 * 8 ? w.tokens : 152 * 8) : 0u;
+    using Operands = void (*)(Codes, __nv_bfloat16*, int64_t, unsigned, Mat, int64_t, int, __nv_bfloat16*, int64_t);
+    const Operands kernels[2][2] = {{wgrad8_operands_kernel<LM_CODE_I8, float>, wgrad8_operands_kernel<LM_CODE_I8, __nv_bfloat16>},
+                                    {wgrad8_operands_kernel<LM_CODE_E4M3, float>, wgrad8_operands_kernel<LM_CODE_E4M3, __nv_bfloat16>}};
     count_launch();
-    if (w.dydt == LM_F32) wgrad8_layout_kernel<float><<<grid, 256, 0, st>>>(w.dy, w.tokens, w.out, static_cast<__nv_bfloat16*>(dy), ld);
-    else wgrad8_layout_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(w.dy, w.tokens, w.out, static_cast<__nv_bfloat16*>(dy), ld);
+    kernels[w.x.format == LM_CODE_I8 ? 0 : 1][w.dydt == LM_F32 ? 0 : 1]<<<x_blocks + dy_blocks, 256, 0, st>>>(
+        w.x, x, l.ldx, x_blocks, w.dy, w.tokens, w.out, static_cast<__nv_bfloat16*>(dy), ld);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
   }
   const PFN_cuTensorMapEncodeTiled_v12000 enc = encode_fn();
   if (enc == nullptr) return cudaErrorNotSupported;
-  const cuuint64_t dims[3] = {(cuuint64_t)w.out, (cuuint64_t)w.tokens, (cuuint64_t)planes};
-  const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * 2 * (cuuint64_t)w.tokens};
-  const cuuint32_t box[3] = {64, kBlockK, 1}, estr[3] = {1, 1, 1};
-  if (enc(&p.dy, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, dy, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-    return cudaErrorInvalidValue;
-
-  const cuuint64_t cdims[2] = {(cuuint64_t)w.in, (cuuint64_t)w.tokens};
-  const cuuint64_t cstride[1] = {(cuuint64_t)w.x.ld};
-  const cuuint32_t cbox[2] = {kHalf, kBlockK};
-  if (enc(&p.codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, w.x.data, cdims, cstride, cbox, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-          CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-    return cudaErrorInvalidValue;
-
-  using Kernel = void (*)(KernelParams);
-  const Kernel kernels[2][2] = {{wgrad8_kernel<LM_CODE_I8, false>, wgrad8_kernel<LM_CODE_I8, true>},
-                                {wgrad8_kernel<LM_CODE_E4M3, false>, wgrad8_kernel<LM_CODE_E4M3, true>}};
-  const int dev = device_slot();
-  static bool ready[kMaxDevices];
-  if (dev < 0 || !ready[dev]) {
-    for (const auto& row : kernels)
-      for (const Kernel k : row) {
-        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
-        if (e != cudaSuccess) return e;
-      }
-    if (dev >= 0) ready[dev] = true;
-  }
+  if (encode_operand(enc, &p.dy, dy, w.out, w.tokens, ld, planes) != CUDA_SUCCESS) return cudaErrorInvalidValue;
+  if (encode_operand(enc, &p.x, x, w.in, w.tokens, l.ldx, 1) != CUDA_SUCCESS) return cudaErrorInvalidValue;
   const int pairs = p.sch.waves > 0 ? kPairs : p.sch.sharers;
-  count_launch();
-  kernels[w.x.format == LM_CODE_I8 ? 0 : 1][w.dwdt == LM_F32 ? 1 : 0]<<<2 * pairs, kThreads, kSmemBytes, st>>>(p);
-  cudaError_t e = cudaGetLastError();
+  cudaError_t e = w.dwdt == LM_F32 ? start<true>(p, pairs, st) : start<false>(p, pairs, st);
   if (e != cudaSuccess || !has_parts(p.sch)) return e;
   count_launch();
   wgrad8_join_kernel<<<dim3(p.sch.rest, kTileM / 4), 256, 0, st>>>(p);
