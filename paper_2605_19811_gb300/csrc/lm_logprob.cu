@@ -1,167 +1,667 @@
 // Token log probabilities, entropy, top alternatives and their gradient
-// (formulas at lm_token_logprob_args in lionmuon.h).  One block per row.
+// (formulas at lm_token_logprob_args in lionmuon.h).
+//
+// A row is read once, 16 bytes a load; each thread keeps a running maximum m
+// with s = sum 2^d and t = sum 2^d d, d = (z - m) log2 e, and scales s and t
+// when m grows:  s <- 2^a s,  t <- 2^a (t + a s),  a = (m_old - m) log2 e <= 0.
+// d is one multiply-add z log2 e - c with c = m log2 e rounded once: c, not m,
+// is the reference, so its rounding cancels.  With the row's C, S, T:
+//   lse = ln2 (C + log2 S),  log p_j = ln2 (d_j - log2 S),  H = ln2 (log2 S - T / S)
+//   dz_j = 2^d_j (a0 + a1 d_j) (+ g_logp at the target),
+//   a1 = -g_H ln2 / S,  a0 = (g_lse - g_logp - g_H (H - ln2 log2 S)) / S
+// The gradient in the same call reads the row again, from L2: at most 2048
+// threads x 152 SMs of rows are in flight, some 60 MB.  The forward is bound by
+// memory; the gradient by memory and, at 74%, the exponential unit (16 a clock
+// and SM; two exponentials a value against 4 bytes moved in bf16).
+//
+// Values below -1e38 (masks: -inf, the type's lowest) are raised to it, which
+// changes nothing in a row whose maximum is within +-1e6.  Rows beyond that
+// take a plain loop with the differences z - m (it also sorts out rows of
+// -inf, +inf and NaN).
+//
+// Few rows: a cluster of up to eight blocks takes a row and joins its parts
+// through distributed shared memory, in order.
 #include <cuda_bf16.h>
 #include <math.h>
 
 #include "lm_train.h"
+#include "lm_tc_ptx.cuh"
 
 namespace lm {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLowest = -9.969209968386869e37f;   // -0x1.2cp126, a bf16 number: what smaller values are raised to
+constexpr float kFar = 1e6f;
+constexpr float kGone = -1e5f;                      // 2^kGone is 0
+constexpr int kMaxCluster = 8;
+constexpr int kCandidates = 1024;                   // of a block's alternatives
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+
+// 16 bytes of a row: kWidth values raised to `low`, and the largest as it is.
+template <typename T> struct Vec;
+template <> struct Vec<__nv_bfloat16> {
+  static constexpr int kWidth = 8;
+  float2 v[4];
+  float most;
+  __device__ __forceinline__ void set(uint4 u, __nv_bfloat162 low) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    __nv_bfloat162 h[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      h[k] = *reinterpret_cast<const __nv_bfloat162*>(&w[k]);
+      v[k] = __bfloat1622float2(__hmax2_nan(h[k], low));
+    }
+    const float2 m = __bfloat1622float2(__hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
+    most = fmaxf(m.x, m.y);
+  }
+  static __device__ __forceinline__ __nv_bfloat162 floor_of(float low) { return __bfloat162bfloat162(__float2bfloat16_rd(low)); }
+};
+template <> struct Vec<float> {
+  static constexpr int kWidth = 4;
+  float2 v[2];
+  float most;
+  __device__ __forceinline__ void set(uint4 u, float low) {
+    const float x[4] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
+    v[0] = make_float2(max_nan(x[0], low), max_nan(x[1], low));
+    v[1] = make_float2(max_nan(x[2], low), max_nan(x[3], low));
+    most = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+  }
+  static __device__ __forceinline__ float floor_of(float low) { return low; }
+};
 
 __device__ __forceinline__ float value(const __nv_bfloat16* p, int64_t i) { return __bfloat162float(p[i]); }
 __device__ __forceinline__ float value(const float* p, int64_t i) { return p[i]; }
 __device__ __forceinline__ void put(__nv_bfloat16* p, int64_t i, float v) { p[i] = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void put(float* p, int64_t i, float v) { p[i] = v; }
 
-// A float's place in the order of floats, as an integer.
-__device__ __forceinline__ uint32_t ordered(float x) {
-  const uint32_t u = __float_as_uint(x);
-  return u ^ ((u >> 31) ? 0xFFFFFFFFu : 0x80000000u);
+// A value's place among the alternatives: the value's order above, the lower
+// index first among equals (-0 counts as 0); 0 for a masked value.
+__device__ __forceinline__ unsigned long long key_of(float x, int j) {
+  if (!(x > -INFINITY)) return 0ull;
+  const uint32_t u = __float_as_uint(x + 0.f);
+  return ((unsigned long long)(u ^ ((u >> 31) ? 0xFFFFFFFFu : 0x80000000u)) << 32) | (uint32_t)~j;
 }
+__device__ __forceinline__ float key_value(unsigned long long k) {
+  const uint32_t o = (uint32_t)(k >> 32);
+  return __uint_as_float(o ^ ((o >> 31) ? 0x80000000u : 0xFFFFFFFFu));
+}
+__device__ __forceinline__ int key_index(unsigned long long k) { return (int)~(uint32_t)k; }
 
-template <typename F>
-__device__ __forceinline__ auto block_reduce(decltype(F::none()) v, F f) {
-  __shared__ decltype(F::none()) part[kThreads / 32];
+// How a row of `vocab` elements at z splits: `head` elements up to a 16-byte
+// boundary, nvec whole vectors, a tail.  Elements of head and tail are single.
+template <typename T>
+struct RowSplit {
+  int head, nvec, tail_at;
+  __device__ __forceinline__ RowSplit(const T* z, int vocab) {
+    constexpr int kW = 16 / (int)sizeof(T);
+    head = min(vocab, (int)(((16u - (uint32_t)(reinterpret_cast<uintptr_t>(z) & 15u)) & 15u) / sizeof(T)));
+    nvec = (vocab - head) / kW;
+    tail_at = head + nvec * kW;
+  }
+};
+// The part of a row that one block of its cluster takes.
+template <typename T>
+struct Part {
+  int v0, v1;       // vectors
+  bool single;      // this block also takes head and tail
+  __device__ __forceinline__ Part(const RowSplit<T>& r, int rank, int blocks) {
+    const int each = (r.nvec + blocks - 1) / blocks;
+    v0 = min(r.nvec, rank * each);
+    v1 = min(r.nvec, v0 + each);
+    single = rank == 0;
+  }
+};
+
+struct Stats {
+  float c, s;
+  float t;
+};
+// Sums of a thread: reference m with c = m log2 e.
+struct Running {
+  float m, c;
+  float2 s, t;
+  __device__ __forceinline__ void start() {
+    m = kLowest;
+    c = kLowest * kLog2e;
+    s = t = make_float2(0.f, 0.f);
+  }
+  __device__ __forceinline__ void raise(float to) {
+    const float c2 = to * kLog2e, a = fmaxf(c - c2, kGone), f = ex2(a);   // a s stays finite where 2^a is 0
+    t = make_float2(f * (t.x + a * s.x), f * (t.y + a * s.y));
+    s = make_float2(f * s.x, f * s.y);
+    m = to;
+    c = c2;
+  }
+  __device__ __forceinline__ void add(float2 x) {
+    const float2 d = fma2(x, make_float2(kLog2e, kLog2e), make_float2(-c, -c));
+    const float2 e = make_float2(ex2(d.x), ex2(d.y));
+    s = add2(s, e);
+    t = fma2(e, d, t);
+  }
+  __device__ __forceinline__ void add1(float x) {
+    x = max_nan(x, kLowest);
+    if (x > m) raise(x);
+    const float d = fmaf(x, kLog2e, -c), e = ex2(d);
+    s.x += e;
+    t.x += e * d;
+  }
+};
+
+template <int kThreads>
+struct Shared {
+  float red[3][kThreads / 32];
+  float zy;                                   // the target's logit
+  Stats part[kMaxCluster];                    // of every block of the cluster
+  float m_part[kMaxCluster];
+  unsigned long long group[kThreads / 4];     // the largest key of every four threads
+  unsigned long long bound;
+  int count;
+  unsigned long long cand[kCandidates];
+  unsigned long long best[kMaxCluster * 32];  // block r's alternatives at 32 r (block 0 of the cluster)
+};
+
+template <int kThreads, typename F>
+__device__ __forceinline__ float block_reduce(float v, float* part, F f) {
+#pragma unroll
   for (int o = 16; o; o >>= 1) v = f(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
-  __syncthreads();
   if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
   __syncthreads();
   v = part[0];
+#pragma unroll
   for (int w = 1; w < kThreads / 32; ++w) v = f(v, part[w]);
   return v;
 }
-struct Sum {
-  static __device__ float none() { return 0.f; }
+struct Add {
   __device__ float operator()(float a, float b) const { return a + b; }
 };
-struct Max {   // NaN where either is
-  static __device__ float none() { return -INFINITY; }
-  __device__ float operator()(float a, float b) const { return (a != a || a > b) ? a : b; }
-};
-struct MaxKey {
-  static __device__ unsigned long long none() { return 0ull; }
-  __device__ unsigned long long operator()(unsigned long long a, unsigned long long b) const { return a > b ? a : b; }
+struct Max {
+  __device__ float operator()(float a, float b) const { return fmaxf(a, b); }
 };
 
-// Largest logit and log of the sum of exponentials above it: log p_j =
-// (z_j - m) - log_s.  Kept apart, since beside a large m a sum m + log_s loses
-// log_s (a row whose logits all are the type's lowest value).
-struct RowStats {
-  float m, s, t;   // t = sum e^(z - m) (z - m)
+// What a row's outputs are made of.  Far rows hold natural-log statistics with
+// the maximum itself as reference (c = m, ls = log s, h = entropy).
+struct Row {
+  bool far, empty, bad;
+  float c, ls, h, lse;
+  __device__ __forceinline__ float logp(float z) const {
+    if (bad) return __int_as_float(0x7FC00000);
+    if (empty || z == -INFINITY) return -INFINITY;
+    if (far) return (z - c) - ls;
+    return fabsf(z) < kFar ? kLn2 * (fmaf(z, kLog2e, -c) - ls) : z - lse;
+  }
 };
-template <typename T>
-__device__ RowStats row_stats(const T* z, int vocab) {
-  float m = -INFINITY;
-  for (int j = threadIdx.x; j < vocab; j += kThreads) m = Max()(m, value(z, j));
-  m = block_reduce(m, Max());
-  float s = 0.f, t = 0.f;
+
+// The plain form of a far row's statistics, by every block of its cluster.
+template <typename T, int kThreads>
+__device__ __noinline__ void far_row(const T* z, int vocab, float (*red)[kThreads / 32], Row& row) {
+  float m = -INFINITY, bad = 0.f;
   for (int j = threadIdx.x; j < vocab; j += kThreads) {
-    const float d = value(z, j) - m, e = expf(d);
-    s += e;
-    if (e > 0.f) t += e * d;
+    const float x = value(z, j);
+    m = fmaxf(m, x);
+    if (!(x < INFINITY)) bad = 1.f;   // NaN or +inf
   }
-  return RowStats{m, block_reduce(s, Sum()), block_reduce(t, Sum())};
-}
-
-template <typename T>
-__device__ void gradient_row(const LogprobParams& p, int64_t row, const T* z, float lse, float m, float log_s, float entropy) {
-  T* d = static_cast<T*>(p.dlogits) + row * p.ld_d;
-  const int64_t y = p.targets != nullptr ? p.targets[row] : -1;
-  float gl = (p.g_logp != nullptr && y >= 0) ? p.g_logp[row] : 0.f;
-  if (y >= p.vocab) gl = __int_as_float(0x7FC00000);
-  const float gh = p.g_entropy != nullptr ? p.g_entropy[row] : 0.f;
-  const float gz = p.g_lse != nullptr ? p.g_lse[row] : 0.f;
-  const bool bad = !(lse < INFINITY) || gl != gl;
-  for (int j = threadIdx.x; j < p.vocab; j += kThreads) {
-    const float lp = (value(z, j) - m) - log_s;
-    const float e = expf(lp);
-    float g = e > 0.f ? e * (gz - gl - gh * (lp + entropy)) : 0.f;
-    if (lse == -INFINITY) g = 0.f;
-    else if (j == y) g += gl;
-    put(d, j, bad ? __int_as_float(0x7FC00000) : g);
-  }
-}
-
-template <typename T>
-__global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobParams p) {
-  const int64_t row = blockIdx.x;
-  const T* z = static_cast<const T*>(p.logits) + row * p.ld;
-  const RowStats r = row_stats(z, p.vocab);
-  const float m = r.m, log_s = logf(r.s);
+  __syncthreads();
+  m = block_reduce<kThreads>(m, red[0], Max());
+  bad = block_reduce<kThreads>(bad, red[1], Max());
+  __syncthreads();
+  row.far = true;
+  row.bad = bad != 0.f;
+  row.empty = !row.bad && m == -INFINITY;
+  float s = 0.f, t = 0.f;
+  if (!row.bad && !row.empty)
+    for (int j = threadIdx.x; j < vocab; j += kThreads) {
+      const float d = value(z, j) - m, e = expf(d);
+      s += e;
+      if (e > 0.f) t += e * d;
+    }
+  s = block_reduce<kThreads>(s, red[0], Add());
+  t = block_reduce<kThreads>(t, red[1], Add());
+  __syncthreads();
   const float nan = __int_as_float(0x7FC00000);
-  float lse = m + log_s, entropy = log_s - r.t / r.s;
-  if (m == -INFINITY) {
-    lse = -INFINITY;
-    entropy = 0.f;
-  } else if (!(m < INFINITY)) {
-    lse = entropy = nan;
+  row.c = m;
+  row.ls = logf(s);
+  row.h = row.bad ? nan : row.empty ? 0.f : row.ls - t / s;
+  row.lse = row.bad ? nan : row.empty ? -INFINITY : m + row.ls;
+}
+
+// Gradient of the part of a row that this block takes.
+template <typename T, int kThreads>
+__device__ __forceinline__ void gradient(const LogprobParams& p, int64_t row_i, const T* z, const RowSplit<T>& split, const Part<T>& part,
+                                         const Row& row, float h) {
+  constexpr int kW = Vec<T>::kWidth;
+  T* d = static_cast<T*>(p.dlogits) + row_i * p.ld_d;
+  const int64_t y = p.targets != nullptr ? p.targets[row_i] : -1;
+  float gl = (p.g_logp != nullptr && y >= 0) ? p.g_logp[row_i] : 0.f;
+  if (y >= p.vocab) gl = __int_as_float(0x7FC00000);
+  const float gh = p.g_entropy != nullptr ? p.g_entropy[row_i] : 0.f;
+  const float gz = p.g_lse != nullptr ? p.g_lse[row_i] : 0.f;
+  const bool together = ((reinterpret_cast<uintptr_t>(d) ^ reinterpret_cast<uintptr_t>(z)) & 15u) == 0;   // d's vectors lie as z's
+  if (row.bad || row.empty || row.far || gl != gl) {
+    const float fill = row.empty && gl == gl ? 0.f : __int_as_float(0x7FC00000);
+    const int j0 = part.single ? 0 : split.head + part.v0 * kW;
+    auto one = [&](int j) {
+      float g = fill;
+      if (row.far && !row.bad && !row.empty && gl == gl) {
+        const float lp = (value(z, j) - row.c) - row.ls, e = expf(lp);
+        g = (e > 0.f ? e * (gz - gl - gh * (lp + h)) : 0.f) + (j == y ? gl : 0.f);
+      }
+      put(d, j, g);
+    };
+    for (int j = j0 + threadIdx.x; j < split.head + part.v1 * kW; j += kThreads) one(j);
+    if (part.single)
+      for (int j = split.tail_at + threadIdx.x; j < p.vocab; j += kThreads) one(j);
+    return;
   }
+  // p_j (a + b lp) with p_j = 2^(d - ls)
+  const float is = ex2(-row.ls), a1 = -gh * kLn2 * is, a0 = (gz - gl - gh * (h - kLn2 * row.ls)) * is;
+  // values with p = 0 are raised to where p is still 0 and a1 d no infinity
+  const float floor = (row.c - 2000.f) * kLn2;
+  const auto low = Vec<T>::floor_of(floor);
+  auto single = [&](int j) {
+    const float x = fmaxf(value(z, j), floor), dd = fmaf(x, kLog2e, -row.c);
+    put(d, j, ex2(dd) * fmaf(a1, dd, a0) + (j == y ? gl : 0.f));
+  };
+  if (part.single) {
+    for (int j = threadIdx.x; j < split.head; j += kThreads) single(j);
+    for (int j = split.tail_at + threadIdx.x; j < p.vocab; j += kThreads) single(j);
+  }
+  const int vy = (y >= split.head && y < split.tail_at) ? (int)(y - split.head) / kW : -1;
+  const uint4* src = reinterpret_cast<const uint4*>(z + split.head);
+  T* dst = d + split.head;
+  constexpr int kBatch = 4;
+  for (int v0 = part.v0 + threadIdx.x; v0 < part.v1; v0 += kBatch * kThreads) {
+    uint4 raw[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k)
+      if (v0 + k * kThreads < part.v1) raw[k] = src[v0 + k * kThreads];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const int v = v0 + k * kThreads;
+      if (v >= part.v1) break;
+      Vec<T> x;
+      x.set(raw[k], low);
+#pragma unroll
+      for (int e = 0; e < kW / 2; ++e) {
+        const float2 dd = fma2(x.v[e], make_float2(kLog2e, kLog2e), make_float2(-row.c, -row.c));
+        x.v[e] = mul2(make_float2(ex2(dd.x), ex2(dd.y)), fma2(make_float2(a1, a1), dd, make_float2(a0, a0)));
+      }
+      if (v == vy) {
+        const int at = (int)(y - split.head) - v * kW;
+#pragma unroll
+        for (int e = 0; e < kW / 2; ++e) {
+          if (at == 2 * e) x.v[e].x += gl;
+          if (at == 2 * e + 1) x.v[e].y += gl;
+        }
+      }
+      uint4 out;
+      if constexpr (sizeof(T) == 2)
+        out = make_uint4(tc::pack_bf2(x.v[0].x, x.v[0].y), tc::pack_bf2(x.v[1].x, x.v[1].y), tc::pack_bf2(x.v[2].x, x.v[2].y), tc::pack_bf2(x.v[3].x, x.v[3].y));
+      else
+        out = make_uint4(__float_as_uint(x.v[0].x), __float_as_uint(x.v[0].y), __float_as_uint(x.v[1].x), __float_as_uint(x.v[1].y));
+      if (together) {
+        __stcs(reinterpret_cast<uint4*>(dst) + v, out);
+      } else {
+        const T* o = reinterpret_cast<const T*>(&out);
+#pragma unroll
+        for (int e = 0; e < kW; ++e) dst[(int64_t)v * kW + e] = o[e];
+      }
+    }
+  }
+}
+
+// This block's top_k alternatives, best first, into out (shared memory; 0 for
+// none).  mine: the largest key of this thread's elements.  The top_k-th
+// largest of the maxima of groups of four threads bounds the answer from
+// below; only threads whose own maximum reaches the bound can hold more of it,
+// and look through their elements again.
+template <typename T, int kThreads>
+__device__ void block_top(Shared<kThreads>& sh, const T* z, int vocab, int top_k, const RowSplit<T>& split, const Part<T>& part,
+                          unsigned long long mine, unsigned long long* out) {
+  constexpr int kW = Vec<T>::kWidth, kGroups = kThreads / 4;
+  unsigned long long g = mine;
+#pragma unroll
+  for (int o = 1; o <= 2; o <<= 1) {
+    const unsigned long long other = __shfl_xor_sync(0xFFFFFFFFu, g, o);
+    g = g > other ? g : other;
+  }
+  if ((threadIdx.x & 3) == 0) sh.group[threadIdx.x >> 2] = g;
   if (threadIdx.x == 0) {
-    if (p.lse != nullptr) p.lse[row] = lse;
-    if (p.entropy != nullptr) p.entropy[row] = entropy;
-    if (p.logp != nullptr) {
-      const int64_t y = p.targets[row];
-      float v = 0.f;
-      if (lse != lse || y >= p.vocab) v = nan;
-      else if (y >= 0) v = lse == -INFINITY ? -INFINITY : (value(z, y) - m) - log_s;
-      p.logp[row] = v;
+    sh.bound = 1ull;   // fewer than top_k groups hold anything: every element counts
+    sh.count = 0;
+  }
+  if (threadIdx.x < 32) out[threadIdx.x] = 0ull;
+  __syncthreads();
+  if (threadIdx.x < kGroups) {
+    const unsigned long long own = sh.group[threadIdx.x];
+    int above = 0;
+    for (int i = 0; i < kGroups; ++i) above += sh.group[i] > own ? 1 : 0;
+    if (own != 0ull && above == top_k - 1) sh.bound = own;
+  }
+  __syncthreads();
+  const unsigned long long bound = sh.bound;
+  if (mine >= bound) {
+    auto look = [&](int j) {
+      const unsigned long long k = key_of(value(z, j), j);
+      if (k >= bound) {
+        const int at = atomicAdd(&sh.count, 1);
+        if (at < kCandidates) sh.cand[at] = k;
+      }
+    };
+    for (int v = part.v0 + threadIdx.x; v < part.v1; v += kThreads)
+      for (int e = 0; e < kW; ++e) look(split.head + v * kW + e);
+    if (part.single) {
+      for (int j = threadIdx.x; j < split.head; j += kThreads) look(j);
+      for (int j = split.tail_at + threadIdx.x; j < vocab; j += kThreads) look(j);
     }
   }
-  // the largest keys (value, then lowest index) one after another
+  __syncthreads();
+  const int n = sh.count;
+  if (n <= kCandidates) {
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+      const unsigned long long own = sh.cand[i];
+      int above = 0;
+      for (int k = 0; k < n && above < top_k; ++k) above += sh.cand[k] > own ? 1 : 0;
+      if (above < top_k) out[above] = own;   // keys differ: one each place
+    }
+    __syncthreads();
+    return;
+  }
+  // Too many elements above the bound (all in a few threads): one after another.
   unsigned long long last = ~0ull;
-  for (int k = 0; k < p.top_k; ++k) {
+  for (int k = 0; k < top_k; ++k) {
     unsigned long long best = 0ull;
-    for (int j = threadIdx.x; j < p.vocab; j += kThreads) {
-      const float v = value(z, j);
-      const unsigned long long key = ((unsigned long long)ordered(v) << 32) | (uint32_t)~j;
-      if (v > -INFINITY && key < last && key > best) best = key;
+    auto look = [&](int j) {
+      const unsigned long long x = key_of(value(z, j), j);
+      if (x < last && x > best) best = x;
+    };
+    for (int j = split.head + part.v0 * kW + threadIdx.x; j < split.head + part.v1 * kW; j += kThreads) look(j);
+    if (part.single) {
+      for (int j = threadIdx.x; j < split.head; j += kThreads) look(j);
+      for (int j = split.tail_at + threadIdx.x; j < vocab; j += kThreads) look(j);
     }
-    best = block_reduce(best, MaxKey());
-    if (threadIdx.x == 0) {
-      const bool has = best != 0ull && lse == lse;
-      const int j = (int)~(uint32_t)best;
-      p.top_index[row * p.top_k + k] = has ? j : -1;
-      p.top_logp[row * p.top_k + k] = lse != lse ? nan : has ? (value(z, j) - m) - log_s : -INFINITY;
+    for (int o = 16; o; o >>= 1) {
+      const unsigned long long other = __shfl_xor_sync(0xFFFFFFFFu, best, o);
+      best = best > other ? best : other;
     }
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) sh.group[threadIdx.x >> 5] = best;
+    __syncthreads();
+    best = 0ull;
+    for (int w = 0; w < kThreads / 32; ++w) best = sh.group[w] > best ? sh.group[w] : best;
+    if (threadIdx.x == 0) out[k] = best;
     last = best;
   }
-  if (p.dlogits != nullptr) {
-    __syncthreads();
-    gradient_row(p, row, z, lse, m, log_s, entropy);
-  }
+  __syncthreads();
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) logprob_grad_kernel(const LogprobParams p) {
-  const int64_t row = blockIdx.x;
-  const T* z = static_cast<const T*>(p.logits) + row * p.ld;
-  const float lse = p.lse[row], entropy = p.g_entropy != nullptr ? p.entropy[row] : 0.f;
-  // lse alone gives p to 2^-24 |lse| relative; beyond 4096 the row's sums are formed anew
-  float m = lse, log_s = 0.f;
-  if (fabsf(lse) > 4096.f && fabsf(lse) < INFINITY) {
-    const RowStats r = row_stats(z, p.vocab);
-    m = r.m;
-    log_s = logf(r.s);
-    __syncthreads();
+// Loads from and stores into the shared memory of block `rank` of the cluster.
+__device__ __forceinline__ uint32_t of_block(const void* p, int rank) { return tc::peer_addr(p, (uint32_t)rank); }
+__device__ __forceinline__ void store_block(float* p, int rank, float v) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(of_block(p, rank)), "f"(v) : "memory");
+}
+__device__ __forceinline__ void store_block(unsigned long long* p, int rank, unsigned long long v) {
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(of_block(p, rank)), "l"(v) : "memory");
+}
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// kTop: with alternatives.  kCluster: several blocks a row.
+template <typename T, int kThreads, bool kTop, bool kCluster>
+__global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobParams p) {
+  constexpr int kW = Vec<T>::kWidth;
+  __shared__ Shared<kThreads> sh;
+  const int blocks = kCluster ? p.cluster : 1;
+  const int rank = kCluster ? (int)tc::cluster_rank() : 0;
+  const int64_t row_i = kCluster ? blockIdx.x / p.cluster : blockIdx.x;
+  if (kCluster) cluster_arrive();   // waited for before another block's memory is written: it has started then
+  const T* z = static_cast<const T*>(p.logits) + row_i * p.ld;
+  const RowSplit<T> split(z, p.vocab);
+  const Part<T> part(split, rank, blocks);
+  const int64_t y = p.targets != nullptr ? p.targets[row_i] : -1;
+  if (threadIdx.x == 0) sh.zy = (y >= 0 && y < p.vocab) ? value(z, y) : 0.f;   // before a gradient may be written over it
+
+  Running r;
+  r.start();
+  const auto low = Vec<T>::floor_of(kLowest);
+  float best = -INFINITY;   // the thread's largest value and where: a vector's or (negative) a single element's place
+  int best_at = 0;
+  const uint4* src = reinterpret_cast<const uint4*>(z + split.head);
+  constexpr int kBatch = 4;
+  if (part.single) {
+    for (int j = threadIdx.x; j < split.head; j += kThreads) {
+      const float x = value(z, j);
+      r.add1(x);
+      if (kTop && x > best) {
+        best = x;
+        best_at = -1 - j;
+      }
+    }
   }
-  gradient_row(p, row, z, lse, m, log_s, entropy);
+  for (int v0 = part.v0 + threadIdx.x; v0 < part.v1; v0 += kBatch * kThreads) {
+    uint4 raw[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k)
+      if (v0 + k * kThreads < part.v1) raw[k] = src[v0 + k * kThreads];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      if (v0 + k * kThreads >= part.v1) break;
+      Vec<T> x;
+      x.set(raw[k], low);
+      if (x.most > r.m) r.raise(x.most);
+      if (kTop && x.most > best) {
+        best = x.most;
+        best_at = v0 + k * kThreads;
+      }
+#pragma unroll
+      for (int e = 0; e < kW / 2; ++e) r.add(x.v[e]);
+    }
+  }
+  if (part.single) {
+    for (int j = split.tail_at + threadIdx.x; j < p.vocab; j += kThreads) {
+      const float x = value(z, j);
+      r.add1(x);
+      if (kTop && x > best) {
+        best = x;
+        best_at = -1 - j;
+      }
+    }
+  }
+  // joined over the block, then over the cluster; s is NaN where a NaN or +inf was
+  const float m = block_reduce<kThreads>(r.m, sh.red[0], Max());
+  r.raise(m);
+  float s = block_reduce<kThreads>(r.s.x + r.s.y, sh.red[1], Add());
+  float t = block_reduce<kThreads>(r.t.x + r.t.y, sh.red[2], Add());
+  float mm = m, c = r.c;
+  if (kCluster) {
+    cluster_wait();
+    if (threadIdx.x < blocks) {
+      store_block(&sh.m_part[rank], threadIdx.x, m);
+      store_block(&sh.part[rank].c, threadIdx.x, c);
+      store_block(&sh.part[rank].s, threadIdx.x, s);
+      store_block(&sh.part[rank].t, threadIdx.x, t);
+    }
+    tc::cluster_sync();
+    for (int b = 0; b < blocks; ++b) mm = fmaxf(mm, sh.m_part[b]);
+    c = mm * kLog2e;
+    s = t = 0.f;
+    for (int b = 0; b < blocks; ++b) {
+      const float a = fmaxf(sh.part[b].c - c, kGone), f = ex2(a);
+      t += f * (sh.part[b].t + a * sh.part[b].s);
+      s += f * sh.part[b].s;
+    }
+  }
+  Row row;
+  row.far = row.empty = row.bad = false;
+  row.c = c;
+  row.ls = log2f(s);
+  row.lse = kLn2 * (c + row.ls);
+  row.h = kLn2 * (row.ls - t / s);
+  if (!(s < INFINITY) || !(fabsf(mm) < kFar)) far_row<T, kThreads>(z, p.vocab, sh.red, row);
+
+  if (rank == 0 && threadIdx.x == 0) {
+    if (p.lse != nullptr) p.lse[row_i] = row.lse;
+    if (p.entropy != nullptr) p.entropy[row_i] = row.h;
+    if (p.logp != nullptr) p.logp[row_i] = (row.bad || y >= p.vocab) ? __int_as_float(0x7FC00000) : y < 0 ? 0.f : row.logp(sh.zy);
+  }
+  if constexpr (kTop) {
+    unsigned long long mine = 0ull;
+    if (best > -INFINITY) {
+      if (best_at < 0) {
+        mine = key_of(best, -1 - best_at);
+      } else {
+        for (int e = 0; e < kW; ++e) {
+          const unsigned long long k = key_of(value(z, split.head + best_at * kW + e), split.head + best_at * kW + e);
+          mine = k > mine ? k : mine;
+        }
+      }
+    }
+    unsigned long long* out = sh.best + 32 * rank;
+    block_top<T, kThreads>(sh, z, p.vocab, p.top_k, split, part, mine, out);
+    if (kCluster) {
+      if (rank != 0 && threadIdx.x < 32) store_block(&sh.best[32 * rank + threadIdx.x], 0, out[threadIdx.x]);
+      tc::cluster_sync();
+      if (rank == 0) {
+        for (int i = threadIdx.x; i < 32 * blocks; i += kThreads) {
+          const unsigned long long own = sh.best[i];
+          int above = 0;
+          for (int k = 0; k < 32 * blocks; ++k) above += sh.best[k] > own ? 1 : 0;
+          if (own != 0ull && above < p.top_k) sh.cand[above] = own;
+        }
+        __syncthreads();
+        out = sh.cand;
+      }
+    }
+    if (rank == 0) {
+      // how many places are filled: all, unless the row holds fewer values
+      int filled = p.top_k;
+      if (kCluster) {
+        filled = 0;
+        for (int i = 0; i < 32 * blocks; ++i) filled += sh.best[i] != 0ull ? 1 : 0;
+      }
+      for (int k = threadIdx.x; k < p.top_k; k += kThreads) {
+        const unsigned long long key = k < filled ? out[k] : 0ull;
+        const bool has = key != 0ull && !row.bad;
+        p.top_index[row_i * p.top_k + k] = has ? key_index(key) : -1;
+        p.top_logp[row_i * p.top_k + k] = row.bad ? __int_as_float(0x7FC00000) : has ? row.logp(key_value(key)) : -INFINITY;
+      }
+    }
+  }
+  if (p.dlogits != nullptr) {
+    if (kCluster && row.far) tc::cluster_sync();   // every block has read the whole row; it may be written over now
+    if (!kCluster) __syncthreads();
+    gradient<T, kThreads>(p, row_i, z, split, part, row, row.h);
+  }
+  if (kCluster) tc::cluster_sync();   // no block leaves while another may write into it
+}
+
+template <typename T, int kThreads, bool kCluster>
+__global__ void __launch_bounds__(kThreads) logprob_grad_kernel(const LogprobParams p) {
+  __shared__ float red[2][kThreads / 32];
+  const int rank = kCluster ? (int)(blockIdx.x % p.cluster) : 0;
+  const int64_t row_i = kCluster ? blockIdx.x / p.cluster : blockIdx.x;
+  const T* z = static_cast<const T*>(p.logits) + row_i * p.ld;
+  const RowSplit<T> split(z, p.vocab);
+  const Part<T> part(split, rank, kCluster ? p.cluster : 1);
+  const float lse = p.lse[row_i], h = p.g_entropy != nullptr ? p.entropy[row_i] : 0.f;
+  Row row;
+  row.bad = !(lse < INFINITY);
+  row.empty = lse == -INFINITY;
+  row.far = false;
+  row.c = lse * kLog2e;
+  row.ls = 0.f;
+  // lse alone gives p to 2^-24 |lse| relative; beyond 4096 the row's sums are
+  // formed anew (the launch then gives such rows to one block)
+  if (!row.bad && !row.empty && fabsf(lse) > 4096.f) far_row<T, kThreads>(z, p.vocab, red, row);
+  gradient<T, kThreads>(p, row_i, z, split, part, row, h);
+}
+
+constexpr int kSmall = 128, kLarge = 256;
+
+// Blocks a row: one where the rows fill the GPU three blocks deep; else as
+// many, up to eight, as leave each thread a vector.
+int cluster_for(int64_t rows, int64_t vectors, int threads) {
+  int c = 1;
+  while (c < kMaxCluster && rows * c < 3 * 152 && vectors / (2 * c) >= threads) c *= 2;
+  return c;
+}
+
+template <typename Kernel>
+cudaError_t start(Kernel kernel, int threads, const LogprobParams& p, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(p.rows * p.cluster), 1, 1);
+  cfg.blockDim = dim3((unsigned)threads, 1, 1);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)p.cluster;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = p.cluster > 1 ? 1 : 0;
+  count_launch();
+  return cudaLaunchKernelEx(&cfg, kernel, p);
+}
+
+template <typename T, int kThreads>
+cudaError_t forward(const LogprobParams& p, cudaStream_t st) {
+  if (p.cluster > 1)
+    return p.top_k > 0 ? start(logprob_kernel<T, kThreads, true, true>, kThreads, p, st) : start(logprob_kernel<T, kThreads, false, true>, kThreads, p, st);
+  return p.top_k > 0 ? start(logprob_kernel<T, kThreads, true, false>, kThreads, p, st) : start(logprob_kernel<T, kThreads, false, false>, kThreads, p, st);
+}
+template <typename T>
+cudaError_t launch(LogprobParams p, bool gradient_only, cudaStream_t st) {
+  const int64_t vectors = p.vocab / Vec<T>::kWidth;
+  // short rows: small blocks, so that few threads idle
+  const int threads = vectors < 2 * kLarge ? kSmall : kLarge;
+  p.cluster = cluster_for(p.rows, vectors, threads);
+  if (!gradient_only) return threads == kSmall ? forward<T, kSmall>(p, st) : forward<T, kLarge>(p, st);
+  const bool inplace = p.dlogits == p.logits;
+  if (inplace) p.cluster = 1;   // a far row is read whole by each of its blocks, before any writes
+  if (threads == kSmall)
+    return p.cluster > 1 ? start(logprob_grad_kernel<T, kSmall, true>, kSmall, p, st) : start(logprob_grad_kernel<T, kSmall, false>, kSmall, p, st);
+  return p.cluster > 1 ? start(logprob_grad_kernel<T, kLarge, true>, kLarge, p, st) : start(logprob_grad_kernel<T, kLarge, false>, kLarge, p, st);
 }
 
 }  // namespace
 
 cudaError_t launch_logprob(lm_dtype dt, const LogprobParams& p, cudaStream_t st) {
-  count_launch();
-  if (dt == LM_BF16) logprob_kernel<__nv_bfloat16><<<(unsigned)p.rows, kThreads, 0, st>>>(p);
-  else logprob_kernel<float><<<(unsigned)p.rows, kThreads, 0, st>>>(p);
-  return cudaGetLastError();
+  return dt == LM_BF16 ? launch<__nv_bfloat16>(p, false, st) : launch<float>(p, false, st);
 }
 cudaError_t launch_logprob_grad(lm_dtype dt, const LogprobParams& p, cudaStream_t st) {
-  count_launch();
-  if (dt == LM_BF16) logprob_grad_kernel<__nv_bfloat16><<<(unsigned)p.rows, kThreads, 0, st>>>(p);
-  else logprob_grad_kernel<float><<<(unsigned)p.rows, kThreads, 0, st>>>(p);
-  return cudaGetLastError();
+  return dt == LM_BF16 ? launch<__nv_bfloat16>(p, true, st) : launch<float>(p, true, st);
 }
 
 }  // namespace lm

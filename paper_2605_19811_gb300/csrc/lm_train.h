@@ -35,6 +35,7 @@ struct LogprobParams {
   const float *g_logp, *g_entropy, *g_lse;
   void* dlogits;        // NULL: no gradient
   int64_t ld_d;
+  int32_t cluster;      // blocks a row, set by the launcher
 };
 cudaError_t launch_logprob(lm_dtype dt, const LogprobParams& p, cudaStream_t st);
 // p.lse and p.entropy are read

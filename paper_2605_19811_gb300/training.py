@@ -146,7 +146,7 @@ def linear_wgrad8(dy, x: Checkpoint8, out=None, accumulate: bool = False, dtype=
             out = torch.empty((m.cols, x.cols), dtype=dtype, device=dy.device)
         w = _matrix(out, "out")
         need = lib.lm_linear_wgrad8_workspace(ctypes.byref(m), ctypes.byref(c), ctypes.byref(w))
-        ws = torch.empty(need, dtype=torch.uint8, device=dy.device) if need else None
+        ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
         _L._check(lib, lib.lm_linear_wgrad8(ctypes.byref(m), ctypes.byref(c), ctypes.byref(w), 1 if accumulate else 0,
                                             ws.data_ptr() if need else None, need, _L._stream_handle(stream)),
                   "lm_linear_wgrad8")
@@ -195,7 +195,7 @@ def rmsnorm_grad(dy, h, rstd, weight=None, dh=None, dx=None, dweight: bool = Tru
             dx = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
         dw = torch.empty(m.cols, dtype=weight.dtype if weight is not None else torch.float32, device=dy.device) if dweight else None
         need = lib.lm_rmsnorm_grad_workspace(m.rows, m.cols) if dweight else 0
-        ws = torch.empty(need, dtype=torch.uint8, device=dy.device) if need else None
+        ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
         kept = isinstance(h, Checkpoint8)
         refs = [m, None if kept else _matrix(h, "h"), h.desc() if kept else None,
                 _vector(weight, "weight") if weight is not None else None, _matrix(dh, "dh") if dh is not None else None,
