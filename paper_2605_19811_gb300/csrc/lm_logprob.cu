@@ -33,6 +33,7 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLowest = -9.969209968386869e37f;   // -0x1.2cp126, a bf16 number: what smaller values are raised to
 constexpr float kFar = 1e6f;
+constexpr float kSlack = 6.f;                       // the reference moves only when a value is this far above it
 constexpr float kGone = -1e5f;                      // 2^kGone is 0
 constexpr int kMaxCluster = 8;
 constexpr int kCandidates = 1024;                   // of a block's alternatives
@@ -70,36 +71,53 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return y;
 }
 
-// 16 bytes of a row: kWidth values raised to `low`, and the largest as it is.
+// 16 bytes of a row: kWidth values raised to `low` (Low: what that compares
+// with), and the largest of several as it is.
 template <typename T> struct Vec;
 template <> struct Vec<__nv_bfloat16> {
   static constexpr int kWidth = 8;
+  using Low = __nv_bfloat162;
   float2 v[4];
-  float most;
-  __device__ __forceinline__ void set(uint4 u, __nv_bfloat162 low) {
+  static __device__ __forceinline__ __nv_bfloat162 pair(uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); }
+  __device__ __forceinline__ Vec(uint4 u, Low low) {
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-    __nv_bfloat162 h[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      h[k] = *reinterpret_cast<const __nv_bfloat162*>(&w[k]);
-      v[k] = __bfloat1622float2(__hmax2_nan(h[k], low));
+      const __nv_bfloat162 h = __hmax2_nan(pair(w[k]), low);
+      const uint32_t b = *reinterpret_cast<const uint32_t*>(&h);
+      v[k] = make_float2(tc::bf_lo(b), tc::bf_hi(b));
     }
-    const float2 m = __bfloat1622float2(__hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
-    most = fmaxf(m.x, m.y);
   }
-  static __device__ __forceinline__ __nv_bfloat162 floor_of(float low) { return __bfloat162bfloat162(__float2bfloat16_rd(low)); }
+  template <int kN>
+  static __device__ __forceinline__ float most(const uint4 (&u)[kN]) {
+    __nv_bfloat162 m = pair(u[0].x);
+#pragma unroll
+    for (int k = 0; k < kN; ++k) {
+      if (k > 0) m = __hmax2(m, pair(u[k].x));
+      m = __hmax2(__hmax2(m, pair(u[k].y)), __hmax2(pair(u[k].z), pair(u[k].w)));
+    }
+    const uint32_t b = *reinterpret_cast<const uint32_t*>(&m);
+    return fmaxf(tc::bf_lo(b), tc::bf_hi(b));
+  }
+  static __device__ __forceinline__ Low floor_of(float low) { return __bfloat162bfloat162(__float2bfloat16_rd(low)); }
 };
 template <> struct Vec<float> {
   static constexpr int kWidth = 4;
+  using Low = float;
   float2 v[2];
-  float most;
-  __device__ __forceinline__ void set(uint4 u, float low) {
-    const float x[4] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
-    v[0] = make_float2(max_nan(x[0], low), max_nan(x[1], low));
-    v[1] = make_float2(max_nan(x[2], low), max_nan(x[3], low));
-    most = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+  __device__ __forceinline__ Vec(uint4 u, Low low) {
+    v[0] = make_float2(max_nan(__uint_as_float(u.x), low), max_nan(__uint_as_float(u.y), low));
+    v[1] = make_float2(max_nan(__uint_as_float(u.z), low), max_nan(__uint_as_float(u.w), low));
   }
-  static __device__ __forceinline__ float floor_of(float low) { return low; }
+  template <int kN>
+  static __device__ __forceinline__ float most(const uint4 (&u)[kN]) {
+    float m = __uint_as_float(u[0].x);
+#pragma unroll
+    for (int k = 0; k < kN; ++k)
+      m = fmaxf(fmaxf(fmaxf(m, __uint_as_float(u[k].x)), fmaxf(__uint_as_float(u[k].y), __uint_as_float(u[k].z))), __uint_as_float(u[k].w));
+    return m;
+  }
+  static __device__ __forceinline__ Low floor_of(float low) { return low; }
 };
 
 __device__ __forceinline__ float value(const __nv_bfloat16* p, int64_t i) { return __bfloat162float(p[i]); }
@@ -145,17 +163,21 @@ struct Part {
   }
 };
 
+// Vectors a thread loads ahead: more for long rows, which have the registers' time.
+constexpr int ahead_of(int threads) { return threads == 128 ? 2 : 4; }
+
 struct Stats {
   float c, s;
   float t;
 };
 // Sums of a thread: reference m with c = m log2 e.
 struct Running {
-  float m, c;
+  float m, c, limit;   // limit: what a value may reach before m moves
   float2 s, t;
   __device__ __forceinline__ void start() {
     m = kLowest;
     c = kLowest * kLog2e;
+    limit = kLowest;
     s = t = make_float2(0.f, 0.f);
   }
   __device__ __forceinline__ void raise(float to) {
@@ -163,6 +185,7 @@ struct Running {
     t = make_float2(f * (t.x + a * s.x), f * (t.y + a * s.y));
     s = make_float2(f * s.x, f * s.y);
     m = to;
+    limit = to + kSlack;
     c = c2;
   }
   __device__ __forceinline__ void add(float2 x) {
@@ -173,19 +196,21 @@ struct Running {
   }
   __device__ __forceinline__ void add1(float x) {
     x = max_nan(x, kLowest);
-    if (x > m) raise(x);
+    if (x > limit) raise(x);
     const float d = fmaf(x, kLog2e, -c), e = ex2(d);
     s.x += e;
     t.x += e * d;
   }
 };
 
-template <int kThreads>
+template <int kThreads, bool kTop>
 struct Shared {
-  float red[3][kThreads / 32];
-  float zy;                                   // the target's logit
+  float join[3][kThreads / 32], red[2][kThreads / 32];
   Stats part[kMaxCluster];                    // of every block of the cluster
   float m_part[kMaxCluster];
+};
+template <int kThreads>
+struct Shared<kThreads, true> : Shared<kThreads, false> {
   unsigned long long group[kThreads / 4];     // the largest key of every four threads
   unsigned long long bound;
   int count;
@@ -216,6 +241,12 @@ struct Max {
 struct Row {
   bool far, empty, bad;
   float c, ls, h, lse;
+  Row() = default;
+  __device__ __forceinline__ Row(float c_, float s, float t) : far(false), empty(false), bad(false), c(c_) {
+    ls = log2f(s);
+    lse = kLn2 * (c + ls);
+    h = kLn2 * (ls - t / s);
+  }
   __device__ __forceinline__ float logp(float z) const {
     if (bad) return __int_as_float(0x7FC00000);
     if (empty || z == -INFINITY) return -INFINITY;
@@ -257,17 +288,114 @@ __device__ __noinline__ void far_row(const T* z, int vocab, float (*red)[kThread
   row.lse = row.bad ? nan : row.empty ? -INFINITY : m + row.ls;
 }
 
+// Every kThreads-th vector of [0, n), a batch of kBatch loaded ahead of the one
+// at work.  f takes an array of vectors, kThreads apart, and the first one's
+// place: kBatch of them, or one where the batch passes the end.
+template <int kThreads, int kBatch, typename F>
+__device__ __forceinline__ void walk(const uint4* src, int n, F f) {
+  uint4 ahead[kBatch];
+  int v = (int)threadIdx.x;
+#pragma unroll
+  for (int k = 0; k < kBatch; ++k)
+    if (v + k * kThreads < n) ahead[k] = src[v + k * kThreads];
+  for (; v < n; v += kBatch * kThreads) {
+    uint4 now[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      now[k] = ahead[k];
+      if (v + (kBatch + k) * kThreads < n) ahead[k] = src[v + (kBatch + k) * kThreads];
+    }
+    if (v + (kBatch - 1) * kThreads < n) {
+      f(now, v);
+    } else {
+#pragma unroll
+      for (int k = 0; k < kBatch - 1; ++k)
+        if (v + k * kThreads < n) {
+          const uint4 one[1] = {now[k]};
+          f(one, v + k * kThreads);
+        }
+    }
+  }
+}
+
+// What a row's end needs, asked for at its start: its target and the loss's weights.
+struct RowArgs {
+  int64_t y;
+  float gl, gh, gz;
+  __device__ __forceinline__ RowArgs(const LogprobParams& p, int64_t row_i, bool grad) : gl(0.f), gh(0.f), gz(0.f) {
+    y = p.targets != nullptr ? p.targets[row_i] : -1;
+    if (!grad) return;
+    if (p.g_logp != nullptr) gl = p.g_logp[row_i];
+    if (p.g_entropy != nullptr) gh = p.g_entropy[row_i];
+    if (p.g_lse != nullptr) gz = p.g_lse[row_i];
+  }
+  // the weight of log p_y: 0 without a target, NaN for one beyond the vocabulary
+  __device__ __forceinline__ float weight(int vocab) const { return y < 0 ? 0.f : y >= vocab ? __int_as_float(0x7FC00000) : gl; }
+};
+
+// A row's gradient, value by value: p_j (a + b lp) with p_j = 2^(d - ls), and
+// g_logp more at the target.
+template <typename T>
+struct Slope {
+  static constexpr int kW = Vec<T>::kWidth;
+  float c, a0, a1, gl, floor;
+  int y, vy, ey;                                  // the target, its vector and its place there (-1: none)
+  typename Vec<T>::Low low;
+  __device__ __forceinline__ Slope(const Row& row, float h, float gl_, float gh, float gz, int64_t target, const RowSplit<T>& split) {
+    const float is = ex2(-row.ls);
+    c = row.c;
+    a1 = -gh * kLn2 * is;
+    a0 = (gz - gl_ - gh * (h - kLn2 * row.ls)) * is;
+    gl = gl_;
+    // values with p = 0 are raised to where p is still 0 and a1 d no infinity
+    floor = (c - 2000.f) * kLn2;
+    low = Vec<T>::floor_of(floor);
+    y = (int)target;
+    const bool in = target >= split.head && target < split.tail_at;
+    vy = in ? (y - split.head) / kW : -1;
+    ey = in ? (y - split.head) % kW : -1;
+  }
+  __device__ __forceinline__ float single(float z, int j) const {
+    const float d = fmaf(fmaxf(z, floor), kLog2e, -c);
+    return ex2(d) * fmaf(a1, d, a0) + (j == y ? gl : 0.f);
+  }
+  __device__ __forceinline__ void vector(uint4 raw, int v, T* dst, bool together) const {
+    Vec<T> x(raw, low);
+#pragma unroll
+    for (int e = 0; e < kW / 2; ++e) {
+      const float2 d = fma2(x.v[e], make_float2(kLog2e, kLog2e), make_float2(-c, -c));
+      x.v[e] = mul2(make_float2(ex2(d.x), ex2(d.y)), fma2(make_float2(a1, a1), d, make_float2(a0, a0)));
+    }
+    if (v == vy) {
+#pragma unroll
+      for (int e = 0; e < kW / 2; ++e) {
+        if (ey == 2 * e) x.v[e].x += gl;
+        if (ey == 2 * e + 1) x.v[e].y += gl;
+      }
+    }
+    uint4 out;
+    if constexpr (sizeof(T) == 2)
+      out = make_uint4(tc::pack_bf2(x.v[0].x, x.v[0].y), tc::pack_bf2(x.v[1].x, x.v[1].y), tc::pack_bf2(x.v[2].x, x.v[2].y), tc::pack_bf2(x.v[3].x, x.v[3].y));
+    else
+      out = make_uint4(__float_as_uint(x.v[0].x), __float_as_uint(x.v[0].y), __float_as_uint(x.v[1].x), __float_as_uint(x.v[1].y));
+    if (together) {
+      __stcs(reinterpret_cast<uint4*>(dst) + v, out);
+    } else {
+      const T* o = reinterpret_cast<const T*>(&out);
+#pragma unroll
+      for (int e = 0; e < kW; ++e) dst[(int64_t)v * kW + e] = o[e];
+    }
+  }
+};
+
 // Gradient of the part of a row that this block takes.
 template <typename T, int kThreads>
 __device__ __forceinline__ void gradient(const LogprobParams& p, int64_t row_i, const T* z, const RowSplit<T>& split, const Part<T>& part,
-                                         const Row& row, float h) {
+                                         const Row& row, float h, const RowArgs& args) {
   constexpr int kW = Vec<T>::kWidth;
   T* d = static_cast<T*>(p.dlogits) + row_i * p.ld_d;
-  const int64_t y = p.targets != nullptr ? p.targets[row_i] : -1;
-  float gl = (p.g_logp != nullptr && y >= 0) ? p.g_logp[row_i] : 0.f;
-  if (y >= p.vocab) gl = __int_as_float(0x7FC00000);
-  const float gh = p.g_entropy != nullptr ? p.g_entropy[row_i] : 0.f;
-  const float gz = p.g_lse != nullptr ? p.g_lse[row_i] : 0.f;
+  const int64_t y = args.y;
+  const float gl = args.weight(p.vocab), gh = args.gh, gz = args.gz;
   const bool together = ((reinterpret_cast<uintptr_t>(d) ^ reinterpret_cast<uintptr_t>(z)) & 15u) == 0;   // d's vectors lie as z's
   if (row.bad || row.empty || row.far || gl != gl) {
     const float fill = row.empty && gl == gl ? 0.f : __int_as_float(0x7FC00000);
@@ -285,61 +413,33 @@ __device__ __forceinline__ void gradient(const LogprobParams& p, int64_t row_i, 
       for (int j = split.tail_at + threadIdx.x; j < p.vocab; j += kThreads) one(j);
     return;
   }
-  // p_j (a + b lp) with p_j = 2^(d - ls)
-  const float is = ex2(-row.ls), a1 = -gh * kLn2 * is, a0 = (gz - gl - gh * (h - kLn2 * row.ls)) * is;
-  // values with p = 0 are raised to where p is still 0 and a1 d no infinity
-  const float floor = (row.c - 2000.f) * kLn2;
-  const auto low = Vec<T>::floor_of(floor);
-  auto single = [&](int j) {
-    const float x = fmaxf(value(z, j), floor), dd = fmaf(x, kLog2e, -row.c);
-    put(d, j, ex2(dd) * fmaf(a1, dd, a0) + (j == y ? gl : 0.f));
-  };
+  const Slope<T> g(row, h, gl, gh, gz, y, split);
+  auto single = [&](int j) { put(d, j, g.single(value(z, j), j)); };
   if (part.single) {
     for (int j = threadIdx.x; j < split.head; j += kThreads) single(j);
     for (int j = split.tail_at + threadIdx.x; j < p.vocab; j += kThreads) single(j);
   }
-  const int vy = (y >= split.head && y < split.tail_at) ? (int)(y - split.head) / kW : -1;
-  const uint4* src = reinterpret_cast<const uint4*>(z + split.head);
   T* dst = d + split.head;
-  constexpr int kBatch = 4;
-  for (int v0 = part.v0 + threadIdx.x; v0 < part.v1; v0 += kBatch * kThreads) {
-    uint4 raw[kBatch];
+  walk<kThreads, ahead_of(kThreads)>(reinterpret_cast<const uint4*>(z + split.head) + part.v0, part.v1 - part.v0, [&](const auto& raw, int i) {
+    constexpr int kN = sizeof(raw) / sizeof(raw[0]);
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k)
-      if (v0 + k * kThreads < part.v1) raw[k] = src[v0 + k * kThreads];
-#pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      const int v = v0 + k * kThreads;
-      if (v >= part.v1) break;
-      Vec<T> x;
-      x.set(raw[k], low);
-#pragma unroll
-      for (int e = 0; e < kW / 2; ++e) {
-        const float2 dd = fma2(x.v[e], make_float2(kLog2e, kLog2e), make_float2(-row.c, -row.c));
-        x.v[e] = mul2(make_float2(ex2(dd.x), ex2(dd.y)), fma2(make_float2(a1, a1), dd, make_float2(a0, a0)));
-      }
-      if (v == vy) {
-        const int at = (int)(y - split.head) - v * kW;
-#pragma unroll
-        for (int e = 0; e < kW / 2; ++e) {
-          if (at == 2 * e) x.v[e].x += gl;
-          if (at == 2 * e + 1) x.v[e].y += gl;
-        }
-      }
-      uint4 out;
-      if constexpr (sizeof(T) == 2)
-        out = make_uint4(tc::pack_bf2(x.v[0].x, x.v[0].y), tc::pack_bf2(x.v[1].x, x.v[1].y), tc::pack_bf2(x.v[2].x, x.v[2].y), tc::pack_bf2(x.v[3].x, x.v[3].y));
-      else
-        out = make_uint4(__float_as_uint(x.v[0].x), __float_as_uint(x.v[0].y), __float_as_uint(x.v[1].x), __float_as_uint(x.v[1].y));
-      if (together) {
-        __stcs(reinterpret_cast<uint4*>(dst) + v, out);
-      } else {
-        const T* o = reinterpret_cast<const T*>(&out);
-#pragma unroll
-        for (int e = 0; e < kW; ++e) dst[(int64_t)v * kW + e] = o[e];
-      }
+    for (int k = 0; k < kN; ++k) g.vector(raw[k], part.v0 + i + k * kThreads, dst, together);
+  });
+}
+
+// The key of a thread's largest value, found in the batch of vectors at a place, or (negative) at a single element's.
+template <typename T, int kThreads>
+__device__ __forceinline__ unsigned long long thread_key(const T* z, const RowSplit<T>& split, const Part<T>& part, float best, int best_at) {
+  if (!(best > -INFINITY)) return 0ull;
+  if (best_at < 0) return key_of(best, -1 - best_at);
+  unsigned long long mine = 0ull;
+  for (int b = 0; b < ahead_of(kThreads) && best_at + b * kThreads < part.v1; ++b)
+    for (int e = 0; e < Vec<T>::kWidth; ++e) {
+      const int j = split.head + (best_at + b * kThreads) * Vec<T>::kWidth + e;
+      const unsigned long long k = key_of(value(z, j), j);
+      mine = k > mine ? k : mine;
     }
-  }
+  return mine;
 }
 
 // This block's top_k alternatives, best first, into out (shared memory; 0 for
@@ -348,8 +448,8 @@ __device__ __forceinline__ void gradient(const LogprobParams& p, int64_t row_i, 
 // below; only threads whose own maximum reaches the bound can hold more of it,
 // and look through their elements again.
 template <typename T, int kThreads>
-__device__ void block_top(Shared<kThreads>& sh, const T* z, int vocab, int top_k, const RowSplit<T>& split, const Part<T>& part,
-                          unsigned long long mine, unsigned long long* out) {
+__device__ void block_top(Shared<kThreads, true>& sh, const T* z, int vocab, int top_k, const RowSplit<T>& split, const Part<T>& part,
+                          unsigned long long mine, bool whole, unsigned long long* out) {
   constexpr int kW = Vec<T>::kWidth, kGroups = kThreads / 4;
   unsigned long long g = mine;
 #pragma unroll
@@ -372,7 +472,7 @@ __device__ void block_top(Shared<kThreads>& sh, const T* z, int vocab, int top_k
   }
   __syncthreads();
   const unsigned long long bound = sh.bound;
-  if (mine >= bound) {
+  if (mine >= bound && !whole) {
     auto look = [&](int j) {
       const unsigned long long k = key_of(value(z, j), j);
       if (k >= bound) {
@@ -389,7 +489,7 @@ __device__ void block_top(Shared<kThreads>& sh, const T* z, int vocab, int top_k
   }
   __syncthreads();
   const int n = sh.count;
-  if (n <= kCandidates) {
+  if (n <= kCandidates && !whole) {
     for (int i = threadIdx.x; i < n; i += kThreads) {
       const unsigned long long own = sh.cand[i];
       int above = 0;
@@ -427,7 +527,18 @@ __device__ void block_top(Shared<kThreads>& sh, const T* z, int vocab, int top_k
   __syncthreads();
 }
 
-// Loads from and stores into the shared memory of block `rank` of the cluster.
+__device__ __forceinline__ void put_stats(const LogprobParams& p, int64_t row_i, int64_t y, float zy, const Row& row) {
+  if (p.lse != nullptr) p.lse[row_i] = row.lse;
+  if (p.entropy != nullptr) p.entropy[row_i] = row.h;
+  if (p.logp != nullptr) p.logp[row_i] = (row.bad || y >= p.vocab) ? __int_as_float(0x7FC00000) : y < 0 ? 0.f : row.logp(zy);
+}
+__device__ __forceinline__ void put_top(const LogprobParams& p, int64_t row_i, int k, unsigned long long key, const Row& row) {
+  const bool has = key != 0ull && !row.bad;
+  p.top_index[row_i * p.top_k + k] = has ? key_index(key) : -1;
+  p.top_logp[row_i * p.top_k + k] = row.bad ? __int_as_float(0x7FC00000) : has ? row.logp(key_value(key)) : -INFINITY;
+}
+
+// Stores into the shared memory of block `rank` of the cluster.
 __device__ __forceinline__ uint32_t of_block(const void* p, int rank) { return tc::peer_addr(p, (uint32_t)rank); }
 __device__ __forceinline__ void store_block(float* p, int rank, float v) {
   asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(of_block(p, rank)), "f"(v) : "memory");
@@ -443,7 +554,7 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 template <typename T, int kThreads, bool kTop, bool kCluster>
 __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobParams p) {
   constexpr int kW = Vec<T>::kWidth;
-  __shared__ Shared<kThreads> sh;
+  __shared__ Shared<kThreads, kTop> sh;
   const int blocks = kCluster ? p.cluster : 1;
   const int rank = kCluster ? (int)tc::cluster_rank() : 0;
   const int64_t row_i = kCluster ? blockIdx.x / p.cluster : blockIdx.x;
@@ -451,16 +562,16 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobParams p
   const T* z = static_cast<const T*>(p.logits) + row_i * p.ld;
   const RowSplit<T> split(z, p.vocab);
   const Part<T> part(split, rank, blocks);
-  const int64_t y = p.targets != nullptr ? p.targets[row_i] : -1;
-  if (threadIdx.x == 0) sh.zy = (y >= 0 && y < p.vocab) ? value(z, y) : 0.f;   // before a gradient may be written over it
+  const int n = part.v1 - part.v0;
+  const uint4* src = reinterpret_cast<const uint4*>(z + split.head) + part.v0;
+  const RowArgs args(p, row_i, p.dlogits != nullptr);
+  const int64_t y = args.y;
 
   Running r;
   r.start();
   const auto low = Vec<T>::floor_of(kLowest);
   float best = -INFINITY;   // the thread's largest value and where: a vector's or (negative) a single element's place
   int best_at = 0;
-  const uint4* src = reinterpret_cast<const uint4*>(z + split.head);
-  constexpr int kBatch = 4;
   if (part.single) {
     for (int j = threadIdx.x; j < split.head; j += kThreads) {
       const float x = value(z, j);
@@ -471,25 +582,21 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobParams p
       }
     }
   }
-  for (int v0 = part.v0 + threadIdx.x; v0 < part.v1; v0 += kBatch * kThreads) {
-    uint4 raw[kBatch];
+  walk<kThreads, ahead_of(kThreads)>(src, n, [&](const auto& raw, int i) {
+    constexpr int kN = sizeof(raw) / sizeof(raw[0]);
+    const float most = Vec<T>::most(raw);
+    if (most > r.limit) r.raise(most);
+    if (kTop && most > best) {
+      best = most;
+      best_at = part.v0 + i;
+    }
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k)
-      if (v0 + k * kThreads < part.v1) raw[k] = src[v0 + k * kThreads];
-#pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      if (v0 + k * kThreads >= part.v1) break;
-      Vec<T> x;
-      x.set(raw[k], low);
-      if (x.most > r.m) r.raise(x.most);
-      if (kTop && x.most > best) {
-        best = x.most;
-        best_at = v0 + k * kThreads;
-      }
+    for (int k = 0; k < kN; ++k) {
+      const Vec<T> x(raw[k], low);
 #pragma unroll
       for (int e = 0; e < kW / 2; ++e) r.add(x.v[e]);
     }
-  }
+  });
   if (part.single) {
     for (int j = split.tail_at + threadIdx.x; j < p.vocab; j += kThreads) {
       const float x = value(z, j);
@@ -500,16 +607,48 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobParams p
       }
     }
   }
-  // joined over the block, then over the cluster; s is NaN where a NaN or +inf was
-  const float m = block_reduce<kThreads>(r.m, sh.red[0], Max());
+  // the target's logit, before a gradient may be written over it
+  const float zy = (threadIdx.x == 0 && y >= 0 && y < p.vocab) ? value(z, y) : 0.f;
+  // Joined over the warp, the block (every warp joins the warps' sums for itself)
+  // and the cluster; s is NaN where a NaN or +inf was.
+  constexpr int kWarps = kThreads / 32;
+  float m = r.m;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
   r.raise(m);
-  float s = block_reduce<kThreads>(r.s.x + r.s.y, sh.red[1], Add());
-  float t = block_reduce<kThreads>(r.t.x + r.t.y, sh.red[2], Add());
-  float mm = m, c = r.c;
+  float s = r.s.x + r.s.y, t = r.t.x + r.t.y;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
+  }
+  if ((threadIdx.x & 31) == 0) {
+    sh.join[0][threadIdx.x >> 5] = m;
+    sh.join[1][threadIdx.x >> 5] = s;
+    sh.join[2][threadIdx.x >> 5] = t;
+  }
+  __syncthreads();
+  m = sh.join[0][threadIdx.x & (kWarps - 1)];
+  s = sh.join[1][threadIdx.x & (kWarps - 1)];
+  t = sh.join[2][threadIdx.x & (kWarps - 1)];
+  float mm = m;
+#pragma unroll
+  for (int o = kWarps / 2; o; o >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xFFFFFFFFu, mm, o));
+  float c = mm * kLog2e;
+  {
+    const float a = fmaxf(m * kLog2e - c, kGone), f = ex2(a);
+    t = f * (t + a * s);
+    s = f * s;
+  }
+#pragma unroll
+  for (int o = kWarps / 2; o; o >>= 1) {
+    s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
+  }
   if (kCluster) {
     cluster_wait();
     if (threadIdx.x < blocks) {
-      store_block(&sh.m_part[rank], threadIdx.x, m);
+      store_block(&sh.m_part[rank], threadIdx.x, mm);
       store_block(&sh.part[rank].c, threadIdx.x, c);
       store_block(&sh.part[rank].s, threadIdx.x, s);
       store_block(&sh.part[rank].t, threadIdx.x, t);
@@ -524,33 +663,14 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobParams p
       s += f * sh.part[b].s;
     }
   }
-  Row row;
-  row.far = row.empty = row.bad = false;
-  row.c = c;
-  row.ls = log2f(s);
-  row.lse = kLn2 * (c + row.ls);
-  row.h = kLn2 * (row.ls - t / s);
+  Row row(c, s, t);
   if (!(s < INFINITY) || !(fabsf(mm) < kFar)) far_row<T, kThreads>(z, p.vocab, sh.red, row);
 
-  if (rank == 0 && threadIdx.x == 0) {
-    if (p.lse != nullptr) p.lse[row_i] = row.lse;
-    if (p.entropy != nullptr) p.entropy[row_i] = row.h;
-    if (p.logp != nullptr) p.logp[row_i] = (row.bad || y >= p.vocab) ? __int_as_float(0x7FC00000) : y < 0 ? 0.f : row.logp(sh.zy);
-  }
+  if (rank == 0 && threadIdx.x == 0) put_stats(p, row_i, y, zy, row);
   if constexpr (kTop) {
-    unsigned long long mine = 0ull;
-    if (best > -INFINITY) {
-      if (best_at < 0) {
-        mine = key_of(best, -1 - best_at);
-      } else {
-        for (int e = 0; e < kW; ++e) {
-          const unsigned long long k = key_of(value(z, split.head + best_at * kW + e), split.head + best_at * kW + e);
-          mine = k > mine ? k : mine;
-        }
-      }
-    }
+    const unsigned long long mine = thread_key<T, kThreads>(z, split, part, best, best_at);
     unsigned long long* out = sh.best + 32 * rank;
-    block_top<T, kThreads>(sh, z, p.vocab, p.top_k, split, part, mine, out);
+    block_top<T, kThreads>(sh, z, p.vocab, p.top_k, split, part, mine, row.far, out);
     if (kCluster) {
       if (rank != 0 && threadIdx.x < 32) store_block(&sh.best[32 * rank + threadIdx.x], 0, out[threadIdx.x]);
       tc::cluster_sync();
@@ -572,18 +692,13 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobParams p
         filled = 0;
         for (int i = 0; i < 32 * blocks; ++i) filled += sh.best[i] != 0ull ? 1 : 0;
       }
-      for (int k = threadIdx.x; k < p.top_k; k += kThreads) {
-        const unsigned long long key = k < filled ? out[k] : 0ull;
-        const bool has = key != 0ull && !row.bad;
-        p.top_index[row_i * p.top_k + k] = has ? key_index(key) : -1;
-        p.top_logp[row_i * p.top_k + k] = row.bad ? __int_as_float(0x7FC00000) : has ? row.logp(key_value(key)) : -INFINITY;
-      }
+      for (int k = threadIdx.x; k < p.top_k; k += kThreads) put_top(p, row_i, k, k < filled ? out[k] : 0ull, row);
     }
   }
   if (p.dlogits != nullptr) {
     if (kCluster && row.far) tc::cluster_sync();   // every block has read the whole row; it may be written over now
     if (!kCluster) __syncthreads();
-    gradient<T, kThreads>(p, row_i, z, split, part, row, row.h);
+    gradient<T, kThreads>(p, row_i, z, split, part, row, row.h, args);
   }
   if (kCluster) tc::cluster_sync();   // no block leaves while another may write into it
 }
@@ -596,6 +711,7 @@ __global__ void __launch_bounds__(kThreads) logprob_grad_kernel(const LogprobPar
   const T* z = static_cast<const T*>(p.logits) + row_i * p.ld;
   const RowSplit<T> split(z, p.vocab);
   const Part<T> part(split, rank, kCluster ? p.cluster : 1);
+  const RowArgs args(p, row_i, true);
   const float lse = p.lse[row_i], h = p.g_entropy != nullptr ? p.entropy[row_i] : 0.f;
   Row row;
   row.bad = !(lse < INFINITY);
@@ -606,10 +722,10 @@ __global__ void __launch_bounds__(kThreads) logprob_grad_kernel(const LogprobPar
   // lse alone gives p to 2^-24 |lse| relative; beyond 4096 the row's sums are
   // formed anew (the launch then gives such rows to one block)
   if (!row.bad && !row.empty && fabsf(lse) > 4096.f) far_row<T, kThreads>(z, p.vocab, red, row);
-  gradient<T, kThreads>(p, row_i, z, split, part, row, h);
+  gradient<T, kThreads>(p, row_i, z, split, part, row, h, args);
 }
 
-constexpr int kSmall = 128, kLarge = 256;
+constexpr int kShort = 1280;   // vectors of a row up to which 128 threads take it
 
 // Blocks a row: one where the rows fill the GPU three blocks deep; else as
 // many, up to eight, as leave each thread a vector.
@@ -644,15 +760,17 @@ cudaError_t forward(const LogprobParams& p, cudaStream_t st) {
 template <typename T>
 cudaError_t launch(LogprobParams p, bool gradient_only, cudaStream_t st) {
   const int64_t vectors = p.vocab / Vec<T>::kWidth;
-  // short rows: small blocks, so that few threads idle
-  const int threads = vectors < 2 * kLarge ? kSmall : kLarge;
+  if (gradient_only) {
+    // short rows: small blocks, so that few threads idle
+    const int threads = vectors < 512 ? 128 : 256;
+    p.cluster = p.dlogits == p.logits ? 1 : cluster_for(p.rows, vectors, threads);   // a far row is read whole by each of its blocks, before any writes
+    if (threads == 128)
+      return p.cluster > 1 ? start(logprob_grad_kernel<T, 128, true>, 128, p, st) : start(logprob_grad_kernel<T, 128, false>, 128, p, st);
+    return p.cluster > 1 ? start(logprob_grad_kernel<T, 256, true>, 256, p, st) : start(logprob_grad_kernel<T, 256, false>, 256, p, st);
+  }
+  const int threads = vectors <= kShort ? 128 : 256;
   p.cluster = cluster_for(p.rows, vectors, threads);
-  if (!gradient_only) return threads == kSmall ? forward<T, kSmall>(p, st) : forward<T, kLarge>(p, st);
-  const bool inplace = p.dlogits == p.logits;
-  if (inplace) p.cluster = 1;   // a far row is read whole by each of its blocks, before any writes
-  if (threads == kSmall)
-    return p.cluster > 1 ? start(logprob_grad_kernel<T, kSmall, true>, kSmall, p, st) : start(logprob_grad_kernel<T, kSmall, false>, kSmall, p, st);
-  return p.cluster > 1 ? start(logprob_grad_kernel<T, kLarge, true>, kLarge, p, st) : start(logprob_grad_kernel<T, kLarge, false>, kLarge, p, st);
+  return threads == 128 ? forward<T, 128>(p, st) : forward<T, 256>(p, st);
 }
 
 }  // namespace

@@ -100,6 +100,33 @@ def test_forward_and_both_gradients(rows, vocab, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,vocab", [(609, 16400), (1000, 8200), (700, 36000), (620, 70001)])
+def test_many_long_rows(rows, vocab, dtype):
+    """Enough rows for every SM several times over, pitches that shift the
+    rows' alignment, masked and missing rows among them; in place as well."""
+    from paper_2605_19811_gb300 import training as T
+    z, y, w = make(rows, vocab, dtype, pad=3, offset=1, seed=rows)
+    z.t[5] = float("-inf")
+    z.t[170, 100:] = float("-inf")
+    z.t[171, 7] = float("nan")
+    z.t[300] = torch.finfo(DT[dtype]).min
+    z.t[rows - 1, ::3] = float("-inf")
+    y[11], y[200] = -100, vocab
+    o = T.token_logprob(z.t, y, top_k=3)
+    check_forward(z.t, y, o, 3)
+    d = Held(rows, vocab, DT[dtype], 3, 1)
+    q = T.token_logprob(z.t, y, top_k=3, g_logp=w[0], g_entropy=w[1], g_lse=w[2], dlogits=d.t)
+    check_forward(z.t, y, q, 3)                 # (another kernel may have summed in another order)
+    check_gradient(z.t, y, d.t, w, dtype)
+    assert d.untouched() and z.untouched()
+    d2 = Held(rows, vocab, DT[dtype], 2, 0)     # vectors that do not line up with the logits'
+    T.token_logprob(z.t, y, g_logp=w[0], g_entropy=w[1], g_lse=w[2], dlogits=d2.t)
+    assert torch.equal(d.t.nan_to_num(9.0), d2.t.nan_to_num(9.0)) and d2.untouched()
+    T.token_logprob(z.t, y, g_logp=w[0], g_entropy=w[1], g_lse=w[2], dlogits=z.t)
+    assert torch.equal(d.t.nan_to_num(9.0), z.t.nan_to_num(9.0)) and z.untouched()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("vocab", [65, 1504, 50304])
 def test_masks_infinities_and_missing_targets(vocab, dtype):
     from paper_2605_19811_gb300 import training as T
@@ -152,7 +179,7 @@ def test_a_row_at_the_lowest_value_is_uniform(dtype):
 
 @pytest.mark.parametrize("order", ["rising", "falling", "one stride", "ties", "two values"])
 @pytest.mark.parametrize("top_k", [1, 7, 32])
-@pytest.mark.parametrize("rows,vocab", [(2, 50304), (400, 20000), (3, 33)])
+@pytest.mark.parametrize("rows,vocab", [(2, 50304), (400, 20000), (3, 33), (700, 20000)])
 def test_alternatives_in_hard_orders(rows, vocab, top_k, order):
     """Arrangements that crowd the largest logits: sorted rows, all of them at
     one stride, many ties."""
