@@ -164,7 +164,8 @@ struct Part {
 };
 
 // Vectors a thread loads ahead: more for long rows, which have the registers' time.
-constexpr int ahead_of(int threads) { return threads == 128 ? 2 : 4; }
+template <typename T>
+constexpr int ahead_of(int threads) { return threads == 128 ? 2 : sizeof(T) == 4 ? 8 : 4; }
 
 struct Stats {
   float c, s;
@@ -211,9 +212,10 @@ struct Shared {
 };
 template <int kThreads>
 struct Shared<kThreads, true> : Shared<kThreads, false> {
-  unsigned long long group[kThreads / 4];     // the largest key of every four threads
-  unsigned long long bound;
+  float group[kThreads / 4];                  // the largest value of every four threads
+  float bound;
   int count;
+  unsigned long long warp_best[kThreads / 32];
   unsigned long long cand[kCandidates];
   unsigned long long best[kMaxCluster * 32];  // block r's alternatives at 32 r (block 0 of the cluster)
 };
@@ -288,22 +290,41 @@ __device__ __noinline__ void far_row(const T* z, int vocab, float (*red)[kThread
   row.lse = row.bad ? nan : row.empty ? -INFINITY : m + row.ls;
 }
 
+// 16 bytes past L1, and how L2 is to treat them: kept in preference to what
+// streams through it (they are read again soon), given up first, or neither.
+enum L2Use { kKeep, kGiveUp, kNeither };
+template <L2Use kUse>
+__device__ __forceinline__ uint64_t l2_policy() {
+  uint64_t p;
+  if (kUse == kKeep) asm("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
+  else if (kUse == kGiveUp) asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+  else asm("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
+  return p;
+}
+__device__ __forceinline__ uint4 load_with(const uint4* at, uint64_t policy) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(at), "l"(policy));
+  return v;
+}
+
 // Every kThreads-th vector of [0, n), a batch of kBatch loaded ahead of the one
 // at work.  f takes an array of vectors, kThreads apart, and the first one's
 // place: kBatch of them, or one where the batch passes the end.
 template <int kThreads, int kBatch, typename F>
-__device__ __forceinline__ void walk(const uint4* src, int n, F f) {
+__device__ __forceinline__ void walk(const uint4* src, int n, uint64_t policy, F f) {
   uint4 ahead[kBatch];
   int v = (int)threadIdx.x;
 #pragma unroll
   for (int k = 0; k < kBatch; ++k)
-    if (v + k * kThreads < n) ahead[k] = src[v + k * kThreads];
+    if (v + k * kThreads < n) ahead[k] = load_with(src + v + k * kThreads, policy);
   for (; v < n; v += kBatch * kThreads) {
     uint4 now[kBatch];
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
       now[k] = ahead[k];
-      if (v + (kBatch + k) * kThreads < n) ahead[k] = src[v + (kBatch + k) * kThreads];
+      if (v + (kBatch + k) * kThreads < n) ahead[k] = load_with(src + v + (kBatch + k) * kThreads, policy);
     }
     if (v + (kBatch - 1) * kThreads < n) {
       f(now, v);
@@ -389,7 +410,7 @@ struct Slope {
 };
 
 // Gradient of the part of a row that this block takes.
-template <typename T, int kThreads>
+template <typename T, int kThreads, L2Use kUse>
 __device__ __forceinline__ void gradient(const LogprobParams& p, int64_t row_i, const T* z, const RowSplit<T>& split, const Part<T>& part,
                                          const Row& row, float h, const RowArgs& args) {
   constexpr int kW = Vec<T>::kWidth;
@@ -420,71 +441,64 @@ __device__ __forceinline__ void gradient(const LogprobParams& p, int64_t row_i, 
     for (int j = split.tail_at + threadIdx.x; j < p.vocab; j += kThreads) single(j);
   }
   T* dst = d + split.head;
-  walk<kThreads, ahead_of(kThreads)>(reinterpret_cast<const uint4*>(z + split.head) + part.v0, part.v1 - part.v0, [&](const auto& raw, int i) {
+  walk<kThreads, ahead_of<T>(kThreads)>(reinterpret_cast<const uint4*>(z + split.head) + part.v0, part.v1 - part.v0, l2_policy<kUse>(), [&](const auto& raw, int i) {
     constexpr int kN = sizeof(raw) / sizeof(raw[0]);
 #pragma unroll
     for (int k = 0; k < kN; ++k) g.vector(raw[k], part.v0 + i + k * kThreads, dst, together);
   });
 }
 
-// The key of a thread's largest value, found in the batch of vectors at a place, or (negative) at a single element's.
-template <typename T, int kThreads>
-__device__ __forceinline__ unsigned long long thread_key(const T* z, const RowSplit<T>& split, const Part<T>& part, float best, int best_at) {
-  if (!(best > -INFINITY)) return 0ull;
-  if (best_at < 0) return key_of(best, -1 - best_at);
-  unsigned long long mine = 0ull;
-  for (int b = 0; b < ahead_of(kThreads) && best_at + b * kThreads < part.v1; ++b)
-    for (int e = 0; e < Vec<T>::kWidth; ++e) {
-      const int j = split.head + (best_at + b * kThreads) * Vec<T>::kWidth + e;
-      const unsigned long long k = key_of(value(z, j), j);
-      mine = k > mine ? k : mine;
-    }
-  return mine;
-}
-
 // This block's top_k alternatives, best first, into out (shared memory; 0 for
-// none).  mine: the largest key of this thread's elements.  The top_k-th
-// largest of the maxima of groups of four threads bounds the answer from
-// below; only threads whose own maximum reaches the bound can hold more of it,
-// and look through their elements again.
+// none).  best: the largest of this thread's elements (whole: not known).  The
+// top_k-th largest of the maxima of groups of four threads bounds the answer
+// from below; only threads whose own maximum reaches the bound can hold more
+// of it, and their warps look through their elements again, a vector a lane.
 template <typename T, int kThreads>
 __device__ void block_top(Shared<kThreads, true>& sh, const T* z, int vocab, int top_k, const RowSplit<T>& split, const Part<T>& part,
-                          unsigned long long mine, bool whole, unsigned long long* out) {
+                          float best, bool whole, unsigned long long* out) {
   constexpr int kW = Vec<T>::kWidth, kGroups = kThreads / 4;
-  unsigned long long g = mine;
-#pragma unroll
-  for (int o = 1; o <= 2; o <<= 1) {
-    const unsigned long long other = __shfl_xor_sync(0xFFFFFFFFu, g, o);
-    g = g > other ? g : other;
-  }
+  float g = best;
+  g = fmaxf(g, __shfl_xor_sync(0xFFFFFFFFu, g, 1));
+  g = fmaxf(g, __shfl_xor_sync(0xFFFFFFFFu, g, 2));
   if ((threadIdx.x & 3) == 0) sh.group[threadIdx.x >> 2] = g;
   if (threadIdx.x == 0) {
-    sh.bound = 1ull;   // fewer than top_k groups hold anything: every element counts
+    sh.bound = -INFINITY;   // fewer than top_k groups hold anything: every element counts
     sh.count = 0;
   }
   if (threadIdx.x < 32) out[threadIdx.x] = 0ull;
   __syncthreads();
   if (threadIdx.x < kGroups) {
-    const unsigned long long own = sh.group[threadIdx.x];
+    const float own = sh.group[threadIdx.x];
     int above = 0;
-    for (int i = 0; i < kGroups; ++i) above += sh.group[i] > own ? 1 : 0;
-    if (own != 0ull && above == top_k - 1) sh.bound = own;
+#pragma unroll 8
+    for (int i = 0; i < kGroups; ++i) {
+      const float o = sh.group[i];
+      above += (o > own || (o == own && i < (int)threadIdx.x)) ? 1 : 0;
+    }
+    if (above == top_k - 1) sh.bound = own;
   }
   __syncthreads();
-  const unsigned long long bound = sh.bound;
-  if (mine >= bound && !whole) {
-    auto look = [&](int j) {
-      const unsigned long long k = key_of(value(z, j), j);
-      if (k >= bound) {
-        const int at = atomicAdd(&sh.count, 1);
-        if (at < kCandidates) sh.cand[at] = k;
-      }
-    };
-    for (int v = part.v0 + threadIdx.x; v < part.v1; v += kThreads)
-      for (int e = 0; e < kW; ++e) look(split.head + v * kW + e);
-    if (part.single) {
-      for (int j = threadIdx.x; j < split.head; j += kThreads) look(j);
-      for (int j = split.tail_at + threadIdx.x; j < vocab; j += kThreads) look(j);
+  const float bound = sh.bound;
+  auto look = [&](float x, int j) {
+    if (x >= bound && x > -INFINITY) {
+      const int at = atomicAdd(&sh.count, 1);
+      if (at < kCandidates) sh.cand[at] = key_of(x, j);
+    }
+  };
+  const bool hot = !whole && best >= bound && best > -INFINITY;
+  if (hot && part.single) {
+    for (int j = threadIdx.x; j < split.head; j += kThreads) look(value(z, j), j);
+    for (int j = split.tail_at + threadIdx.x; j < vocab; j += kThreads) look(value(z, j), j);
+  }
+  const uint4* src = reinterpret_cast<const uint4*>(z + split.head);
+  for (unsigned todo = __ballot_sync(0xFFFFFFFFu, hot); todo != 0u; todo &= todo - 1u) {
+    const int thread = (int)(threadIdx.x & ~31u) + __ffs(todo) - 1;
+    for (int v = part.v0 + thread + (int)(threadIdx.x & 31) * kThreads; v < part.v1; v += 32 * kThreads) {
+      const uint4 raw[1] = {src[v]};
+      if (!(Vec<T>::most(raw) >= bound)) continue;
+      const T* e = reinterpret_cast<const T*>(raw);
+#pragma unroll
+      for (int k = 0; k < kW; ++k) look(value(e, k), split.head + v * kW + k);
     }
   }
   __syncthreads();
@@ -517,10 +531,10 @@ __device__ void block_top(Shared<kThreads, true>& sh, const T* z, int vocab, int
       best = best > other ? best : other;
     }
     __syncthreads();
-    if ((threadIdx.x & 31) == 0) sh.group[threadIdx.x >> 5] = best;
+    if ((threadIdx.x & 31) == 0) sh.warp_best[threadIdx.x >> 5] = best;
     __syncthreads();
     best = 0ull;
-    for (int w = 0; w < kThreads / 32; ++w) best = sh.group[w] > best ? sh.group[w] : best;
+    for (int w = 0; w < kThreads / 32; ++w) best = sh.warp_best[w] > best ? sh.warp_best[w] : best;
     if (threadIdx.x == 0) out[k] = best;
     last = best;
   }
@@ -570,26 +584,19 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobParams p
   Running r;
   r.start();
   const auto low = Vec<T>::floor_of(kLowest);
-  float best = -INFINITY;   // the thread's largest value and where: a vector's or (negative) a single element's place
-  int best_at = 0;
+  float best = -INFINITY;   // the thread's largest value
   if (part.single) {
     for (int j = threadIdx.x; j < split.head; j += kThreads) {
       const float x = value(z, j);
       r.add1(x);
-      if (kTop && x > best) {
-        best = x;
-        best_at = -1 - j;
-      }
+      if (kTop) best = fmaxf(best, x);
     }
   }
-  walk<kThreads, ahead_of(kThreads)>(src, n, [&](const auto& raw, int i) {
+  walk<kThreads, ahead_of<T>(kThreads)>(src, n, p.dlogits != nullptr ? l2_policy<kKeep>() : l2_policy<kGiveUp>(), [&](const auto& raw, int i) {
     constexpr int kN = sizeof(raw) / sizeof(raw[0]);
     const float most = Vec<T>::most(raw);
     if (most > r.limit) r.raise(most);
-    if (kTop && most > best) {
-      best = most;
-      best_at = part.v0 + i;
-    }
+    if (kTop) best = fmaxf(best, most);
 #pragma unroll
     for (int k = 0; k < kN; ++k) {
       const Vec<T> x(raw[k], low);
@@ -601,10 +608,7 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobParams p
     for (int j = split.tail_at + threadIdx.x; j < p.vocab; j += kThreads) {
       const float x = value(z, j);
       r.add1(x);
-      if (kTop && x > best) {
-        best = x;
-        best_at = -1 - j;
-      }
+      if (kTop) best = fmaxf(best, x);
     }
   }
   // the target's logit, before a gradient may be written over it
@@ -668,9 +672,8 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobParams p
 
   if (rank == 0 && threadIdx.x == 0) put_stats(p, row_i, y, zy, row);
   if constexpr (kTop) {
-    const unsigned long long mine = thread_key<T, kThreads>(z, split, part, best, best_at);
     unsigned long long* out = sh.best + 32 * rank;
-    block_top<T, kThreads>(sh, z, p.vocab, p.top_k, split, part, mine, row.far, out);
+    block_top<T, kThreads>(sh, z, p.vocab, p.top_k, split, part, best, row.far, out);
     if (kCluster) {
       if (rank != 0 && threadIdx.x < 32) store_block(&sh.best[32 * rank + threadIdx.x], 0, out[threadIdx.x]);
       tc::cluster_sync();
@@ -698,7 +701,7 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobParams p
   if (p.dlogits != nullptr) {
     if (kCluster && row.far) tc::cluster_sync();   // every block has read the whole row; it may be written over now
     if (!kCluster) __syncthreads();
-    gradient<T, kThreads>(p, row_i, z, split, part, row, row.h, args);
+    gradient<T, kThreads, kGiveUp>(p, row_i, z, split, part, row, row.h, args);
   }
   if (kCluster) tc::cluster_sync();   // no block leaves while another may write into it
 }
@@ -722,10 +725,10 @@ __global__ void __launch_bounds__(kThreads) logprob_grad_kernel(const LogprobPar
   // lse alone gives p to 2^-24 |lse| relative; beyond 4096 the row's sums are
   // formed anew (the launch then gives such rows to one block)
   if (!row.bad && !row.empty && fabsf(lse) > 4096.f) far_row<T, kThreads>(z, p.vocab, red, row);
-  gradient<T, kThreads>(p, row_i, z, split, part, row, h, args);
+  gradient<T, kThreads, kNeither>(p, row_i, z, split, part, row, h, args);
 }
 
-constexpr int kShort = 1280;   // vectors of a row up to which 128 threads take it
+constexpr int kShort = 2500;   // vectors of a row up to which 128 threads take it
 
 // Blocks a row: one where the rows fill the GPU three blocks deep; else as
 // many, up to eight, as leave each thread a vector.

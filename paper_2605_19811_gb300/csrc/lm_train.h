@@ -64,9 +64,9 @@ struct NormGradParams {
   const float* rstd;
   const void* weight;
   void* dweight;
-  float* parts;         // dweight summed over each block's rows: blocks x cols
+  float* parts;         // dweight summed over the rows of each of at most kNormGradParts shares: shares x cols
 };
-constexpr int kNormGradBlocks = 608;   // most blocks that share the rows of a norm's gradient
+constexpr int kNormGradParts = 1216;   // most shares of the rows in a norm's gradient
 cudaError_t launch_rmsnorm_grad(lm_dtype dt, const NormGradParams& p, cudaStream_t st);
 
 cudaError_t launch_pack8(lm_dtype dt, const Mat& x, int64_t rows, int64_t cols, const Codes& c, cudaStream_t st);
