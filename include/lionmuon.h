@@ -527,8 +527,8 @@ lm_status lm_rmsnorm(const lm_matrix* x, const lm_matrix* residual, const lm_ten
 
 /* Its gradient.  With xh = h rstd:
  *   dx = dh + rstd (weight dy - xh mean_c(weight dy xh)),   dweight = sum_rows dy xh
- * h comes either from the stored matrix h or from its 8-bit checkpoint h8
- * (exactly one of them is not NULL); dx is the gradient of x and of residual
+ * h comes either from the stored matrix h (dtype of dy) or from its 8-bit
+ * checkpoint h8 (exactly one of them is not NULL); dx is the gradient of x and of residual
  * alike.  dh: the gradient that reaches h past the norm, or NULL.  dx (dtype of
  * dy; may be dy or dh itself) and dweight (C elements, bf16 or fp32) may be
  * NULL, not both.  dweight is summed in a fixed order: the same inputs give

@@ -58,7 +58,6 @@ struct NormGradParams {
   int32_t cols;
   int32_t wdt;          // dtype of weight
   int32_t dwdt;         // dtype of dweight
-  int32_t hdt;          // dtype of h where it is a matrix
   Mat dy, h, dh, dx;
   Codes h8;
   const float* rstd;

@@ -281,9 +281,9 @@ lm_status lm_rmsnorm_grad(const lm_matrix* dy, const lm_matrix* h, const lm_chec
   LM_TRY(check_matrix(*dy, rows, cols, "dy"));
   if (h != nullptr) LM_TRY(check_matrix(*h, rows, cols, "h"));
   else LM_TRY(check_codes(*h8, rows, cols, "h8"));
-  const lm_matrix* same[] = {dh, dx};
-  const char* names[] = {"dh", "dx"};
-  for (int i = 0; i < 2; ++i) {
+  const lm_matrix* same[] = {h, dh, dx};
+  const char* names[] = {"h", "dh", "dx"};
+  for (int i = 0; i < 3; ++i) {
     if (same[i] == nullptr) continue;
     LM_TRY(check_matrix(*same[i], rows, cols, names[i]));
     if (same[i]->dtype != dy->dtype) return fail(LM_ERR_DTYPE, "%s and dy differ in dtype", names[i]);
@@ -325,7 +325,6 @@ lm_status lm_rmsnorm_grad(const lm_matrix* dy, const lm_matrix* h, const lm_chec
   p.cols = (int32_t)cols;
   p.dy = mat(dy);
   p.h = mat(h);
-  p.hdt = h != nullptr ? (int)h->dtype : LM_F32;
   p.h8 = codes(h8);
   p.dh = mat(dh);
   p.dx = mat(dx);
