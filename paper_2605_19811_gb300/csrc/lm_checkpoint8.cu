@@ -1,86 +1,103 @@
 // Packing a matrix into 8-bit codes with a power-of-two scale for each group
 // of 128 channels (the format is stated at lm_checkpoint8 in lionmuon.h), and
-// back.  A warp takes one group, four channels to a lane.
-#include <cuda_bf16.h>
-
-#include "lm_code8.cuh"
-#include "lm_train.h"
+// back.  Bound by memory: 3 bytes an element in bf16.  A warp takes 256
+// channels of a row, eight a lane, so that a group is half a warp; four such
+// pieces are loaded before the first is worked on.
+#include "lm_rows.cuh"
 
 namespace lm {
 namespace {
 
-constexpr int kThreads = 256;
+using namespace rows;
 
-__device__ __forceinline__ float get(const __nv_bfloat16* p) { return __bfloat162float(*p); }
-__device__ __forceinline__ float get(const float* p) { return *p; }
-__device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
-__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+constexpr int kThreads = 256, kPiece = 256, kAhead = 4;
 
-template <typename T, int kFormat>
-__global__ void __launch_bounds__(kThreads) pack8_kernel(Mat x, int64_t rows, int64_t cols, Codes c) {
-  const int64_t groups = (cols + LM_CODE_GROUP - 1) / LM_CODE_GROUP;
-  const int lane = threadIdx.x & 31;
-  const int64_t nwarps = (int64_t)gridDim.x * (kThreads / 32);
-  for (int64_t w = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); w < rows * groups; w += nwarps) {
-    const int64_t row = w / groups, group = w % groups, c0 = group * LM_CODE_GROUP + 4 * lane;
-    const T* src = static_cast<const T*>(x.data) + row * x.ld + c0;
-    float v[4];
-    uint32_t most = 0;
-    for (int k = 0; k < 4; ++k) {
-      v[k] = c0 + k < cols ? get(src + k) : 0.f;
-      most = max(most, code8::magnitude(v[k]));
+// Piece i of the matrix: 256 channels of a row, this lane's first.
+struct Place {
+  int64_t row;
+  int c;
+  __device__ __forceinline__ Place(int64_t i, int64_t per_row) {
+    row = i / per_row;
+    c = (int)(i - row * per_row) * kPiece + 8 * (int)(threadIdx.x & 31);
+  }
+};
+
+template <typename T, int kFormat, bool kVec>
+__global__ void __launch_bounds__(kThreads) pack8_kernel(Mat x, int64_t nrows, int cols, Codes out) {
+  const int64_t per = (cols + kPiece - 1) / kPiece, all = nrows * per, step = (int64_t)gridDim.x * (kThreads / 32);
+  for (int64_t i0 = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); i0 < all; i0 += kAhead * step) {
+    Raw<T> raw[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const Place at(i0 + k * step, per);
+      const int left = i0 + k * step < all ? cols - at.c : 0;
+      if (left > 0) raw[k].template load<kVec>(row_of<const T>(x, at.row) + at.c, left);
+      else raw[k].zero();
     }
-    most = __reduce_max_sync(0xFFFFFFFFu, most);
-    const float scale = code8::group_scale<kFormat>(most), inv = code8::inverse_scale(scale);
-    if (lane == 0) c.scales[group * c.ld_scales + row] = scale;
-    const uint32_t four = code8::encode2<kFormat>(v[0], v[1], inv) | (code8::encode2<kFormat>(v[2], v[3], inv) << 16);
-    if (c0 < cols) *reinterpret_cast<uint32_t*>(c.data + row * c.ld + c0) = four;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (i0 + k * step >= all) break;
+      const Place at(i0 + k * step, per);
+      float v[8];
+      raw[k].get(v);
+      keep8<kFormat>(out, at.row, at.c, cols, v);
+    }
   }
+}
+
+template <typename T, int kFormat, bool kVec>
+__global__ void __launch_bounds__(kThreads) unpack8_kernel(Codes in, int64_t nrows, int cols, Mat x) {
+  const int64_t per = (cols + kPiece - 1) / kPiece, all = nrows * per, step = (int64_t)gridDim.x * (kThreads / 32);
+  for (int64_t i0 = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); i0 < all; i0 += kAhead * step) {
+    RawCodes<kFormat> raw[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const Place at(i0 + k * step, per);
+      if (i0 + k * step < all && at.c < cols) raw[k].load(in, at.row, at.c);
+      else raw[k].zero();
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const Place at(i0 + k * step, per);
+      if (i0 + k * step >= all || at.c >= cols) continue;
+      float v[8];
+      raw[k].get(v);
+      store8<kVec>(row_of<T>(x, at.row) + at.c, cols - at.c, v);
+    }
+  }
+}
+
+unsigned grid_for(int64_t nrows, int64_t cols) {
+  const int64_t pieces = nrows * ((cols + kPiece - 1) / kPiece), blocks = (pieces + kThreads / 32 - 1) / (kThreads / 32);
+  return (unsigned)(blocks < 152 * 8 ? blocks : 152 * 8);
 }
 
 template <typename T, int kFormat>
-__global__ void __launch_bounds__(kThreads) unpack8_kernel(Codes c, int64_t rows, int64_t cols, Mat x) {
-  const int64_t groups = (cols + LM_CODE_GROUP - 1) / LM_CODE_GROUP;
-  const int lane = threadIdx.x & 31;
-  const int64_t nwarps = (int64_t)gridDim.x * (kThreads / 32);
-  for (int64_t w = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); w < rows * groups; w += nwarps) {
-    const int64_t row = w / groups, group = w % groups, c0 = group * LM_CODE_GROUP + 4 * lane;
-    if (c0 >= cols) continue;
-    const float scale = c.scales[group * c.ld_scales + row];
-    const uint32_t four = *reinterpret_cast<const uint32_t*>(c.data + row * c.ld + c0);
-    const float2 lo = code8::decode2<kFormat>(four), hi = code8::decode2<kFormat>(four >> 16);
-    const float v[4] = {lo.x * scale, lo.y * scale, hi.x * scale, hi.y * scale};
-    T* dst = static_cast<T*>(x.data) + row * x.ld + c0;
-    for (int k = 0; k < 4; ++k)
-      if (c0 + k < cols) put(dst + k, v[k]);
-  }
+void pack(const Mat& x, int64_t nrows, int cols, const Codes& c, cudaStream_t st) {
+  if (aligned(x, sizeof(T), nrows)) pack8_kernel<T, kFormat, true><<<grid_for(nrows, cols), kThreads, 0, st>>>(x, nrows, cols, c);
+  else pack8_kernel<T, kFormat, false><<<grid_for(nrows, cols), kThreads, 0, st>>>(x, nrows, cols, c);
 }
-
-unsigned grid_for(int64_t rows, int64_t cols) {
-  const int64_t warps = rows * ((cols + LM_CODE_GROUP - 1) / LM_CODE_GROUP);
-  const int64_t blocks = (warps + kThreads / 32 - 1) / (kThreads / 32);
-  return (unsigned)(blocks < 152 * 16 ? blocks : 152 * 16);
+template <typename T, int kFormat>
+void unpack(const Codes& c, int64_t nrows, int cols, const Mat& x, cudaStream_t st) {
+  if (aligned(x, sizeof(T), nrows)) unpack8_kernel<T, kFormat, true><<<grid_for(nrows, cols), kThreads, 0, st>>>(c, nrows, cols, x);
+  else unpack8_kernel<T, kFormat, false><<<grid_for(nrows, cols), kThreads, 0, st>>>(c, nrows, cols, x);
 }
 
 }  // namespace
 
-cudaError_t launch_pack8(lm_dtype dt, const Mat& x, int64_t rows, int64_t cols, const Codes& c, cudaStream_t st) {
-  const unsigned grid = grid_for(rows, cols);
+cudaError_t launch_pack8(lm_dtype dt, const Mat& x, int64_t nrows, int64_t cols, const Codes& c, cudaStream_t st) {
   count_launch();
-  if (dt == LM_BF16 && c.format == LM_CODE_I8) pack8_kernel<__nv_bfloat16, LM_CODE_I8><<<grid, kThreads, 0, st>>>(x, rows, cols, c);
-  else if (dt == LM_BF16) pack8_kernel<__nv_bfloat16, LM_CODE_E4M3><<<grid, kThreads, 0, st>>>(x, rows, cols, c);
-  else if (c.format == LM_CODE_I8) pack8_kernel<float, LM_CODE_I8><<<grid, kThreads, 0, st>>>(x, rows, cols, c);
-  else pack8_kernel<float, LM_CODE_E4M3><<<grid, kThreads, 0, st>>>(x, rows, cols, c);
+  const int n = (int)cols;
+  if (dt == LM_BF16) c.format == LM_CODE_I8 ? pack<__nv_bfloat16, LM_CODE_I8>(x, nrows, n, c, st) : pack<__nv_bfloat16, LM_CODE_E4M3>(x, nrows, n, c, st);
+  else c.format == LM_CODE_I8 ? pack<float, LM_CODE_I8>(x, nrows, n, c, st) : pack<float, LM_CODE_E4M3>(x, nrows, n, c, st);
   return cudaGetLastError();
 }
 
-cudaError_t launch_unpack8(lm_dtype dt, const Codes& c, int64_t rows, int64_t cols, const Mat& x, cudaStream_t st) {
-  const unsigned grid = grid_for(rows, cols);
+cudaError_t launch_unpack8(lm_dtype dt, const Codes& c, int64_t nrows, int64_t cols, const Mat& x, cudaStream_t st) {
   count_launch();
-  if (dt == LM_BF16 && c.format == LM_CODE_I8) unpack8_kernel<__nv_bfloat16, LM_CODE_I8><<<grid, kThreads, 0, st>>>(c, rows, cols, x);
-  else if (dt == LM_BF16) unpack8_kernel<__nv_bfloat16, LM_CODE_E4M3><<<grid, kThreads, 0, st>>>(c, rows, cols, x);
-  else if (c.format == LM_CODE_I8) unpack8_kernel<float, LM_CODE_I8><<<grid, kThreads, 0, st>>>(c, rows, cols, x);
-  else unpack8_kernel<float, LM_CODE_E4M3><<<grid, kThreads, 0, st>>>(c, rows, cols, x);
+  const int n = (int)cols;
+  if (dt == LM_BF16) c.format == LM_CODE_I8 ? unpack<__nv_bfloat16, LM_CODE_I8>(c, nrows, n, x, st) : unpack<__nv_bfloat16, LM_CODE_E4M3>(c, nrows, n, x, st);
+  else c.format == LM_CODE_I8 ? unpack<float, LM_CODE_I8>(c, nrows, n, x, st) : unpack<float, LM_CODE_E4M3>(c, nrows, n, x, st);
   return cudaGetLastError();
 }
 

@@ -15,7 +15,7 @@ namespace {
 
 using namespace rows;
 
-// kVec: rows are 16-byte aligned and whole eights.  kFormat < 0: no 8-bit copy.
+// kVec: rows are 16-byte aligned.  kFormat < 0: no 8-bit copy.
 // kResidual: x + residual is normed.
 template <typename T, int kFormat, bool kResidual, typename S, bool kVec>
 __global__ void __launch_bounds__(S::kBlock, S::kBlock <= 256 ? 768 / S::kBlock : 1) rmsnorm_kernel(const NormParams p) {
@@ -136,7 +136,7 @@ void forward(const NormParams& p, bool vec, cudaStream_t st) {
 
 cudaError_t launch_rmsnorm(lm_dtype dt, const NormParams& p, cudaStream_t st) {
   const int size = dt == LM_F32 ? 4 : 2;
-  const bool vec = p.cols % 8 == 0 && aligned(p.x, size, p.rows) && aligned(p.residual, size, p.rows) && aligned(p.h, size, p.rows) && aligned(p.y, size, p.rows);
+  const bool vec = aligned(p.x, size, p.rows) && aligned(p.residual, size, p.rows) && aligned(p.h, size, p.rows) && aligned(p.y, size, p.rows);
   count_launch();
   const int format = p.kept.data == nullptr ? -1 : p.kept.format;
   if (dt == LM_BF16) {

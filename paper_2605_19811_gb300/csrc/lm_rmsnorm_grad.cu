@@ -188,7 +188,7 @@ cudaError_t launch_rmsnorm_grad(lm_dtype dt, const NormGradParams& p, cudaStream
   int parts = 0;
   if (p.rows > 0) {
     const int size = dt == LM_F32 ? 4 : 2;
-    const bool vec = p.cols % 8 == 0 && aligned(p.dy, size, p.rows) && aligned(p.h, size, p.rows) &&
+    const bool vec = aligned(p.dy, size, p.rows) && aligned(p.h, size, p.rows) &&
                      aligned(p.dh, size, p.rows) && aligned(p.dx, size, p.rows);
     count_launch();
     parts = dt == LM_BF16 ? backward<__nv_bfloat16>(p, vec, st) : backward<float>(p, vec, st);

@@ -16,15 +16,15 @@ namespace {
 
 constexpr uint32_t kAll = 0xFFFFFFFFu;
 
-// Eight channels as they are read.  kVec: they lie on a 16-byte boundary and
-// inside the row; else one by one, `left` of them inside (zeros beyond).
+// Eight channels as they are read, `left` of them inside the row (zeros
+// beyond).  kVec: eights lie on 16-byte boundaries; else one by one.
 template <typename T> struct Raw;
 template <> struct Raw<__nv_bfloat16> {
   uint4 u;
   __device__ __forceinline__ void zero() { u = make_uint4(0u, 0u, 0u, 0u); }
   template <bool kVec>
   __device__ __forceinline__ void load(const __nv_bfloat16* p, int left) {
-    if (kVec) {
+    if (kVec && left >= 8) {
       u = __ldcs(reinterpret_cast<const uint4*>(p));
     } else {
       const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
@@ -48,7 +48,7 @@ template <> struct Raw<float> {
   __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
   template <bool kVec>
   __device__ __forceinline__ void load(const float* p, int left) {
-    if (kVec) {
+    if (kVec && left >= 8) {
       a = __ldcs(reinterpret_cast<const float4*>(p));
       b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
     } else {
@@ -94,7 +94,7 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 }
 template <bool kVec>
 __device__ __forceinline__ void store8(__nv_bfloat16* p, int left, const float (&v)[8]) {
-  if (kVec) {
+  if (kVec && left >= 8) {
     __stcs(reinterpret_cast<uint4*>(p), make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])));
   } else {
 #pragma unroll
@@ -104,7 +104,7 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, int left, const float (
 }
 template <bool kVec>
 __device__ __forceinline__ void store8(float* p, int left, const float (&v)[8]) {
-  if (kVec) {
+  if (kVec && left >= 8) {
     __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
     __stcs(reinterpret_cast<float4*>(p) + 1, make_float4(v[4], v[5], v[6], v[7]));
   } else {
