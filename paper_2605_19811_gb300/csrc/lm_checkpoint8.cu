@@ -1,8 +1,8 @@
 // Packing a matrix into 8-bit codes with a power-of-two scale for each group
 // of 128 channels (the format is stated at lm_checkpoint8 in lionmuon.h), and
 // back.  Bound by memory: 3 bytes an element in bf16.  A warp takes 256
-// channels of a row, eight a lane, so that a group is half a warp; four such
-// pieces are loaded before the first is worked on.
+// channels of a row, eight a lane, so that a group is half a warp; several
+// such pieces are loaded before the first is worked on.
 #include "lm_rows.cuh"
 
 namespace lm {
@@ -10,66 +10,84 @@ namespace {
 
 using namespace rows;
 
-constexpr int kThreads = 256, kPiece = 256, kAhead = 4;
+constexpr int kThreads = 256, kPiece = 256;
+constexpr int kPackAhead = 2, kUnpackAhead = 4;   // pieces loaded at once: packing has more to do for each
 
-// Piece i of the matrix: 256 channels of a row, this lane's first.
-struct Place {
-  int64_t row;
-  int c;
-  __device__ __forceinline__ Place(int64_t i, int64_t per_row) {
-    row = i / per_row;
-    c = (int)(i - row * per_row) * kPiece + 8 * (int)(threadIdx.x & 31);
+// A warp's way over the pieces (256 channels of a row each), `warps` apart.
+struct Way {
+  int64_t row, drow;
+  int k, dk, per;
+  __device__ __forceinline__ explicit Way(int cols) {
+    per = (cols + kPiece - 1) / kPiece;
+    const int64_t first = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), warps = (int64_t)gridDim.x * (kThreads / 32);
+    row = first / per;
+    k = (int)(first - row * per);
+    drow = warps / per;
+    dk = (int)(warps - drow * per);
+  }
+  __device__ __forceinline__ int column() const { return k * kPiece + 8 * (int)(threadIdx.x & 31); }
+  __device__ __forceinline__ void advance() {
+    row += drow;
+    k += dk;
+    if (k >= per) {
+      k -= per;
+      ++row;
+    }
   }
 };
 
 template <typename T, int kFormat, bool kVec>
 __global__ void __launch_bounds__(kThreads) pack8_kernel(Mat x, int64_t nrows, int cols, Codes out) {
-  const int64_t per = (cols + kPiece - 1) / kPiece, all = nrows * per, step = (int64_t)gridDim.x * (kThreads / 32);
-  for (int64_t i0 = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); i0 < all; i0 += kAhead * step) {
-    Raw<T> raw[kAhead];
+  Way at(cols);
+  while (at.row < nrows) {
+    Raw<T> raw[kPackAhead];
+    int64_t row[kPackAhead];
+    int c[kPackAhead];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const Place at(i0 + k * step, per);
-      const int left = i0 + k * step < all ? cols - at.c : 0;
-      if (left > 0) raw[k].template load<kVec>(row_of<const T>(x, at.row) + at.c, left);
+    for (int k = 0; k < kPackAhead; ++k, at.advance()) {
+      row[k] = at.row;
+      c[k] = at.column();
+      const int left = at.row < nrows ? cols - c[k] : 0;
+      if (left > 0) raw[k].template load<kVec>(row_of<const T>(x, at.row) + c[k], left);
       else raw[k].zero();
     }
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      if (i0 + k * step >= all) break;
-      const Place at(i0 + k * step, per);
+    for (int k = 0; k < kPackAhead; ++k) {
+      if (row[k] >= nrows) break;
       float v[8];
       raw[k].get(v);
-      keep8<kFormat>(out, at.row, at.c, cols, v);
+      keep8<kFormat>(out, row[k], c[k], cols, v);
     }
   }
 }
 
 template <typename T, int kFormat, bool kVec>
 __global__ void __launch_bounds__(kThreads) unpack8_kernel(Codes in, int64_t nrows, int cols, Mat x) {
-  const int64_t per = (cols + kPiece - 1) / kPiece, all = nrows * per, step = (int64_t)gridDim.x * (kThreads / 32);
-  for (int64_t i0 = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); i0 < all; i0 += kAhead * step) {
-    RawCodes<kFormat> raw[kAhead];
+  Way at(cols);
+  while (at.row < nrows) {
+    RawCodes<kFormat> raw[kUnpackAhead];
+    int64_t row[kUnpackAhead];
+    int c[kUnpackAhead];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const Place at(i0 + k * step, per);
-      if (i0 + k * step < all && at.c < cols) raw[k].load(in, at.row, at.c);
+    for (int k = 0; k < kUnpackAhead; ++k, at.advance()) {
+      row[k] = at.row;
+      c[k] = at.column();
+      if (at.row < nrows && c[k] < cols) raw[k].load(in, at.row, c[k]);
       else raw[k].zero();
     }
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const Place at(i0 + k * step, per);
-      if (i0 + k * step >= all || at.c >= cols) continue;
+    for (int k = 0; k < kUnpackAhead; ++k) {
+      if (row[k] >= nrows || c[k] >= cols) continue;
       float v[8];
       raw[k].get(v);
-      store8<kVec>(row_of<T>(x, at.row) + at.c, cols - at.c, v);
+      store8<kVec>(row_of<T>(x, row[k]) + c[k], cols - c[k], v);
     }
   }
 }
 
 unsigned grid_for(int64_t nrows, int64_t cols) {
   const int64_t pieces = nrows * ((cols + kPiece - 1) / kPiece), blocks = (pieces + kThreads / 32 - 1) / (kThreads / 32);
-  return (unsigned)(blocks < 152 * 8 ? blocks : 152 * 8);
+  return (unsigned)(blocks < 152 * 16 ? blocks : 152 * 16);
 }
 
 template <typename T, int kFormat>

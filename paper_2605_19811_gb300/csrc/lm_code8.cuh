@@ -47,8 +47,11 @@ __device__ __forceinline__ uint32_t encode2(float a, float b, float inv) {
     a = fminf(fmaxf(a, -kCap), kCap);
     b = fminf(fmaxf(b, -kCap), kCap);
   }
-  if (kFormat == LM_CODE_I8)
-    return ((uint32_t)__float2int_rn(a) & 0xFFu) | (((uint32_t)__float2int_rn(b) & 0xFFu) << 8);
+  if (kFormat == LM_CODE_I8) {
+    // 1.5 2^23 + a rounds a to an integer (nearest even); its low byte is the code
+    constexpr float kRound = 12582912.f;
+    return __byte_perm(__float_as_uint(a + kRound), __float_as_uint(b + kRound), 0x0040) & 0xFFFFu;
+  }
   return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
 }
 // The values of the two codes in the low half of `two`, before the scale.

@@ -75,6 +75,7 @@ struct Schedule {
   int32_t waves;        // whole waves: tiles [0, waves * kPairs) go one to a pair
   int32_t rest;         // tiles left over
   int32_t sharers;      // pairs that share them; 0: none left over
+  int64_t begin[kPairs + 1];   // sharer k's first unit (tile, token block) in the line of left-over work
 };
 struct KernelParams {
   CUtensorMap dy, x;
@@ -97,11 +98,6 @@ __device__ __forceinline__ void tile_place(const Schedule& s, int tile, int& tm,
   tn = r / rows;
   tm = g * kGroup + r - tn * rows;
 }
-// First unit (tile, token block) of sharer k in the line of left-over work.
-__host__ __device__ __forceinline__ int64_t share_begin(const Schedule& s, int k) {
-  return (int64_t)s.rest * s.nkb * k / s.sharers;
-}
-
 // A pair's work items in order: a tile, its token blocks, and where the sum goes.
 struct Item {
   int tile, kb0, kb1;
@@ -113,8 +109,8 @@ struct Items {
   bool first;
   __device__ __forceinline__ Items(const Schedule& s, int p) : pair(p), wave(0), at(0), end(0), first(true) {
     if (s.sharers > 0 && p < s.sharers) {
-      at = share_begin(s, p);
-      end = share_begin(s, p + 1);
+      at = s.begin[p];
+      end = s.begin[p + 1];
     }
   }
   __device__ __forceinline__ bool next(const Schedule& s, Item& it) {
@@ -301,6 +297,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad8_
   tc_fence_before();
   cluster_sync();   // barriers of both CTAs initialised
   tc_fence_after();
+  griddep_wait();   // the operands are there
+  griddep_launch_dependents();
   const uint32_t tmem_base = *tmem_slot;
   const uint64_t wait_ns = p.wait_ns;
 
@@ -486,19 +484,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad8_
 __global__ void __launch_bounds__(256) wgrad8_join_kernel(const __grid_constant__ KernelParams p) {
   const Schedule& s = p.sch;
   const int t = blockIdx.x;
+  griddep_wait();
   const int64_t u0 = (int64_t)t * s.nkb, u1 = u0 + s.nkb;
-  // the sharer whose range holds unit u0
-  int k = (int)(u0 * s.sharers / ((int64_t)s.rest * s.nkb));
-  while (k > 0 && share_begin(s, k) > u0) --k;
-  while (share_begin(s, k + 1) <= u0) ++k;
-  if (share_begin(s, k) <= u0 && share_begin(s, k + 1) >= u1) return;   // one pair wrote it whole
+  int k = (int)((int64_t)t * s.sharers / s.rest);   // the sharer whose range holds unit u0
+  while (k > 0 && s.begin[k] > u0) --k;
+  while (s.begin[k + 1] <= u0) ++k;
+  if (s.begin[k] <= u0 && s.begin[k + 1] >= u1) return;   // one pair wrote it whole
   int tm, tn;
   tile_place(s, s.waves * kPairs + t, tm, tn);
   int last = k;   // the last sharer of the tile
-  while (last + 1 < s.sharers && share_begin(s, last + 1) < u1) ++last;
+  while (last + 1 < s.sharers && s.begin[last + 1] < u1) ++last;
   const int rows = min(kTileM, p.out - tm * kTileM), cols = min(kTileN, p.in - tn * kTileN);
   // the first part may be its pair's second item; every later one is a first
-  const float* part0 = p.parts + (size_t)(2 * k + (share_begin(s, k) / s.nkb == t ? 0 : 1)) * (kTileM * kTileN);
+  const float* part0 = p.parts + (size_t)(2 * k + (s.begin[k] >= u0 ? 0 : 1)) * (kTileM * kTileN);
   const int r = blockIdx.y * 4 + (threadIdx.x >> 6), c = 4 * (threadIdx.x & 63);
   if (r >= rows || c >= cols) return;
   const size_t at = (size_t)r * kTileN + c;
@@ -524,7 +522,7 @@ __global__ void __launch_bounds__(256) wgrad8_zero_kernel(Mat dw, int dwdt, int 
 }
 
 // The operands as the TMA takes them.  Blocks below x_blocks: X = code * scale
-// as bf16, 16 codes a thread and step.  The others: dY in rows of a 16-byte
+// as bf16.  The others: dY in rows of a 16-byte
 // pitch where its own are not; fp32 values as three planes whose sum is
 // exactly the value (each takes the next 8 significant bits by truncation, so
 // that no piece rounds up to infinity; a non-finite value keeps its first
@@ -532,26 +530,40 @@ __global__ void __launch_bounds__(256) wgrad8_zero_kernel(Mat dw, int dwdt, int 
 template <int kFormat, typename T>
 __global__ void __launch_bounds__(256) wgrad8_operands_kernel(Codes x, __nv_bfloat16* xdst, int64_t ldx, unsigned x_blocks, Mat dy, int64_t tokens,
                                                               int out, __nv_bfloat16* dst, int64_t ld) {
+  griddep_launch_dependents();
   if (blockIdx.x < x_blocks) {
-    const int64_t per = ldx / 16, all = tokens * per, step = (int64_t)x_blocks * 256;
-    for (int64_t i0 = (int64_t)blockIdx.x * 256 + threadIdx.x; i0 < all; i0 += 4 * step) {
-      uint4 q[4];
-      uint32_t s[4];
-      int64_t t[4];
-      int c[4];
+    // a warp takes 512 channels of a token, 16 a lane, kAhead such pieces at once
+    constexpr int kAhead = 4, kPiece = 512;
+    const int per = (int)((ldx + kPiece - 1) / kPiece);
+    const int64_t first = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), warps = (int64_t)x_blocks * 8;
+    int64_t row = first / per;
+    int piece = (int)(first - row * per);
+    const int64_t drow = warps / per;
+    const int dpiece = (int)(warps - drow * per);
+    while (row < tokens) {
+      uint4 q[kAhead];
+      float sc[kAhead];
+      int64_t t[kAhead];
+      int c[kAhead];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int64_t i = i0 + k * step;
-        if (i >= all) break;
-        t[k] = i / per;
-        c[k] = (int)(i - t[k] * per) * 16;
-        q[k] = __ldcs(reinterpret_cast<const uint4*>(x.data + t[k] * x.ld + c[k]));
-        s[k] = __float_as_uint(__ldg(x.scales + (int64_t)(c[k] / LM_CODE_GROUP) * x.ld_scales + t[k]));
+      for (int k = 0; k < kAhead; ++k) {
+        t[k] = row;
+        c[k] = piece * kPiece + 16 * (int)(threadIdx.x & 31);
+        if (row < tokens && c[k] < ldx) {
+          q[k] = __ldcs(reinterpret_cast<const uint4*>(x.data + row * x.ld + c[k]));
+          sc[k] = x.scales[(int64_t)(c[k] / LM_CODE_GROUP) * x.ld_scales + row];
+        }
+        row += drow;
+        piece += dpiece;
+        if (piece >= per) {
+          piece -= per;
+          ++row;
+        }
       }
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        if (i0 + k * step >= all) break;
-        const uint32_t s2 = __byte_perm(s[k], s[k], 0x3232);
+      for (int k = 0; k < kAhead; ++k) {
+        if (t[k] >= tokens || c[k] >= ldx) continue;
+        const uint32_t s2 = __byte_perm(__float_as_uint(sc[k]), __float_as_uint(sc[k]), 0x3232);
         const uint2 w0 = convert4<kFormat>(q[k].x, s2), w1 = convert4<kFormat>(q[k].y, s2);
         const uint2 w2 = convert4<kFormat>(q[k].z, s2), w3 = convert4<kFormat>(q[k].w, s2);
         uint4* d = reinterpret_cast<uint4*>(xdst + t[k] * ldx + c[k]);
@@ -604,6 +616,7 @@ Schedule make_schedule(int64_t tokens, int64_t out, int64_t in, int planes) {
     // a share of at least kChunk blocks, and never more sharers than pairs
     const int64_t most = (int64_t)s.rest * s.nkb / kChunk;
     s.sharers = (int32_t)(most < s.rest ? s.rest : most < kPairs ? most : kPairs);
+    for (int k = 0; k <= s.sharers; ++k) s.begin[k] = (int64_t)s.rest * s.nkb * k / s.sharers;
   }
   return s;
 }
@@ -638,6 +651,24 @@ CUresult encode_operand(PFN_cuTensorMapEncodeTiled_v12000 enc, CUtensorMap* m, v
              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
+// A launch whose set-up may overlap the end of the kernel before it (which it
+// waits for itself, griddepcontrol.wait).
+template <typename Kernel>
+cudaError_t launch_after(Kernel kernel, dim3 grid, int threads, size_t smem, cudaStream_t st, const KernelParams& p) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  count_launch();
+  return cudaLaunchKernelEx(&cfg, kernel, p);
+}
+
 template <bool kLong>
 cudaError_t start(const KernelParams& p, int pairs, cudaStream_t st) {
   const int dev = device_slot();
@@ -647,9 +678,7 @@ cudaError_t start(const KernelParams& p, int pairs, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     if (dev >= 0) ready[dev] = true;
   }
-  count_launch();
-  wgrad8_kernel<kLong><<<2 * pairs, kThreads, kSmemBytes, st>>>(p);
-  return cudaGetLastError();
+  return launch_after(wgrad8_kernel<kLong>, dim3(2 * pairs), kThreads, kSmemBytes, st, p);
 }
 
 }  // namespace
@@ -687,7 +716,7 @@ cudaError_t launch_wgrad8(const WgradParams& w, cudaStream_t st) {
   }
   __nv_bfloat16* x = reinterpret_cast<__nv_bfloat16*>(static_cast<uint8_t*>(w.workspace) + l.parts + l.dy);
   {
-    const int64_t steps = (w.tokens * (l.ldx / 16) + 1023) / 1024;   // four a thread
+    const int64_t pieces = w.tokens * ((l.ldx + 511) / 512), steps = (pieces + 7) / 8;   // a warp's pieces, blocks of eight warps
     const unsigned x_blocks = (unsigned)(steps < 152 * 8 ? steps : 152 * 8);
     const unsigned dy_blocks = l.copy ? (unsigned)(w.tokens < 152 * 8 ? w.tokens : 152 * 8) : 0u;
     using Operands = void (*)(Codes, __nv_bfloat16*, int64_t, unsigned, Mat, int64_t, int, __nv_bfloat16*, int64_t);
@@ -706,9 +735,7 @@ cudaError_t launch_wgrad8(const WgradParams& w, cudaStream_t st) {
   const int pairs = p.sch.waves > 0 ? kPairs : p.sch.sharers;
   cudaError_t e = w.dwdt == LM_F32 ? start<true>(p, pairs, st) : start<false>(p, pairs, st);
   if (e != cudaSuccess || !has_parts(p.sch)) return e;
-  count_launch();
-  wgrad8_join_kernel<<<dim3(p.sch.rest, kTileM / 4), 256, 0, st>>>(p);
-  return cudaGetLastError();
+  return launch_after(wgrad8_join_kernel, dim3(p.sch.rest, kTileM / 4), 256, 0, st, p);
 }
 
 }  // namespace lm
