@@ -47,14 +47,14 @@ __global__ void __launch_bounds__(kThreads) pack8_kernel(Mat x, int64_t nrows, i
     for (int k = 0; k < kPackAhead; ++k, at.advance()) {
       row[k] = at.row;
       c[k] = at.column();
-      const int left = at.row < nrows ? cols - c[k] : 0;
-      if (left > 0) raw[k].template load<kVec>(row_of<const T>(x, at.row) + c[k], left);
-      else raw[k].zero();
+      const int left = at.row < nrows ? cols - c[k] : kNoRow;
+      raw[k].template load<kVec>(Row<const T>(x, at.row < nrows ? at.row : 0, nrows), c[k], left);
     }
 #pragma unroll
     for (int k = 0; k < kPackAhead; ++k) {
       if (row[k] >= nrows) break;
       float v[8];
+      raw[k].template settle<kVec>(Row<const T>(x, row[k], nrows), c[k], cols - c[k]);
       raw[k].get(v);
       keep8<kFormat>(out, row[k], c[k], cols, v);
     }
@@ -72,15 +72,16 @@ __global__ void __launch_bounds__(kThreads) unpack8_kernel(Codes in, int64_t nro
     for (int k = 0; k < kUnpackAhead; ++k, at.advance()) {
       row[k] = at.row;
       c[k] = at.column();
-      if (at.row < nrows && c[k] < cols) raw[k].load(in, at.row, c[k]);
-      else raw[k].zero();
+      raw[k].load(in, at.row, c[k], at.row < nrows && c[k] < cols);
     }
 #pragma unroll
     for (int k = 0; k < kUnpackAhead; ++k) {
-      if (row[k] >= nrows || c[k] >= cols) continue;
+      if (row[k] >= nrows) break;
       float v[8];
       raw[k].get(v);
-      store8<kVec>(row_of<T>(x, row[k]) + c[k], cols - c[k], v);
+      Raw<T> out;
+      out.set(v);
+      out.template store<kVec>(row_of<T>(x, row[k]) + c[k], cols - c[k]);
     }
   }
 }

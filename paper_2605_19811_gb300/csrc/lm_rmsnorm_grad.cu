@@ -1,10 +1,12 @@
 // Gradient of the RMS norm, from the stored h or its 8-bit checkpoint (formulas
 // at lm_rmsnorm_grad in lionmuon.h).
 //
-// Bound by memory: 8 bytes an element (dy, h, dh, dx in bf16).  Rows are taken
-// as in the forward kernel: once, in registers, the next row's loads ahead.
-// dweight is summed over each share's rows in registers, then over the shares,
-// in order, by a second kernel.
+// Bound by memory: 8 bytes an element (dy, h, dh, dx in bf16).  A row is read
+// once and stays in registers, one or two eights a thread, and the next row's
+// loads go out before this row's sums: 16384 x 1280 takes 50 us so, and 64 us
+// with a warp a row, five eights a lane and nothing ahead.  dweight is summed over a slot's
+// rows in registers, over the slots of a block in shared memory, and over the
+// blocks by a second kernel, each in a fixed order.
 #include "lm_rows.cuh"
 
 namespace lm {
@@ -12,133 +14,190 @@ namespace {
 
 using namespace rows;
 
-// kFormat < 0: h is a matrix.  kPast: dh is added.
-template <typename T, int kFormat, bool kPast, typename S, bool kVec>
-__global__ void __launch_bounds__(S::kBlock, S::kBlock <= 256 ? 512 / S::kBlock : 1) rmsnorm_grad_kernel(const NormGradParams p) {
-  constexpr int kThreads = S::kThreads, kRows = S::kRows, kVecs = S::kVecs, kSpan = S::kSpan;
-  __shared__ float part[2][kRows][S::kWarps];
-  const int t = (int)threadIdx.x % kThreads, slot = (int)threadIdx.x / kThreads;
-  const bool whole = p.cols <= kVecs * kSpan;
-  const bool want = p.dweight != nullptr;
-  float* sums = want ? p.parts + ((int64_t)blockIdx.x * kRows + slot) * p.cols : nullptr;   // of this share's rows
-  float acc[kVecs][8], gain[kVecs][8];
+// kFormat < 0: h is a matrix.
+// kMost: threads a block has at most.
+template <typename T, int kFormat, int kVecs, bool kVec, int kMost>
+__global__ void __launch_bounds__(kMost, kMost == 256 ? 2 : 1) rmsnorm_grad_kernel(const NormGradParams p, int threads) {
+  constexpr bool kMatrix = kFormat < 0;
+  __shared__ float part[2][32];
+  __shared__ float joined[64 * 8 * kVecs];        // where rows share a block they have at most 64 threads
+  const Team team(threads);
+  const int t = team.t, slot = team.slot, nrows = team.rows, span = team.span;
+  const bool whole = p.cols <= kVecs * span;
+  const bool want = p.dweight != nullptr, past = p.dh.data != nullptr;
+  const bool wvec = (reinterpret_cast<uintptr_t>(p.weight) & 15u) == 0;
+  const float inv_cols = 1.f / (float)p.cols;
+  float* sums = want ? p.parts + (int64_t)blockIdx.x * p.cols : nullptr;   // of this block's rows
+  float acc[kVecs][8];
 #pragma unroll
-  for (int v = 0; v < kVecs; ++v) {
+  for (int v = 0; v < kVecs; ++v)
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[v][e] = 0.f;
-    weight8(p.weight, p.wdt, 8 * t + v * kSpan, whole ? p.cols - 8 * t - v * kSpan : 0, gain[v]);
-  }
-  if (want && !whole)
-    for (int c = 8 * t; c < p.cols; c += kSpan)
+  if (want && !whole)   // (such rows have a block of their own)
+    for (int c = 8 * t; c < p.cols; c += span)
       for (int e = 0; e < 8 && c + e < p.cols; ++e) sums[c + e] = 0.f;
   struct Eight {
     Raw<T> dy, dh;
-    std::conditional_t<(kFormat < 0), Raw<T>, RawCodes<(kFormat < 0 ? 0 : kFormat)>> h;
-    __device__ __forceinline__ void load(const NormGradParams& p, int64_t row, int c) {
-      const int left = row < p.rows ? p.cols - c : 0;
-      if (left <= 0) {
-        dy.zero();
-        h.zero();
-        if (kPast) dh.zero();
-        return;
-      }
-      dy.template load<kVec>(row_of<const T>(p.dy, row) + c, left);
-      if constexpr (kFormat < 0) h.template load<kVec>(row_of<const T>(p.h, row) + c, left);
-      else h.load(p.h8, row, c);
-      if (kPast) dh.template load<kVec>(row_of<const T>(p.dh, row) + c, left);
-    }
-    // dy and xh = h rstd; codes beyond the row are no numbers
-    __device__ __forceinline__ void get(float rstd, int left, float (&g)[8], float (&x)[8]) const {
-      dy.get(g);
-      h.get(x);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = (kFormat < 0 || e < left) ? x[e] * rstd : 0.f;
-    }
+    std::conditional_t<kMatrix, Raw<T>, RawCodes<kMatrix ? 0 : kFormat>> h;
   };
-  auto dot = [](const Eight& e8, float rstd, int left, const float (&w)[8]) {
-    float g[8], x[8], q = 0.f;
-    e8.get(rstd, left, g, x);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) q += w[e] * g[e] * x[e];
-    return q;
+  auto load = [&](int64_t row, int c, Eight& e8) {
+    const bool live = row < p.rows;
+    const int64_t at = live ? row : 0;
+    const int left = live ? p.cols - c : kNoRow;
+    e8.dy.template load<kVec>(Row<const T>(p.dy, at, p.rows), c, left);
+    if constexpr (kMatrix) e8.h.template load<kVec>(Row<const T>(p.h, at, p.rows), c, left);
+    else e8.h.load(p.h8, at, c, left > 0);
+    e8.dh.zero();
+    if (past) e8.dh.template load<kVec>(Row<const T>(p.dh, at, p.rows), c, left);
   };
+  auto settle = [&](int64_t row, int c, Eight& e8) {
+    const int64_t at = row < p.rows ? row : 0;
+    const int left = row < p.rows ? p.cols - c : kNoRow;
+    e8.dy.template settle<kVec>(Row<const T>(p.dy, at, p.rows), c, left);
+    if constexpr (kMatrix) e8.h.template settle<kVec>(Row<const T>(p.h, at, p.rows), c, left);
+    if (past) e8.dh.template settle<kVec>(Row<const T>(p.dh, at, p.rows), c, left);
+  };
+  // The gain of the thread's channels, for every row.
+  float gain[kVecs][8];
+#pragma unroll
+  for (int v = 0; v < kVecs; ++v) weight8(p.weight, p.wdt, 8 * t + v * span, whole ? p.cols - 8 * t - v * span : 0, wvec, gain[v]);
+  const int64_t step = (int64_t)gridDim.x * nrows;
+  int64_t row0 = (int64_t)blockIdx.x * nrows;
   Eight now[kVecs];
-  float rstd = 0.f;
-  const int64_t step = (int64_t)gridDim.x * kRows;
-  int64_t row0 = (int64_t)blockIdx.x * kRows;
-  if (row0 + slot < p.rows) rstd = p.rstd[row0 + slot];
+  float rstd = row0 + slot < p.rows ? p.rstd[row0 + slot] : 0.f;
   if (whole) {
 #pragma unroll
-    for (int v = 0; v < kVecs; ++v) now[v].load(p, row0 + slot, 8 * t + v * kSpan);
+    for (int v = 0; v < kVecs; ++v) load(row0 + slot, 8 * t + v * span, now[v]);
   }
   for (int turn = 0; row0 < p.rows; row0 += step, turn ^= 1) {
     const int64_t row = row0 + slot;
     const bool live = row < p.rows;
+    auto left_of = [&](int c) { return live ? p.cols - c : kNoRow; };
+    // dy and xh = h rstd; codes beyond the row are no numbers
+    auto get = [&](const Eight& e8, int left, float (&g)[8], float (&x)[8]) {
+      e8.dy.get(g);
+      e8.h.get(x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = (kMatrix || e < left) ? x[e] * rstd : 0.f;
+    };
+    auto dot = [&](int c, const Eight& e8, const float (&w)[8]) {
+      float g[8], x[8], q = 0.f;
+      get(e8, left_of(c), g, x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) q += w[e] * g[e] * x[e];
+      return q;
+    };
     Eight next[kVecs];
     const float rstd_next = row + step < p.rows ? p.rstd[row + step] : 0.f;
     float s = 0.f;
     if (whole) {
 #pragma unroll
-      for (int v = 0; v < kVecs; ++v) next[v].load(p, row0 + step + slot, 8 * t + v * kSpan);
+      for (int v = 0; v < kVecs; ++v) load(row + step, 8 * t + v * span, next[v]);
 #pragma unroll
-      for (int v = 0; v < kVecs; ++v) s += dot(now[v], rstd, live ? p.cols - 8 * t - v * kSpan : 0, gain[v]);
+      for (int v = 0; v < kVecs; ++v) {
+        settle(row, 8 * t + v * span, now[v]);
+        s += dot(8 * t + v * span, now[v], gain[v]);
+      }
     } else {
-      for (int c = 8 * t; c < p.cols; c += kSpan) {
-        now[0].load(p, row, c);
-        weight8(p.weight, p.wdt, c, p.cols - c, gain[0]);
-        s += dot(now[0], rstd, live ? p.cols - c : 0, gain[0]);
+      for (int c = 8 * t; c - 8 * t < p.cols; c += span) {
+        load(row, c, now[0]);
+        settle(row, c, now[0]);
+        weight8(p.weight, p.wdt, c, left_of(c), wvec, gain[0]);
+        s += dot(c, now[0], gain[0]);
       }
     }
-    s = row_sum<kThreads, kRows>(s, part, slot, turn);
-    const float mean = s / (float)p.cols;
-    auto put = [&](int c, const Eight& e8, const float (&w)[8], float (&a)[8]) {
-      const int left = live ? p.cols - c : 0;
-      if (left <= 0) return;
-      float g[8], x[8], dx[8];
-      e8.get(rstd, left, g, x);
+    s = team.sum(s, part, turn);
+    const float mean = s * inv_cols;
+    T* dxp = row_of<T>(p.dx, live ? row : 0);
+    auto put = [&](int c, const Eight& q, const float (&w)[8], float (&a)[8]) {
+      const int left = left_of(c);
+      float g[8], x[8], d[8];
+      get(q, left, g, x);
 #pragma unroll
       for (int e = 0; e < 8; ++e) a[e] += g[e] * x[e];
       if (p.dx.data == nullptr) return;
+      q.dh.get(d);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) dx[e] = rstd * (w[e] * g[e] - x[e] * mean);
-      if (kPast) {
-        float d[8];
-        e8.dh.get(d);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) dx[e] += d[e];
-      }
-      store8<kVec>(row_of<T>(p.dx, row) + c, left, dx);
+      for (int e = 0; e < 8; ++e) d[e] += rstd * (w[e] * g[e] - x[e] * mean);
+      Raw<T> out;
+      out.set(d);
+      out.template store<kVec>(dxp + c, left);
     };
     if (whole) {
 #pragma unroll
       for (int v = 0; v < kVecs; ++v) {
-        put(8 * t + v * kSpan, now[v], gain[v], acc[v]);
+        if (v * span < p.cols) put(8 * t + v * span, now[v], gain[v], acc[v]);
         now[v] = next[v];
       }
     } else {
-      for (int c = 8 * t; c < p.cols; c += kSpan) {
+      for (int c = 8 * t; c - 8 * t < p.cols; c += span) {
         float a[8] = {};
-        now[0].load(p, row, c);
-        weight8(p.weight, p.wdt, c, p.cols - c, gain[0]);
+        load(row, c, now[0]);
+        settle(row, c, now[0]);
+        weight8(p.weight, p.wdt, c, left_of(c), wvec, gain[0]);
         put(c, now[0], gain[0], a);
-        if (want && live)
+        if (want)
           for (int e = 0; e < 8 && c + e < p.cols; ++e) sums[c + e] += a[e];
       }
     }
     rstd = rstd_next;
   }
-  if (want && whole) {
+  if (!want || !whole) return;
+  if (nrows > 1) {
+    for (int k = 0; k < nrows; ++k) {   // slot by slot
+      if (slot == k) {
 #pragma unroll
-    for (int v = 0; v < kVecs; ++v) {
-      const int c = 8 * t + v * kSpan;
+        for (int v = 0; v < kVecs; ++v)
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (c + e < p.cols) sums[c + e] = acc[v][e];
+          for (int e = 0; e < 8; ++e) {
+            const int i = 8 * t + v * span + e;
+            if (k > 0) acc[v][e] += joined[i];
+            joined[i] = acc[v][e];
+          }
+      }
+      __syncthreads();
     }
+    if (slot != nrows - 1) return;
+  }
+#pragma unroll
+  for (int v = 0; v < kVecs; ++v) {
+    const int c = 8 * t + v * span;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (c + e < p.cols) sums[c + e] = acc[v][e];
   }
 }
 
-// dweight from the parts: 32 columns a block, 32 runs of parts each, both in order.
+template <typename T, int kFormat, int kVecs, bool kVec, int kMost>
+int backward(const NormGradParams& p, cudaStream_t st) {
+  const int threads = row_threads(p.cols, kVecs, 1024), nrows = block_rows(threads), block = threads * nrows;
+  const int64_t blocks = (p.rows + nrows - 1) / nrows;
+  const int fit = block <= 512 ? 152 * (512 / block) : 152, most = fit < kNormGradParts ? fit : kNormGradParts;
+  const int grid = (int)(blocks < most ? blocks : most);
+  rmsnorm_grad_kernel<T, kFormat, kVecs, kVec, kMost><<<(unsigned)grid, block, 0, st>>>(p, threads);
+  return grid;
+}
+// One eight a thread up to 4096 channels; beyond, two of bf16 (16384 x 1280:
+// one 50 us, two 68 us; 2048 x 8192: 89 and 56 us).
+template <typename T, int kFormat, bool kVec>
+int backward(const NormGradParams& p, cudaStream_t st) {
+  if (p.cols <= 2048) return backward<T, kFormat, 1, kVec, 256>(p, st);
+  if (p.cols <= 4096) return backward<T, kFormat, 1, kVec, 512>(p, st);
+  if constexpr (sizeof(T) == 4) return backward<T, kFormat, 1, kVec, 1024>(p, st);
+  else return p.cols <= 8192 ? backward<T, kFormat, 2, kVec, 512>(p, st) : backward<T, kFormat, 2, kVec, 1024>(p, st);
+}
+// Returns the number of blocks, each of which leaves a part of dweight.
+template <typename T>
+int backward(const NormGradParams& p, cudaStream_t st) {
+  constexpr int size = sizeof(T);
+  const bool vec = aligned(p.dy, size, p.rows) && aligned(p.h, size, p.rows) && aligned(p.dh, size, p.rows) && aligned(p.dx, size, p.rows);
+  count_launch();
+  if (p.h8.data == nullptr) return vec ? backward<T, -1, true>(p, st) : backward<T, -1, false>(p, st);
+  if (p.h8.format == LM_CODE_I8) return vec ? backward<T, LM_CODE_I8, true>(p, st) : backward<T, LM_CODE_I8, false>(p, st);
+  return vec ? backward<T, LM_CODE_E4M3, true>(p, st) : backward<T, LM_CODE_E4M3, false>(p, st);
+}
+
+// dweight from the blocks' parts: 32 columns a block, 32 runs of parts each, both in order.
 __global__ void __launch_bounds__(1024) norm_dweight_kernel(const float* parts, int nparts, int cols, void* dweight, int dwdt) {
   __shared__ float run[32][33];
   const int c = blockIdx.x * 32 + (threadIdx.x & 31), k = threadIdx.x >> 5;
@@ -158,40 +217,12 @@ __global__ void __launch_bounds__(1024) norm_dweight_kernel(const float* parts, 
   else static_cast<__nv_bfloat16*>(dweight)[c] = __float2bfloat16_rn(s);
 }
 
-template <typename T, int kFormat, bool kPast>
-int backward(const NormGradParams& p, bool vec, cudaStream_t st) {
-  int parts = 0;
-  by_shape<T>(p.cols, [&](auto shape) {
-    using S = decltype(shape);
-    const int64_t blocks = (p.rows + S::kRows - 1) / S::kRows;
-    constexpr int kFit = 152 * (S::kBlock <= 512 ? 512 / S::kBlock : 1), kMost = kFit * S::kRows < kNormGradParts ? kFit : kNormGradParts / S::kRows;
-    const unsigned grid = (unsigned)(blocks < kMost ? blocks : kMost);
-    parts = (int)grid * S::kRows;
-    if (vec) rmsnorm_grad_kernel<T, kFormat, kPast, S, true><<<grid, S::kBlock, 0, st>>>(p);
-    else rmsnorm_grad_kernel<T, kFormat, kPast, S, false><<<grid, S::kBlock, 0, st>>>(p);
-  });
-  return parts;
-}
-template <typename T, int kFormat>
-int backward(const NormGradParams& p, bool vec, cudaStream_t st) {
-  return p.dh.data != nullptr ? backward<T, kFormat, true>(p, vec, st) : backward<T, kFormat, false>(p, vec, st);
-}
-template <typename T>
-int backward(const NormGradParams& p, bool vec, cudaStream_t st) {
-  if (p.h8.data != nullptr) return p.h8.format == LM_CODE_I8 ? backward<T, LM_CODE_I8>(p, vec, st) : backward<T, LM_CODE_E4M3>(p, vec, st);
-  return backward<T, -1>(p, vec, st);
-}
-
 }  // namespace
 
 cudaError_t launch_rmsnorm_grad(lm_dtype dt, const NormGradParams& p, cudaStream_t st) {
   int parts = 0;
   if (p.rows > 0) {
-    const int size = dt == LM_F32 ? 4 : 2;
-    const bool vec = aligned(p.dy, size, p.rows) && aligned(p.h, size, p.rows) &&
-                     aligned(p.dh, size, p.rows) && aligned(p.dx, size, p.rows);
-    count_launch();
-    parts = dt == LM_BF16 ? backward<__nv_bfloat16>(p, vec, st) : backward<float>(p, vec, st);
+    parts = dt == LM_BF16 ? backward<__nv_bfloat16>(p, st) : backward<float>(p, st);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
   }

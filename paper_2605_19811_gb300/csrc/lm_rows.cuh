@@ -1,5 +1,6 @@
-// What the RMS norm's kernels (lm_rmsnorm.cu, lm_rmsnorm_grad.cu) share: eight
-// channels of a row as they are read, sums over a row, shapes by channels.
+// What the row kernels (lm_rmsnorm.cu, lm_rmsnorm_grad.cu, lm_checkpoint8.cu)
+// share: eight channels of a row to a lane, 256 consecutive ones to a warp,
+// whatever the row's alignment; sums over a row; shapes by channel count.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -15,53 +16,178 @@ namespace rows {
 namespace {
 
 constexpr uint32_t kAll = 0xFFFFFFFFu;
+constexpr int kNoRow = -(1 << 30);
 
-// Eight channels as they are read, `left` of them inside the row (zeros
-// beyond).  kVec: eights lie on 16-byte boundaries; else one by one.
-template <typename T> struct Raw;
-template <> struct Raw<__nv_bfloat16> {
-  uint4 u;
-  __device__ __forceinline__ void zero() { u = make_uint4(0u, 0u, 0u, 0u); }
-  template <bool kVec>
-  __device__ __forceinline__ void load(const __nv_bfloat16* p, int left) {
-    if (kVec && left >= 8) {
-      u = __ldcs(reinterpret_cast<const uint4*>(p));
-    } else {
-      const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
-      uint32_t e[8];
+// A row of a matrix for loads in 16-byte pieces: `edge` where such a piece,
+// begun in the row, could reach beyond the matrix's first or last element (its
+// first and last rows, and all where a row is shorter than a piece).
+template <typename T>
+struct Row {
+  T* p;
+  bool edge;
+  __device__ __forceinline__ Row(const Mat& m, int64_t row, int64_t nrows)
+      : p(static_cast<T*>(m.data) + row * m.ld), edge(row == 0 || row == nrows - 1 || m.ld * (int64_t)sizeof(T) < 16) {}
+};
+
+// 16 bytes into registers of their own, zero without `in`: one piece of code, so
+// that nothing waits for the load before its values are used.
+__device__ __forceinline__ void load16(uint32_t* w, const void* p, bool in) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "mov.u32 %0, 0;\n\tmov.u32 %1, 0;\n\tmov.u32 %2, 0;\n\tmov.u32 %3, 0;\n\t"
+      "@q ld.global.cs.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+      : "=&r"(w[0]), "=&r"(w[1]), "=&r"(w[2]), "=&r"(w[3])
+      : "l"(p), "r"((int)in));
+}
+
+// Eight channels of a row as they are read; `left`: channels from the first of
+// them to the row's end (kNoRow where there is no row), zeros beyond.  All 32
+// lanes of a warp take part, each with the eight after its neighbour's.  load
+// sends the loads out, settle (with the same arguments) makes the eight of them.
+//   kVec: eights lie on 16-byte boundaries, one or two 16-byte loads.
+//   else: the warp's 256 channels begin `shift` bytes after such a boundary;
+//   the lanes load the 16-byte pieces from there on, lane 31 one more, and
+//   each puts its eight together from its own pieces and its neighbour's.
+template <typename T>
+struct Raw {
+  static constexpr int kPieces = 8 * (int)sizeof(T) / 16, kWords = 4 * kPieces;
+  uint32_t w[kWords + 4];     // the last four: lane 31's further piece, until settle
+  __device__ __forceinline__ void zero() {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) e[k] = k < left ? q[k] : 0u;
-      u = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
-    }
+    for (int k = 0; k < kWords + 4; ++k) w[k] = 0u;
   }
-  __device__ __forceinline__ void get(float (&v)[8]) const {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  template <bool kVec>
+  __device__ __forceinline__ void load(const Row<const T>& row, int c, int left) {
+    const T* p = row.p + c;
+    if (kVec) {
+#pragma unroll
+      for (int k = 0; k < kPieces; ++k) load16(w + 4 * k, reinterpret_cast<const uint4*>(p) + k, left >= 8);
+      if (left > 0 && left < 8) single(p, left);
+      return;
+    }
+    const int shift = (int)(reinterpret_cast<uintptr_t>(p) & 15u), bytes = max(left, -8) * (int)sizeof(T);   // to the row's end
+    const uint8_t* first = reinterpret_cast<const uint8_t*>(p) - shift;
+    const int mine = (threadIdx.x & 31) == 31 ? kPieces + 1 : kPieces;
+#pragma unroll
+    for (int k = 0; k <= kPieces; ++k) load16(w + 4 * k, first + 16 * k, !row.edge && left != kNoRow && k < mine && 16 * k - shift < bytes);
+  }
+  template <bool kVec>
+  __device__ __forceinline__ void settle(const Row<const T>& row, int c, int left) {
+    if (kVec) return;
+    const T* p = row.p + c;
+    if (row.edge) {
+      single(p, left);
+      return;
+    }
+    const uint32_t shift = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15u);   // the same in every lane: eights are 16 or 32 bytes apart
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      v[2 * k] = __uint_as_float(w[k] << 16);
-      v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+      const uint32_t next = __shfl_down_sync(kAll, w[k], 1);
+      if ((threadIdx.x & 31) != 31) w[kWords + k] = next;
+    }
+    // by two words, one word, and half a word
+#pragma unroll
+    for (int k = 0; k < kWords + 2; ++k) w[k] = (shift & 8u) ? w[k + 2] : w[k];
+#pragma unroll
+    for (int k = 0; k < kWords + 1; ++k) w[k] = (shift & 4u) ? w[k + 1] : w[k];
+#pragma unroll
+    for (int k = 0; k < kWords; ++k) w[k] = sizeof(T) == 2 ? __funnelshift_r(w[k], w[k + 1], (shift & 2u) * 8u) : w[k];
+    if (left < 8) {
+#pragma unroll
+      for (int k = 0; k < kWords; ++k) {
+        if (sizeof(T) == 4) w[k] = k < left ? w[k] : 0u;
+        else w[k] = 2 * k + 1 < left ? w[k] : 2 * k < left ? w[k] & 0xFFFFu : 0u;
+      }
     }
   }
-};
-template <> struct Raw<float> {
-  float4 a, b;
-  __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
-  template <bool kVec>
-  __device__ __forceinline__ void load(const float* p, int left) {
-    if (kVec && left >= 8) {
-      a = __ldcs(reinterpret_cast<const float4*>(p));
-      b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
-    } else {
-      float e[8];
+  __device__ __forceinline__ void single(const T* p, int left) {
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) e[k] = k < left ? p[k] : 0.f;
-      a = make_float4(e[0], e[1], e[2], e[3]);
-      b = make_float4(e[4], e[5], e[6], e[7]);
+      for (int k = 0; k < 8; ++k) w[k] = k < left ? reinterpret_cast<const uint32_t*>(p)[k] : 0u;
+    } else {
+      const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[k] = (2 * k < left ? (uint32_t)q[2 * k] : 0u) | (2 * k + 1 < left ? (uint32_t)q[2 * k + 1] << 16 : 0u);
     }
   }
   __device__ __forceinline__ void get(float (&v)[8]) const {
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(w[k]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v[2 * k] = __uint_as_float(w[k] << 16);
+        v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+      }
+    }
+  }
+  __device__ __forceinline__ void set(const float (&v)[8]) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(v[k]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
+        w[k] = *reinterpret_cast<const uint32_t*>(&h);
+      }
+    }
+  }
+  // The counterpart of load: all 32 lanes.  Pieces that a warp's 256 channels
+  // fill are stored 16 bytes at a time, the others one element at a time.
+  template <bool kVec>
+  __device__ __forceinline__ void store(T* p, int left) const {
+    if (kVec) {
+      if (left >= 8) {
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) __stcs(reinterpret_cast<uint4*>(p) + k, make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]));
+      } else {
+        put_single(p, 0, left);
+      }
+      return;
+    }
+    const int lane = (int)threadIdx.x & 31;
+    const int shift = (int)(reinterpret_cast<uintptr_t>(p) & 15u), bytes = max(left, 0) * (int)sizeof(T);   // to the row's end
+    // c: the neighbour's last words, then this lane's; taken back by `shift` bytes
+    uint32_t c[kWords + 4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) c[k] = __shfl_up_sync(kAll, w[kWords - 4 + k], 1);
+#pragma unroll
+    for (int k = 0; k < kWords; ++k) c[4 + k] = w[k];
+    // words from 4 - shift / 4 on: first the whole words, then half a word
+#pragma unroll
+    for (int k = kWords + 3; k >= 2; --k) c[k] = (shift & 8) ? c[k - 2] : c[k];
+#pragma unroll
+    for (int k = kWords + 3; k >= 3; --k) c[k] = (shift & 4) ? c[k - 1] : c[k];
+    uint32_t o[kWords];
+#pragma unroll
+    for (int k = 0; k < kWords; ++k) o[k] = sizeof(T) == 2 ? ((shift & 2) ? __funnelshift_l(c[k + 3], c[k + 4], 16u) : c[k + 4]) : c[k + 4];
+    uint8_t* first = reinterpret_cast<uint8_t*>(p) - shift;
+    // Piece k is stored whole where it begins among the warp's channels and ends
+    // inside the row; the last, the neighbour's first, by the neighbour.
+    bool whole[kPieces + 1];
+#pragma unroll
+    for (int k = 0; k <= kPieces; ++k) whole[k] = 16 * k + 16 - shift <= bytes && (k > 0 || lane != 0 || shift == 0) && (k < kPieces || lane != 31);
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k)
+      if (whole[k]) __stcs(reinterpret_cast<uint4*>(first) + k, make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]));
+    // the elements that no whole piece took
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int b = e * (int)sizeof(T);   // pieces b / 16 (shift below 16 - b % 16) or the next
+      const bool taken = shift + b % 16 < 16 ? whole[b / 16] : whole[b / 16 + 1];
+      if (e < left && !taken) put_one(p, e);
+    }
+  }
+  __device__ __forceinline__ void put_one(T* p, int e) const {
+    if constexpr (sizeof(T) == 4) reinterpret_cast<uint32_t*>(p)[e] = w[e];
+    else reinterpret_cast<uint16_t*>(p)[e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
+  }
+  __device__ __forceinline__ void put_single(T* p, int from, int left) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e >= from && e < left) put_one(p, e);
   }
 };
 // Eight channels of an 8-bit checkpoint: their codes and scale.
@@ -73,9 +199,14 @@ struct RawCodes {
     q = make_uint2(0u, 0u);
     scale = 0.f;
   }
-  __device__ __forceinline__ void load(const Codes& k, int64_t row, int c) {
-    q = __ldcs(reinterpret_cast<const uint2*>(k.data + row * k.ld + c));
-    scale = k.scales[(int64_t)(c / LM_CODE_GROUP) * k.ld_scales + row];
+  __device__ __forceinline__ void load(const Codes& k, int64_t row, int c, bool in) {
+    const uint8_t* q_at = k.data + row * k.ld + c;
+    const float* s_at = k.scales + (int64_t)(c / LM_CODE_GROUP) * k.ld_scales + row;
+    asm volatile(
+        "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\tmov.u32 %0, 0;\n\tmov.u32 %1, 0;\n\tmov.f32 %2, 0f00000000;\n\t"
+        "@q ld.global.cs.v2.u32 {%0, %1}, [%3];\n\t@q ld.global.f32 %2, [%4];\n\t}"
+        : "=&r"(q.x), "=&r"(q.y), "=&f"(scale)
+        : "l"(q_at), "l"(s_at), "r"((int)in));
   }
   __device__ __forceinline__ void get(float (&v)[8]) const {
     const uint32_t two[4] = {q.x, q.x >> 16, q.y, q.y >> 16};
@@ -88,57 +219,60 @@ struct RawCodes {
   }
 };
 
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-template <bool kVec>
-__device__ __forceinline__ void store8(__nv_bfloat16* p, int left, const float (&v)[8]) {
-  if (kVec && left >= 8) {
-    __stcs(reinterpret_cast<uint4*>(p), make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])));
+// Eight channels of the gain (ones where there is none); from L1 after a
+// block's first row.
+__device__ __forceinline__ void weight8(const void* w, int dt, int c, int left, bool vec, float (&v)[8]) {
+  if (w == nullptr) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = 1.f;
+  } else if (vec && left >= 8) {
+    if (dt == LM_F32) {
+      const float4 a = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(w) + c)), b = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(w) + c) + 1);
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+      v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else {
+      const uint4 u = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(w) + c));
+      const uint32_t x[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v[2 * k] = __uint_as_float(x[k] << 16);
+        v[2 * k + 1] = __uint_as_float(x[k] & 0xFFFF0000u);
+      }
+    }
   } else {
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-      if (k < left) p[k] = __float2bfloat16_rn(v[k]);
-  }
-}
-template <bool kVec>
-__device__ __forceinline__ void store8(float* p, int left, const float (&v)[8]) {
-  if (kVec && left >= 8) {
-    __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
-    __stcs(reinterpret_cast<float4*>(p) + 1, make_float4(v[4], v[5], v[6], v[7]));
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (k < left) p[k] = v[k];
-  }
-}
-// Eight channels of the gain (ones where there is none).
-__device__ __forceinline__ void weight8(const void* w, int dt, int c, int left, float (&v)[8]) {
-#pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    v[k] = 1.f;
-    if (w != nullptr && k < left) v[k] = dt == LM_F32 ? static_cast<const float*>(w)[c + k] : __bfloat162float(static_cast<const __nv_bfloat16*>(w)[c + k]);
+      v[k] = k < left ? (dt == LM_F32 ? static_cast<const float*>(w)[c + k] : __bfloat162float(static_cast<const __nv_bfloat16*>(w)[c + k])) : 1.f;
   }
 }
 
-// Sum over the kThreads threads of a row; rows of a block are told apart by
-// `slot`, `turn` alternates so that one barrier a sum is enough.
-template <int kThreads, int kRows>
-__device__ __forceinline__ float row_sum(float s, float (*part)[kRows][kThreads < 32 ? 1 : kThreads / 32], int slot, int turn) {
+// How a block takes rows: `threads` (whole warps) to a row, `rows` of them side
+// by side, a thread kVecs eights, `span` channels apart.
+struct Team {
+  int threads, rows, span, t, slot;
+  __device__ __forceinline__ explicit Team(int per_row)
+      : threads(per_row), rows((int)blockDim.x / per_row), span(8 * per_row), t((int)threadIdx.x % per_row), slot((int)threadIdx.x / per_row) {}
+  // Sum over a row's threads; `turn` alternates so that one barrier a sum is
+  // enough (every thread of the block calls it).
+  __device__ __forceinline__ float sum(float s, float (*part)[32], int turn) const {
 #pragma unroll
-  for (int o = (kThreads < 32 ? kThreads : 32) / 2; o; o >>= 1) s += __shfl_xor_sync(kAll, s, o);
-  if constexpr (kThreads > 32) {
-    constexpr int kWarps = kThreads / 32;
-    const int t = (int)threadIdx.x % kThreads;
-    if ((t & 31) == 0) part[turn][slot][t >> 5] = s;
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(kAll, s, o);
+    if (threads == 32) return s;
+    const int warps = threads >> 5;
+    if ((t & 31) == 0) part[turn][slot * warps + (t >> 5)] = s;
     __syncthreads();
     s = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) s += part[turn][slot][w];
+    for (int w = 0; w < warps; ++w) s += part[turn][slot * warps + w];
+    return s;
   }
-  return s;
+};
+// Threads for rows of cols channels, kVecs eights each, at most `most`; and how
+// many rows make a block of about 128 threads.
+int row_threads(int cols, int vecs, int most) {
+  const int t = (cols + 256 * vecs - 1) / (256 * vecs) * 32;
+  return t < most ? t : most;
 }
+int block_rows(int threads) { return threads < 128 ? 128 / threads : 1; }
 
 // The 8-bit copy of eight channels: the scale of the 16 lanes' 128 channels,
 // the codes, eight bytes a lane (the row pitch is a multiple of 16, so eight
@@ -163,30 +297,8 @@ __device__ __forceinline__ T* row_of(const Mat& m, int64_t row) {
   return static_cast<T*>(m.data) + row * m.ld;
 }
 
-// Of a block's shape: threads a row, rows at a time, eights a thread.
-template <int kThreads_, int kRows_, int kVecs_>
-struct Shape {
-  static constexpr int kThreads = kThreads_, kRows = kRows_, kVecs = kVecs_;
-  static constexpr int kBlock = kThreads * kRows, kSpan = 8 * kThreads;
-  static constexpr int kWarps = kThreads < 32 ? 1 : kThreads / 32;
-};
-
-bool aligned(const Mat& m, int size, int64_t rows) {
-  return m.data == nullptr || (reinterpret_cast<uintptr_t>(m.data) % 16 == 0 && (rows == 1 || m.ld * size % 16 == 0));
-}
-
-// Shape by channels: registers hold a row of up to 8192 (fp32) or 16384 (bf16)
-// channels; what is longer is read twice.  An eight of fp32 takes the registers
-// of two of bf16.
-template <typename T, typename F>
-void by_shape(int cols, F f) {
-  constexpr int v = sizeof(T) == 4 ? 1 : 2, m = 3 - v;   // fp32: twice the threads
-  if (cols <= 256) f(Shape<32, 8, 1>());
-  else if (cols <= 512) f(Shape<32 * m, 8 / m, v>());
-  else if (cols <= 1024) f(Shape<64 * m, 4 / m, v>());
-  else if (cols <= 2048) f(Shape<128 * m, 2 / m, v>());
-  else if (cols <= 4096) f(Shape<256 * m, 1, v>());
-  else f(Shape<512 * m, 1, v>());
+bool aligned(const Mat& m, int size, int64_t nrows) {
+  return m.data == nullptr || (reinterpret_cast<uintptr_t>(m.data) % 16 == 0 && (nrows == 1 || m.ld * size % 16 == 0));
 }
 
 }  // namespace

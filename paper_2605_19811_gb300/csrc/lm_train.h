@@ -63,9 +63,9 @@ struct NormGradParams {
   const float* rstd;
   const void* weight;
   void* dweight;
-  float* parts;         // dweight summed over the rows of each of at most kNormGradParts shares: shares x cols
+  float* parts;         // dweight summed over each block's rows: blocks x cols
 };
-constexpr int kNormGradParts = 1216;   // most shares of the rows in a norm's gradient
+constexpr int kNormGradParts = 608;    // most blocks of a norm's gradient
 cudaError_t launch_rmsnorm_grad(lm_dtype dt, const NormGradParams& p, cudaStream_t st);
 
 cudaError_t launch_pack8(lm_dtype dt, const Mat& x, int64_t rows, int64_t cols, const Codes& c, cudaStream_t st);

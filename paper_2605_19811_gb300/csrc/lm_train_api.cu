@@ -266,9 +266,8 @@ lm_status lm_rmsnorm(const lm_matrix* x, const lm_matrix* residual, const lm_ten
 
 size_t lm_rmsnorm_grad_workspace(int64_t rows, int64_t cols) {
   if (rows <= 0 || cols <= 0) return 0;
-  // rows are shared out in eights at most: up to seven shares may be empty
-  const int64_t shares = rows + 7 < kNormGradParts ? rows + 7 : kNormGradParts;
-  return (size_t)shares * (size_t)cols * sizeof(float);
+  const int64_t blocks = rows < kNormGradParts ? rows : kNormGradParts;
+  return (size_t)blocks * (size_t)cols * sizeof(float);
 }
 
 lm_status lm_rmsnorm_grad(const lm_matrix* dy, const lm_matrix* h, const lm_checkpoint8* h8, const float* rstd,

@@ -21,7 +21,7 @@ DT = {"bf16": torch.bfloat16, "f32": torch.float32}
 ROUND = {"bf16": 2.0 ** -8, "f32": 2.0 ** -22}
 U = 2.0 ** -24
 SIZES = [(1, 1), (2, 3), (1, 128), (3, 130), (5, 768), (4, 1280), (2, 1283), (3, 4096), (2, 8200), (1, 16384), (2, 33000),
-         (700, 96), (1300, 256)]
+         (700, 96), (1300, 256), (6, 500), (9, 1000), (7, 1200), (5, 2047), (3, 3001), (2, 6000), (2, 9999)]
 
 
 def terms(cols):
