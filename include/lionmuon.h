@@ -492,7 +492,9 @@ lm_status lm_token_logprob_grad(const lm_token_logprob_args* a, void* cuda_strea
  * are powers of two so that code * s is a bf16 number: the tensor cores take
  * a checkpoint without a second rounding.  A group that holds a NaN or an
  * infinity has scale NaN and reads back as NaN.  A code that would stand for 2^128
- * is lowered to the one below it (63 under a scale of 2^122, 240 under 2^120). */
+ * is lowered to the one below it (63 under a scale of 2^122, 240 under 2^120).
+ * Readers take checkpoints as lm_checkpoint8_pack writes them: a scale is a
+ * power of two or NaN, and no e4m3 code is a NaN. */
 #define LM_CODE_GROUP 128
 typedef enum { LM_CODE_I8 = 0, LM_CODE_E4M3 = 1 } lm_code_format;
 typedef struct {
@@ -518,7 +520,8 @@ lm_status lm_checkpoint8_unpack(const lm_checkpoint8* c, const lm_matrix* x, voi
  * x or residual itself.  weight: C elements (1 x C or C x 1, bf16 or fp32),
  * NULL for ones.  rstd: T floats or NULL.  kept: NULL, or a T x C checkpoint
  * that receives y in 8 bits (from y before its rounding to x's dtype).  The
- * norm is taken of h before its rounding.  eps >= 0, finite.
+ * norm is taken of h before its rounding.  eps >= 0, finite.  The sum of
+ * squares is fp32: a row where it passes the largest float has rstd 0.
  * Errors: LM_ERR_INVALID_ARG, LM_ERR_DTYPE, LM_ERR_ALIGN, LM_ERR_UNSUPPORTED,
  * LM_ERR_CUDA. */
 lm_status lm_rmsnorm(const lm_matrix* x, const lm_matrix* residual, const lm_tensor* weight, double eps,

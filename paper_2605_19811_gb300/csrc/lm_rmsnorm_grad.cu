@@ -23,6 +23,7 @@ __global__ void __launch_bounds__(kMost, kMost == 256 ? 2 : 1) rmsnorm_grad_kern
   __shared__ float joined[64 * 8 * kVecs];        // where rows share a block they have at most 64 threads
   const Team team(threads);
   const int t = team.t, slot = team.slot, nrows = team.rows, span = team.span;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const bool whole = p.cols <= kVecs * span;
   const bool want = p.dweight != nullptr, past = p.dh.data != nullptr;
   const bool wvec = (reinterpret_cast<uintptr_t>(p.weight) & 15u) == 0;
@@ -197,17 +198,19 @@ int backward(const NormGradParams& p, cudaStream_t st) {
   return vec ? backward<T, LM_CODE_E4M3, true>(p, st) : backward<T, LM_CODE_E4M3, false>(p, st);
 }
 
-// dweight from the blocks' parts: 32 columns a block, 32 runs of parts each, both in order.
-__global__ void __launch_bounds__(1024) norm_dweight_kernel(const float* parts, int nparts, int cols, void* dweight, int dwdt) {
-  __shared__ float run[32][33];
-  const int c = blockIdx.x * 32 + (threadIdx.x & 31), k = threadIdx.x >> 5;
+// dweight from the blocks' parts: 8 columns a block, 32 runs of parts each, both
+// in order.  Its set-up overlaps the gradient kernel's end.
+__global__ void __launch_bounds__(256) norm_dweight_kernel(const float* parts, int nparts, int cols, void* dweight, int dwdt) {
+  __shared__ float run[32][9];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int c = blockIdx.x * 8 + (threadIdx.x & 7), k = threadIdx.x >> 3;
   const int each = (nparts + 31) / 32, p0 = min(nparts, k * each), p1 = min(nparts, p0 + each);
   float s = 0.f;
   if (c < cols) {
 #pragma unroll 8
     for (int i = p0; i < p1; ++i) s += parts[(int64_t)i * cols + c];
   }
-  run[k][threadIdx.x & 31] = s;
+  run[k][threadIdx.x & 7] = s;
   __syncthreads();
   if (k != 0 || c >= cols) return;
   s = 0.f;
@@ -227,8 +230,17 @@ cudaError_t launch_rmsnorm_grad(lm_dtype dt, const NormGradParams& p, cudaStream
     if (e != cudaSuccess) return e;
   }
   if (p.dweight != nullptr) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((p.cols + 7) / 8), 1, 1);
+    cfg.blockDim = dim3(256, 1, 1);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = parts > 0 ? 1 : 0;
     count_launch();
-    norm_dweight_kernel<<<(p.cols + 31) / 32, 1024, 0, st>>>(p.parts, parts, p.cols, p.dweight, p.dwdt);
+    return cudaLaunchKernelEx(&cfg, norm_dweight_kernel, (const float*)p.parts, parts, (int)p.cols, p.dweight, (int)p.dwdt);
   }
   return cudaGetLastError();
 }

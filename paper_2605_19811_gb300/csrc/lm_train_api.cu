@@ -350,6 +350,10 @@ lm_status lm_linear_wgrad8(const lm_matrix* dy, const lm_checkpoint8* x, const l
   LM_TRY(check_codes(*x, tokens, in, "x"));
   LM_TRY(check_matrix(*dw, out, in, "dw"));
   if (out == 0 || in == 0 || (tokens == 0 && accumulate != 0)) return LM_OK;
+  // the tensor maps hold strides below 2^40 bytes
+  constexpr int64_t kMost = (int64_t)1 << 38;
+  if (tokens > 0 && ((tokens > 1 && dy->ld > kMost / tokens) || out > kMost / tokens || in > kMost / tokens || x->ld_codes > kMost / tokens))
+    return fail(LM_ERR_UNSUPPORTED, "dy or x of 2^38 elements or more");
   const size_t need = lm_linear_wgrad8_workspace(dy, x, dw);
   if (need > 0) {
     if (workspace == nullptr || workspace_bytes < need)

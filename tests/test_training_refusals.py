@@ -152,6 +152,8 @@ def test_checkpoint_refusals(L):
     assert wg(dw=mat(L, rows=8, dtype=4)) == DTYPE
     assert wg(dw=mat(L, rows=8, ld=4)) == INVALID
     assert wg(x=code(L, ld=8)) == ALIGN
+    n, m = 1 << 30, 1 << 10
+    assert wg(dy=mat(L, rows=n, cols=m), x=code(L, rows=n, lds=n), dw=mat(L, rows=m)) == UNSUPPORTED
     assert wg(dy=mat(L, cols=0), dw=mat(L, rows=0)) == 0
 
 
