@@ -45,13 +45,12 @@ __device__ __forceinline__ void load16(uint32_t* w, const void* p, bool in) {
 // lanes of a warp take part, each with the eight after its neighbour's.  load
 // sends the loads out, settle (with the same arguments) makes the eight of them.
 //   kVec: eights lie on 16-byte boundaries, one or two 16-byte loads.
-//   else, bf16: the warp's 256 channels begin `shift` bytes after such a
-//   boundary; the lanes load the 16-byte pieces from there on, lane 31 one more,
-//   and each puts its eight together from its own pieces and its neighbour's
-//   (8191 x 1283: norm 72 -> 48 us against elements one by one).
-//   else, fp32: one by one (the pieces cost more than they save: the gradient of
-//   8191 x 1283 takes 46 us so, 70 us in pieces).
-template <typename T>
+//   else: the warp's 256 channels begin `shift` bytes after such a boundary; the
+//   lanes load the 16-byte pieces from there on, lane 31 one more, and each puts
+//   its eight together from its own pieces and its neighbour's (8191 x 1283:
+//   bf16 norm 48 us, 72 us with elements one by one; fp32 unpacking 16 and 37 us).
+//   kSingly: where not kVec, elements are loaded one by one.
+template <typename T, bool kSingly = false>
 struct Raw {
   static constexpr int kPieces = 8 * (int)sizeof(T) / 16, kWords = 4 * kPieces;
   uint32_t w[kWords + 4];     // the last four: lane 31's further piece, until settle
@@ -68,7 +67,7 @@ struct Raw {
       if (left > 0 && left < 8) single(p, left);
       return;
     }
-    if constexpr (sizeof(T) == 4) {
+    if constexpr (kSingly) {
       single(p, left);
       return;
     }
@@ -80,7 +79,7 @@ struct Raw {
   }
   template <bool kVec>
   __device__ __forceinline__ void settle(const Row<const T>& row, int c, int left) {
-    if (kVec || sizeof(T) == 4) return;
+    if (kVec || kSingly) return;
     const T* p = row.p + c;
     if (row.edge) {
       single(p, left);
@@ -98,10 +97,13 @@ struct Raw {
 #pragma unroll
     for (int k = 0; k < kWords + 1; ++k) w[k] = (shift & 4u) ? w[k + 1] : w[k];
 #pragma unroll
-    for (int k = 0; k < kWords; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], (shift & 2u) * 8u);
+    for (int k = 0; k < kWords; ++k) w[k] = sizeof(T) == 2 ? __funnelshift_r(w[k], w[k + 1], (shift & 2u) * 8u) : w[k];
     if (left < 8) {
 #pragma unroll
-      for (int k = 0; k < kWords; ++k) w[k] = 2 * k + 1 < left ? w[k] : 2 * k < left ? w[k] & 0xFFFFu : 0u;
+      for (int k = 0; k < kWords; ++k) {
+        if (sizeof(T) == 4) w[k] = k < left ? w[k] : 0u;
+        else w[k] = 2 * k + 1 < left ? w[k] : 2 * k < left ? w[k] & 0xFFFFu : 0u;
+      }
     }
   }
   __device__ __forceinline__ void single(const T* p, int left) {
@@ -151,10 +153,6 @@ struct Raw {
       }
       return;
     }
-    if constexpr (sizeof(T) == 4) {
-      put_single(p, 0, left);
-      return;
-    }
     const int lane = (int)threadIdx.x & 31;
     const int shift = (int)(reinterpret_cast<uintptr_t>(p) & 15u), bytes = max(left, 0) * (int)sizeof(T);   // to the row's end
     // c: the neighbour's last words, then this lane's; taken back by `shift` bytes
@@ -170,7 +168,7 @@ struct Raw {
     for (int k = kWords + 3; k >= 3; --k) c[k] = (shift & 4) ? c[k - 1] : c[k];
     uint32_t o[kWords];
 #pragma unroll
-    for (int k = 0; k < kWords; ++k) o[k] = (shift & 2) ? __funnelshift_l(c[k + 3], c[k + 4], 16u) : c[k + 4];
+    for (int k = 0; k < kWords; ++k) o[k] = sizeof(T) == 2 ? ((shift & 2) ? __funnelshift_l(c[k + 3], c[k + 4], 16u) : c[k + 4]) : c[k + 4];
     uint8_t* first = reinterpret_cast<uint8_t*>(p) - shift;
     // Piece k is stored whole where it begins among the warp's channels and ends
     // inside the row; the last, the neighbour's first, by the neighbour.
