@@ -9,10 +9,13 @@
 //   lse = ln2 (C + log2 S),  log p_j = ln2 (d_j - log2 S),  H = ln2 (log2 S - T / S)
 //   dz_j = 2^d_j (a0 + a1 d_j) (+ g_logp at the target),
 //   a1 = -g_H ln2 / S,  a0 = (g_lse - g_logp - g_H (H - ln2 log2 S)) / S
-// The gradient in the same call reads the row again, from L2: at most 2048
-// threads x 152 SMs of rows are in flight, some 60 MB.  The forward is bound by
-// memory; the gradient by memory and, at 74%, the exponential unit (16 a clock
-// and SM; two exponentials a value against 4 bytes moved in bf16).
+// The gradient in the same call reads the row again, from L2, which its first
+// reading asks to keep it and its second to give it up: 2432 x 50304 bf16 (245
+// MB) then reads 270 MB from memory; an earlier form without the hints, 403 MB.
+// Bound by memory: 16384 x 50304 bf16, forward 262 us (6.3 TB/s), with the
+// gradient 552 us (6.0 TB/s read and written once), gradient alone 483 us (6.8
+// TB/s).  Issue slots are 59% and the exponential unit 31% busy.  fp32 forward
+// 2049 x 50257: 80 us (5.1 TB/s), with five alternatives 100 us.
 //
 // Values below -1e38 (masks: -inf, the type's lowest) are raised to it, which
 // changes nothing in a row whose maximum is within +-1e6.  Rows beyond that
@@ -33,7 +36,6 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLowest = -9.969209968386869e37f;   // -0x1.2cp126, a bf16 number: what smaller values are raised to
 constexpr float kFar = 1e6f;
-constexpr float kSlack = 6.f;                       // the reference moves only when a value is this far above it
 constexpr float kGone = -1e5f;                      // 2^kGone is 0
 constexpr int kMaxCluster = 8;
 constexpr int kCandidates = 1024;                   // of a block's alternatives
@@ -163,7 +165,9 @@ struct Part {
   }
 };
 
-// Vectors a thread loads ahead: more for long rows, which have the registers' time.
+// Vectors a thread loads ahead, by what measured best with the gradient: bf16
+// 16384 x 50304 four 557 us, six 564, eight 621; fp32 2049 x 50257 four 188 us,
+// eight 162.  Two for 128 threads: 16384 x 2000 54 us, four 59 us.
 template <typename T>
 constexpr int ahead_of(int threads) { return threads == 128 ? 2 : sizeof(T) == 4 ? 8 : 4; }
 
@@ -173,12 +177,11 @@ struct Stats {
 };
 // Sums of a thread: reference m with c = m log2 e.
 struct Running {
-  float m, c, limit;   // limit: what a value may reach before m moves
+  float m, c;
   float2 s, t;
   __device__ __forceinline__ void start() {
     m = kLowest;
     c = kLowest * kLog2e;
-    limit = kLowest;
     s = t = make_float2(0.f, 0.f);
   }
   __device__ __forceinline__ void raise(float to) {
@@ -186,7 +189,6 @@ struct Running {
     t = make_float2(f * (t.x + a * s.x), f * (t.y + a * s.y));
     s = make_float2(f * s.x, f * s.y);
     m = to;
-    limit = to + kSlack;
     c = c2;
   }
   __device__ __forceinline__ void add(float2 x) {
@@ -197,7 +199,7 @@ struct Running {
   }
   __device__ __forceinline__ void add1(float x) {
     x = max_nan(x, kLowest);
-    if (x > limit) raise(x);
+    if (x > m) raise(x);
     const float d = fmaf(x, kLog2e, -c), e = ex2(d);
     s.x += e;
     t.x += e * d;
@@ -595,7 +597,7 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobParams p
   walk<kThreads, ahead_of<T>(kThreads)>(src, n, p.dlogits != nullptr ? l2_policy<kKeep>() : l2_policy<kGiveUp>(), [&](const auto& raw, int i) {
     constexpr int kN = sizeof(raw) / sizeof(raw[0]);
     const float most = Vec<T>::most(raw);
-    if (most > r.limit) r.raise(most);
+    if (most > r.m) r.raise(most);
     if (kTop) best = fmaxf(best, most);
 #pragma unroll
     for (int k = 0; k < kN; ++k) {
@@ -728,13 +730,19 @@ __global__ void __launch_bounds__(kThreads) logprob_grad_kernel(const LogprobPar
   gradient<T, kThreads, kNeither>(p, row_i, z, split, part, row, h, args);
 }
 
-constexpr int kShort = 2500;   // vectors of a row up to which 128 threads take it
+// Vectors of a row up to which 128 threads take it, else 256: 16384 x 2000 bf16
+// with the gradient 54 us with 128 threads, 99 with 256; 16384 x 5000 bf16
+// gradient alone 61 and 82; 16384 x 50304 with the gradient 757 and 717 us
+// (both before the later steps).
+constexpr int kShort = 2500;
 
-// Blocks a row: one where the rows fill the GPU three blocks deep; else as
-// many, up to eight, as leave each thread a vector.
+// Blocks a row: as many, up to eight, as give every SM a block and leave each
+// thread a vector.  V 50304 bf16, forward: 1 row 8 us with a cluster, 10 without;
+// 200 rows 17 us with clusters up to three blocks an SM, 12 without; gradient of
+// 64 rows 8 us with, 12 without.
 int cluster_for(int64_t rows, int64_t vectors, int threads) {
   int c = 1;
-  while (c < kMaxCluster && rows * c < 3 * 152 && vectors / (2 * c) >= threads) c *= 2;
+  while (c < kMaxCluster && rows * c < 152 && vectors / (2 * c) >= threads) c *= 2;
   return c;
 }
 
@@ -763,15 +771,13 @@ cudaError_t forward(const LogprobParams& p, cudaStream_t st) {
 template <typename T>
 cudaError_t launch(LogprobParams p, bool gradient_only, cudaStream_t st) {
   const int64_t vectors = p.vocab / Vec<T>::kWidth;
+  const int threads = vectors <= kShort ? 128 : 256;
   if (gradient_only) {
-    // short rows: small blocks, so that few threads idle
-    const int threads = vectors < 512 ? 128 : 256;
     p.cluster = p.dlogits == p.logits ? 1 : cluster_for(p.rows, vectors, threads);   // a far row is read whole by each of its blocks, before any writes
     if (threads == 128)
       return p.cluster > 1 ? start(logprob_grad_kernel<T, 128, true>, 128, p, st) : start(logprob_grad_kernel<T, 128, false>, 128, p, st);
     return p.cluster > 1 ? start(logprob_grad_kernel<T, 256, true>, 256, p, st) : start(logprob_grad_kernel<T, 256, false>, 256, p, st);
   }
-  const int threads = vectors <= kShort ? 128 : 256;
   p.cluster = cluster_for(p.rows, vectors, threads);
   return threads == 128 ? forward<T, 128>(p, st) : forward<T, 256>(p, st);
 }
