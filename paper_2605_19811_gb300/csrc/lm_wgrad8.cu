@@ -12,6 +12,11 @@
 // cost more: the conversion shares the shared memory's bandwidth with the MMA,
 // 440 ns instead of 350 for a pair's 64 tokens.)
 //
+// Measured (X made bf16, product, join; kernels alone): 16384 x 768 x 2304
+// e4m3 to bf16 9 + 47 + 9 us, a call 62 us; 16384 x 4096 x 14336 int8 to fp32
+// 43 + 1086 + 11 us, a call 1230 to 1270 us (1.51 to 1.56 PFLOP/s).  Bound by
+// the tensor pipe where dW has many tiles, else by the three launches.
+//
 // Both operands lie token by token in memory, so both are MN-major: rows of
 // 64 channels (128 bytes, 128-byte swizzle), one row a token.  CTA r of the
 // pair holds output channels 128 r .. of the tile (A, from dY) and input
