@@ -18,7 +18,7 @@ using namespace rows;
 // kMost: threads a block has at most.
 template <typename T, int kFormat, int kVecs, bool kVec, int kMost>
 __global__ void __launch_bounds__(kMost, kMost == 256 ? 2 : 1) rmsnorm_grad_kernel(const NormGradParams p, int threads) {
-  constexpr bool kMatrix = kFormat < 0;
+  constexpr bool kMatrix = kFormat < 0, kAhead = kMost < 1024;   // the next row's loads before this row's sums
   __shared__ float part[2][32];
   __shared__ float joined[64 * 8 * kVecs];        // where rows share a block they have at most 64 threads
   const Team team(threads);
@@ -68,7 +68,7 @@ __global__ void __launch_bounds__(kMost, kMost == 256 ? 2 : 1) rmsnorm_grad_kern
   int64_t row0 = (int64_t)blockIdx.x * nrows;
   Eight now[kVecs];
   float rstd = row0 + slot < p.rows ? p.rstd[row0 + slot] : 0.f;
-  if (whole) {
+  if (kAhead && whole) {
 #pragma unroll
     for (int v = 0; v < kVecs; ++v) load(row0 + slot, 8 * t + v * span, now[v]);
   }
@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(kMost, kMost == 256 ? 2 : 1) rmsnorm_grad_kern
     float s = 0.f;
     if (whole) {
 #pragma unroll
-      for (int v = 0; v < kVecs; ++v) load(row + step, 8 * t + v * span, next[v]);
+      for (int v = 0; v < kVecs; ++v) load(kAhead ? row + step : row, 8 * t + v * span, kAhead ? next[v] : now[v]);
 #pragma unroll
       for (int v = 0; v < kVecs; ++v) {
         settle(row, 8 * t + v * span, now[v]);
@@ -130,7 +130,7 @@ __global__ void __launch_bounds__(kMost, kMost == 256 ? 2 : 1) rmsnorm_grad_kern
 #pragma unroll
       for (int v = 0; v < kVecs; ++v) {
         if (v * span < p.cols) put(8 * t + v * span, now[v], gain[v], acc[v]);
-        now[v] = next[v];
+        if (kAhead) now[v] = next[v];
       }
     } else {
       for (int c = 8 * t; c - 8 * t < p.cols; c += span) {
@@ -182,6 +182,10 @@ int backward(const NormGradParams& p, cudaStream_t st) {
 }
 // One eight a thread up to 4096 channels; beyond, two of bf16 (16384 x 1280:
 // one 50 us, two 68 us; 2048 x 8192: 89 and 56 us).
+// 1024 threads (fp32 beyond 4096 channels, bf16 beyond 8192) have 64 registers
+// each, too few for the next row's loads too: 2048 x 8192 fp32 158 us with
+// them, 70 without (two eights and 512 threads: 88); 2048 x 16384 bf16 225 and
+// 123; 2047 x 12001 bf16 352 and 132.
 template <typename T, int kFormat, bool kVec>
 int backward(const NormGradParams& p, cudaStream_t st) {
   if (p.cols <= 2048) return backward<T, kFormat, 1, kVec, 256>(p, st);
