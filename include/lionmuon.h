@@ -549,7 +549,9 @@ lm_status lm_rmsnorm_grad(const lm_matrix* dy, const lm_matrix* h, const lm_chec
  *   dw (+)= dy^T x      dw: out x in, dy: T x out, x: T x in
  * dw is bf16 or fp32, dy bf16 or fp32 (independently); accumulate != 0 adds to
  * dw, else dw is overwritten.  Products are exact and the sum over tokens is
- * taken in a fixed order: the same inputs give the same bits.
+ * taken in a fixed order: the same inputs give the same bits.  The tensor cores
+ * add at most 512 tokens (each addition of 16 may drop 2^-23 of what it has);
+ * their sums are added in fp32, whatever the type of dw.
  * workspace: lm_linear_wgrad8_workspace(...) bytes of device memory for the
  * same arguments, 256-byte aligned, free again when the work is done (x in
  * bf16, dy where it is fp32 or its rows are not 16-byte aligned, and partial

@@ -27,12 +27,14 @@
 //   warp 1      TMEM allocation; MMA issuer (CTA 0, one lane)
 //   warps 4-11  epilogue: one TMEM lane quadrant and half of the columns each
 //
-// Accumulation: the tensor cores lose up to a unit of the last place of the
-// accumulator at each addition (16 tokens).  For a bf16 result that is far
-// below its own rounding and a tile's whole sum stays in TMEM.  For an fp32
-// result the sum is cut every kChunk blocks (512 tokens): the epilogue adds
-// the accumulator to sums it holds in registers while the MMA fills the other
-// accumulator.
+// Accumulation: the tensor cores drop up to a unit of the last place of the
+// accumulator at each addition (16 tokens), always towards zero, so what a long
+// sum loses grows with its length (left in TMEM to its end, 16384 tokens of fp32
+// dY lost 5e-5 to 7e-5 of a result).  A sum of more than kChunk blocks (512
+// tokens, at most 2^-19 of them lost on average) is therefore cut every kChunk
+// blocks, for bf16 results too: the epilogue adds the accumulator, in fp32, to
+// sums it holds in registers while the MMA fills the other accumulator.  That
+// costs a bf16 result 3 to 10% (16384 x 4096 x 14336: 1091 -> 1130 us).
 //
 // Schedule: as many tiles as fill whole waves of the pairs go one to a pair.
 // The tiles left over are one line of (tile, token block) work cut into equal
@@ -43,6 +45,8 @@
 // what its CTA had yet to write, is filled with NaN.
 #include <cuda_bf16.h>
 #include <cudaTypedefs.h>
+
+#include <algorithm>
 
 #include "lm_code8.cuh"
 #include "lm_ns_tc_shared.cuh"
@@ -62,7 +66,7 @@ constexpr int kABytes = kHalf * kBlockK * 2, kBBytes = kHalf * kBlockK * 2;
 constexpr int kStages = 6, kStageBytes = kABytes + kBBytes;
 constexpr int kFirstEpi = 4, kEpiWarps = 8;            // whole warpgroups: a warp reads the TMEM lanes of its number mod 4
 constexpr int kThreads = 32 * (kFirstEpi + kEpiWarps);
-constexpr int kChunk = 8;                              // token blocks summed in one accumulator (fp32 results)
+constexpr int kChunk = 8;                              // most token blocks summed in one accumulator
 constexpr int kPairs = 76;                             // CTA pairs of the GPU (152 SMs)
 constexpr int kTmemCols = 512;
 constexpr int kTransBytes = 32 * 20 * 4;               // an epilogue warp's transpose tile: 32 rows x 16 columns, 80-byte rows
@@ -260,7 +264,9 @@ __device__ __forceinline__ void put_block(const KernelParams& p, const Item& it,
   }
 }
 
-// kLong: sums of fp32 results, cut every kChunk token blocks.
+// kLong: some item sums more than kChunk token blocks, and the sums are cut.  Where
+// none does, the accumulator is stored as it is (512 x 768 x 50304, bf16: 56 us so,
+// 70 through the registers' sums).
 template <bool kLong>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad8_kernel(const __grid_constant__ KernelParams p) {
   extern __shared__ uint8_t smem_raw[];
@@ -625,6 +631,12 @@ Schedule make_schedule(int64_t tokens, int64_t out, int64_t in, int planes) {
   }
   return s;
 }
+// Token blocks of the longest item.
+int64_t longest_item(const Schedule& s) {
+  int64_t most = s.waves > 0 ? s.nkb : 0;
+  for (int k = 0; k < s.sharers; ++k) most = std::max(most, std::min<int64_t>(s.nkb, s.begin[k + 1] - s.begin[k]));
+  return most;
+}
 // Whether any left-over tile falls to more than one pair.
 bool has_parts(const Schedule& s) { return s.rest > 0 && s.sharers > s.rest; }
 
@@ -738,7 +750,7 @@ cudaError_t launch_wgrad8(const WgradParams& w, cudaStream_t st) {
   if (encode_operand(enc, &p.dy, dy, w.out, w.tokens, ld, planes) != CUDA_SUCCESS) return cudaErrorInvalidValue;
   if (encode_operand(enc, &p.x, x, w.in, w.tokens, l.ldx, 1) != CUDA_SUCCESS) return cudaErrorInvalidValue;
   const int pairs = p.sch.waves > 0 ? kPairs : p.sch.sharers;
-  cudaError_t e = w.dwdt == LM_F32 ? start<true>(p, pairs, st) : start<false>(p, pairs, st);
+  const cudaError_t e = longest_item(p.sch) > kChunk ? start<true>(p, pairs, st) : start<false>(p, pairs, st);
   if (e != cudaSuccess || !has_parts(p.sch)) return e;
   return launch_after(wgrad8_join_kernel, dim3(p.sch.rest, kTileM / 4), 256, 0, st, p);
 }
