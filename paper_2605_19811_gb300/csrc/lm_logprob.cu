@@ -17,10 +17,12 @@
 // TB/s).  Issue slots are 59% and the exponential unit 31% busy.  fp32 forward
 // 2049 x 50257: 80 us (5.1 TB/s), with five alternatives 100 us.
 //
-// Values below -1e38 (masks: -inf, the type's lowest) are raised to it, which
-// changes nothing in a row whose maximum is within +-1e6.  Rows beyond that
-// take a plain loop with the differences z - m (it also sorts out rows of
-// -inf, +inf and NaN).
+// Values below -2^21 (masks: -inf, the type's lowest, -1e9 ..) are raised to it,
+// which changes nothing in a row whose maximum is within +-1e6: p = 0 for both.
+// A reference is then never large: at z = m, d is c's rounding error, which
+// would itself be 100 and more for masks beyond 1e9 and overflow s and t of a
+// thread that has met nothing else.  Rows beyond that take a plain loop with the
+// differences z - m (it also sorts out rows of -inf, +inf and NaN).
 //
 // Few rows: a cluster of up to eight blocks takes a row and joins its parts
 // through distributed shared memory, in order.
@@ -34,8 +36,8 @@ namespace lm {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kLowest = -9.969209968386869e37f;   // -0x1.2cp126, a bf16 number: what smaller values are raised to
-constexpr float kFar = 1e6f;
+constexpr float kLowest = -2097152.f;               // -2^21, a bf16 number: what smaller values are raised to
+constexpr float kFar = 1e6f;                        // 2^((kLowest + kFar) log2 e) is 0
 constexpr float kGone = -1e5f;                      // 2^kGone is 0
 constexpr int kMaxCluster = 8;
 constexpr int kCandidates = 1024;                   // of a block's alternatives
