@@ -5,8 +5,11 @@
 // with s = sum 2^d and t = sum 2^d d, d = (z - m) log2 e, and scales s and t
 // when m grows:  s <- 2^a s,  t <- 2^a (t + a s),  a = (m_old - m) log2 e <= 0.
 // d is one multiply-add z log2 e - c with c = m log2 e rounded once: c, not m,
-// is the reference, so its rounding cancels.  With the row's C, S, T:
-//   lse = ln2 (C + log2 S),  log p_j = ln2 (d_j - log2 S),  H = ln2 (log2 S - T / S)
+// is the reference, so its rounding cancels (log p: 2e-6 off at most for logits
+// around 0 and around 20000 alike).  With the row's M, C, S, T:
+//   lse = M + ln2 (log2 S - (M log2 e - C)),  log p_j = ln2 (d_j - log2 S),  H = ln2 (log2 S - T / S)
+// (M log2 e - C is exact, so lse is rounded once at its own size: for logits of
+// 1000 to 1250 6.1e-5 off, half a unit, where ln2 (C + log2 S) was 1.1e-4 off.)
 //   dz_j = 2^d_j (a0 + a1 d_j) (+ g_logp at the target),
 //   a1 = -g_H ln2 / S,  a0 = (g_lse - g_logp - g_H (H - ln2 log2 S)) / S
 // The gradient in the same call reads the row again, from L2, which its first
@@ -177,17 +180,20 @@ struct Stats {
   float c, s;
   float t;
 };
+// The rounded product that is a reference; never fused into what is done with it.
+__device__ __forceinline__ float reference(float m) { return __fmul_rn(m, kLog2e); }
+
 // Sums of a thread: reference m with c = m log2 e.
 struct Running {
   float m, c;
   float2 s, t;
   __device__ __forceinline__ void start() {
     m = kLowest;
-    c = kLowest * kLog2e;
+    c = reference(kLowest);
     s = t = make_float2(0.f, 0.f);
   }
   __device__ __forceinline__ void raise(float to) {
-    const float c2 = to * kLog2e, a = fmaxf(c - c2, kGone), f = ex2(a);   // a s stays finite where 2^a is 0
+    const float c2 = reference(to), a = fmaxf(c - c2, kGone), f = ex2(a);   // a s stays finite where 2^a is 0
     t = make_float2(f * (t.x + a * s.x), f * (t.y + a * s.y));
     s = make_float2(f * s.x, f * s.y);
     m = to;
@@ -248,9 +254,9 @@ struct Row {
   bool far, empty, bad;
   float c, ls, h, lse;
   Row() = default;
-  __device__ __forceinline__ Row(float c_, float s, float t) : far(false), empty(false), bad(false), c(c_) {
+  __device__ __forceinline__ Row(float m, float c_, float s, float t) : far(false), empty(false), bad(false), c(c_) {
     ls = log2f(s);
-    lse = kLn2 * (c + ls);
+    lse = fmaf(kLn2, ls - fmaf(m, kLog2e, -c), m);
     h = kLn2 * (ls - t / s);
   }
   __device__ __forceinline__ float logp(float z) const {
@@ -642,9 +648,9 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobParams p
   float mm = m;
 #pragma unroll
   for (int o = kWarps / 2; o; o >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xFFFFFFFFu, mm, o));
-  float c = mm * kLog2e;
+  float c = reference(mm);
   {
-    const float a = fmaxf(m * kLog2e - c, kGone), f = ex2(a);
+    const float a = fmaxf(reference(m) - c, kGone), f = ex2(a);
     t = f * (t + a * s);
     s = f * s;
   }
@@ -663,7 +669,7 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobParams p
     }
     tc::cluster_sync();
     for (int b = 0; b < blocks; ++b) mm = fmaxf(mm, sh.m_part[b]);
-    c = mm * kLog2e;
+    c = reference(mm);
     s = t = 0.f;
     for (int b = 0; b < blocks; ++b) {
       const float a = fmaxf(sh.part[b].c - c, kGone), f = ex2(a);
@@ -671,7 +677,7 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const LogprobParams p
       s += f * sh.part[b].s;
     }
   }
-  Row row(c, s, t);
+  Row row(mm, c, s, t);
   if (!(s < INFINITY) || !(fabsf(mm) < kFar)) far_row<T, kThreads>(z, p.vocab, sh.red, row);
 
   if (rank == 0 && threadIdx.x == 0) put_stats(p, row_i, y, zy, row);
