@@ -33,6 +33,9 @@ lm_status launched(cudaError_t e, const char* what) {
 // last byte of a matrix in 63.
 constexpr int64_t kMaxCols = 0x7FFFFF00ll;
 constexpr int64_t kMaxBytes = (int64_t)1 << 62;
+// The norm's kernels count channels in whole rounds of a block's threads (8192
+// channels at most), past the row's end.
+constexpr int64_t kMaxNormCols = 0x7FFF0000ll;
 
 lm_status current_device(int* dev) {
   if (cudaGetDevice(dev) != cudaSuccess) return fail(LM_ERR_CUDA, "no CUDA device");
@@ -48,6 +51,10 @@ lm_status check_extent(int64_t rows, int64_t cols, const char* what) {
   if (rows < 0 || cols < 0) return fail(LM_ERR_INVALID_ARG, "%s: negative extent", what);
   if (cols > kMaxCols || rows > kMaxCols) return fail(LM_ERR_UNSUPPORTED, "%s: more than 2^31 - 256 rows or columns", what);
   return LM_OK;
+}
+
+lm_status check_norm_cols(int64_t cols) {
+  return cols > kMaxNormCols ? fail(LM_ERR_UNSUPPORTED, "%lld channels, more than 2^31 - 2^16", (long long)cols) : LM_OK;
 }
 
 // Shape, type, pitch and element alignment of a matrix argument (no device access).
@@ -222,6 +229,7 @@ lm_status lm_rmsnorm(const lm_matrix* x, const lm_matrix* residual, const lm_ten
   if (!(eps >= 0.0) || !isfinite(eps)) return fail(LM_ERR_INVALID_ARG, "eps must be finite and >= 0");
   const int64_t rows = x->rows, cols = x->cols;
   LM_TRY(check_matrix(*x, rows, cols, "x"));
+  LM_TRY(check_norm_cols(cols));
   if (h != nullptr && residual == nullptr) return fail(LM_ERR_INVALID_ARG, "h is x itself without a residual");
   const lm_matrix* others[] = {residual, h, y};
   const char* names[] = {"residual", "h", "y"};
@@ -278,6 +286,7 @@ lm_status lm_rmsnorm_grad(const lm_matrix* dy, const lm_matrix* h, const lm_chec
   if (dx == nullptr && dweight == nullptr) return fail(LM_ERR_INVALID_ARG, "dx and dweight are both NULL");
   const int64_t rows = dy->rows, cols = dy->cols;
   LM_TRY(check_matrix(*dy, rows, cols, "dy"));
+  LM_TRY(check_norm_cols(cols));
   if (h != nullptr) LM_TRY(check_matrix(*h, rows, cols, "h"));
   else LM_TRY(check_codes(*h8, rows, cols, "h8"));
   const lm_matrix* same[] = {h, dh, dx};
