@@ -54,6 +54,9 @@ template <typename T, bool kSingly = false>
 struct Raw {
   static constexpr int kPieces = 8 * (int)sizeof(T) / 16, kWords = 4 * kPieces;
   uint32_t w[kWords + 4];     // the last four: lane 31's further piece, until settle
+  // Bytes to the row's end, from `least` elements up; no more of them than the
+  // pieces of load and store reach (in a long row they would pass 31 bits).
+  static __device__ __forceinline__ int bytes_left(int left, int least) { return min(max(left, least), 16) * (int)sizeof(T); }
   __device__ __forceinline__ void zero() {
 #pragma unroll
     for (int k = 0; k < kWords + 4; ++k) w[k] = 0u;
@@ -71,7 +74,7 @@ struct Raw {
       single(p, left);
       return;
     }
-    const int shift = (int)(reinterpret_cast<uintptr_t>(p) & 15u), bytes = max(left, -8) * (int)sizeof(T);   // to the row's end
+    const int shift = (int)(reinterpret_cast<uintptr_t>(p) & 15u), bytes = bytes_left(left, -8);
     const uint8_t* first = reinterpret_cast<const uint8_t*>(p) - shift;
     const int mine = (threadIdx.x & 31) == 31 ? kPieces + 1 : kPieces;
 #pragma unroll
@@ -154,7 +157,7 @@ struct Raw {
       return;
     }
     const int lane = (int)threadIdx.x & 31;
-    const int shift = (int)(reinterpret_cast<uintptr_t>(p) & 15u), bytes = max(left, 0) * (int)sizeof(T);   // to the row's end
+    const int shift = (int)(reinterpret_cast<uintptr_t>(p) & 15u), bytes = bytes_left(left, 0);
     // c: the neighbour's last words, then this lane's; taken back by `shift` bytes
     uint32_t c[kWords + 4];
 #pragma unroll

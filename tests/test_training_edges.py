@@ -21,3 +21,20 @@ def test_more_channels_than_the_norm_counts(L):  # noqa: F811
     for cols in (0x7FFFFF00, 0x7FFFFC01, (1 << 31) - 65535):
         assert both(cols) == (UNSUPPORTED, UNSUPPORTED)
     assert UNSUPPORTED not in both((1 << 31) - 65536)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,cols", [(torch.float32, (1 << 29) + 37), (torch.bfloat16, (1 << 30) + 37)])
+def test_rows_of_more_than_2_31_bytes_off_16_byte_boundaries(dtype, cols):
+    """The middle row of three, whose first element is on no such boundary, has
+    the codes of the same row by itself, which is; and reads back the same."""
+    from paper_2605_19811_gb300 import training as T
+    some = torch.randn((1 << 20) + 7, device="cuda").to(dtype)
+    x = some.repeat(-(-3 * cols // some.numel()))[:3 * cols].view(3, cols)
+    assert x[1].data_ptr() % 16 != 0
+    all_three, alone = T.checkpoint8(x, "i8"), T.checkpoint8(x[1].clone(), "i8")
+    assert torch.equal(all_three.scales[:, 1], alone.scales[:, 0])
+    assert torch.equal(all_three.codes[1, :cols], alone.codes[0, :cols])
+    x.zero_()
+    all_three.unpack(out=x)
+    assert torch.equal(x[1], alone.unpack(dtype)[0])
