@@ -521,7 +521,8 @@ lm_status lm_checkpoint8_unpack(const lm_checkpoint8* c, const lm_matrix* x, voi
  * NULL for ones.  rstd: T floats or NULL.  kept: NULL, or a T x C checkpoint
  * that receives y in 8 bits (from y before its rounding to x's dtype).  The
  * norm is taken of h before its rounding.  eps >= 0, finite.  The sum of
- * squares is fp32: a row where it passes the largest float has rstd 0.  At most
+ * squares is fp32: a row where it passes the largest float has rstd 0.  Rows of
+ * no channels have the mean square 0: rstd = 1 / sqrt(eps).  At most
  * 2^31 - 2^16 channels, here and in the gradient.
  * Errors: LM_ERR_INVALID_ARG, LM_ERR_DTYPE, LM_ERR_ALIGN, LM_ERR_UNSUPPORTED,
  * LM_ERR_CUDA. */

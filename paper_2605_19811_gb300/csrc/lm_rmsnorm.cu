@@ -160,9 +160,20 @@ cudaError_t forward(const NormParams& p, cudaStream_t st) {
   return cudaGetLastError();
 }
 
+// rstd of rows without channels, whose mean square is 0.
+__global__ void __launch_bounds__(256) rstd_of_nothing_kernel(float* rstd, int64_t rows, float value) {
+  for (int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x; r < rows; r += (int64_t)gridDim.x * 256) rstd[r] = value;
+}
+
 }  // namespace
 
 cudaError_t launch_rmsnorm(lm_dtype dt, const NormParams& p, cudaStream_t st) {
+  if (p.cols == 0) {
+    const int64_t blocks = (p.rows + 255) / 256;
+    count_launch();
+    rstd_of_nothing_kernel<<<(unsigned)(blocks < 152 * 8 ? blocks : 152 * 8), 256, 0, st>>>(p.rstd, p.rows, 1.f / sqrtf(p.eps));
+    return cudaGetLastError();
+  }
   return dt == LM_BF16 ? forward<__nv_bfloat16>(p, st) : forward<float>(p, st);
 }
 

@@ -245,15 +245,17 @@ lm_status lm_rmsnorm(const lm_matrix* x, const lm_matrix* residual, const lm_ten
   if (weight != nullptr) LM_TRY(check_vector(*weight, cols, "weight"));
   if (kept != nullptr) LM_TRY(check_codes(*kept, rows, cols, "kept"));
   LM_TRY(check_aligned(rstd, 4, "rstd"));
-  if (rows == 0 || cols == 0) return LM_OK;
+  if (rows == 0 || (cols == 0 && rstd == nullptr)) return LM_OK;
   int dev = 0;
   LM_TRY(current_device(&dev));
-  LM_TRY(check_memory(x->data, dev, "x"));
-  for (int i = 0; i < 3; ++i)
-    if (others[i] != nullptr) LM_TRY(check_memory(others[i]->data, dev, names[i]));
-  if (weight != nullptr) LM_TRY(check_memory(weight->data, dev, "weight"));
+  if (cols > 0) {   // (without channels rstd alone is written, nothing is read)
+    LM_TRY(check_memory(x->data, dev, "x"));
+    for (int i = 0; i < 3; ++i)
+      if (others[i] != nullptr) LM_TRY(check_memory(others[i]->data, dev, names[i]));
+    if (weight != nullptr) LM_TRY(check_memory(weight->data, dev, "weight"));
+  }
   LM_TRY(check_memory(rstd, dev, "rstd"));
-  if (kept != nullptr) {
+  if (kept != nullptr && cols > 0) {
     LM_TRY(check_memory(kept->codes, dev, "codes"));
     LM_TRY(check_memory(kept->scales, dev, "scales"));
   }

@@ -38,3 +38,18 @@ def test_rows_of_more_than_2_31_bytes_off_16_byte_boundaries(dtype, cols):
     x.zero_()
     all_three.unpack(out=x)
     assert torch.equal(x[1], alone.unpack(dtype)[0])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows", [1, 5, 70001])
+def test_norm_of_no_channels(rows, dtype):
+    """A sum over nothing is zero: rstd = 1 / sqrt(eps)."""
+    from paper_2605_19811_gb300 import training as T
+    torch.full((rows,), 7.0, device="cuda")                # what a new rstd would be found to hold
+    x = torch.empty(rows, 0, device="cuda", dtype=dtype)
+    o = T.rmsnorm(x, torch.empty(0, device="cuda", dtype=dtype), residual=x, eps=1e-4, checkpoint="i8")
+    assert o.y.shape == o.h.shape == (rows, 0) and o.rstd.shape == (rows,) and o.checkpoint.rows == rows
+    assert float((o.rstd - 100.0).abs().max()) <= 100.0 * 2.0 ** -22
+    dx, dw = T.rmsnorm_grad(x, x, o.rstd, torch.empty(0, device="cuda", dtype=dtype))
+    assert dx.shape == (rows, 0) and dw.shape == (0,)
