@@ -15,6 +15,7 @@ freed early.
 
 from __future__ import annotations
 
+import math
 from typing import NamedTuple, Optional
 
 import torch
@@ -47,8 +48,8 @@ def _matrix(t, what: str) -> LmMatrix:
         if dims == 1:
             t = t.unsqueeze(0)
         else:
-            try:
-                t = t.view(-1, t.shape[-1]) if t.numel() else t.reshape(-1, t.shape[-1])
+            try:   # (the rows spelt out: -1 says nothing where there are no elements)
+                t = t.view(math.prod(t.shape[:-1]), t.shape[-1])
             except RuntimeError:
                 raise ValueError(f"{what}: the leading dimensions do not fold into rows of one pitch") from None
     rows, cols = t.shape

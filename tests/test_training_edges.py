@@ -53,3 +53,21 @@ def test_norm_of_no_channels(rows, dtype):
     assert float((o.rstd - 100.0).abs().max()) <= 100.0 * 2.0 ** -22
     dx, dw = T.rmsnorm_grad(x, x, o.rstd, torch.empty(0, device="cuda", dtype=dtype))
     assert dx.shape == (rows, 0) and dw.shape == (0,)
+
+
+def test_empty_tensors_fold():
+    from paper_2605_19811_gb300 import training as T
+    for shape, want in (((2, 3, 0), (6, 0)), ((0, 3, 8), (0, 8)), ((2, 0, 8), (0, 8)), ((0, 3, 0), (0, 0)), ((0,), (1, 0))):
+        m = T._matrix(torch.zeros(shape), "x")
+        assert (m.rows, m.cols) == want
+    m = T._matrix(torch.zeros(2, 3, 16)[:, :, :8], "x")
+    assert (m.rows, m.cols, m.ld) == (6, 8, 16)
+    m = T._matrix(torch.zeros(2, 0, 16)[:, :, :8], "x")
+    assert (m.rows, m.cols) == (0, 8)
+
+
+@pytest.mark.gpu
+def test_norm_of_no_channels_over_two_leading_dimensions():
+    from paper_2605_19811_gb300 import training as T
+    o = T.rmsnorm(torch.empty(2, 3, 0, device="cuda"), eps=1.0)
+    assert o.y.shape == (2, 3, 0) and bool((o.rstd == torch.ones(2, 3, device="cuda")).all())
