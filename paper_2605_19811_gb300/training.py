@@ -125,7 +125,8 @@ class Checkpoint8:
         codes, scales = self.codes, self.scales
         rows, pitch = codes.shape
         groups, lds = scales.shape
-        return LmCheckpoint8(codes.data_ptr(), scales.data_ptr(), rows, self.cols, codes.stride(0) if rows > 1 else pitch,
+        # (one row of a wider buffer keeps its buffer's pitch, as several do)
+        return LmCheckpoint8(codes.data_ptr(), scales.data_ptr(), rows, self.cols, codes.stride(0) if rows > 1 else max(codes.stride(0), pitch),
                              scales.stride(0) if groups > 1 else lds, FORMATS[self.format])
 
     def unpack(self, dtype=torch.bfloat16, out=None, stream=None):

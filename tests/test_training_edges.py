@@ -71,3 +71,26 @@ def test_norm_of_no_channels_over_two_leading_dimensions():
     from paper_2605_19811_gb300 import training as T
     o = T.rmsnorm(torch.empty(2, 3, 0, device="cuda"), eps=1.0)
     assert o.y.shape == (2, 3, 0) and bool((o.rstd == torch.ones(2, 3, device="cuda")).all())
+
+
+def test_one_row_of_a_wider_checkpoint():
+    """A view of one row has the pitch of its buffer, as a view of several has."""
+    from paper_2605_19811_gb300 import training as T
+    codes, scales = torch.zeros(4, 64, dtype=torch.uint8), torch.zeros(1, 4)
+    for rows in (1, 2, 4):
+        d = T.Checkpoint8(codes[:rows, :20], scales, 20, "i8").desc()
+        assert (d.rows, d.cols, d.ld_codes) == (rows, 20, 64)
+    assert T.Checkpoint8(torch.zeros(64, dtype=torch.uint8)[None], scales, 20, "i8").desc().ld_codes == 64
+    assert T.Checkpoint8(torch.zeros(1, dtype=torch.uint8).expand(1, 1).expand(1, 1), scales, 1, "i8").desc().ld_codes == 1
+
+
+@pytest.mark.gpu
+def test_one_row_of_a_wider_checkpoint_is_used():
+    from paper_2605_19811_gb300 import training as T
+    whole = T.checkpoint8(torch.randn(3, 64, device="cuda"), "e4m3")
+    for rows in (1, 2):
+        part = T.Checkpoint8(whole.codes[:rows, :20], whole.scales, 20, "e4m3")
+        assert torch.equal(part.unpack(), whole.unpack()[:rows, :20])
+        dy = torch.randn(rows, 7, device="cuda")
+        assert torch.equal(T.linear_wgrad8(dy, part, dtype=torch.float32),
+                           T.linear_wgrad8(dy, T.Checkpoint8(whole.codes[:rows], whole.scales, 64, "e4m3"), dtype=torch.float32)[:, :20])
