@@ -553,7 +553,8 @@ lm_status lm_rmsnorm_grad(const lm_matrix* dy, const lm_matrix* h, const lm_chec
  * dw, else dw is overwritten.  Products are exact and the sum over tokens is
  * taken in a fixed order: the same inputs give the same bits.  The tensor cores
  * add at most 512 tokens (each addition of 16 may drop 2^-23 of what it has);
- * their sums are added in fp32, whatever the type of dw.
+ * their sums are added in fp32, whatever the type of dw.  Infinities and NaN in
+ * dy are what they are in dy^T x, whatever the type of dy.
  * workspace: lm_linear_wgrad8_workspace(...) bytes of device memory for the
  * same arguments, 256-byte aligned, free again when the work is done (x in
  * bf16, dy where it is fp32 or its rows are not 16-byte aligned, and partial

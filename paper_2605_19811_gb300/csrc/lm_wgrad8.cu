@@ -45,6 +45,7 @@
 // what its CTA had yet to write, is filled with NaN.
 #include <cuda_bf16.h>
 #include <cudaTypedefs.h>
+#include <math.h>
 
 #include <algorithm>
 
@@ -536,8 +537,8 @@ __global__ void __launch_bounds__(256) wgrad8_zero_kernel(Mat dw, int dwdt, int 
 // as bf16.  The others: dY in rows of a 16-byte
 // pitch where its own are not; fp32 values as three planes whose sum is
 // exactly the value (each takes the next 8 significant bits by truncation, so
-// that no piece rounds up to infinity; a non-finite value keeps its first
-// piece and has NaN in the second).
+// that no piece rounds up to infinity; an infinity or a NaN is its own first
+// piece, with zeros in the others).
 template <int kFormat, typename T>
 __global__ void __launch_bounds__(256) wgrad8_operands_kernel(Codes x, __nv_bfloat16* xdst, int64_t ldx, unsigned x_blocks, Mat dy, int64_t tokens,
                                                               int out, __nv_bfloat16* dst, int64_t ld) {
@@ -593,7 +594,8 @@ __global__ void __launch_bounds__(256) wgrad8_operands_kernel(Codes x, __nv_bflo
         *d = src[c];
       } else {
         const float v = src[c];
-        const float hi = __uint_as_float(__float_as_uint(v) & 0xFFFF0000u), r = v - hi;
+        const bool finite = fabsf(v) < INFINITY;
+        const float hi = finite ? __uint_as_float(__float_as_uint(v) & 0xFFFF0000u) : v, r = finite ? v - hi : 0.f;
         const float mid = __uint_as_float(__float_as_uint(r) & 0xFFFF0000u);
         d[0] = __float2bfloat16_rn(hi);
         d[plane] = __float2bfloat16_rn(mid);
