@@ -451,7 +451,8 @@ typedef struct {
  * Gradient, for weights g of the loss sum_rows (g_logp logp + g_entropy entropy
  * + g_lse lse):
  *   dlogits_j = p_j (g_lse - g_logp - g_entropy (log p_j + entropy)) + g_logp [j = y]
- * where g_logp counts as 0 in a row without a target, and p_j = 0 gives 0.
+ * where g_logp counts as 0 in a row without a target, and p_j = 0 gives 0; a row
+ * whose target is >= V has a NaN gradient, unless g_logp is NULL.
  * dlogits has the shape and dtype of logits and may be logits itself (same
  * data and ld). */
 typedef struct {

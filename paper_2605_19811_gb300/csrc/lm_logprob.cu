@@ -353,15 +353,16 @@ __device__ __forceinline__ void walk(const uint4* src, int n, uint64_t policy, F
 struct RowArgs {
   int64_t y;
   float gl, gh, gz;
-  __device__ __forceinline__ RowArgs(const LogprobParams& p, int64_t row_i, bool grad) : gl(0.f), gh(0.f), gz(0.f) {
+  bool weighed;           // log p is in the loss
+  __device__ __forceinline__ RowArgs(const LogprobParams& p, int64_t row_i, bool grad) : gl(0.f), gh(0.f), gz(0.f), weighed(p.g_logp != nullptr) {
     y = p.targets != nullptr ? p.targets[row_i] : -1;
     if (!grad) return;
     if (p.g_logp != nullptr) gl = p.g_logp[row_i];
     if (p.g_entropy != nullptr) gh = p.g_entropy[row_i];
     if (p.g_lse != nullptr) gz = p.g_lse[row_i];
   }
-  // the weight of log p_y: 0 without a target, NaN for one beyond the vocabulary
-  __device__ __forceinline__ float weight(int vocab) const { return y < 0 ? 0.f : y >= vocab ? __int_as_float(0x7FC00000) : gl; }
+  // the weight of log p_y: 0 without a target or weights, NaN for a target beyond the vocabulary
+  __device__ __forceinline__ float weight(int vocab) const { return y < 0 || !weighed ? 0.f : y >= vocab ? __int_as_float(0x7FC00000) : gl; }
 };
 
 // A row's gradient, value by value: p_j (a + b lp) with p_j = 2^(d - ls), and

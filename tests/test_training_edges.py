@@ -94,3 +94,20 @@ def test_one_row_of_a_wider_checkpoint_is_used():
         dy = torch.randn(rows, 7, device="cuda")
         assert torch.equal(T.linear_wgrad8(dy, part, dtype=torch.float32),
                            T.linear_wgrad8(dy, T.Checkpoint8(whole.codes[:rows], whole.scales, 64, "e4m3"), dtype=torch.float32)[:, :20])
+
+
+@pytest.mark.gpu
+def test_a_target_beyond_the_vocabulary_and_no_weight_on_log_p():
+    """logp is NaN there; the gradient of a loss without logp is not."""
+    from paper_2605_19811_gb300 import training as T
+    z = torch.randn(4, 900, device="cuda")
+    y = torch.tensor([3, 900, 1 << 40, -1], device="cuda")
+    gh, gz, gl = (torch.randn(4, device="cuda") for _ in range(3))
+    o = T.token_logprob(z, y, g_entropy=gh, g_lse=gz)
+    assert o.logp.isnan().tolist() == [False, True, True, False]
+    want = T.token_logprob(z, None, g_entropy=gh, g_lse=gz).dlogits
+    assert torch.equal(o.dlogits, want)
+    assert torch.equal(T.token_logprob_grad(z, y, o.lse, o.entropy, None, gh, gz),
+                       T.token_logprob_grad(z, None, o.lse, o.entropy, None, gh, gz))
+    d = T.token_logprob(z, y, g_logp=gl).dlogits
+    assert d.isnan().all(dim=1).tolist() == [False, True, True, False]
