@@ -494,6 +494,8 @@ lm_status lm_token_logprob_grad(const lm_token_logprob_args* a, void* cuda_strea
  * a checkpoint without a second rounding.  A group that holds a NaN or an
  * infinity has scale NaN and reads back as NaN.  A code that would stand for 2^128
  * is lowered to the one below it (63 under a scale of 2^122, 240 under 2^120).
+ * The bytes from a row's last code to the next multiple of 16 belong to the
+ * checkpoint: they may be read and written.
  * Readers take checkpoints as lm_checkpoint8_pack writes them: a scale is a
  * power of two or NaN, and no e4m3 code is a NaN. */
 #define LM_CODE_GROUP 128
@@ -555,7 +557,8 @@ lm_status lm_rmsnorm_grad(const lm_matrix* dy, const lm_matrix* h, const lm_chec
  * taken in a fixed order: the same inputs give the same bits.  The tensor cores
  * add at most 512 tokens (each addition of 16 may drop 2^-23 of what it has);
  * their sums are added in fp32, whatever the type of dw.  Infinities and NaN in
- * dy are what they are in dy^T x, whatever the type of dy.
+ * dy are what they are in dy^T x, whatever the type of dy.  (fp32 dy below 2^-110
+ * in magnitude counts to a multiple of 2^-133.)
  * workspace: lm_linear_wgrad8_workspace(...) bytes of device memory for the
  * same arguments, 256-byte aligned, free again when the work is done (x in
  * bf16, dy where it is fp32 or its rows are not 16-byte aligned, and partial

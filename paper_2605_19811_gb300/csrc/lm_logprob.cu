@@ -5,13 +5,15 @@
 // with s = sum 2^d and t = sum 2^d d, d = (z - m) log2 e, and scales s and t
 // when m grows:  s <- 2^a s,  t <- 2^a (t + a s),  a = (m_old - m) log2 e <= 0.
 // d is one multiply-add z log2 e - c with c = m log2 e rounded once: c, not m,
-// is the reference, so its rounding cancels (log p: 2e-6 off at most for logits
+// is the reference, so its rounding cancels (log p: 2.5e-6 off at most for logits
 // around 0 and around 20000 alike).  With the row's M, C, S, T:
 //   lse = M + ln2 (log2 S - (M log2 e - C)),  log p_j = ln2 (d_j - log2 S),  H = ln2 (log2 S - T / S)
 // (M log2 e - C is exact, so lse is rounded once at its own size: for logits of
 // 1000 to 1250 6.1e-5 off, half a unit, where ln2 (C + log2 S) was 1.1e-4 off.)
 //   dz_j = 2^d_j (a0 + a1 d_j) (+ g_logp at the target),
 //   a1 = -g_H ln2 / S,  a0 = (g_lse - g_logp - g_H (H - ln2 log2 S)) / S
+// 2^d is the exponential unit's (2^-22 relative), and 0 below 2^-126: a token that
+// much less likely than the most likely one has p = 0 (and its own log p).
 // The gradient in the same call reads the row again, from L2, which its first
 // reading asks to keep it and its second to give it up: 2432 x 50304 bf16 (245
 // MB) then reads 270 MB from memory; an earlier form without the hints, 403 MB.

@@ -8,7 +8,8 @@
 // root, its addresses) is then shared by many channels.  16384 x 1280 with
 // residual and 8-bit copy: 44 us with a warp and five eights a lane, 50 us with
 // 128 threads and two eights each.  A lane has 8 consecutive channels of every
-// 256, so a scale's 128 channels are half a warp.
+// 256, so a scale's 128 channels are half a warp.  rstd is rsqrtf's, within two
+// units of the last place.
 #include "lm_rows.cuh"
 
 namespace lm {

@@ -37,8 +37,10 @@ __global__ void __launch_bounds__(kMost, kMost == 256 ? 2 : 1) rmsnorm_grad_kern
   if (want && !whole)   // (such rows have a block of their own)
     for (int c = 8 * t; c < p.cols; c += span)
       for (int e = 0; e < 8 && c + e < p.cols; ++e) sums[c + e] = 0.f;
-  // fp32 rows off 16-byte boundaries are read one by one here (8191 x 1283: 49 us
-  // so, 72 us in pieces; 2047 x 8191: 196 and 295 us).
+  // fp32 rows off 16-byte boundaries are read one by one here: 8191 x 1283 49 us
+  // so, 70 us in pieces; 4095 x 4095 64 and 92.  Beyond 4096 channels, where the
+  // next row is not loaded ahead, pieces would be ahead by a little (2047 x 8191
+  // 102 and 98, 2047 x 12001 332 and 297).
   struct Eight {
     Raw<T, sizeof(T) == 4> dy, dh;
     std::conditional_t<kMatrix, Raw<T, sizeof(T) == 4>, RawCodes<kMatrix ? 0 : kFormat>> h;

@@ -6,16 +6,19 @@
 // A code times its power-of-two scale is a bf16 number, so a first kernel
 // writes X as bf16 into the workspace without a rounding; dY is taken as it is
 // (bf16), or laid out as three bf16 planes whose sum is the fp32 value (8 + 8 +
-// 8 significant bits, summed as three times as many tokens).  Every product is
-// then exact and only the sums are rounded.
+// 8 significant bits, summed as three times as many tokens; below 2^-110 the
+// last ones pass bf16's least number, 2^-133).  Every product is then exact and
+// only the sums are rounded.
 // (The codes made bf16 inside the product's kernel, by warps of their own,
 // cost more: the conversion shares the shared memory's bandwidth with the MMA,
 // 440 ns instead of 350 for a pair's 64 tokens.)
 //
 // Measured (X made bf16, product, join; kernels alone): 16384 x 768 x 2304
-// e4m3 to bf16 9 + 47 + 9 us, a call 62 us; 16384 x 4096 x 14336 int8 to fp32
-// 43 + 1086 + 11 us, a call 1230 to 1270 us (1.51 to 1.56 PFLOP/s).  Bound by
-// the tensor pipe where dW has many tiles, else by the three launches.
+// e4m3 to bf16 10 + 54 + 9 us, a call 64 us; 16384 x 4096 x 14336 int8 to fp32
+// 42 + 1076 + 12 us, a call 1117 to 1140 us by itself (1.7 PFLOP/s) and 1230 to
+// 1290 us among others (1.5); 16384 x 4096 x 4096 from bf16 dY 362 us, from fp32
+// 1210 us.  Bound by the tensor pipe where dW has many tiles, else by the three
+// launches.
 //
 // Both operands lie token by token in memory, so both are MN-major: rows of
 // 64 channels (128 bytes, 128-byte swizzle), one row a token.  CTA r of the
@@ -167,12 +170,11 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
       : "memory");
 }
 
-// Arrive on a barrier of CTA 0.  What the arrival announces is in the arriving
-// CTA's own SM: operand bytes in its shared memory, which the arriving threads
-// have fenced towards the tensor core (fence.proxy.async) before, or TMEM
-// columns read to the end (tcgen05.wait::ld).  Nothing in global memory hangs
-// on it, so the arrival needs no fence of cluster scope; with one
-// (.release.cluster) it took 1300 cycles, against 512 of a token block's MMA.
+// Arrive on a barrier of CTA 0.  What the arrival announces is TMEM columns of the
+// arriving CTA read to the end (tcgen05.wait::ld, fence before_thread_sync).
+// Nothing in global memory hangs on it, so the arrival needs no fence of cluster
+// scope; with one (.release.cluster) it took 1300 cycles, against 512 of a token
+// block's MMA.
 __device__ __forceinline__ void arrive_cta0(uint64_t* bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(peer_addr(bar, 0)) : "memory");
 }
@@ -536,7 +538,7 @@ __global__ void __launch_bounds__(256) wgrad8_zero_kernel(Mat dw, int dwdt, int 
 // The operands as the TMA takes them.  Blocks below x_blocks: X = code * scale
 // as bf16.  The others: dY in rows of a 16-byte
 // pitch where its own are not; fp32 values as three planes whose sum is
-// exactly the value (each takes the next 8 significant bits by truncation, so
+// exactly the value, from 2^-110 up (each takes the next 8 significant bits by truncation, so
 // that no piece rounds up to infinity; an infinity or a NaN is its own first
 // piece, with zeros in the others).
 template <int kFormat, typename T>
