@@ -571,6 +571,160 @@ size_t lm_linear_wgrad8_workspace(const lm_matrix* dy, const lm_checkpoint8* x, 
 lm_status lm_linear_wgrad8(const lm_matrix* dy, const lm_checkpoint8* x, const lm_matrix* dw, int accumulate,
                            void* workspace, size_t workspace_bytes, void* cuda_stream);
 
+/* Log probabilities of given tokens from the last hidden states h (T x C) and
+ * the head's matrix weight (V x C), both bf16, without the logits: with
+ * z = h weight^T, the results of lm_token_logprob for the logits z (its
+ * formulas, its targets and their rules, its rows of -inf, +inf and NaN), and
+ * the gradients of the same loss:
+ *   dh = dz weight,   dweight (+)= dz^T h
+ * z is summed in fp32 and never rounded below it; dz is rounded to bf16, as the
+ * tensor cores take it, and both products are summed in fp32.  The tensor cores
+ * add at most 512 products (each addition of 16 may drop 2^-23 of what it has);
+ * their sums are added in fp32.  Sums are taken in a fixed order: the same
+ * inputs give the same bits.
+ * dh has the dtype of h; dweight is bf16 or fp32, accumulate != 0 adds to it. */
+typedef struct {
+  lm_matrix h;
+  lm_matrix weight;
+  const int64_t* targets;   /* T, device; NULL only when neither logp nor g_logp is given */
+  float* logp;              /* T floats each, device, or NULL */
+  float* entropy;
+  float* lse;
+  const float* g_logp;      /* T floats each, device, or NULL for zero */
+  const float* g_entropy;
+  const float* g_lse;
+  lm_matrix dh;             /* data NULL: not wanted */
+  lm_matrix dweight;        /* data NULL: not wanted */
+  int accumulate;
+} lm_linear_logprob_args;
+
+/* Forward (logp, entropy, lse: those that are not NULL) and, where dh or dweight
+ * is given, the gradients in the same call, for weights g that are known
+ * beforehand.  rows == 0 is accepted (dweight is then zero, or left as it is
+ * with accumulate); an empty vocabulary or C == 0 is not.
+ * workspace: lm_linear_logprob_workspace(args) bytes of device memory,
+ * 256-byte aligned, free again when the work is done (with gradients, T x
+ * up to 512 MB / T columns of dz, at least 2048; fp32 sums of dh where the
+ * vocabulary takes several such pieces; copies of h and weight where their rows
+ * are not 16-byte aligned; partial sums of at most 40 MB).
+ * Should a device-side wait give up (LM_WAIT_LIMIT_NS), what was not computed
+ * is NaN.
+ * Errors: LM_ERR_INVALID_ARG (also a workspace that is too small),
+ * LM_ERR_DTYPE, LM_ERR_ALIGN, LM_ERR_UNSUPPORTED, LM_ERR_CUDA. */
+size_t lm_linear_logprob_workspace(const lm_linear_logprob_args* a);
+lm_status lm_linear_logprob(const lm_linear_logprob_args* a, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* The gradients alone, for weights known only after the forward call: lse, and
+ * entropy where g_entropy is not NULL, are read, as lm_linear_logprob wrote
+ * them; logp is ignored.  The workspace is the same call's.  Errors as above. */
+lm_status lm_linear_logprob_grad(const lm_linear_logprob_args* a, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* 8-bit weights of a linear layer, rows (out) x cols (in): e4m3 codes, one byte
+ * an element (row pitch ld_codes, a multiple of 16, codes 16-byte aligned), and
+ * one scale for each block of LM_CODE_GROUP x LM_CODE_GROUP (the last blocks of
+ * a row or column may be short): the scale of element (r, c) is
+ * scales[r / 128 * ld_scales + c / 128].  Scales and codes are those of
+ * lm_checkpoint8's LM_CODE_E4M3, over blocks: a scale is the least power of two
+ * s with max |w| <= 448 s, at least 2^-117; a block that holds a NaN or an
+ * infinity has scale NaN and reads back as NaN.  One scale for a block, not for a
+ * row's group: the same codes serve the product with W^T and with W.
+ * The bytes from a row's last code to the next multiple of 16 belong to the
+ * weights: they may be read and written.  Readers take weights as
+ * lm_weight8_pack writes them. */
+typedef struct {
+  void* codes;
+  float* scales;
+  int64_t rows;
+  int64_t cols;
+  int64_t ld_codes;
+  int64_t ld_scales;
+} lm_weight8;
+
+/* c <- w, and w <- c (w in bf16 or fp32; the values are bf16 numbers, so both
+ * are exact).  Errors: LM_ERR_INVALID_ARG, LM_ERR_DTYPE, LM_ERR_ALIGN,
+ * LM_ERR_UNSUPPORTED, LM_ERR_CUDA. */
+lm_status lm_weight8_pack(const lm_matrix* w, const lm_weight8* c, void* cuda_stream);
+lm_status lm_weight8_unpack(const lm_weight8* c, const lm_matrix* w, void* cuda_stream);
+
+/* Linear layer in 8 bits and its input gradient:
+ *   lm_linear8:       y = x W^T     x: T x in,   y: T x out
+ *   lm_linear8_grad:  dx = dy W     dy: T x out, dx: T x in
+ * x and dy are checkpoints in LM_CODE_E4M3 (lm_checkpoint8_pack, or kept by
+ * lm_rmsnorm), w the layer's weights (out x in); y and dx are bf16 or fp32.
+ * Products of codes are exact and the sums fp32, in a fixed order: the same
+ * inputs give the same bits.  The weight gradient is lm_linear_wgrad8's.
+ * workspace: lm_linear8_workspace(x, w, grad) bytes of device memory, 256-byte
+ * aligned, free again when the work is done.
+ * Should a device-side wait give up (LM_WAIT_LIMIT_NS), what was not computed
+ * is NaN.
+ * Errors: LM_ERR_INVALID_ARG (also a workspace that is too small),
+ * LM_ERR_DTYPE (also a checkpoint in LM_CODE_I8), LM_ERR_ALIGN,
+ * LM_ERR_UNSUPPORTED, LM_ERR_CUDA. */
+size_t lm_linear8_workspace(const lm_checkpoint8* x, const lm_weight8* w, int grad);
+lm_status lm_linear8(const lm_checkpoint8* x, const lm_weight8* w, const lm_matrix* y, void* workspace,
+                     size_t workspace_bytes, void* cuda_stream);
+lm_status lm_linear8_grad(const lm_checkpoint8* dy, const lm_weight8* w, const lm_matrix* dx, void* workspace,
+                          size_t workspace_bytes, void* cuda_stream);
+
+/* Heads of queries or keys: channel c of head h of token t at
+ * data[t * ld_token + h * ld_head + c], as a view of one QKV product has them
+ * (a token's heads side by side) or with the heads apart.  No two of a tensor's
+ * elements share a place: ld_head >= dim and ld_token >= heads' extent, or
+ * ld_token >= dim and ld_head >= the tokens' (ld_token is not read for one
+ * token, ld_head not for one head). */
+typedef struct {
+  void* data;
+  int64_t tokens;
+  int64_t heads;
+  int64_t dim;
+  int64_t ld_token;
+  int64_t ld_head;
+  lm_dtype dtype;
+} lm_heads;
+
+/* Norm, gain and rotation of queries and keys.  For each head x of a token at
+ * position i:
+ *   u = weight x / sqrt(mean x^2 + eps)   (norm != 0; else u = x)
+ *   y_a = u_a cos - u_b sin,  y_b = u_b cos + u_a sin   for each pair (a, b)
+ * where (cos, sin) of pair j are table[(i * turned / 2 + j) * 2], [.. + 1].
+ * Pair j is channels (j, j + turned / 2), or (2 j, 2 j + 1) with interleaved;
+ * the channels from `turned` on keep u.  A position outside 0 .. table_rows - 1
+ * has cos = sin = NaN.  The table is the caller's: cos and sin of position times
+ * frequency, with whatever scaling a longer context asks for.
+ * Gradient, for dy:  du = dy turned back,  xh = x / sqrt(mean x^2 + eps)
+ *   dx = (weight du - xh mean(weight du xh)) / sqrt(mean x^2 + eps)   (du without norm)
+ *   dweight = sum over tokens and heads of du xh
+ * Everything between reading and the one rounding of a result is fp32. */
+typedef struct {
+  lm_heads x;               /* forward: read; gradient: the forward call's, read with norm (else ignored) */
+  lm_heads y;               /* forward: written, may be x itself (same strides); gradient: dy, read */
+  lm_heads dx;              /* gradient: written, may be dy itself (same strides) */
+  lm_tensor weight;         /* dim elements, bf16 or fp32; data NULL for ones; with norm only */
+  lm_tensor dweight;        /* gradient: dim elements, bf16 or fp32, or data NULL; with norm only */
+} lm_rotary_part;
+typedef struct {
+  lm_rotary_part q;
+  lm_rotary_part k;         /* y.heads == 0: none, the rest is not read */
+  const int64_t* positions; /* one a token, device; not read when turned == 0 */
+  const float* table;       /* table_rows x turned / 2 x 2, dense, device */
+  int64_t table_rows;
+  int turned;               /* even, 0 .. dim */
+  int norm;
+  int interleaved;
+  double eps;               /* >= 0, finite */
+} lm_qk_rotary_args;
+
+/* All tensors of a call have one dtype (bf16 or fp32), one number of tokens and
+ * one dim, at most 1024.  dweight is summed in a fixed order: the same inputs
+ * give the same bits.  workspace: lm_qk_rotary_grad_workspace(args) bytes of
+ * device memory, 16-byte aligned, free again when the work is done (not read
+ * when no dweight is wanted).
+ * Errors: LM_ERR_INVALID_ARG (also a workspace that is too small),
+ * LM_ERR_DTYPE, LM_ERR_ALIGN, LM_ERR_UNSUPPORTED, LM_ERR_CUDA. */
+lm_status lm_qk_rotary(const lm_qk_rotary_args* a, void* cuda_stream);
+size_t lm_qk_rotary_grad_workspace(const lm_qk_rotary_args* a);
+lm_status lm_qk_rotary_grad(const lm_qk_rotary_args* a, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

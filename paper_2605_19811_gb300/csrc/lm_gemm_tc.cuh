@@ -1,0 +1,641 @@
+// Matrix product on the tensor cores, D = A B^T with bf16 operands: CTA pairs
+// (tcgen05.mma, cta_group::2), one 256 x 256 tile of D a pair, 64 of the summed
+// dimension at a time, operands by TMA, what happens to a finished tile in an
+// epilogue that the caller supplies.
+//
+// Either operand lies K-major (rows of the summed dimension: one box of 64 x
+// 128 rows a CTA) or MN-major (rows of D's dimension, one row an element of the
+// sum: two boxes of 64 x 64).  CTA r of the pair holds rows 128 r .. of the
+// tile (A) and columns 128 r .. (B).
+//
+// CTA roles (12 warps, one CTA per SM):
+//   warp 0      TMA producer (one lane); both CTAs' copies signal CTA 0
+//   warp 1      TMEM allocation; MMA issuer (CTA 0, one lane)
+//   warps 4-11  epilogue: one TMEM lane quadrant and half of the columns each
+//
+// Accumulation: the tensor cores drop up to a unit of the last place of the
+// accumulator at each addition (16 of the sum), always towards zero, so a sum of
+// more than kChunk blocks (512) is cut: the epilogue adds the accumulator, in
+// fp32, to sums that it holds in registers while the MMA fills the other one.
+//
+// Schedule: units of `strip` tiles of one tile row, dealt to the pairs in turn.
+// With split sums, as many tiles as fill whole waves go one to a pair, and the
+// tiles left over are one line of (tile, block) work cut into equal ranges; a
+// tile that falls to several pairs is summed from their fp32 parts, in order,
+// by a second kernel.
+//
+// Every wait is bounded (LM_WAIT_LIMIT_NS); a tile whose wait gave up, and what
+// its CTA had yet to do, reach the epilogue as NaN.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cudaTypedefs.h>
+
+#include <algorithm>
+
+#include "lm_ns_tc_shared.cuh"
+#include "lm_train.h"
+
+namespace lm {
+namespace gemm {
+namespace {
+
+using namespace tc;
+using tcs::ProducerLog;
+using tcs::pair_finish;
+using tcs::kCleanupWaitNs;
+
+constexpr int kTileM = 256, kTileN = 256, kBlockK = 64;
+constexpr int kHalf = 128;
+constexpr int kABytes = kHalf * kBlockK * 2, kBBytes = kHalf * kBlockK * 2;
+constexpr int kStages = 6, kStageBytes = kABytes + kBBytes;
+constexpr int kFirstEpi = 4, kEpiWarps = 8;            // whole warpgroups: a warp reads the TMEM lanes of its number mod 4
+constexpr int kThreads = 32 * (kFirstEpi + kEpiWarps);
+constexpr int kChunk = 8;                              // most blocks summed in one accumulator
+constexpr int kPairs = 76;                             // CTA pairs of the GPU (152 SMs)
+constexpr int kTmemCols = 512;
+constexpr int kTransBytes = 32 * 20 * 4;               // an epilogue warp's transpose tile: 32 rows x 16 columns, 80-byte rows
+constexpr size_t kTransOffset = (size_t)kStages * kStageBytes;
+constexpr size_t kBarOffset = kTransOffset + (size_t)kEpiWarps * kTransBytes;
+constexpr size_t kSmemBytes = 1024 + kBarOffset + 512;
+static_assert(kSmemBytes <= 232448, "shared memory of one SM");
+constexpr size_t kPartBytes = (size_t)kTileM * kTileN * 4;
+constexpr int kMostSharers = kPairs;
+
+// How the work falls to the pairs.
+struct Schedule {
+  int32_t tiles_m, tiles_n;
+  int32_t nkb;          // blocks of the sum
+  int32_t strip;        // tiles of one row taken in turn by one pair
+  int32_t strips;       // of a tile row
+  int32_t units;        // units dealt to the pairs in turn (tile row, strip)
+  int32_t rest;         // tiles left over, shared by range (strip 1)
+  int32_t sharers;      // pairs that share them; 0: none left over
+  int64_t begin[kMostSharers + 1];   // sharer k's first (tile, block) in the line of left-over work
+};
+template <typename Epi>
+struct Params {
+  CUtensorMap a, b;
+  Schedule sch;
+  int32_t m, n;
+  float* parts;
+  uint64_t wait_ns;
+  Epi epi;
+};
+
+// Units run over groups of 8 tile rows, strip by strip, so that the units of a
+// wave cover a compact block of D and share its operands in L2.
+__device__ __forceinline__ void unit_place(const Schedule& s, int unit, int& tm, int& strip) {
+  constexpr int kGroup = 8;
+  const int per = kGroup * s.strips, g = unit / per, r = unit - g * per;
+  const int rows = min(kGroup, s.tiles_m - g * kGroup);
+  strip = r / rows;
+  tm = g * kGroup + r - strip * rows;
+}
+// A pair's work items in order: a tile, its blocks, and where the sum goes.
+struct Item {
+  int tm, tn, kb0, kb1;
+  int slot;             // -1: the whole sum; else part slot of the workspace
+  int strip;            // the tile's strip, where the item ends it; else -1 (units dealt in turn)
+};
+struct Items {
+  int pair, unit, tn, tn_end, tm, strip;
+  int64_t at, end;      // left-over (tile, block) yet to do
+  bool first;
+  __device__ __forceinline__ Items(const Schedule& s, int p) : pair(p), unit(p), tn(0), tn_end(0), tm(0), strip(0), at(0), end(0), first(true) {
+    if (s.sharers > 0 && p < s.sharers) {
+      at = s.begin[p];
+      end = s.begin[p + 1];
+    }
+  }
+  __device__ __forceinline__ bool next(const Schedule& s, Item& it) {
+    if (tn >= tn_end && unit < s.units) {
+      unit_place(s, unit, tm, strip);
+      tn = strip * s.strip;
+      tn_end = min(tn + s.strip, s.tiles_n);
+      unit += kPairs;
+    }
+    if (tn < tn_end) {
+      it = Item{tm, tn, 0, s.nkb, -1, tn + 1 == tn_end ? strip : -1};
+      ++tn;
+      return true;
+    }
+    if (at >= end) return false;
+    const int t = (int)(at / s.nkb), kb0 = (int)(at - (int64_t)t * s.nkb);
+    const int kb1 = (int)min((int64_t)s.nkb, kb0 + (end - at));
+    unit_place(s, s.units + t, it.tm, it.tn);
+    it.kb0 = kb0;
+    it.kb1 = kb1;
+    it.slot = (kb0 == 0 && kb1 == s.nkb) ? -1 : 2 * pair + (first ? 0 : 1);
+    it.strip = -1;
+    at += kb1 - kb0;
+    first = false;
+    return true;
+  }
+};
+
+// Bounded wait; false where it gave up.  Without a call: a call would spill the
+// sums that the epilogue holds in registers.
+__device__ __forceinline__ bool await(uint64_t* bar, uint32_t parity, volatile int* abort_flag, uint64_t limit_ns) {
+  // the clock is read every 256 probes (each may already sleep a while), at
+  // every probe under a limit below a millisecond
+  const uint32_t every = limit_ns < 1000000ull ? 0u : 255u;
+  uint64_t t0 = 0;
+  for (uint32_t i = 0; !mbar_try_wait(bar, parity); ++i) {
+    if ((i & every) != every) continue;
+    if (*abort_flag) return false;
+    const uint64_t now = globaltimer();
+    if (t0 == 0) t0 = now;
+    else if (now - t0 > limit_ns) return false;
+  }
+  return true;
+}
+
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32"
+      " {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+}
+
+// Arrive on a barrier of CTA 0.  What the arrival announces is TMEM columns of the
+// arriving CTA read to the end (tcgen05.wait::ld, fence before_thread_sync).
+// Nothing in global memory hangs on it, so the arrival needs no fence of cluster
+// scope.
+__device__ __forceinline__ void arrive_cta0(uint64_t* bar) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(peer_addr(bar, 0)) : "memory");
+}
+
+// Where an epilogue warp stands: lane l holds row `row + l` of D, columns
+// `col` .. `col` + 127 (of them < n inside).
+struct Place {
+  int tm, tn;
+  int row, col;
+  int lane, half;       // half: which 128 columns of the tile
+  float* stage;         // the warp's transpose tile
+};
+
+// Four elements of a row, `left` of them inside.
+struct Store {
+  Mat d;
+  int32_t dt;
+  int32_t accumulate;   // adds to d
+  int32_t vec;          // d takes four elements at a time
+  const float* add;     // NULL, or fp32 values added (may be d itself)
+  int64_t ld_add;
+  __device__ __forceinline__ void put(int64_t row, int col, float4 v, int left) const {
+    float e[4] = {v.x, v.y, v.z, v.w};
+    if (add != nullptr) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k < left) e[k] += add[row * ld_add + col + k];
+    }
+    const int64_t at = row * d.ld + col;
+    if (dt == LM_F32) {
+      float* o = static_cast<float*>(d.data) + at;
+      if (vec && left >= 4) {
+        if (accumulate) {
+          const float4 q = *reinterpret_cast<const float4*>(o);
+          e[0] += q.x;
+          e[1] += q.y;
+          e[2] += q.z;
+          e[3] += q.w;
+        }
+        *reinterpret_cast<float4*>(o) = make_float4(e[0], e[1], e[2], e[3]);
+        return;
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k < left) o[k] = accumulate ? o[k] + e[k] : e[k];
+    } else {
+      __nv_bfloat16* o = static_cast<__nv_bfloat16*>(d.data) + at;
+      if (vec && left >= 4) {
+        if (accumulate) {
+          const uint2 q = *reinterpret_cast<const uint2*>(o);
+          e[0] += bf_lo(q.x);
+          e[1] += bf_hi(q.x);
+          e[2] += bf_lo(q.y);
+          e[3] += bf_hi(q.y);
+        }
+        *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf2(e[0], e[1]), pack_bf2(e[2], e[3]));
+        return;
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k < left) o[k] = __float2bfloat16_rn(accumulate ? __bfloat162float(o[k]) + e[k] : e[k]);
+    }
+  }
+};
+inline Store make_store(const Mat& d, int dt, int64_t rows, bool accumulate) {
+  Store s{};
+  s.d = d;
+  s.dt = dt;
+  s.accumulate = accumulate ? 1 : 0;
+  const uintptr_t four = dt == LM_F32 ? 16 : 8;   // bytes of four elements
+  s.vec = reinterpret_cast<uintptr_t>(d.data) % four == 0 && (rows == 1 || d.ld % 4 == 0);
+  return s;
+}
+
+// 32 rows (one a lane) x 32 columns from column c: through the warp's transpose
+// tile, 16 columns at a time, then eight rows a step, four columns a lane.
+template <typename Put>
+__device__ __forceinline__ void put_block(const float (&v)[32], const Place& at, int rows, int c, const Put& put) {
+  const int q = 4 * (at.lane & 3), r8 = at.lane >> 2;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+#pragma unroll
+    for (int e = 0; e < 16; e += 4)
+      *reinterpret_cast<float4*>(at.stage + at.lane * 20 + e) = make_float4(v[16 * h + e], v[16 * h + e + 1], v[16 * h + e + 2], v[16 * h + e + 3]);
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int r = r8 + 8 * k;
+      if (r < rows) put(r, c + 16 * h + q, *reinterpret_cast<const float4*>(at.stage + r * 20 + q));
+    }
+    __syncwarp();
+  }
+}
+
+// Epilogue that stores D.
+struct StoreEpi {
+  Store out;
+  template <typename P>
+  struct Warp {
+    __device__ __forceinline__ Warp(const P&, const Place&) {}
+    __device__ __forceinline__ void tile(const P& p, const Item& it, const Place& at, float (&acc)[4][32]) {
+      const int rows = min(32, p.m - at.row);
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const int c = at.col + 32 * b;
+        if (c >= p.n || rows <= 0) continue;
+        if (it.slot >= 0) {
+          float* part = p.parts + (size_t)it.slot * (kTileM * kTileN);
+          const int r0 = at.row - at.tm * kTileM, c0 = at.tn * kTileN;
+          put_block(acc[b], at, rows, c, [&](int r, int col, float4 v) {
+            *reinterpret_cast<float4*>(part + (size_t)(r0 + r) * kTileN + (col - c0)) = v;
+          });
+        } else {
+          put_block(acc[b], at, rows, c, [&](int r, int col, float4 v) {
+            if (col < p.n) p.epi.out.put(at.row + r, col, v, p.n - col);
+          });
+        }
+      }
+    }
+  };
+};
+
+template <bool kAMn, bool kBMn, typename Epi>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_kernel(const __grid_constant__ Params<Epi> p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + kBarOffset);
+  uint64_t* empty = full + kStages;
+  uint64_t* accfull = empty + kStages;
+  uint64_t* accempty = accfull + 2;
+  uint64_t* done = accempty + 2;
+  ProducerLog<kStages>* log = reinterpret_cast<ProducerLog<kStages>*>(done + 1);
+  int* armed = reinterpret_cast<int*>(log + 1);       // last phase CTA 0 armed on each stage, or -1 (producer lane)
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(armed + kStages);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+  const int pair = blockIdx.x >> 1;
+  const Schedule& sch = p.sch;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+      armed[s] = -1;
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&accfull[b], 1);
+      mbar_init(&accempty[b], 2 * kEpiWarps);
+    }
+    mbar_init(done, 1);
+    log->n = 0;
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    tmem_alloc(tmem_slot, kTmemCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  cluster_sync();   // barriers of both CTAs initialised
+  tc_fence_after();
+  griddep_wait();   // the operands are there
+  griddep_launch_dependents();
+  const uint32_t tmem_base = *tmem_slot;
+  const uint64_t wait_ns = p.wait_ns;
+
+  if (warp == 0) {
+    // -------------------------------- producer ---------------------------------
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      Items items(sch, pair);
+      Item it;
+      while (ok && items.next(sch, it)) {
+        const int row = it.tm * kTileM + (int)rank * kHalf, col = it.tn * kTileN + (int)rank * kHalf;
+        for (int kb = it.kb0; kb < it.kb1; ++kb) {
+          if (!await(&empty[stage], ph ^ 1u, abort_flag, wait_ns)) {
+            ok = false;
+            break;
+          }
+          uint8_t* sa = smem + (size_t)stage * kStageBytes;
+          uint8_t* sb = sa + kABytes;
+          const uint32_t fb = peer_addr(&full[stage], 0);
+          if (rank == 0) {
+            mbar_arrive_expect_tx(&full[stage], 2u * kStageBytes);
+            armed[stage] = (int)ph;
+          }
+          log->bytes[stage] = kStageBytes;
+          log->n += 1u;
+          if (kAMn) {
+            tma_load_3d(sa, &p.a, fb, row, kb * kBlockK, 0);
+            tma_load_3d(sa + kABytes / 2, &p.a, fb, row + 64, kb * kBlockK, 0);
+          } else {
+            tma_load_3d(sa, &p.a, fb, kb * kBlockK, row, 0);
+          }
+          if (kBMn) {
+            tma_load_3d(sb, &p.b, fb, col, kb * kBlockK, 0);
+            tma_load_3d(sb + kBBytes / 2, &p.b, fb, col + 64, kb * kBlockK, 0);
+          } else {
+            tma_load_3d(sb, &p.b, fb, kb * kBlockK, col, 0);
+          }
+          if (++stage == kStages) {
+            stage = 0;
+            ph ^= 1u;
+          }
+        }
+      }
+      if (!ok) *abort_flag = 1;
+    }
+  } else if (warp == 1) {
+    // -------------------------------- MMA issuer -------------------------------
+    if (lane == 0 && rank == 0) {
+      const uint32_t idesc = make_idesc(kTileM, kTileN, kAMn, kBMn);
+      // 16 of the sum: 16 rows of 128 bytes (MN-major), 32 bytes of a row (K-major)
+      constexpr uint64_t a_step = (kAMn ? 2048 : 32) >> 4, b_step = (kBMn ? 2048 : 32) >> 4;
+      int stage = 0, ab = 0;
+      uint32_t ph = 0, aph = 0;
+      bool ok = true;
+      Items items(sch, pair);
+      Item it;
+      while (ok && items.next(sch, it)) {
+        for (int kc = it.kb0; ok && kc < it.kb1;) {
+          const int ke = min(kc + kChunk, it.kb1);
+          if (!await(&accempty[ab], aph ^ 1u, abort_flag, wait_ns)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t d = tmem_base + (uint32_t)(ab * kTileN);
+          for (int kb = kc; kb < ke; ++kb) {
+            if (!await(&full[stage], ph, abort_flag, wait_ns)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            const uint32_t sa = smem_u32(smem + (size_t)stage * kStageBytes);
+            const uint64_t a0 = sw128_desc(sa, kAMn ? kABytes / 2 : 16, 1024), b0 = sw128_desc(sa + kABytes, kBMn ? kBBytes / 2 : 16, 1024);
+#pragma unroll
+            for (int kk = 0; kk < kBlockK / 16; ++kk)
+              umma_bf16(d, a0 + kk * a_step, b0 + kk * b_step, idesc, (kb == kc && kk == 0) ? 0u : 1u);
+            umma_commit_pair(&empty[stage]);
+            if (++stage == kStages) {
+              stage = 0;
+              ph ^= 1u;
+            }
+          }
+          if (!ok) break;
+          umma_commit_pair(&accfull[ab]);
+          ab ^= 1;
+          if (ab == 0) aph ^= 1u;
+          kc = ke;
+        }
+      }
+      if (!ok) *abort_flag = 1;
+      umma_commit_local(done);   // all issued MMAs complete before TMEM is released
+      volatile int never = 0;
+      await(done, 0, &never, kCleanupWaitNs);
+    }
+  } else if (warp >= kFirstEpi) {
+    // --------------------------------- epilogue ----------------------------------
+    Place at;
+    at.lane = lane;
+    at.half = (warp - kFirstEpi) >> 2;
+    at.stage = reinterpret_cast<float*>(smem + kTransOffset + (size_t)(warp - kFirstEpi) * kTransBytes);
+    const int q = warp & 3, r0 = (int)rank * kHalf + q * 32;      // the warp's first row of the tile
+    const uint32_t lanes = (uint32_t)(q * 32) << 16;
+    const float nan = __int_as_float(0x7FC00000);
+    int ab = 0;
+    uint32_t aph = 0;
+    bool ok = true;
+    Items items(sch, pair);
+    Item it;
+    at.tm = at.tn = at.row = at.col = 0;
+    typename Epi::template Warp<Params<Epi>> epi(p, at);
+    while (items.next(sch, it)) {
+      at.tm = it.tm;
+      at.tn = it.tn;
+      at.row = it.tm * kTileM + r0;
+      at.col = it.tn * kTileN + at.half * 128;
+      float acc[4][32];
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int e = 0; e < 32; ++e) acc[b][e] = 0.f;
+      for (int kc = it.kb0; kc < it.kb1; kc += kChunk) {
+        // one answer for the warp: the TMEM loads below are taken by all lanes or none
+        ok = ok && __all_sync(0xFFFFFFFFu, await(&accfull[ab], aph, abort_flag, wait_ns));
+        if (!ok) {
+          *abort_flag = 1;
+          break;
+        }
+        tc_fence_after();
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+          for (int o = 0; o < 32; o += 16) {
+            uint32_t r[16];
+            tmem_ld16(tmem_base + (uint32_t)(ab * kTileN + at.half * 128 + 32 * b + o) + lanes, r);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[b][o + e] += __uint_as_float(r[e]);
+          }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive_cta0(&accempty[ab]);
+        ab ^= 1;
+        if (ab == 0) aph ^= 1u;
+      }
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int e = 0; e < 32; ++e) acc[b][e] = ok ? acc[b][e] : nan;
+      epi.tile(p, it, at, acc);
+    }
+  }
+
+  __syncwarp();
+  pair_finish<kStages>(*log, abort_flag, full, armed, rank);
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, kTmemCols);
+  }
+}
+
+// Left-over tiles that several pairs shared: the parts added in the order of
+// the sum, then stored like a whole tile.
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Params<StoreEpi> p) {
+  const Schedule& s = p.sch;
+  const int t = blockIdx.x;
+  griddep_wait();
+  griddep_launch_dependents();
+  const int64_t u0 = (int64_t)t * s.nkb, u1 = u0 + s.nkb;
+  int k = (int)((int64_t)t * s.sharers / s.rest);   // the sharer whose range holds unit u0
+  while (k > 0 && s.begin[k] > u0) --k;
+  while (s.begin[k + 1] <= u0) ++k;
+  if (s.begin[k] <= u0 && s.begin[k + 1] >= u1) return;   // one pair stored it whole
+  int tm, tn;
+  unit_place(s, s.units + t, tm, tn);
+  int last = k;   // the last sharer of the tile
+  while (last + 1 < s.sharers && s.begin[last + 1] < u1) ++last;
+  const int rows = min(kTileM, p.m - tm * kTileM), cols = min(kTileN, p.n - tn * kTileN);
+  // the first part may be its pair's second item; every later one is a first
+  const float* part0 = p.parts + (size_t)(2 * k + (s.begin[k] >= u0 ? 0 : 1)) * (kTileM * kTileN);
+  const int r = blockIdx.y * 4 + (threadIdx.x >> 6), c = 4 * (threadIdx.x & 63);
+  if (r >= rows || c >= cols) return;
+  const size_t at = (size_t)r * kTileN + c;
+  float4 sum = *reinterpret_cast<const float4*>(part0 + at);
+#pragma unroll 4
+  for (int j = k + 1; j <= last; ++j) {
+    const float4 v = *reinterpret_cast<const float4*>(p.parts + (size_t)(2 * j) * (kTileM * kTileN) + at);
+    sum.x += v.x;
+    sum.y += v.y;
+    sum.z += v.z;
+    sum.w += v.w;
+  }
+  p.epi.out.put(tm * kTileM + r, tn * kTileN + c, sum, cols - c);
+}
+
+// D of an empty sum.
+__global__ void __launch_bounds__(256) zero_kernel(Mat d, int dt, int64_t rows, int cols) {
+  griddep_wait();
+  griddep_launch_dependents();
+  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
+    for (int c = threadIdx.x; c < cols; c += 256) {
+      if (dt == LM_F32) static_cast<float*>(d.data)[r * d.ld + c] = 0.f;
+      else static_cast<__nv_bfloat16*>(d.data)[r * d.ld + c] = __float2bfloat16_rn(0.f);
+    }
+}
+
+inline PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
+  static PFN_cuTensorMapEncodeTiled_v12000 fn = []() {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    const bool ok = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+                    q == cudaDriverEntryPointSuccess;
+    return ok ? reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f) : nullptr;
+  }();
+  return fn;
+}
+
+// A map of a bf16 matrix (cols, rows, 1) whose boxes are 64 columns x 128 rows
+// (K-major operands) or x 64 rows (MN-major), 128-byte swizzle.
+inline cudaError_t encode_operand(CUtensorMap* m, const void* base, int64_t cols, int64_t rows, int64_t ld, bool mn_major) {
+  const PFN_cuTensorMapEncodeTiled_v12000 enc = encode_fn();
+  if (enc == nullptr) return cudaErrorNotSupported;
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, 1};
+  const cuuint64_t pitch = (cuuint64_t)ld * 2, strides[2] = {pitch, pitch * (cuuint64_t)rows};
+  const cuuint32_t box[3] = {64, mn_major ? 64u : 128u, 1}, estr[3] = {1, 1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+             ? cudaSuccess
+             : cudaErrorInvalidValue;
+}
+
+// Whether the TMA takes the rows of a bf16 matrix as they lie.
+inline bool tma_rows(const Mat& m, int64_t rows, int64_t cols) {
+  return reinterpret_cast<uintptr_t>(m.data) % 16 == 0 && (rows > 1 ? m.ld % 8 == 0 : cols % 8 == 0);
+}
+
+// Units of `strip` tiles dealt in turn, no sum split.
+inline Schedule plain_schedule(int64_t m, int64_t n, int64_t k, int strip) {
+  Schedule s{};
+  s.tiles_m = (int32_t)((m + kTileM - 1) / kTileM);
+  s.tiles_n = (int32_t)((n + kTileN - 1) / kTileN);
+  s.nkb = (int32_t)((k + kBlockK - 1) / kBlockK);
+  s.strip = strip;
+  s.strips = (s.tiles_n + strip - 1) / strip;
+  s.units = s.tiles_m * s.strips;
+  return s;
+}
+// Whole waves of tiles, the rest shared by ranges of the sum.
+inline Schedule split_schedule(int64_t m, int64_t n, int64_t k) {
+  Schedule s = plain_schedule(m, n, k, 1);
+  const int32_t tiles = s.units;
+  s.units = tiles / kPairs * kPairs;
+  s.rest = tiles - s.units;
+  if (s.rest > 0) {
+    // a share of at least kChunk blocks, and never more sharers than pairs
+    const int64_t most = (int64_t)s.rest * s.nkb / kChunk;
+    s.sharers = (int32_t)(most < s.rest ? s.rest : most < kPairs ? most : kPairs);
+    for (int k2 = 0; k2 <= s.sharers; ++k2) s.begin[k2] = (int64_t)s.rest * s.nkb * k2 / s.sharers;
+  }
+  return s;
+}
+inline bool has_parts(const Schedule& s) { return s.rest > 0 && s.sharers > s.rest; }
+inline size_t parts_bytes(const Schedule& s) { return has_parts(s) ? 2 * (size_t)s.sharers * kPartBytes : 0; }
+inline int pairs_of(const Schedule& s) { return std::min(kPairs, std::max(s.units, s.sharers)); }
+
+// A launch whose set-up may overlap the end of the kernel before it (which it
+// waits for itself, griddepcontrol.wait).
+template <typename Kernel, typename... Args>
+cudaError_t launch_after(Kernel kernel, dim3 grid, int threads, size_t smem, cudaStream_t st, const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  count_launch();
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <bool kAMn, bool kBMn, typename Epi>
+cudaError_t start(const Params<Epi>& p, cudaStream_t st) {
+  const int dev = device_slot();
+  static bool ready[kMaxDevices];
+  if (dev < 0 || !ready[dev]) {
+    const cudaError_t e = cudaFuncSetAttribute(gemm_kernel<kAMn, kBMn, Epi>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
+    if (e != cudaSuccess) return e;
+    if (dev >= 0) ready[dev] = true;
+  }
+  return launch_after(gemm_kernel<kAMn, kBMn, Epi>, dim3(2 * pairs_of(p.sch)), kThreads, kSmemBytes, st, p);
+}
+inline cudaError_t start_zero(const Mat& d, int dt, int64_t rows, int cols, cudaStream_t st) {
+  return launch_after(zero_kernel, dim3((unsigned)std::min<int64_t>(rows, 152 * 8)), 256, 0, st, d, dt, rows, cols);
+}
+// A product whose sums may be split: the kernel, and the join where parts are left.
+template <bool kAMn, bool kBMn>
+cudaError_t start_store(const Params<StoreEpi>& p, cudaStream_t st) {
+  const cudaError_t e = start<kAMn, kBMn, StoreEpi>(p, st);
+  if (e != cudaSuccess || !has_parts(p.sch)) return e;
+  return launch_after(join_kernel, dim3(p.sch.rest, kTileM / 4), 256, 0, st, p);
+}
+
+}  // namespace
+}  // namespace gemm
+}  // namespace lm

@@ -1,6 +1,7 @@
 // Internal declarations of the training-step operators: the launch parameters
 // that lm_train_api.cu fills from checked arguments, and the launchers of
-// lm_logprob.cu, lm_rmsnorm.cu, lm_checkpoint8.cu and lm_wgrad8.cu.
+// lm_logprob.cu, lm_linlogp.cu, lm_rmsnorm.cu, lm_rotary.cu, lm_checkpoint8.cu,
+// lm_wgrad8.cu and lm_linear8.cu.
 #pragma once
 
 #include <cuda_runtime.h>
@@ -82,5 +83,71 @@ struct WgradParams {
 };
 size_t wgrad8_workspace(const Mat& dy, int dydt, int64_t tokens, int64_t out, int64_t in);
 cudaError_t launch_wgrad8(const WgradParams& p, cudaStream_t st);
+
+struct LinLogpParams {
+  int64_t rows;
+  int32_t vocab, width;
+  Mat h, w;             // bf16
+  const int64_t* targets;
+  float *logp, *entropy, *lse;
+  const float *g_logp, *g_entropy, *g_lse;
+  bool gradient_only;   // lse and entropy are read
+  Mat dh, dw;           // data NULL where absent; dh bf16
+  int dwdt;
+  int accumulate;       // adds to dw
+  void* workspace;
+};
+size_t linlogp_workspace(const LinLogpParams& p);
+cudaError_t launch_linlogp(const LinLogpParams& p, cudaStream_t st);
+
+// A checked 8-bit weight matrix.
+struct Blocks {
+  uint8_t* data;
+  float* scales;
+  int64_t ld, ld_scales;
+};
+cudaError_t launch_weight8_pack(lm_dtype dt, const Mat& w, int64_t rows, int64_t cols, const Blocks& c, cudaStream_t st);
+cudaError_t launch_weight8_unpack(lm_dtype dt, const Blocks& c, int64_t rows, int64_t cols, const Mat& w, cudaStream_t st);
+
+struct Linear8Params {
+  int64_t tokens;
+  int32_t out, in;      // of the weights
+  Codes x;              // tokens x in; tokens x out for the input gradient
+  Blocks w;
+  Mat y;
+  int ydt;
+  bool grad;
+  void* workspace;
+};
+size_t linear8_workspace(const Linear8Params& p);
+cudaError_t launch_linear8(const Linear8Params& p, cudaStream_t st);
+
+// Heads of one tensor: channel c of head h of token t at data[t * ld_token + h * ld_head + c].
+struct Heads {
+  void* data;
+  int64_t ld_token, ld_head;
+};
+struct RotaryPart {
+  int32_t heads;        // 0: absent
+  Heads x, y, dy, dx;   // forward: x -> y; gradient: dy (and x with the norm) -> dx
+  const void* weight;   // NULL for ones
+  int wdt;
+  void* dweight;        // NULL: not wanted
+  int dwdt;
+};
+struct RotaryParams {
+  int64_t tokens;
+  int32_t dim, turned;
+  const int64_t* positions;
+  const float* table;   // table_rows x turned / 2 x (cos, sin)
+  int64_t table_rows;
+  RotaryPart part[2];   // queries, keys
+  bool norm, interleaved;
+  float eps;
+  float* sums;          // dweight's parts: blocks x dim for each part
+};
+size_t rotary_grad_workspace(int64_t tokens, int64_t heads, int32_t dim);
+cudaError_t launch_rotary(lm_dtype dt, const RotaryParams& p, cudaStream_t st);
+cudaError_t launch_rotary_grad(lm_dtype dt, const RotaryParams& p, cudaStream_t st);
 
 }  // namespace lm

@@ -5,6 +5,8 @@
 #include <stdarg.h>
 #include <stdio.h>
 
+#include <algorithm>
+
 #include "lm_train.h"
 
 namespace lm {
@@ -184,6 +186,264 @@ lm_status logprob_call(const lm_token_logprob_args* a, bool gradient_only, void*
   const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   return gradient_only ? launched(launch_logprob_grad(a->logits.dtype, p, st), "lm_token_logprob_grad")
                        : launched(launch_logprob(a->logits.dtype, p, st), "lm_token_logprob");
+}
+
+// At most 2^46 elements in a product's result, so that tiles count in 31 bits.
+lm_status check_product(int64_t rows, int64_t cols) {
+  return rows > 0 && cols > ((int64_t)1 << 46) / rows ? fail(LM_ERR_UNSUPPORTED, "a product of more than 2^46 elements") : LM_OK;
+}
+// The tensor maps hold strides below 2^40 bytes.
+constexpr int64_t kMostMapped = (int64_t)1 << 38;
+bool too_large_to_map(int64_t rows, int64_t ld) { return rows > 0 && ld > kMostMapped / rows; }
+
+lm_status check_workspace(const void* workspace, size_t bytes, size_t need, size_t align) {
+  if (need == 0) return LM_OK;
+  if (workspace == nullptr || bytes < need)
+    return fail(LM_ERR_INVALID_ARG, "workspace of %zu bytes, %zu are needed", workspace == nullptr ? (size_t)0 : bytes, need);
+  return check_aligned(workspace, align, "workspace");
+}
+
+LinLogpParams linlogp_params(const lm_linear_logprob_args& a, bool gradient_only) {
+  LinLogpParams p{};
+  p.rows = a.h.rows;
+  p.vocab = (int32_t)a.weight.rows;
+  p.width = (int32_t)a.h.cols;
+  p.h = mat(&a.h);
+  p.w = mat(&a.weight);
+  p.targets = a.targets;
+  p.logp = gradient_only ? nullptr : a.logp;
+  p.entropy = a.entropy;
+  p.lse = a.lse;
+  p.g_logp = a.g_logp;
+  p.g_entropy = a.g_entropy;
+  p.g_lse = a.g_lse;
+  p.gradient_only = gradient_only;
+  if (a.dh.data != nullptr) p.dh = mat(&a.dh);
+  if (a.dweight.data != nullptr) p.dw = mat(&a.dweight);
+  p.dwdt = (int)a.dweight.dtype;
+  p.accumulate = a.accumulate != 0;
+  return p;
+}
+
+lm_status linlogp_call(const lm_linear_logprob_args* a, bool gradient_only, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  if (a == nullptr) return fail(LM_ERR_INVALID_ARG, "args is NULL");
+  const int64_t n = a->h.rows, c = a->h.cols, v = a->weight.rows;
+  LM_TRY(check_matrix(a->h, n, c, "h"));
+  LM_TRY(check_matrix(a->weight, v, c, "weight"));
+  if (a->h.dtype != LM_BF16 || a->weight.dtype != LM_BF16) return fail(LM_ERR_DTYPE, "h and weight are bf16");
+  if (v == 0 || c == 0) return fail(LM_ERR_INVALID_ARG, "an empty vocabulary or width");
+  const bool dh = a->dh.data != nullptr, dw = a->dweight.data != nullptr, g = a->g_logp != nullptr || a->g_entropy != nullptr || a->g_lse != nullptr;
+  if (dh) {
+    LM_TRY(check_matrix(a->dh, n, c, "dh"));
+    if (a->dh.dtype != LM_BF16) return fail(LM_ERR_DTYPE, "dh and h differ in dtype");
+  }
+  if (dw) LM_TRY(check_matrix(a->dweight, v, c, "dweight"));
+  if (gradient_only && !dh && !dw && n > 0) return fail(LM_ERR_INVALID_ARG, "dh and dweight are both NULL");
+  if ((dh || dw) && !g && n > 0) return fail(LM_ERR_INVALID_ARG, "dh or dweight without any of g_logp, g_entropy, g_lse");
+  if (g && !dh && !dw && n > 0) return fail(LM_ERR_INVALID_ARG, "g_logp, g_entropy or g_lse without dh or dweight");
+  const float* logp = gradient_only ? nullptr : a->logp;
+  if (a->targets == nullptr && n > 0 && (logp != nullptr || a->g_logp != nullptr)) return fail(LM_ERR_INVALID_ARG, "targets is NULL");
+  if (gradient_only && n > 0 && (a->lse == nullptr || (a->g_entropy != nullptr && a->entropy == nullptr)))
+    return fail(LM_ERR_INVALID_ARG, "the gradient reads lse, and entropy with g_entropy");
+  LM_TRY(check_aligned(a->targets, 8, "targets"));
+  const void* floats[] = {logp, a->entropy, a->lse, a->g_logp, a->g_entropy, a->g_lse};
+  for (const void* f : floats) LM_TRY(check_aligned(f, 4, "a float array"));
+  LM_TRY(check_product(n, v));
+  if (too_large_to_map(n, n > 1 ? a->h.ld : c) || too_large_to_map(v, v > 1 ? a->weight.ld : c) || too_large_to_map(n, c) || too_large_to_map(v, c) ||
+      too_large_to_map(n, 4096))
+    return fail(LM_ERR_UNSUPPORTED, "h or weight of 2^38 elements or more, or more than 2^26 rows");
+  if (n == 0 && (!dw || a->accumulate != 0)) return LM_OK;
+  LinLogpParams p = linlogp_params(*a, gradient_only);
+  const size_t need = linlogp_workspace(p);
+  LM_TRY(check_workspace(workspace, workspace_bytes, need, 256));
+  int dev = 0;
+  LM_TRY(current_device(&dev));
+  if (n > 0) {
+    LM_TRY(check_memory(a->h.data, dev, "h"));
+    LM_TRY(check_memory(a->weight.data, dev, "weight"));
+    if (dh) LM_TRY(check_memory(a->dh.data, dev, "dh"));
+    LM_TRY(check_memory(a->targets, dev, "targets"));
+    for (const void* f : floats) LM_TRY(check_memory(f, dev, "a float array"));
+    LM_TRY(check_memory(workspace, dev, "workspace"));
+  }
+  if (dw) LM_TRY(check_memory(a->dweight.data, dev, "dweight"));
+  p.workspace = workspace;
+  return launched(launch_linlogp(p, static_cast<cudaStream_t>(cuda_stream)), gradient_only ? "lm_linear_logprob_grad" : "lm_linear_logprob");
+}
+
+lm_status check_weight8(const lm_weight8& c, int64_t rows, int64_t cols, const char* what) {
+  if (c.rows != rows || c.cols != cols)
+    return fail(LM_ERR_INVALID_ARG, "%s is %lld x %lld, expected %lld x %lld", what, (long long)c.rows, (long long)c.cols,
+                (long long)rows, (long long)cols);
+  LM_TRY(check_extent(rows, cols, what));
+  if (rows == 0 || cols == 0) return LM_OK;
+  const int64_t per = (cols + LM_CODE_GROUP - 1) / LM_CODE_GROUP;
+  if (c.codes == nullptr || c.scales == nullptr) return fail(LM_ERR_INVALID_ARG, "%s: NULL codes or scales", what);
+  if (c.ld_codes < cols || c.ld_scales < per) return fail(LM_ERR_INVALID_ARG, "%s: pitch of codes or scales below the extent", what);
+  if (c.ld_codes % 16 != 0 || reinterpret_cast<uintptr_t>(c.codes) % 16 != 0 || reinterpret_cast<uintptr_t>(c.scales) % 4 != 0)
+    return fail(LM_ERR_ALIGN, "%s: codes and their pitch must be multiples of 16 bytes, scales of 4", what);
+  if (c.ld_codes > kMaxBytes / rows || c.ld_scales > kMaxBytes / 4 / rows) return fail(LM_ERR_UNSUPPORTED, "%s: pitch too large", what);
+  return LM_OK;
+}
+Blocks blocks(const lm_weight8& c) { return Blocks{static_cast<uint8_t*>(c.codes), c.scales, c.ld_codes, c.ld_scales}; }
+
+lm_status weight8_call(const lm_matrix* w, const lm_weight8* c, bool pack, void* cuda_stream) {
+  if (w == nullptr || c == nullptr) return fail(LM_ERR_INVALID_ARG, "w or c is NULL");
+  LM_TRY(check_matrix(*w, w->rows, w->cols, "w"));
+  LM_TRY(check_weight8(*c, w->rows, w->cols, "c"));
+  if (w->rows == 0 || w->cols == 0) return LM_OK;
+  int dev = 0;
+  LM_TRY(current_device(&dev));
+  LM_TRY(check_memory(w->data, dev, "w"));
+  LM_TRY(check_memory(c->codes, dev, "codes"));
+  LM_TRY(check_memory(c->scales, dev, "scales"));
+  const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  return pack ? launched(launch_weight8_pack(w->dtype, mat(w), w->rows, w->cols, blocks(*c), st), "lm_weight8_pack")
+              : launched(launch_weight8_unpack(w->dtype, blocks(*c), w->rows, w->cols, mat(w), st), "lm_weight8_unpack");
+}
+
+lm_status linear8_call(const lm_checkpoint8* x, const lm_weight8* w, const lm_matrix* y, bool grad, void* workspace, size_t workspace_bytes,
+                       void* cuda_stream) {
+  const char *xn = grad ? "dy" : "x", *yn = grad ? "dx" : "y";
+  if (x == nullptr || w == nullptr || y == nullptr) return fail(LM_ERR_INVALID_ARG, "%s, w or %s is NULL", xn, yn);
+  const int64_t tokens = x->rows, k = grad ? w->rows : w->cols, n = grad ? w->cols : w->rows;
+  LM_TRY(check_codes(*x, tokens, k, xn));
+  if (x->format != LM_CODE_E4M3) return fail(LM_ERR_DTYPE, "%s: the product takes LM_CODE_E4M3", xn);
+  LM_TRY(check_weight8(*w, w->rows, w->cols, "w"));
+  LM_TRY(check_matrix(*y, tokens, n, yn));
+  if (tokens == 0 || n == 0) return LM_OK;
+  LM_TRY(check_product(tokens, n));
+  if (too_large_to_map(tokens, x->ld_codes) || too_large_to_map(w->rows, w->ld_codes) || too_large_to_map(tokens, k) || too_large_to_map(w->rows, w->cols))
+    return fail(LM_ERR_UNSUPPORTED, "%s or w of 2^38 elements or more", xn);
+  const size_t need = lm_linear8_workspace(x, w, grad);
+  LM_TRY(check_workspace(workspace, workspace_bytes, need, 256));
+  int dev = 0;
+  LM_TRY(current_device(&dev));
+  if (k > 0) {
+    LM_TRY(check_memory(x->codes, dev, "codes"));
+    LM_TRY(check_memory(x->scales, dev, "scales"));
+    LM_TRY(check_memory(w->codes, dev, "the weights' codes"));
+    LM_TRY(check_memory(w->scales, dev, "the weights' scales"));
+    if (need > 0) LM_TRY(check_memory(workspace, dev, "workspace"));
+  }
+  LM_TRY(check_memory(y->data, dev, yn));
+  Linear8Params p{};
+  p.tokens = tokens;
+  p.out = (int32_t)w->rows;
+  p.in = (int32_t)w->cols;
+  p.x = codes(x);
+  p.w = blocks(*w);
+  p.y = mat(y);
+  p.ydt = (int)y->dtype;
+  p.grad = grad;
+  p.workspace = workspace;
+  return launched(launch_linear8(p, static_cast<cudaStream_t>(cuda_stream)), grad ? "lm_linear8_grad" : "lm_linear8");
+}
+
+lm_status check_heads(const lm_heads& h, int64_t tokens, int64_t heads, int64_t dim, lm_dtype dtype, const char* what) {
+  if (h.dtype != LM_F32 && h.dtype != LM_BF16) return fail(LM_ERR_DTYPE, "%s: dtype %d is not LM_F32 or LM_BF16", what, (int)h.dtype);
+  if (h.dtype != dtype) return fail(LM_ERR_DTYPE, "%s: the call's tensors differ in dtype", what);
+  if (h.tokens != tokens || h.heads != heads || h.dim != dim)
+    return fail(LM_ERR_INVALID_ARG, "%s is %lld x %lld x %lld, expected %lld x %lld x %lld", what, (long long)h.tokens, (long long)h.heads,
+                (long long)h.dim, (long long)tokens, (long long)heads, (long long)dim);
+  if (tokens < 0 || heads < 0 || dim < 0) return fail(LM_ERR_INVALID_ARG, "%s: negative extent", what);
+  if (dim > 1024) return fail(LM_ERR_UNSUPPORTED, "%s: heads of more than 1024 channels", what);
+  if (tokens > kMaxCols || heads > kMaxCols) return fail(LM_ERR_UNSUPPORTED, "%s: more than 2^31 - 256 tokens or heads", what);
+  if (tokens == 0 || heads == 0 || dim == 0) return LM_OK;
+  if (h.data == nullptr) return fail(LM_ERR_INVALID_ARG, "%s: NULL data", what);
+  const int64_t size = dtype == LM_F32 ? 4 : 2;
+  if (reinterpret_cast<uintptr_t>(h.data) % size != 0) return fail(LM_ERR_ALIGN, "%s: data is not aligned to its element", what);
+  const int64_t lt = tokens > 1 ? h.ld_token : 0, lh = heads > 1 ? h.ld_head : 0;
+  if (lt < 0 || lh < 0) return fail(LM_ERR_INVALID_ARG, "%s: negative stride", what);
+  if (lt > kMaxBytes / 2 / size / tokens || lh > kMaxBytes / 2 / size / heads) return fail(LM_ERR_UNSUPPORTED, "%s: stride too large", what);
+  const bool side_by_side = (heads == 1 || lh >= dim) && (tokens == 1 || lt >= (heads - 1) * lh + dim);
+  const bool apart = (tokens == 1 || lt >= dim) && (heads == 1 || lh >= (tokens - 1) * lt + dim);
+  if (!side_by_side && !apart) return fail(LM_ERR_INVALID_ARG, "%s: elements share places (strides %lld, %lld)", what, (long long)h.ld_token, (long long)h.ld_head);
+  return LM_OK;
+}
+Heads heads(const lm_heads& h) { return Heads{h.data, h.tokens > 1 ? h.ld_token : 0, h.heads > 1 ? h.ld_head : 0}; }
+
+lm_status rotary_call(const lm_qk_rotary_args* a, bool grad, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  if (a == nullptr) return fail(LM_ERR_INVALID_ARG, "args is NULL");
+  const int64_t tokens = a->q.y.tokens, dim = a->q.y.dim;
+  const lm_dtype dt = a->q.y.dtype;
+  RotaryParams p{};
+  bool any_dw = false;
+  const lm_rotary_part* parts[2] = {&a->q, &a->k};
+  const bool reads_x = !grad || a->norm != 0;
+  for (int i = 0; i < 2; ++i) {
+    const lm_rotary_part& r = *parts[i];
+    const int64_t n = r.y.heads;
+    if (i == 1 && n == 0) continue;
+    const char *yn = grad ? (i ? "dk" : "dq") : (i ? "k's output" : "q's output"), *xn = i ? "k" : "q", *dn = i ? "k's gradient" : "q's gradient";
+    LM_TRY(check_heads(r.y, tokens, n, dim, dt, yn));
+    if (reads_x) LM_TRY(check_heads(r.x, tokens, n, dim, dt, xn));
+    if (grad) LM_TRY(check_heads(r.dx, tokens, n, dim, dt, dn));
+    const lm_heads &out = grad ? r.dx : r.y, &in = grad ? r.y : r.x;
+    if (out.data == in.data && tokens > 0 && n > 0 && ((tokens > 1 && out.ld_token != in.ld_token) || (n > 1 && out.ld_head != in.ld_head)))
+      return fail(LM_ERR_INVALID_ARG, "%s written over its input needs the same strides", grad ? dn : yn);
+    if (a->norm == 0 && (r.weight.data != nullptr || (grad && r.dweight.data != nullptr))) return fail(LM_ERR_INVALID_ARG, "a weight without the norm");
+    if (r.weight.data != nullptr) LM_TRY(check_vector(r.weight, dim, "weight"));
+    if (grad && r.dweight.data != nullptr) {
+      LM_TRY(check_vector(r.dweight, dim, "dweight"));
+      any_dw = true;
+    }
+    RotaryPart& o = p.part[i];
+    o.heads = (int32_t)n;
+    if (reads_x) o.x = heads(r.x);
+    if (grad) {
+      o.dy = heads(r.y);
+      o.dx = heads(r.dx);
+      o.dweight = r.dweight.data;
+      o.dwdt = (int)r.dweight.dtype;
+    } else {
+      o.y = heads(r.y);
+    }
+    o.weight = r.weight.data;
+    o.wdt = (int)r.weight.dtype;
+  }
+  if ((int64_t)p.part[0].heads + p.part[1].heads > kMaxCols) return fail(LM_ERR_UNSUPPORTED, "more than 2^31 - 256 heads");
+  if (a->turned < 0 || a->turned > dim || a->turned % 2 != 0) return fail(LM_ERR_INVALID_ARG, "turned %d is not even or outside 0 .. dim", a->turned);
+  if (a->table_rows < 0 || a->table_rows > kMaxBytes / 8 / 1024) return fail(LM_ERR_INVALID_ARG, "table_rows %lld", (long long)a->table_rows);
+  if (a->turned > 0 && tokens > 0) {
+    if (a->positions == nullptr || (a->table == nullptr && a->table_rows > 0)) return fail(LM_ERR_INVALID_ARG, "positions or table is NULL");
+    LM_TRY(check_aligned(a->positions, 8, "positions"));
+    LM_TRY(check_aligned(a->table, 4, "table"));
+  }
+  if (a->norm != 0 && (!(a->eps >= 0.0) || !isfinite(a->eps))) return fail(LM_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  const bool rows = tokens > 0 && p.part[0].heads + p.part[1].heads > 0;
+  if (dim == 0 || (!rows && !any_dw)) return LM_OK;
+  if (any_dw) LM_TRY(check_workspace(workspace, workspace_bytes, lm_qk_rotary_grad_workspace(a), 16));
+  int dev = 0;
+  LM_TRY(current_device(&dev));
+  for (int i = 0; i < 2; ++i) {
+    const lm_rotary_part& r = *parts[i];
+    if (i == 1 && r.y.heads == 0) continue;
+    if (tokens > 0 && r.y.heads > 0) {
+      LM_TRY(check_memory(r.y.data, dev, grad ? "dq or dk" : "an output"));
+      if (reads_x) LM_TRY(check_memory(r.x.data, dev, "q or k"));
+      if (grad) LM_TRY(check_memory(r.dx.data, dev, "a gradient"));
+      LM_TRY(check_memory(r.weight.data, dev, "weight"));
+    }
+    if (grad) LM_TRY(check_memory(r.dweight.data, dev, "dweight"));
+  }
+  if (a->turned > 0 && tokens > 0) {
+    LM_TRY(check_memory(a->positions, dev, "positions"));
+    LM_TRY(check_memory(a->table, dev, "table"));
+    p.positions = a->positions;
+    p.table = a->table;
+  }
+  if (any_dw && rows) LM_TRY(check_memory(workspace, dev, "workspace"));
+  p.tokens = tokens;
+  p.dim = (int32_t)dim;
+  p.turned = a->turned;
+  p.table_rows = a->table_rows;
+  p.norm = a->norm != 0;
+  p.interleaved = a->interleaved != 0;
+  p.eps = (float)a->eps;
+  p.sums = static_cast<float*>(workspace);
+  const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  return grad ? launched(launch_rotary_grad(dt, p, st), "lm_qk_rotary_grad") : launched(launch_rotary(dt, p, st), "lm_qk_rotary");
 }
 
 }  // namespace
@@ -392,6 +652,47 @@ lm_status lm_linear_wgrad8(const lm_matrix* dy, const lm_checkpoint8* x, const l
   p.accumulate = accumulate != 0;
   p.workspace = workspace;
   return launched(launch_wgrad8(p, static_cast<cudaStream_t>(cuda_stream)), "lm_linear_wgrad8");
+}
+
+size_t lm_linear_logprob_workspace(const lm_linear_logprob_args* a) {
+  if (a == nullptr || a->h.rows <= 0 || a->h.cols <= 0 || a->weight.rows <= 0 || a->h.rows > kMaxCols || a->h.cols > kMaxCols || a->weight.rows > kMaxCols) return 0;
+  // the call alone knows whether the forward pass is wanted too: room for both
+  return std::max(linlogp_workspace(linlogp_params(*a, false)), linlogp_workspace(linlogp_params(*a, true)));
+}
+lm_status lm_linear_logprob(const lm_linear_logprob_args* a, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  return linlogp_call(a, false, workspace, workspace_bytes, cuda_stream);
+}
+lm_status lm_linear_logprob_grad(const lm_linear_logprob_args* a, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  return linlogp_call(a, true, workspace, workspace_bytes, cuda_stream);
+}
+
+lm_status lm_weight8_pack(const lm_matrix* w, const lm_weight8* c, void* cuda_stream) { return weight8_call(w, c, true, cuda_stream); }
+lm_status lm_weight8_unpack(const lm_weight8* c, const lm_matrix* w, void* cuda_stream) { return weight8_call(w, c, false, cuda_stream); }
+
+size_t lm_linear8_workspace(const lm_checkpoint8* x, const lm_weight8* w, int grad) {
+  if (x == nullptr || w == nullptr || x->rows <= 0 || w->rows <= 0 || w->cols <= 0 || x->rows > kMaxCols || w->rows > kMaxCols || w->cols > kMaxCols) return 0;
+  Linear8Params p{};
+  p.tokens = x->rows;
+  p.out = (int32_t)w->rows;
+  p.in = (int32_t)w->cols;
+  p.grad = grad != 0;
+  return linear8_workspace(p);
+}
+lm_status lm_linear8(const lm_checkpoint8* x, const lm_weight8* w, const lm_matrix* y, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  return linear8_call(x, w, y, false, workspace, workspace_bytes, cuda_stream);
+}
+lm_status lm_linear8_grad(const lm_checkpoint8* dy, const lm_weight8* w, const lm_matrix* dx, void* workspace, size_t workspace_bytes,
+                          void* cuda_stream) {
+  return linear8_call(dy, w, dx, true, workspace, workspace_bytes, cuda_stream);
+}
+
+lm_status lm_qk_rotary(const lm_qk_rotary_args* a, void* cuda_stream) { return rotary_call(a, false, nullptr, 0, cuda_stream); }
+size_t lm_qk_rotary_grad_workspace(const lm_qk_rotary_args* a) {
+  if (a == nullptr || a->q.y.dim <= 0 || a->q.y.dim > 1024) return 0;
+  return rotary_grad_workspace(a->q.y.tokens, a->q.y.heads > a->k.y.heads ? a->q.y.heads : a->k.y.heads, (int32_t)a->q.y.dim);
+}
+lm_status lm_qk_rotary_grad(const lm_qk_rotary_args* a, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  return rotary_call(a, true, workspace, workspace_bytes, cuda_stream);
 }
 
 }  // extern "C"

@@ -34,7 +34,10 @@ EXPORTED = ("lm_config_default", "lm_create", "lm_step", "lm_set_lr", "lm_msign_
             "lm_msign_ns_noalloc_status", "lm_shard_owners", "lm_config_size",
             "lm_token_logprob", "lm_token_logprob_grad", "lm_checkpoint8_pack", "lm_checkpoint8_unpack",
             "lm_rmsnorm", "lm_rmsnorm_grad", "lm_rmsnorm_grad_workspace",
-            "lm_linear_wgrad8", "lm_linear_wgrad8_workspace")
+            "lm_linear_wgrad8", "lm_linear_wgrad8_workspace",
+            "lm_linear_logprob", "lm_linear_logprob_grad", "lm_linear_logprob_workspace",
+            "lm_weight8_pack", "lm_weight8_unpack", "lm_linear8", "lm_linear8_grad", "lm_linear8_workspace",
+            "lm_qk_rotary", "lm_qk_rotary_grad", "lm_qk_rotary_grad_workspace")
 
 KERNEL_FAMILIES = ("lion", "momentum_norm", "ns_gram", "ns_poly", "ns_apply", "finalize", "other", "adamw",
                    "srank")
@@ -82,6 +85,34 @@ class LmTokenLogprobArgs(ctypes.Structure):
                 ("logp", ctypes.c_void_p), ("entropy", ctypes.c_void_p), ("lse", ctypes.c_void_p),
                 ("top_logp", ctypes.c_void_p), ("top_index", ctypes.c_void_p), ("g_logp", ctypes.c_void_p),
                 ("g_entropy", ctypes.c_void_p), ("g_lse", ctypes.c_void_p), ("dlogits", LmMatrix)]
+
+
+class LmLinearLogprobArgs(ctypes.Structure):
+    _fields_ = [("h", LmMatrix), ("weight", LmMatrix), ("targets", ctypes.c_void_p), ("logp", ctypes.c_void_p),
+                ("entropy", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("g_logp", ctypes.c_void_p),
+                ("g_entropy", ctypes.c_void_p), ("g_lse", ctypes.c_void_p), ("dh", LmMatrix), ("dweight", LmMatrix),
+                ("accumulate", ctypes.c_int)]
+
+
+class LmWeight8(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64), ("ld_codes", ctypes.c_int64), ("ld_scales", ctypes.c_int64)]
+
+
+class LmHeads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("tokens", ctypes.c_int64), ("heads", ctypes.c_int64),
+                ("dim", ctypes.c_int64), ("ld_token", ctypes.c_int64), ("ld_head", ctypes.c_int64),
+                ("dtype", ctypes.c_int)]
+
+
+class LmRotaryPart(ctypes.Structure):
+    _fields_ = [("x", LmHeads), ("y", LmHeads), ("dx", LmHeads), ("weight", LmTensor), ("dweight", LmTensor)]
+
+
+class LmQkRotaryArgs(ctypes.Structure):
+    _fields_ = [("q", LmRotaryPart), ("k", LmRotaryPart), ("positions", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("table_rows", ctypes.c_int64), ("turned", ctypes.c_int), ("norm", ctypes.c_int),
+                ("interleaved", ctypes.c_int), ("eps", ctypes.c_double)]
 
 
 class LionMuonError(RuntimeError):
@@ -183,6 +214,27 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.lm_linear_wgrad8.argtypes = [P(LmMatrix), P(LmCheckpoint8), P(LmMatrix), c_int, c_void_p, ctypes.c_size_t,
                                      c_void_p]
     lib.lm_linear_wgrad8.restype = c_int
+    size = ctypes.c_size_t
+    for fn in ("lm_linear_logprob", "lm_linear_logprob_grad"):
+        getattr(lib, fn).argtypes = [P(LmLinearLogprobArgs), c_void_p, size, c_void_p]
+        getattr(lib, fn).restype = c_int
+    lib.lm_linear_logprob_workspace.argtypes = [P(LmLinearLogprobArgs)]
+    lib.lm_linear_logprob_workspace.restype = size
+    lib.lm_weight8_pack.argtypes = [P(LmMatrix), P(LmWeight8), c_void_p]
+    lib.lm_weight8_pack.restype = c_int
+    lib.lm_weight8_unpack.argtypes = [P(LmWeight8), P(LmMatrix), c_void_p]
+    lib.lm_weight8_unpack.restype = c_int
+    for fn in ("lm_linear8", "lm_linear8_grad"):
+        getattr(lib, fn).argtypes = [P(LmCheckpoint8), P(LmWeight8), P(LmMatrix), c_void_p, size, c_void_p]
+        getattr(lib, fn).restype = c_int
+    lib.lm_linear8_workspace.argtypes = [P(LmCheckpoint8), P(LmWeight8), c_int]
+    lib.lm_linear8_workspace.restype = size
+    lib.lm_qk_rotary.argtypes = [P(LmQkRotaryArgs), c_void_p]
+    lib.lm_qk_rotary.restype = c_int
+    lib.lm_qk_rotary_grad.argtypes = [P(LmQkRotaryArgs), c_void_p, size, c_void_p]
+    lib.lm_qk_rotary_grad.restype = c_int
+    lib.lm_qk_rotary_grad_workspace.argtypes = [P(LmQkRotaryArgs)]
+    lib.lm_qk_rotary_grad_workspace.restype = size
     if path is None:
         _LIB = lib
     return lib

@@ -1,8 +1,10 @@
 """Training-step operators next to the optimizer (the second half of
 ``include/lionmuon.h``): token log probabilities with entropy, top alternatives
-and gradient; RMS norm with the residual's addition, an 8-bit output and
-gradient; 8-bit activation checkpoints and the weight gradient of a linear
-layer taken from them.
+and gradient, from logits or from hidden states without them; RMS norm with the
+residual's addition, an 8-bit output and gradient; 8-bit activation checkpoints,
+8-bit weights and the linear layer's products with them (forward, input
+gradient, weight gradient); the norm of queries and keys with their rotation by
+position, and its gradient.
 
 Argument marshalling only: results and workspaces are torch tensors, allocated
 on the stream that the call runs on.  Matrices are torch tensors whose last
@@ -21,7 +23,8 @@ from typing import NamedTuple, Optional
 import torch
 
 from . import lionmuon as _L
-from .lionmuon import LM_BF16, LM_F32, LmCheckpoint8, LmMatrix, LmTensor, LmTokenLogprobArgs
+from .lionmuon import (LM_BF16, LM_F32, LmCheckpoint8, LmHeads, LmLinearLogprobArgs, LmMatrix, LmQkRotaryArgs,
+                       LmTensor, LmTokenLogprobArgs, LmWeight8)
 
 GROUP = 128                                   # channels that share one scale (LM_CODE_GROUP)
 FORMATS = {"i8": 0, "e4m3": 1}                # lm_code_format
@@ -180,6 +183,107 @@ def linear_wgrad8(dy, x: Checkpoint8, out=None, accumulate: bool = False, dtype=
     return out
 
 
+class Weight8:
+    """8-bit weights of a linear layer (``lm_weight8``): ``codes``, uint8 (e4m3),
+    out x pitch with the pitch a multiple of 16; ``scales``, float32, one for each
+    block of 128 x 128; ``cols`` input channels."""
+
+    __slots__ = ("codes", "scales", "cols")
+
+    def __init__(self, codes, scales, cols: int):
+        if codes.dtype != torch.uint8 or scales.dtype != torch.float32:
+            raise TypeError("codes are uint8 and scales float32")
+        if codes.dim() != 2 or codes.stride(1) != 1 or codes.shape[1] < cols:
+            raise ValueError("codes: expected rows x at least cols bytes, the last dimension of stride 1")
+        if scales.dim() != 2 or scales.shape[0] != -(-codes.shape[0] // GROUP) or scales.shape[1] < -(-cols // GROUP) or \
+                (scales.shape[1] > 1 and scales.stride(1) != 1):
+            raise ValueError("scales: expected blocks of rows x at least blocks of columns, the last dimension of stride 1")
+        self.codes, self.scales, self.cols = codes, scales, int(cols)
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, device="cuda") -> "Weight8":
+        w = cls.__new__(cls)
+        w.codes = torch.empty((rows, -(-cols // 16) * 16), dtype=torch.uint8, device=device)
+        w.scales = torch.empty((-(-rows // GROUP), -(-cols // GROUP)), dtype=torch.float32, device=device)
+        w.cols = cols
+        return w
+
+    @property
+    def rows(self) -> int:
+        return self.codes.shape[0]
+
+    def nbytes(self) -> int:
+        return self.codes.numel() + 4 * self.scales.numel()
+
+    def desc(self) -> LmWeight8:
+        codes, scales = self.codes, self.scales
+        rows, pitch = codes.shape
+        down, across = scales.shape
+        return LmWeight8(codes.data_ptr(), scales.data_ptr(), rows, self.cols, codes.stride(0) if rows > 1 else max(codes.stride(0), pitch),
+                         scales.stride(0) if down > 1 else across)
+
+    def unpack(self, dtype=torch.bfloat16, out=None, stream=None):
+        """The values the codes stand for (exact in bf16 and in fp32)."""
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.unpack(dtype, out)
+        lib = _L.load_library()
+        codes = self.codes
+        if out is None:
+            out = torch.empty((codes.shape[0], self.cols), dtype=dtype, device=codes.device)
+        st = lib.lm_weight8_unpack(self.desc(), _matrix(out, "out"), _stream_of(codes))
+        if st:
+            _L._check(lib, st, "lm_weight8_unpack")
+        return out
+
+
+def weight8(w, out: Optional[Weight8] = None, stream=None) -> Weight8:
+    """Weights (out x in, bf16 or fp32) in 8 bits."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return weight8(w, out)
+    lib = _L.load_library()
+    m = _matrix(w, "w")
+    if out is None:
+        out = Weight8.empty(m.rows, m.cols, w.device)
+    st = lib.lm_weight8_pack(m, out.desc(), _stream_of(w))
+    if st:
+        _L._check(lib, st, "lm_weight8_pack")
+    return out
+
+
+def _linear8(fn: str, x: Checkpoint8, w: Weight8, cols: int, out, dtype, grad: int):
+    lib = _L.load_library()
+    cx, cw = x.desc(), w.desc()
+    if out is None:
+        out = torch.empty((x.rows, cols), dtype=dtype, device=x.codes.device)
+    m = _matrix(out, "out")
+    need = lib.lm_linear8_workspace(cx, cw, grad)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
+    st = getattr(lib, fn)(cx, cw, m, ws.data_ptr() if need else None, need, _stream_of(x.codes))
+    if st:
+        _L._check(lib, st, fn)
+    return out
+
+
+def linear8(x: Checkpoint8, w: Weight8, out=None, dtype=torch.bfloat16, stream=None):
+    """x W^T: the forward product of a linear layer whose input (e4m3) and
+    weights are kept in 8 bits."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return linear8(x, w, out, dtype)
+    return _linear8("lm_linear8", x, w, w.rows, out, dtype, 0)
+
+
+def linear8_grad(dy: Checkpoint8, w: Weight8, out=None, dtype=torch.bfloat16, stream=None):
+    """dy W: the input gradient of the same layer, dy in 8 bits (e4m3).  (The
+    weight gradient is ``linear_wgrad8``.)"""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return linear8_grad(dy, w, out, dtype)
+    return _linear8("lm_linear8_grad", dy, w, w.cols, out, dtype, 1)
+
+
 class RmsNorm(NamedTuple):
     """``y``; ``h`` = x + residual (x itself without one); ``rstd``, one a row;
     ``checkpoint``: y in 8 bits, or None."""
@@ -317,3 +421,235 @@ def token_logprob_grad(logits, targets, lse, entropy, g_logp, g_entropy=None, g_
     if st:
         _L._check(lib, st, "lm_token_logprob_grad")
     return dlogits
+
+
+class LinearLogprob(NamedTuple):
+    """``logp``, ``entropy`` and ``lse``, one entry a row (``logp`` None without
+    targets); the gradients ``dh`` and ``dweight`` None without weights."""
+    logp: Optional[torch.Tensor]
+    entropy: torch.Tensor
+    lse: torch.Tensor
+    dh: Optional[torch.Tensor]
+    dweight: Optional[torch.Tensor]
+
+
+def _linear_logprob_args(h, weight, targets, g_logp, g_entropy, g_lse, dh, dweight, accumulate):
+    m = _matrix(h, "h")
+    a = LmLinearLogprobArgs()
+    a.h = m
+    a.weight = _matrix(weight, "weight")
+    a.targets = _array(targets, m.rows, torch.int64, "targets")
+    a.g_logp = _array(g_logp, m.rows, torch.float32, "g_logp")
+    a.g_entropy = _array(g_entropy, m.rows, torch.float32, "g_entropy")
+    a.g_lse = _array(g_lse, m.rows, torch.float32, "g_lse")
+    if dh is not None:
+        a.dh = _matrix(dh, "dh")
+    if dweight is not None:
+        a.dweight = _matrix(dweight, "dweight")
+    a.accumulate = 1 if accumulate else 0
+    return a, m.rows
+
+
+def _gradients(h, weight, dh, dweight, accumulate, none):
+    """What receives the gradients: new tensors for None (None with ``none``), None for False."""
+    if accumulate and (dweight is None or dweight is False):
+        raise ValueError("accumulate adds to dweight: give it")
+    made = lambda t, like: None if t is False or (none and t is None) else torch.empty(like.shape, dtype=like.dtype, device=like.device) if t is None else t  # noqa: E731
+    return made(dh, h), made(dweight, weight)
+
+
+def _linear_logprob(fn, lib, a, device_of):
+    need = lib.lm_linear_logprob_workspace(a)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
+    st = getattr(lib, fn)(a, ws.data_ptr() if need else None, need, _stream_of(device_of))
+    if st:
+        _L._check(lib, st, fn)
+
+
+def linear_logprob(h, weight, targets=None, g_logp=None, g_entropy=None, g_lse=None, dh=None, dweight=None,
+                   accumulate: bool = False, stream=None) -> LinearLogprob:
+    """``token_logprob`` of the logits h weight^T (bf16, rows x width and
+    vocabulary x width), which are never formed.  With any of the weights
+    ``g_*`` the gradients of sum(g_logp logp + g_entropy entropy + g_lse lse) by
+    h and weight come from the same call, in ``dh`` and ``dweight`` (new tensors
+    if None, not computed if False; ``dweight``, bf16 or fp32, has its gradient
+    added with ``accumulate``)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return linear_logprob(h, weight, targets, g_logp, g_entropy, g_lse, dh, dweight, accumulate)
+    lib = _L.load_library()
+    dh, dweight = _gradients(h, weight, dh, dweight, accumulate, g_logp is None and g_entropy is None and g_lse is None)
+    a, _ = _linear_logprob_args(h, weight, targets, g_logp, g_entropy, g_lse, dh, dweight, accumulate)
+    lead, device = h.shape[:-1], h.device
+    entropy, lse = torch.empty(lead, dtype=torch.float32, device=device), torch.empty(lead, dtype=torch.float32, device=device)
+    a.entropy, a.lse = entropy.data_ptr(), lse.data_ptr()
+    logp = None
+    if targets is not None:
+        logp = torch.empty(lead, dtype=torch.float32, device=device)
+        a.logp = logp.data_ptr()
+    _linear_logprob("lm_linear_logprob", lib, a, h)
+    return LinearLogprob(logp, entropy, lse, dh, dweight)
+
+
+def linear_logprob_grad(h, weight, targets, lse, entropy, g_logp, g_entropy=None, g_lse=None, dh=None, dweight=None,
+                        accumulate: bool = False, stream=None):
+    """(dh, dweight) of ``linear_logprob`` for weights known after the forward
+    call, from its ``lse`` and (with ``g_entropy``) ``entropy``; None for what
+    is False."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return linear_logprob_grad(h, weight, targets, lse, entropy, g_logp, g_entropy, g_lse, dh, dweight, accumulate)
+    lib = _L.load_library()
+    dh, dweight = _gradients(h, weight, dh, dweight, accumulate, False)
+    a, n = _linear_logprob_args(h, weight, targets, g_logp, g_entropy, g_lse, dh, dweight, accumulate)
+    a.lse = _array(lse, n, torch.float32, "lse")
+    a.entropy = _array(entropy, n, torch.float32, "entropy")
+    _linear_logprob("lm_linear_logprob_grad", lib, a, h)
+    return dh, dweight
+
+
+def rotary_frequencies(dims: int, base: float = 10000.0, factor: float = 1.0, original: int = 0, low: float = 1.0,
+                       high: float = 4.0):
+    """Angles a position, one for each of dims / 2 pairs (float64, CPU):
+    base^(-2 j / dims), for contexts ``factor`` times as long divided by it.
+    With ``original`` (positions the model was trained on) only the slow ones
+    are: those that turn at least ``high`` times within them stay, those that
+    turn at most ``low`` times are divided, the others lie between, by their
+    number of turns."""
+    if dims < 0 or dims % 2:
+        raise ValueError(f"dims {dims} is not even")
+    if not base > 0 or not factor > 0 or (original and not high > low):
+        raise ValueError("base and factor are positive, and high is above low")
+    f = base ** (-torch.arange(0, dims, 2, dtype=torch.float64) / max(dims, 1))
+    if not original:
+        return f / factor
+    keep = ((original * f / (2 * math.pi) - low) / (high - low)).clamp(0.0, 1.0)
+    return f * keep + f / factor * (1 - keep)
+
+
+def rotary_table(positions: int, frequencies, amplitude: float = 1.0, device="cuda"):
+    """The table that ``qk_rotary`` reads: amplitude times cosine and sine of
+    position times frequency, positions x dims / 2 x 2, float32 (angles in 64
+    bits, rounded once)."""
+    f = torch.as_tensor(frequencies, dtype=torch.float64, device=device)
+    a = torch.arange(positions, dtype=torch.float64, device=device)[:, None] * f
+    return torch.stack((a.cos(), a.sin()), dim=-1).mul_(amplitude).float()
+
+
+class QkRotary(NamedTuple):
+    q: torch.Tensor
+    k: Optional[torch.Tensor]
+
+
+class QkRotaryGrad(NamedTuple):
+    """Gradients of the queries, of the keys (None without them) and of their
+    gains (None where there is no norm or none was wanted)."""
+    dq: torch.Tensor
+    dk: Optional[torch.Tensor]
+    dq_weight: Optional[torch.Tensor]
+    dk_weight: Optional[torch.Tensor]
+
+
+def _heads(t, what: str) -> LmHeads:
+    """lm_heads of a tensor (.., heads, dim): the leading dimensions fold into
+    tokens of one pitch."""
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{what}: unsupported dtype {t.dtype}")
+    if t.dim() < 2:
+        raise ValueError(f"{what}: expected (.., heads, dim)")
+    if t.dim() != 3:
+        try:
+            t = t.view(math.prod(t.shape[:-2]), *t.shape[-2:])
+        except RuntimeError:
+            raise ValueError(f"{what}: the leading dimensions do not fold into tokens of one pitch") from None
+    tokens, heads, dim = t.shape
+    if t.stride(2) != 1 and dim > 1 and tokens > 0 and heads > 0:
+        raise ValueError(f"{what}: the last dimension must have stride 1")
+    return LmHeads(t.data_ptr(), tokens, heads, dim, t.stride(0), t.stride(1), code)
+
+
+def _rotary_args(tokens: int, positions, table, norm, eps, interleaved) -> LmQkRotaryArgs:
+    a = LmQkRotaryArgs()
+    if table is not None:
+        if table.dtype != torch.float32:
+            raise TypeError(f"table: expected float32, got {table.dtype}")
+        if table.dim() != 3 or table.shape[2] != 2 or not table.is_contiguous():
+            raise ValueError("table: expected positions x dims / 2 x 2, contiguous")
+        if positions is None:
+            raise ValueError("a table goes with positions")
+        a.positions = _array(positions, tokens, torch.int64, "positions")
+        a.table, a.table_rows, a.turned = table.data_ptr(), table.shape[0], 2 * table.shape[1]
+    a.norm, a.eps, a.interleaved = (1 if norm else 0), eps, (1 if interleaved else 0)
+    return a
+
+
+def qk_rotary(q, k, positions, table, q_weight=None, k_weight=None, norm: bool = True, eps: float = 1e-6,
+              interleaved: bool = False, q_out=None, k_out=None, stream=None) -> QkRotary:
+    """Queries and keys (.., heads, dim; k may be None) with each head's RMS norm
+    and gain (``norm``) and the rotation by position: ``positions`` (int64, one a
+    token) into ``table`` (``rotary_table``; its width says how many channels
+    turn; None for none).  ``q_out`` and ``k_out`` receive the results (new
+    tensors if None; q and k themselves are allowed)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return qk_rotary(q, k, positions, table, q_weight, k_weight, norm, eps, interleaved, q_out, k_out)
+    lib = _L.load_library()
+    hq = _heads(q, "q")
+    a = _rotary_args(hq.tokens, positions, table, norm, eps, interleaved)
+    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
+    a.q.x, a.q.y = hq, _heads(q_out, "q_out")
+    if q_weight is not None:
+        a.q.weight = _vector(q_weight, "q_weight")
+    if k is not None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out
+        a.k.x, a.k.y = _heads(k, "k"), _heads(k_out, "k_out")
+        if k_weight is not None:
+            a.k.weight = _vector(k_weight, "k_weight")
+    elif k_weight is not None or k_out is not None:
+        raise ValueError("k_weight or k_out without k")
+    st = lib.lm_qk_rotary(a, _stream_of(q))
+    if st:
+        _L._check(lib, st, "lm_qk_rotary")
+    return QkRotary(q_out, k_out)
+
+
+def qk_rotary_grad(dq, dk, positions, table, q=None, k=None, q_weight=None, k_weight=None, norm: bool = True,
+                   eps: float = 1e-6, interleaved: bool = False, dq_out=None, dk_out=None, dweight: bool = True,
+                   stream=None) -> QkRotaryGrad:
+    """The gradient of ``qk_rotary``.  q and k, the forward call's inputs, are
+    read with the norm only.  ``dq_out`` and ``dk_out`` receive the gradients
+    (new tensors if None; dq and dk themselves are allowed).  The gains'
+    gradients have the dtype of the gains, float32 where there are none."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return qk_rotary_grad(dq, dk, positions, table, q, k, q_weight, k_weight, norm, eps, interleaved, dq_out,
+                                  dk_out, dweight)
+    lib = _L.load_library()
+    hq = _heads(dq, "dq")
+    a = _rotary_args(hq.tokens, positions, table, norm, eps, interleaved)
+    gains = [None, None]
+    outs = [dq_out, dk_out]
+    for i, (part, d, x, w) in enumerate(((a.q, dq, q, q_weight), (a.k, dk, k, k_weight))):
+        if d is None:
+            if w is not None or outs[i] is not None or x is not None:
+                raise ValueError("keys, their gain or gradient without dk")
+            continue
+        if outs[i] is None:
+            outs[i] = torch.empty(d.shape, dtype=d.dtype, device=d.device)
+        part.y, part.dx = _heads(d, "dq" if i == 0 else "dk"), _heads(outs[i], "dq_out" if i == 0 else "dk_out")
+        if norm:
+            if x is None:
+                raise ValueError("the gradient of the norm reads q and k")
+            part.x = _heads(x, "q" if i == 0 else "k")
+            if dweight:
+                gains[i] = torch.empty(part.y.dim, dtype=w.dtype if w is not None else torch.float32, device=d.device)
+                part.dweight = _vector(gains[i], "dweight")
+        if w is not None:
+            part.weight = _vector(w, "q_weight" if i == 0 else "k_weight")
+    need = lib.lm_qk_rotary_grad_workspace(a) if norm and dweight else 0
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
+    st = lib.lm_qk_rotary_grad(a, ws.data_ptr() if need else None, need, _stream_of(dq))
+    if st:
+        _L._check(lib, st, "lm_qk_rotary_grad")
+    return QkRotaryGrad(outs[0], outs[1], gains[0], gains[1])
