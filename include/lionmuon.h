@@ -577,8 +577,10 @@ lm_status lm_linear_wgrad8(const lm_matrix* dy, const lm_checkpoint8* x, const l
  * formulas, its targets and their rules, its rows of -inf, +inf and NaN), and
  * the gradients of the same loss:
  *   dh = dz weight,   dweight (+)= dz^T h
- * z is summed in fp32 and never rounded below it; dz is rounded to bf16, as the
- * tensor cores take it, and both products are summed in fp32.  The tensor cores
+ * z is summed in fp32; for the gradients of one call with the forward results it
+ * is kept in 16 bits, in steps of 2^-10 below the row's maximum (p is off by
+ * 2^-11 of itself at most, and 0 where the logit is 64 below).  dz is rounded to
+ * bf16, as the tensor cores take it, and both products are summed in fp32.  The tensor cores
  * add at most 512 products (each addition of 16 may drop 2^-23 of what it has);
  * their sums are added in fp32.  Sums are taken in a fixed order: the same
  * inputs give the same bits.
@@ -603,10 +605,11 @@ typedef struct {
  * beforehand.  rows == 0 is accepted (dweight is then zero, or left as it is
  * with accumulate); an empty vocabulary or C == 0 is not.
  * workspace: lm_linear_logprob_workspace(args) bytes of device memory,
- * 256-byte aligned, free again when the work is done (with gradients, T x
- * up to 512 MB / T columns of dz, at least 2048; fp32 sums of dh where the
- * vocabulary takes several such pieces; copies of h and weight where their rows
- * are not 16-byte aligned; partial sums of at most 40 MB).
+ * 256-byte aligned, free again when the work is done (with gradients, 16 bits
+ * a logit for as many tokens as take 512 MB, at least 1024; fp32 sums of a bf16
+ * dweight where the tokens take several such pieces; copies of h and weight where
+ * their rows are not 16-byte aligned; statistics, a tenth of the logits' at most;
+ * partial sums of at most 40 MB).
  * Should a device-side wait give up (LM_WAIT_LIMIT_NS), what was not computed
  * is NaN.
  * Errors: LM_ERR_INVALID_ARG (also a workspace that is too small),

@@ -5,7 +5,7 @@
 //
 // Either operand lies K-major (rows of the summed dimension: one box of 64 x
 // 128 rows a CTA) or MN-major (rows of D's dimension, one row an element of the
-// sum: two boxes of 64 x 64).  CTA r of the pair holds rows 128 r .. of the
+// sum: two boxes of 64 x 64), as a matrix or in blocks of 64 columns.  CTA r of the pair holds rows 128 r .. of the
 // tile (A) and columns 128 r .. (B).
 //
 // CTA roles (12 warps, one CTA per SM):
@@ -48,17 +48,21 @@ using tcs::kCleanupWaitNs;
 constexpr int kTileM = 256, kTileN = 256, kBlockK = 64;
 constexpr int kHalf = 128;
 constexpr int kABytes = kHalf * kBlockK * 2, kBBytes = kHalf * kBlockK * 2;
-constexpr int kStages = 6, kStageBytes = kABytes + kBBytes;
+constexpr int kStageBytes = kABytes + kBBytes;
 constexpr int kFirstEpi = 4, kEpiWarps = 8;            // whole warpgroups: a warp reads the TMEM lanes of its number mod 4
 constexpr int kThreads = 32 * (kFirstEpi + kEpiWarps);
 constexpr int kChunk = 8;                              // most blocks summed in one accumulator
 constexpr int kPairs = 76;                             // CTA pairs of the GPU (152 SMs)
 constexpr int kTmemCols = 512;
-constexpr int kTransBytes = 32 * 20 * 4;               // an epilogue warp's transpose tile: 32 rows x 16 columns, 80-byte rows
-constexpr size_t kTransOffset = (size_t)kStages * kStageBytes;
-constexpr size_t kBarOffset = kTransOffset + (size_t)kEpiWarps * kTransBytes;
-constexpr size_t kSmemBytes = 1024 + kBarOffset + 512;
-static_assert(kSmemBytes <= 232448, "shared memory of one SM");
+constexpr int kBoxBytes = 32 * 128;                    // an epilogue warp's 32 rows of 128 bytes (128-byte swizzle), as the TMA stores them
+// Shared memory of a CTA: stages, the epilogue warps' boxes, barriers.
+template <typename Epi>
+struct Smem {
+  static constexpr size_t kBoxes = (size_t)Epi::kStages * kStageBytes;
+  static constexpr size_t kBars = kBoxes + (size_t)kEpiWarps * Epi::kBoxes * kBoxBytes;
+  static constexpr size_t kBytes = 1024 + kBars + 512;
+  static_assert(kBytes <= 232448, "shared memory of one SM");
+};
 constexpr size_t kPartBytes = (size_t)kTileM * kTileN * 4;
 constexpr int kMostSharers = kPairs;
 
@@ -75,7 +79,7 @@ struct Schedule {
 };
 template <typename Epi>
 struct Params {
-  CUtensorMap a, b;
+  CUtensorMap a, b, out;
   Schedule sch;
   int32_t m, n;
   float* parts;
@@ -170,14 +174,32 @@ __device__ __forceinline__ void arrive_cta0(uint64_t* bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(peer_addr(bar, 0)) : "memory");
 }
 
+__device__ __forceinline__ void few_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 56;"); }
+__device__ __forceinline__ void many_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 224;"); }
+
 // Where an epilogue warp stands: lane l holds row `row + l` of D, columns
 // `col` .. `col` + 127 (of them < n inside).
 struct Place {
   int tm, tn;
   int row, col;
   int lane, half;       // half: which 128 columns of the tile
-  float* stage;         // the warp's transpose tile
+  uint8_t* box;         // the warp's boxes
 };
+
+// Where 16 bytes of a box lie (chunk 0 .. 7 of a row's 128 bytes).
+__device__ __forceinline__ uint4* box_at(uint8_t* box, int row, int chunk) {
+  return reinterpret_cast<uint4*>(box + row * 128 + ((chunk ^ (row & 7)) << 4));
+}
+// The TMA has read the warp's boxes: they may be written again.
+__device__ __forceinline__ void box_free(int lane) {
+  if (lane == 0) bulk_wait_read();
+  __syncwarp();
+}
+// What the warp wrote into its boxes is there for the TMA (then lane 0 stores and commits).
+__device__ __forceinline__ void box_ready() {
+  fence_proxy_async_smem();
+  __syncwarp();
+}
 
 // Four elements of a row, `left` of them inside.
 struct Store {
@@ -185,6 +207,7 @@ struct Store {
   int32_t dt;
   int32_t accumulate;   // adds to d
   int32_t vec;          // d takes four elements at a time
+  int32_t tma;          // whole tiles go to d by the TMA (a map of it, nothing added)
   const float* add;     // NULL, or fp32 values added (may be d itself)
   int64_t ld_add;
   __device__ __forceinline__ void put(int64_t row, int col, float4 v, int left) const {
@@ -240,34 +263,71 @@ inline Store make_store(const Mat& d, int dt, int64_t rows, bool accumulate) {
   return s;
 }
 
-// 32 rows (one a lane) x 32 columns from column c: through the warp's transpose
-// tile, 16 columns at a time, then eight rows a step, four columns a lane.
+// 32 rows (one a lane) x 32 columns from column c: through a box, then four
+// rows a step, four columns a lane.
 template <typename Put>
 __device__ __forceinline__ void put_block(const float (&v)[32], const Place& at, int rows, int c, const Put& put) {
-  const int q = 4 * (at.lane & 3), r8 = at.lane >> 2;
+  const int q = at.lane & 7, r4 = at.lane >> 3;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
+  for (int e = 0; e < 8; ++e)
+    *box_at(at.box, at.lane, e) = make_uint4(__float_as_uint(v[4 * e]), __float_as_uint(v[4 * e + 1]), __float_as_uint(v[4 * e + 2]), __float_as_uint(v[4 * e + 3]));
+  __syncwarp();
 #pragma unroll
-    for (int e = 0; e < 16; e += 4)
-      *reinterpret_cast<float4*>(at.stage + at.lane * 20 + e) = make_float4(v[16 * h + e], v[16 * h + e + 1], v[16 * h + e + 2], v[16 * h + e + 3]);
-    __syncwarp();
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int r = r8 + 8 * k;
-      if (r < rows) put(r, c + 16 * h + q, *reinterpret_cast<const float4*>(at.stage + r * 20 + q));
-    }
-    __syncwarp();
+  for (int k = 0; k < 8; ++k) {
+    const int r = r4 + 4 * k;
+    if (r < rows) put(r, c + 4 * q, *reinterpret_cast<const float4*>(box_at(at.box, r, q)));
   }
+  __syncwarp();
 }
 
 // Epilogue that stores D.
 struct StoreEpi {
+  static constexpr int kStages = 6, kBoxes = 1;
   Store out;
   template <typename P>
   struct Warp {
     __device__ __forceinline__ Warp(const P&, const Place&) {}
     __device__ __forceinline__ void tile(const P& p, const Item& it, const Place& at, float (&acc)[4][32]) {
       const int rows = min(32, p.m - at.row);
+      if (it.slot < 0 && p.epi.out.tma) {
+        if (rows <= 0) return;
+        if (p.epi.out.dt == LM_F32) {
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            const int c = at.col + 32 * b;
+            if (c >= p.n) continue;
+            box_free(at.lane);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              *box_at(at.box, at.lane, e) = make_uint4(__float_as_uint(acc[b][4 * e]), __float_as_uint(acc[b][4 * e + 1]), __float_as_uint(acc[b][4 * e + 2]),
+                                                       __float_as_uint(acc[b][4 * e + 3]));
+            box_ready();
+            if (at.lane == 0) {
+              tma_store_3d(&p.out, at.box, c, at.row, 0);
+              bulk_commit();
+            }
+          }
+        } else {
+#pragma unroll
+          for (int b = 0; b < 4; b += 2) {
+            const int c = at.col + 32 * b;
+            if (c >= p.n) continue;
+            box_free(at.lane);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float* v = &acc[b + e / 4][8 * (e % 4)];
+              *box_at(at.box, at.lane, e) = make_uint4(pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3]), pack_bf2(v[4], v[5]), pack_bf2(v[6], v[7]));
+            }
+            box_ready();
+            if (at.lane == 0) {
+              tma_store_3d(&p.out, at.box, c, at.row, 0);
+              bulk_commit();
+            }
+          }
+        }
+        return;
+      }
+      box_free(at.lane);
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         const int c = at.col + 32 * b;
@@ -288,11 +348,35 @@ struct StoreEpi {
   };
 };
 
-template <bool kAMn, bool kBMn, typename Epi>
+// How an operand lies: K-major, MN-major, or MN-major's or K-major's elements in
+// column blocks of 64 (block, row, 64: each TMA box is one piece of memory).
+enum Lie { kRowsK = 0, kRowsMn = 1, kBlocksK = 2, kBlocksMn = 3 };
+__host__ __device__ constexpr bool is_mn(int lie) { return (lie & 1) != 0; }
+__host__ __device__ constexpr bool is_blocks(int lie) { return lie >= 2; }
+
+// One K block (kb) of an operand's half tile from row or column `mn` on.
+template <int kLie>
+__device__ __forceinline__ void load_operand(uint8_t* dst, const CUtensorMap* map, uint32_t bar, int mn, int kb) {
+  constexpr int kBytes = kHalf * kBlockK * 2;
+  if (kLie == kRowsK) tma_load_3d(dst, map, bar, kb * kBlockK, mn, 0);
+  if (kLie == kBlocksK) tma_load_3d(dst, map, bar, 0, mn, kb);
+  if (kLie == kRowsMn) {
+    tma_load_3d(dst, map, bar, mn, kb * kBlockK, 0);
+    tma_load_3d(dst + kBytes / 2, map, bar, mn + 64, kb * kBlockK, 0);
+  }
+  if (kLie == kBlocksMn) {
+    tma_load_3d(dst, map, bar, 0, kb * kBlockK, mn / 64);
+    tma_load_3d(dst + kBytes / 2, map, bar, 0, kb * kBlockK, mn / 64 + 1);
+  }
+}
+
+template <int kALie, int kBLie, typename Epi>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_kernel(const __grid_constant__ Params<Epi> p) {
+  constexpr int kStages = Epi::kStages;
+  constexpr bool kAMn = is_mn(kALie), kBMn = is_mn(kBLie);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + kBarOffset);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + Smem<Epi>::kBars);
   uint64_t* empty = full + kStages;
   uint64_t* accfull = empty + kStages;
   uint64_t* accempty = accfull + 2;
@@ -334,8 +418,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_ke
   const uint32_t tmem_base = *tmem_slot;
   const uint64_t wait_ns = p.wait_ns;
 
+  // 384 threads x 168 registers at launch = 128 x 56 + 256 x 224: the epilogue
+  // holds 128 sums and what it makes of them
   if (warp == 0) {
     // -------------------------------- producer ---------------------------------
+    few_registers();
     if (lane == 0) {
       int stage = 0;
       uint32_t ph = 0;
@@ -358,18 +445,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_ke
           }
           log->bytes[stage] = kStageBytes;
           log->n += 1u;
-          if (kAMn) {
-            tma_load_3d(sa, &p.a, fb, row, kb * kBlockK, 0);
-            tma_load_3d(sa + kABytes / 2, &p.a, fb, row + 64, kb * kBlockK, 0);
-          } else {
-            tma_load_3d(sa, &p.a, fb, kb * kBlockK, row, 0);
-          }
-          if (kBMn) {
-            tma_load_3d(sb, &p.b, fb, col, kb * kBlockK, 0);
-            tma_load_3d(sb + kBBytes / 2, &p.b, fb, col + 64, kb * kBlockK, 0);
-          } else {
-            tma_load_3d(sb, &p.b, fb, kb * kBlockK, col, 0);
-          }
+          load_operand<kALie>(sa, &p.a, fb, row, kb);
+          load_operand<kBLie>(sb, &p.b, fb, col, kb);
           if (++stage == kStages) {
             stage = 0;
             ph ^= 1u;
@@ -380,6 +457,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_ke
     }
   } else if (warp == 1) {
     // -------------------------------- MMA issuer -------------------------------
+    few_registers();
     if (lane == 0 && rank == 0) {
       const uint32_t idesc = make_idesc(kTileM, kTileN, kAMn, kBMn);
       // 16 of the sum: 16 rows of 128 bytes (MN-major), 32 bytes of a row (K-major)
@@ -429,10 +507,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_ke
     }
   } else if (warp >= kFirstEpi) {
     // --------------------------------- epilogue ----------------------------------
+    many_registers();
     Place at;
     at.lane = lane;
     at.half = (warp - kFirstEpi) >> 2;
-    at.stage = reinterpret_cast<float*>(smem + kTransOffset + (size_t)(warp - kFirstEpi) * kTransBytes);
+    at.box = smem + Smem<Epi>::kBoxes + (size_t)(warp - kFirstEpi) * Epi::kBoxes * kBoxBytes;
     const int q = warp & 3, r0 = (int)rank * kHalf + q * 32;      // the warp's first row of the tile
     const uint32_t lanes = (uint32_t)(q * 32) << 16;
     const float nan = __int_as_float(0x7FC00000);
@@ -482,6 +561,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_ke
         for (int e = 0; e < 32; ++e) acc[b][e] = ok ? acc[b][e] : nan;
       epi.tile(p, it, at, acc);
     }
+    if (lane == 0) bulk_wait_all();   // stores from the boxes
+  } else {
+    few_registers();
   }
 
   __syncwarp();
@@ -548,18 +630,24 @@ inline PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   return fn;
 }
 
-// A map of a bf16 matrix (cols, rows, 1) whose boxes are 64 columns x 128 rows
-// (K-major operands) or x 64 rows (MN-major), 128-byte swizzle.
-inline cudaError_t encode_operand(CUtensorMap* m, const void* base, int64_t cols, int64_t rows, int64_t ld, bool mn_major) {
+// A map of (cols, rows, planes) elements whose boxes are 128 bytes x box_rows, 128-byte swizzle.
+inline cudaError_t encode_boxes(CUtensorMap* m, int dt, const void* base, int64_t cols, int64_t rows, int64_t planes, int64_t ld, int64_t plane, int box_rows) {
   const PFN_cuTensorMapEncodeTiled_v12000 enc = encode_fn();
   if (enc == nullptr) return cudaErrorNotSupported;
-  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, 1};
-  const cuuint64_t pitch = (cuuint64_t)ld * 2, strides[2] = {pitch, pitch * (cuuint64_t)rows};
-  const cuuint32_t box[3] = {64, mn_major ? 64u : 128u, 1}, estr[3] = {1, 1, 1};
-  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+  const cuuint64_t size = dt == LM_F32 ? 4 : 2;
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes}, strides[2] = {(cuuint64_t)ld * size, (cuuint64_t)plane * size};
+  const cuuint32_t box[3] = {dt == LM_F32 ? 32u : 64u, (cuuint32_t)box_rows, 1}, estr[3] = {1, 1, 1};
+  return enc(m, dt == LM_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
              ? cudaSuccess
              : cudaErrorInvalidValue;
+}
+// The rows of a bf16 matrix as an operand, and its 64-column blocks (block, row, 64).
+inline cudaError_t encode_operand(CUtensorMap* m, const void* base, int64_t cols, int64_t rows, int64_t ld, bool mn_major) {
+  return encode_boxes(m, LM_BF16, base, cols, rows, 1, ld, ld * rows, mn_major ? 64 : 128);
+}
+inline cudaError_t encode_blocks(CUtensorMap* m, const void* base, int64_t cols, int64_t rows, int box_rows) {
+  return encode_boxes(m, LM_BF16, base, 64, rows, (cols + 63) / 64, 64, 64 * rows, box_rows);
 }
 
 // Whether the TMA takes the rows of a bf16 matrix as they lie.
@@ -614,24 +702,32 @@ cudaError_t launch_after(Kernel kernel, dim3 grid, int threads, size_t smem, cud
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-template <bool kAMn, bool kBMn, typename Epi>
+template <int kALie, int kBLie, typename Epi>
 cudaError_t start(const Params<Epi>& p, cudaStream_t st) {
   const int dev = device_slot();
   static bool ready[kMaxDevices];
   if (dev < 0 || !ready[dev]) {
-    const cudaError_t e = cudaFuncSetAttribute(gemm_kernel<kAMn, kBMn, Epi>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
+    const cudaError_t e = cudaFuncSetAttribute(gemm_kernel<kALie, kBLie, Epi>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem<Epi>::kBytes);
     if (e != cudaSuccess) return e;
     if (dev >= 0) ready[dev] = true;
   }
-  return launch_after(gemm_kernel<kAMn, kBMn, Epi>, dim3(2 * pairs_of(p.sch)), kThreads, kSmemBytes, st, p);
+  return launch_after(gemm_kernel<kALie, kBLie, Epi>, dim3(2 * pairs_of(p.sch)), kThreads, Smem<Epi>::kBytes, st, p);
 }
 inline cudaError_t start_zero(const Mat& d, int dt, int64_t rows, int cols, cudaStream_t st) {
   return launch_after(zero_kernel, dim3((unsigned)std::min<int64_t>(rows, 152 * 8)), 256, 0, st, d, dt, rows, cols);
 }
 // A product whose sums may be split: the kernel, and the join where parts are left.
-template <bool kAMn, bool kBMn>
-cudaError_t start_store(const Params<StoreEpi>& p, cudaStream_t st) {
-  const cudaError_t e = start<kAMn, kBMn, StoreEpi>(p, st);
+template <int kALie, int kBLie>
+cudaError_t start_store(Params<StoreEpi>& p, cudaStream_t st) {
+  const Store& o = p.epi.out;
+  const int64_t size = o.dt == LM_F32 ? 4 : 2;
+  cudaError_t e = cudaSuccess;
+  const int64_t ld = p.m > 1 ? o.d.ld : (int64_t)p.n;
+  if (o.add == nullptr && !o.accumulate && reinterpret_cast<uintptr_t>(o.d.data) % 16 == 0 && ld * size % 16 == 0 && ld < ((int64_t)1 << 37) / p.m) {
+    e = encode_boxes(&p.out, o.dt, o.d.data, p.n, p.m, 1, ld, ld * p.m, 32);
+    p.epi.out.tma = 1;
+  }
+  if (e == cudaSuccess) e = start<kALie, kBLie, StoreEpi>(p, st);
   if (e != cudaSuccess || !has_parts(p.sch)) return e;
   return launch_after(join_kernel, dim3(p.sch.rest, kTileM / 4), 256, 0, st, p);
 }

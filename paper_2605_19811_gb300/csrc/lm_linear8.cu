@@ -171,7 +171,7 @@ cudaError_t launch_linear8(const Linear8Params& q, cudaStream_t st) {
   s.epi.out = make_store(y, q.ydt, q.tokens, false);
   if ((e = encode_operand(&s.a, x, l.k, q.tokens, l.ldx, false)) != cudaSuccess) return e;
   if ((e = encode_operand(&s.b, w, q.in, q.out, l.ldw, q.grad)) != cudaSuccess) return e;
-  return q.grad ? start_store<false, true>(s, st) : start_store<false, false>(s, st);
+  return q.grad ? start_store<kRowsK, kRowsMn>(s, st) : start_store<kRowsK, kRowsK>(s, st);
 }
 
 }  // namespace lm

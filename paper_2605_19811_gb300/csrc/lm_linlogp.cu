@@ -7,12 +7,19 @@
 // target's z where the tile holds it.  A second kernel joins a row's parts:
 //   lse = M + log S,  logp = (z_y - M) - log S,  H = log S - T / S.
 //
-// Gradients, for a piece of the vocabulary at a time: the piece's logits are
-// computed once more, and the epilogue writes
+// Gradients, for a piece of the tokens at a time.  In the forward call the
+// product's epilogue also leaves every logit in the workspace in 16 bits, as
+// its distance below the row's running maximum r in steps of 2^-10,
+//   q = rint((r - z) 2^10),  65535 and more (64 below): p = 0
+// (p is then off by 2^-11 of itself at most, a quarter of the bf16 rounding that
+// follows).  Once lse is known, a kernel makes of q, in its place,
 //   d = p (a - g_H (log p + H)) (+ g_logp at the target),  a = g_lse - g_logp
-// as bf16 (its one rounding below 32 bits: the tensor cores take it so) into the
-// workspace; two products of it follow, dh += d W and dW = d^T h.  Where there
-// are several pieces dh is summed in fp32 in the workspace.
+// as bf16 (the rounding that the tensor cores ask for), and two products of it
+// follow, dh = d W and dW = d^T h.  Where lse comes from an earlier call the
+// logits' product writes d itself.  Over several pieces dW is summed in fp32.
+//
+// q and d lie in blocks of 64 columns, so that a box of either product is one
+// piece of memory.
 #include <cuda_bf16.h>
 #include <math.h>
 
@@ -27,7 +34,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kGone = -1e4f;      // e^kGone is 0
 constexpr int kForwardUnits = 16 * kPairs, kLeastStrips = 8;   // of the forward product (forward_strip)
 constexpr int64_t kPieceBytes = (int64_t)512 << 20;   // of the gradient's bf16 values in the workspace
-constexpr int64_t kLeastPiece = 2048;                 // columns
+constexpr int64_t kLeastPiece = 1024;                 // tokens
+constexpr float kSteps = 1024.f;                      // of q
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -37,6 +45,20 @@ __device__ __forceinline__ float ex2(float x) {
 // the reference of a maximum: -inf (nothing there) counts from 0
 __device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.f : m; }
 
+// 2^23 + q holds q in its low bits
+constexpr float kWhole = 8388608.f;
+__device__ __forceinline__ uint32_t two_q(float a, float b) { return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x5410); }
+
+// The warp's two boxes (64 columns each) to their blocks.
+template <typename P>
+__device__ __forceinline__ void store_boxes(const P& p, const Place& at) {
+  box_ready();
+  if (at.lane != 0 || at.row >= p.m) return;
+  if (at.col < p.n) tma_store_3d(&p.out, at.box, 0, at.row, at.col / 64);
+  if (at.col + 64 < p.n) tma_store_3d(&p.out, at.box + kBoxBytes, 0, at.row, at.col / 64 + 1);
+  bulk_commit();
+}
+
 // What a row's gradient takes: lse, a = g_lse - g_logp, g_H, H.
 struct RowTerms {
   float4* terms;
@@ -44,7 +66,11 @@ struct RowTerms {
   int32_t* target;    // -1 in a row without one
 };
 
+// kKeep: the logits are kept in 16 bits for the gradient.
+template <bool kKeep>
 struct ForwardEpi {
+  static constexpr int kStages = kKeep ? 5 : 6, kBoxes = kKeep ? 2 : 0;
+  float* from;          // kKeep: r of each half tile's rows, (2 tiles_n) x rows
   const int64_t* targets;
   float *m, *s, *t;     // (2 strips) x rows
   float* z_target;
@@ -83,18 +109,30 @@ struct ForwardEpi {
         t = k * (t + d * s);
         s = k * s;
       }
+      if (kKeep) {
+        if (in) p.epi.from[(int64_t)(2 * at.tn + at.half) * p.epi.rows + row] = from;
+        box_free(at.lane);
+      }
       float s4[4], t4[4];
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         s4[b] = t4[b] = 0.f;
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          const float d = acc[b][e] - from;
-          const float x = ex2(d * kLog2e);      // NaN for a NaN, and for infinity
-          s4[b] += x;
-          t4[b] += x * fmaxf(d, kGone);
+        for (int o = 0; o < 32; o += 8) {
+          float q[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float d = acc[b][o + e] - from;
+            const float x = ex2(d * kLog2e);      // NaN for a NaN, and for infinity
+            s4[b] += x;
+            t4[b] += x * fmaxf(d, kGone);
+            if (kKeep) q[e] = fminf(fmaf(d, -kSteps, kWhole), kWhole + 65535.f);
+          }
+          if (kKeep)
+            *box_at(at.box + (b >> 1) * kBoxBytes, at.lane, (b & 1) * 4 + o / 8) = make_uint4(two_q(q[0], q[1]), two_q(q[2], q[3]), two_q(q[4], q[5]), two_q(q[6], q[7]));
         }
       }
+      if (kKeep) store_boxes(p, at);
       s += (s4[0] + s4[1]) + (s4[2] + s4[3]);
       t += (t4[0] + t4[1]) + (t4[2] + t4[3]);
       m = most;
@@ -112,35 +150,38 @@ struct ForwardEpi {
   };
 };
 
+__device__ __forceinline__ float gradient(float lp, const float4& w) {
+  return ex2(lp * kLog2e) * (w.y - w.z * (fmaxf(lp, kGone) + w.w));
+}
+
 struct GradEpi {
+  static constexpr int kStages = 5, kBoxes = 2;
   RowTerms rows;
-  int32_t first;        // the piece's first token of the vocabulary
-  Store out;
   template <typename P>
   struct Warp {
     __device__ __forceinline__ Warp(const P&, const Place&) {}
     __device__ __forceinline__ void tile(const P& p, const Item&, const Place& at, float (&acc)[4][32]) {
-      const int row = at.row + at.lane, rows = min(32, p.m - at.row);
-      if (rows <= 0) return;
+      const int row = at.row + at.lane;
       const bool in = row < p.m;
       const float4 w = in ? p.epi.rows.terms[row] : make_float4(0.f, 0.f, 0.f, 0.f);
-      const float gl = in ? p.epi.rows.g_logp[row] : 0.f;
-      const int y = in ? p.epi.rows.target[row] : -1;
-      const int yc = y >= 0 ? y - p.epi.first - at.col : -1;
+      const int y = in ? p.epi.rows.target[row] - at.col : -1;
+      box_free(at.lane);
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
-        const int c = at.col + 32 * b;
-        if (c >= p.n) continue;
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          const float lp = acc[b][e] - w.x;
-          const float d = ex2(lp * kLog2e) * (w.y - w.z * (fmaxf(lp, kGone) + w.w));
-          acc[b][e] = yc == 32 * b + e ? d + gl : d;
+        for (int e = 0; e < 32; ++e) acc[b][e] = gradient(acc[b][e] - w.x, w);
+        if ((unsigned)(y - 32 * b) < 32u) {
+          const float gl = p.epi.rows.g_logp[row];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) acc[b][e] += y == 32 * b + e ? gl : 0.f;
         }
-        put_block(acc[b], at, rows, c, [&](int r, int col, float4 v) {
-          if (col < p.n) p.epi.out.put(at.row + r, col, v, p.n - col);
-        });
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float* v = &acc[b][8 * e];
+          *box_at(at.box + (b >> 1) * kBoxBytes, at.lane, (b & 1) * 4 + e) = make_uint4(pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3]), pack_bf2(v[4], v[5]), pack_bf2(v[6], v[7]));
+        }
       }
+      store_boxes(p, at);
     }
   };
 };
@@ -229,6 +270,44 @@ __global__ void __launch_bounds__(256) linlogp_terms_kernel(const JoinParams p) 
             p.targets != nullptr ? p.targets[row] : -1, p.vocab, p.g_logp, p.g_entropy, p.g_lse);
 }
 
+// d in the place of q: eight lanes to a row of a block (64 columns), a block of
+// threads 32 rows of kDzBlocks column blocks one after another.
+constexpr int kDzBlocks = 16;
+__global__ void __launch_bounds__(256) linlogp_dz_kernel(uint4* q, const float* from, RowTerms t, int64_t rows, int blocks) {
+  griddep_wait();
+  griddep_launch_dependents();
+  const int64_t row = (int64_t)blockIdx.x * 32 + (threadIdx.x >> 3);
+  if (row >= rows) return;
+  const int part = threadIdx.x & 7;
+  const float4 w = t.terms[row];
+  const int y = t.target[row];
+  const int b1 = min((int)(blockIdx.y + 1) * kDzBlocks, blocks);
+#pragma unroll 4
+  for (int b = blockIdx.y * kDzBlocks; b < b1; ++b) {
+    uint4* at = q + ((int64_t)b * rows + row) * 8 + part;
+    const uint4 v = __ldcs(at);
+    const float ref = from[(int64_t)(b >> 1) * rows + row] - w.x;
+    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+    uint32_t o[4];
+    const int c = y - 64 * b - 8 * part;
+    float gl = 0.f;
+    if ((unsigned)c < 8u) gl = t.g_logp[row];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float d[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t x = h ? u[k] >> 16 : u[k] & 0xFFFFu;
+        const float whole = __uint_as_float(x | 0x4B000000u) - kWhole;
+        d[h] = gradient(x == 0xFFFFu ? -INFINITY : fmaf(whole, -1.f / kSteps, ref), w);
+        if (c == 2 * k + h) d[h] += gl;
+      }
+      o[k] = pack_bf2(d[0], d[1]);
+    }
+    *at = make_uint4(o[0], o[1], o[2], o[3]);
+  }
+}
+
 // A matrix laid out anew with rows that the TMA takes.
 __global__ void __launch_bounds__(256) linlogp_copy_kernel(Mat from, int64_t rows, int cols, __nv_bfloat16* to, int64_t ld) {
   griddep_wait();
@@ -251,12 +330,15 @@ int forward_strip(int64_t rows, int64_t vocab) {
 struct Layout {
   bool copy_h, copy_w;
   int64_t ld;                        // of the copies
+  int64_t piece;                     // tokens of a piece
   int32_t pieces;
-  int64_t piece;                     // columns of a piece
-  Schedule forward;
+  int32_t blocks;                    // column blocks of q and d
+  int32_t strip;                     // of the forward product
+  int32_t parts;                     // of a row's statistics
   // offsets in the workspace
-  size_t h, w, z, terms, gl, target, stats, d, dh, parts, total;
+  size_t h, w, z, terms, gl, target, stats, from, d, dw, partial, total;
 };
+bool dw_is_sum(const LinLogpParams& q) { return q.dwdt == LM_F32; }   // several pieces are summed in dW itself
 Layout make_layout(const LinLogpParams& q) {
   Layout l{};
   size_t at = 0;
@@ -265,37 +347,40 @@ Layout make_layout(const LinLogpParams& q) {
     at += (bytes + 255) / 256 * 256;
     return o;
   };
-  const size_t n = (size_t)q.rows;
   const bool grad = q.dh.data != nullptr || q.dw.data != nullptr;
   l.ld = ((int64_t)q.width + 7) / 8 * 8;
   l.copy_h = !tma_rows(q.h, q.rows, q.width);
   l.copy_w = !tma_rows(q.w, q.vocab, q.width);
-  l.h = take(l.copy_h ? n * l.ld * 2 : 0);
+  l.h = take(l.copy_h ? (size_t)q.rows * l.ld * 2 : 0);
   l.w = take(l.copy_w ? (size_t)q.vocab * l.ld * 2 : 0);
-  l.forward = plain_schedule(q.rows, q.vocab, q.width, forward_strip(q.rows, q.vocab));
-  l.z = take(n * 4);
-  l.terms = take(grad ? n * 16 : 0);
-  l.gl = take(grad ? n * 4 : 0);
-  l.target = take(grad ? n * 4 : 0);
-  // the forward pass's parts and the gradient's values are not wanted at once
-  const size_t stats = q.gradient_only ? 0 : (size_t)l.forward.strips * 2 * n * 4 * 3;
-  size_t d = 0;
+  l.blocks = (q.vocab + 63) / 64;
+  l.piece = q.rows;
   if (grad) {
-    const int64_t most = std::max<int64_t>(kLeastPiece, kPieceBytes / 2 / q.rows);
-    l.pieces = (int32_t)((q.vocab + most - 1) / most);
-    l.piece = ((q.vocab + l.pieces - 1) / l.pieces + kTileN - 1) / kTileN * kTileN;
-    l.pieces = (int32_t)((q.vocab + l.piece - 1) / l.piece);
-    d = n * (size_t)l.piece * 2;
+    const int64_t most = std::max<int64_t>(kLeastPiece, kPieceBytes / 128 / l.blocks);
+    const int64_t pieces = (q.rows + most - 1) / most;
+    l.piece = std::min<int64_t>(((q.rows + pieces - 1) / pieces + kTileM - 1) / kTileM * kTileM, q.rows);
   }
-  l.stats = l.d = take(std::max(stats, d));
-  if (q.dh.data != nullptr && l.pieces > 1) l.dh = take(n * (size_t)l.ld * 4);
-  size_t parts = 0;
-  for (int i = 0; grad && i < 2; ++i) {      // the last piece may be smaller
-    const int64_t cols = i == 0 ? l.piece : q.vocab - (l.pieces - 1) * l.piece;
-    if (q.dh.data != nullptr) parts = std::max(parts, parts_bytes(split_schedule(q.rows, q.width, cols)));
-    if (q.dw.data != nullptr) parts = std::max(parts, parts_bytes(split_schedule(cols, q.width, q.rows)));
+  l.pieces = (int32_t)((q.rows + l.piece - 1) / l.piece);
+  const size_t n = (size_t)l.piece;
+  l.strip = forward_strip(l.piece, q.vocab);
+  l.parts = 2 * plain_schedule(l.piece, q.vocab, q.width, l.strip).strips;
+  l.z = take(n * 4);
+  l.stats = take(q.gradient_only ? 0 : n * l.parts * 12);
+  if (grad) {
+    l.terms = take(n * 16);
+    l.gl = take(n * 4);
+    l.target = take(n * 4);
+    l.from = take(q.gradient_only ? 0 : n * (2 * (((size_t)q.vocab + kTileN - 1) / kTileN)) * 4);
+    l.d = take(n * l.blocks * 128);
+    if (q.dw.data != nullptr && l.pieces > 1 && !dw_is_sum(q)) l.dw = take((size_t)q.vocab * l.ld * 4);
+    size_t parts = 0;
+    for (int i = 0; i < 2; ++i) {      // the last piece may be smaller
+      const int64_t rows = i == 0 ? l.piece : q.rows - (l.pieces - 1) * l.piece;
+      if (q.dh.data != nullptr) parts = std::max(parts, parts_bytes(split_schedule(rows, q.width, q.vocab)));
+      if (q.dw.data != nullptr) parts = std::max(parts, parts_bytes(split_schedule(q.vocab, q.width, rows)));
+    }
+    l.partial = take(parts);
   }
-  l.parts = take(parts);
   l.total = at;
   return l;
 }
@@ -305,6 +390,109 @@ Layout make_layout(const LinLogpParams& q) {
     const cudaError_t e_ = (call);            \
     if (e_ != cudaSuccess) return e_;         \
   } while (0)
+
+template <typename T>
+T* from_row(T* p, int64_t first) {
+  return p != nullptr ? p + first : nullptr;
+}
+
+// Tokens first .. first + rows - 1; h begins at the first of them.
+cudaError_t piece(const LinLogpParams& q, const Layout& l, const Mat& h, const Mat& w, int64_t first, int64_t rows, bool last, bool grad, cudaStream_t st) {
+  const uint64_t wait_ns = env_wait_limit_ns();
+  uint8_t* ws = static_cast<uint8_t*>(q.workspace);
+  JoinParams j{};
+  j.rows = rows;
+  j.vocab = q.vocab;
+  j.targets = from_row(q.targets, first);
+  j.logp = from_row(q.logp, first);
+  j.entropy = from_row(q.entropy, first);
+  j.lse = from_row(q.lse, first);
+  j.g_logp = from_row(q.g_logp, first);
+  j.g_entropy = from_row(q.g_entropy, first);
+  j.g_lse = from_row(q.g_lse, first);
+  if (grad) j.out = RowTerms{reinterpret_cast<float4*>(ws + l.terms), reinterpret_cast<float*>(ws + l.gl), reinterpret_cast<int32_t*>(ws + l.target)};
+  // the operands of the logits' product, and the blocks that its epilogue fills
+  auto logits = [&](auto& p) {
+    p.m = (int32_t)rows;
+    p.n = q.vocab;
+    p.wait_ns = wait_ns;
+    cudaError_t e = encode_operand(&p.a, h.data, q.width, rows, h.ld, false);
+    if (e == cudaSuccess) e = encode_operand(&p.b, w.data, q.width, q.vocab, w.ld, false);
+    if (e == cudaSuccess && grad) e = encode_blocks(&p.out, ws + l.d, q.vocab, rows, 32);
+    return e;
+  };
+  if (q.gradient_only) {
+    LM_RUN(launch_after(linlogp_terms_kernel, dim3((unsigned)((rows + 255) / 256)), 256, 0, st, j));
+    Params<GradEpi> g{};
+    g.sch = plain_schedule(rows, q.vocab, q.width, 1);
+    g.epi.rows = j.out;
+    LM_RUN(logits(g));
+    LM_RUN((start<kRowsK, kRowsK, GradEpi>(g, st)));
+  } else {
+    auto forward = [&](auto& f) {
+      f.sch = plain_schedule(rows, q.vocab, q.width, l.strip);
+      const size_t each = (size_t)2 * f.sch.strips * rows;
+      f.epi.targets = j.targets;
+      f.epi.m = reinterpret_cast<float*>(ws + l.stats);
+      f.epi.s = f.epi.m + each;
+      f.epi.t = f.epi.s + each;
+      f.epi.z_target = reinterpret_cast<float*>(ws + l.z);
+      f.epi.from = reinterpret_cast<float*>(ws + l.from);
+      f.epi.rows = rows;
+      j.m = f.epi.m;
+      j.s = f.epi.s;
+      j.t = f.epi.t;
+      j.z_target = f.epi.z_target;
+      j.parts = 2 * f.sch.strips;
+      return logits(f);
+    };
+    if (grad) {
+      Params<ForwardEpi<true>> f{};
+      LM_RUN(forward(f));
+      LM_RUN((start<kRowsK, kRowsK, ForwardEpi<true>>(f, st)));
+    } else {
+      Params<ForwardEpi<false>> f{};
+      LM_RUN(forward(f));
+      LM_RUN((start<kRowsK, kRowsK, ForwardEpi<false>>(f, st)));
+    }
+    LM_RUN(launch_after(linlogp_join_kernel, dim3((unsigned)((rows + 31) / 32)), 32 * kJoinParts, 0, st, j));
+    if (grad)
+      LM_RUN(launch_after(linlogp_dz_kernel, dim3((unsigned)((rows + 31) / 32), (unsigned)((l.blocks + kDzBlocks - 1) / kDzBlocks)), 256, 0, st,
+                          reinterpret_cast<uint4*>(ws + l.d), (const float*)(ws + l.from), j.out, rows, (int)l.blocks));
+  }
+  if (q.dh.data != nullptr) {
+    Params<StoreEpi> s{};
+    s.sch = split_schedule(rows, q.width, q.vocab);
+    s.m = (int32_t)rows;
+    s.n = q.width;
+    s.wait_ns = wait_ns;
+    s.parts = reinterpret_cast<float*>(ws + l.partial);
+    s.epi.out = make_store(Mat{static_cast<__nv_bfloat16*>(q.dh.data) + first * q.dh.ld, q.dh.ld}, LM_BF16, rows, false);
+    LM_RUN(encode_blocks(&s.a, ws + l.d, q.vocab, rows, 128));
+    LM_RUN(encode_operand(&s.b, w.data, q.width, q.vocab, w.ld, true));
+    LM_RUN((start_store<kBlocksK, kRowsMn>(s, st)));
+  }
+  if (q.dw.data != nullptr) {
+    Params<StoreEpi> s{};
+    s.sch = split_schedule(q.vocab, q.width, rows);
+    s.m = q.vocab;
+    s.n = q.width;
+    s.wait_ns = wait_ns;
+    s.parts = reinterpret_cast<float*>(ws + l.partial);
+    const bool own_sum = !dw_is_sum(q) && l.pieces > 1;
+    const Mat sum{ws + l.dw, l.ld};
+    if (own_sum && !last) s.epi.out = make_store(sum, LM_F32, q.vocab, first > 0);
+    else s.epi.out = make_store(q.dw, q.dwdt, q.vocab, q.accumulate != 0 || (!own_sum && first > 0));
+    if (own_sum && last) {
+      s.epi.out.add = static_cast<const float*>(sum.data);
+      s.epi.out.ld_add = l.ld;
+    }
+    LM_RUN(encode_blocks(&s.a, ws + l.d, q.vocab, rows, 64));
+    LM_RUN(encode_operand(&s.b, h.data, q.width, rows, h.ld, true));
+    LM_RUN((start_store<kBlocksMn, kRowsMn>(s, st)));
+  }
+  return cudaSuccess;
+}
 
 cudaError_t copy_rows(const Mat& from, int64_t rows, int cols, void* to, int64_t ld, cudaStream_t st) {
   return launch_after(linlogp_copy_kernel, dim3((unsigned)std::min<int64_t>(rows, 152 * 8)), 256, 0, st, from, rows, cols,
@@ -328,89 +516,10 @@ cudaError_t launch_linlogp(const LinLogpParams& q, cudaStream_t st) {
     LM_RUN(copy_rows(q.w, q.vocab, q.width, ws + l.w, l.ld, st));
     w = Mat{ws + l.w, l.ld};
   }
-  const uint64_t wait_ns = env_wait_limit_ns();
   const bool grad = q.dh.data != nullptr || q.dw.data != nullptr;
-  JoinParams j{};
-  j.rows = q.rows;
-  j.vocab = q.vocab;
-  j.targets = q.targets;
-  j.logp = q.logp;
-  j.entropy = q.entropy;
-  j.lse = q.lse;
-  j.g_logp = q.g_logp;
-  j.g_entropy = q.g_entropy;
-  j.g_lse = q.g_lse;
-  if (grad) j.out = RowTerms{reinterpret_cast<float4*>(ws + l.terms), reinterpret_cast<float*>(ws + l.gl), reinterpret_cast<int32_t*>(ws + l.target)};
-  if (q.gradient_only) {
-    LM_RUN(launch_after(linlogp_terms_kernel, dim3((unsigned)((q.rows + 255) / 256)), 256, 0, st, j));
-  } else {
-    Params<ForwardEpi> f{};
-    f.sch = l.forward;
-    f.m = (int32_t)q.rows;
-    f.n = q.vocab;
-    f.wait_ns = wait_ns;
-    const size_t each = (size_t)l.forward.strips * 2 * q.rows;
-    f.epi.targets = q.targets;
-    f.epi.m = reinterpret_cast<float*>(ws + l.stats);
-    f.epi.s = f.epi.m + each;
-    f.epi.t = f.epi.s + each;
-    f.epi.z_target = reinterpret_cast<float*>(ws + l.z);
-    f.epi.rows = q.rows;
-    LM_RUN(encode_operand(&f.a, h.data, q.width, q.rows, h.ld, false));
-    LM_RUN(encode_operand(&f.b, w.data, q.width, q.vocab, w.ld, false));
-    LM_RUN((start<false, false, ForwardEpi>(f, st)));
-    j.m = f.epi.m;
-    j.s = f.epi.s;
-    j.t = f.epi.t;
-    j.z_target = f.epi.z_target;
-    j.parts = 2 * l.forward.strips;
-    LM_RUN(launch_after(linlogp_join_kernel, dim3((unsigned)((q.rows + 31) / 32)), 32 * kJoinParts, 0, st, j));
-  }
-  for (int32_t i = 0; grad && i < l.pieces; ++i) {
-    const int64_t first = i * l.piece, cols = std::min<int64_t>(l.piece, q.vocab - first);
-    const __nv_bfloat16* wp = static_cast<const __nv_bfloat16*>(w.data) + first * w.ld;
-    const Mat d{ws + l.d, l.piece};
-    Params<GradEpi> g{};
-    g.sch = plain_schedule(q.rows, cols, q.width, 1);
-    g.m = (int32_t)q.rows;
-    g.n = (int32_t)cols;
-    g.wait_ns = wait_ns;
-    g.epi.rows = j.out;
-    g.epi.first = (int32_t)first;
-    g.epi.out = make_store(d, LM_BF16, q.rows, false);
-    LM_RUN(encode_operand(&g.a, h.data, q.width, q.rows, h.ld, false));
-    LM_RUN(encode_operand(&g.b, wp, q.width, cols, w.ld, false));
-    LM_RUN((start<false, false, GradEpi>(g, st)));
-    if (q.dh.data != nullptr) {
-      Params<StoreEpi> s{};
-      s.sch = split_schedule(q.rows, q.width, cols);
-      s.m = (int32_t)q.rows;
-      s.n = q.width;
-      s.wait_ns = wait_ns;
-      s.parts = reinterpret_cast<float*>(ws + l.parts);
-      const Mat sum{ws + l.dh, l.ld};
-      s.epi.out = i + 1 < l.pieces ? make_store(sum, LM_F32, q.rows, false) : make_store(q.dh, LM_BF16, q.rows, false);
-      if (i > 0) {
-        s.epi.out.add = static_cast<const float*>(sum.data);
-        s.epi.out.ld_add = l.ld;
-      }
-      LM_RUN(encode_operand(&s.a, d.data, cols, q.rows, d.ld, false));
-      LM_RUN(encode_operand(&s.b, wp, q.width, cols, w.ld, true));
-      LM_RUN((start_store<false, true>(s, st)));
-    }
-    if (q.dw.data != nullptr) {
-      Params<StoreEpi> s{};
-      s.sch = split_schedule(cols, q.width, q.rows);
-      s.m = (int32_t)cols;
-      s.n = q.width;
-      s.wait_ns = wait_ns;
-      s.parts = reinterpret_cast<float*>(ws + l.parts);
-      const int64_t size = q.dwdt == LM_F32 ? 4 : 2;
-      s.epi.out = make_store(Mat{static_cast<uint8_t*>(q.dw.data) + first * q.dw.ld * size, q.dw.ld}, q.dwdt, cols, q.accumulate != 0);
-      LM_RUN(encode_operand(&s.a, d.data, cols, q.rows, d.ld, true));
-      LM_RUN(encode_operand(&s.b, h.data, q.width, q.rows, h.ld, true));
-      LM_RUN((start_store<true, true>(s, st)));
-    }
+  for (int32_t i = 0; i < l.pieces; ++i) {
+    const int64_t first = i * l.piece, rows = std::min<int64_t>(l.piece, q.rows - first);
+    LM_RUN(piece(q, l, Mat{static_cast<__nv_bfloat16*>(h.data) + first * h.ld, h.ld}, w, first, rows, i + 1 == l.pieces, grad, st));
   }
   return cudaSuccess;
 }

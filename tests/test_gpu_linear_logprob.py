@@ -13,7 +13,8 @@ from z_y - max, with E twice.  The entropy moves by sum p |log p + H| E <=
 2 ln V E, and its rounding errors are as those of lse, times the 1 + ln V that
 its terms add up to.
 dz = p (a - g_H (log p + H)) + g_logp: p is off by E + 2^-18 of itself (the
-exponential and lse), then rounded to bf16, 2^-8.  A product's sum of them adds
+exponential and lse); a call that computes lse and the gradients together keeps
+logits in steps of 2^-10, 2^-11 more; then dz is rounded to bf16, 2^-8.  A product's sum of them adds
 2^-18 of the magnitudes it adds up, and its result is rounded to its type, 2^-8
 (bf16) of itself."""
 
@@ -71,7 +72,7 @@ def reference(h, w, y, gl=None, gh=None, gz=None):
             a, b, k = (q[at:at + 8192, None].double() for q in (gl, gh, gz))
             a = torch.where(has, a, 0.0)
             d = p * ((k - a) - b * (lp + ent))
-            db = (e + 2.0 ** -18) * p * ((k - a).abs() + b.abs() * ((lp + ent).abs() + 1 + 2 * math.log(v)))
+            db = (e + 2.0 ** -18 + 2.0 ** -11) * p * ((k - a).abs() + b.abs() * ((lp + ent).abs() + 1 + 2 * math.log(v)))
             d.scatter_add_(1, t.clamp(min=0)[:, None], a)
             db += (U + 2.0 ** -18) * (d.abs() + db)
             r["dh"] = d @ w
@@ -111,13 +112,20 @@ def test_against_64_bits(T, rows, vocab, width, pad, offset):
     near(dh.t, ref, "dh")
     near(dw.t, ref, "dweight", U)
     assert dh.untouched() and dw.untouched() and h.untouched() and w.untouched()
-    # afterwards, from lse and entropy; twice the same bits
+    # twice the same bits; afterwards, from lse and entropy
+    o3 = T.linear_logprob(h.t, w.t, y, gl, gh, gz)
+    assert torch.equal(o3.dh, dh.t) and torch.equal(o3.dweight, dw.t)
+    o4 = T.linear_logprob_grad(h.t, w.t, y, o.lse, o.entropy, gl, gh, gz, dh=dh.t, dweight=dw.t)
+    assert o4[0] is dh.t and o4[1] is dw.t
+    near(dh.t, ref, "dh")
+    near(dw.t, ref, "dweight", U)
+    assert dh.untouched() and dw.untouched()
     dh2, dw2 = T.linear_logprob_grad(h.t, w.t, y, o.lse, o.entropy, gl, gh, gz)
     assert torch.equal(dh2, dh.t) and torch.equal(dw2, dw.t)
 
 
-def test_several_pieces_of_the_vocabulary(T):
-    rows, vocab, width = 131073, 5003, 40
+@pytest.mark.parametrize("rows,vocab,width", [(131073, 5003, 40), (2500, 270001, 24)])
+def test_several_pieces_of_the_tokens(T, rows, vocab, width):
     h, w, y, gl, gh, gz = inputs(rows, vocab, width, 5)
     ref = reference(h.t, w.t, y, gl, gh, gz)
     o = T.linear_logprob(h.t, w.t, y, gl, gh, gz)
@@ -125,6 +133,12 @@ def test_several_pieces_of_the_vocabulary(T):
         near(getattr(o, k), ref, k)
     near(o.dweight, ref, "dweight", U)
     assert torch.equal(T.linear_logprob(h.t, w.t, y, gl, gh, gz).dh, o.dh)
+    dw = torch.ones_like(w.t, dtype=torch.float32)
+    T.linear_logprob(h.t, w.t, y, gl, gh, gz, dh=False, dweight=dw, accumulate=True)
+    ref["dweight"] = ref["dweight"] + 1.0
+    near(dw, ref, "dweight", 2.0 ** -22)       # four pieces' additions and the first value's
+    again = T.linear_logprob_grad(h.t, w.t, y, o.lse, o.entropy, gl, gh, gz)
+    near(again[0], ref, "dh")
 
 
 @pytest.mark.parametrize("to", [torch.bfloat16, torch.float32])

@@ -84,9 +84,9 @@ def test_linear_logprob_refusals(L):
 
 
 def test_linear_logprob_workspace_is_bounded(L):
-    """dz takes at most 512 MB, or 2048 columns of it (the forward call's
-    statistics, 24 bytes a row for each of the vocabulary's strips, lie in the same
-    place); fp32 sums of dh, 28 bytes a row, and 40 MB beside it."""
+    """16-bit logits of a piece of the tokens take at most 512 MB, or 1024 rows
+    of them; 12 bytes of statistics for each half tile of a strip and 4 for each
+    half tile, 28 bytes a row, fp32 sums of dW and 40 MB beside them."""
     lib = L.load_library()
 
     def need(rows, width, vocab, grad):
@@ -99,8 +99,8 @@ def test_linear_logprob_workspace_is_bounded(L):
     assert 0 < need(1, 768, 50304, False) < 1 << 20
     assert need(16384, 768, 50304, False) < 1 << 28
     for rows, width, vocab in ((16384, 768, 50304), (4096, 4096, 50257), (1 << 20, 64, 160000), (7, 64, 1 << 20)):
-        most = max(1 << 29, rows * 2048 * 2) + rows * 256 * 2 + 4 * rows * width + 28 * rows + (41 << 20)
-        assert need(rows, width, vocab, True) <= most
+        most = max(1 << 29, 1024 * vocab * 2)
+        assert need(rows, width, vocab, True) <= most * (1 + (12 + 4) / 256 + 0.01) + 4 * vocab * width + (42 << 20)
 
 
 def test_weight8_refusals(L):
