@@ -22,7 +22,10 @@
 // With split sums, as many tiles as fill whole waves go one to a pair, and the
 // tiles left over are one line of (tile, block) work cut into equal ranges; a
 // tile that falls to several pairs is summed from their fp32 parts, in order,
-// by a second kernel.
+// by a second kernel.  Where D has few tile columns, as many pairs walk a tile
+// row together, one a column, and the line is of (tile row, block): they read
+// the same blocks of A at the same time, from L2 (each column for itself, A came
+// from memory once for each: 4096 x 768 over 50304, 284 us).
 //
 // Every wait is bounded (LM_WAIT_LIMIT_NS); a tile whose wait gave up, and what
 // its CTA had yet to do, reach the epilogue as NaN.
@@ -70,11 +73,12 @@ constexpr int kMostSharers = kPairs;
 struct Schedule {
   int32_t tiles_m, tiles_n;
   int32_t nkb;          // blocks of the sum
+  int32_t team;         // pairs that take a unit together, one a tile column; 1: each for itself
   int32_t strip;        // tiles of one row taken in turn by one pair
   int32_t strips;       // of a tile row
-  int32_t units;        // units dealt to the pairs in turn (tile row, strip)
-  int32_t rest;         // tiles left over, shared by range (strip 1)
-  int32_t sharers;      // pairs that share them; 0: none left over
+  int32_t units;        // units dealt to the teams in turn (tile row, strip)
+  int32_t rest;         // units left over, shared by range (strip 1)
+  int32_t sharers;      // teams that share them; 0: none left over
   int64_t begin[kMostSharers + 1];   // sharer k's first (tile, block) in the line of left-over work
 };
 template <typename Epi>
@@ -91,6 +95,11 @@ struct Params {
 // wave cover a compact block of D and share its operands in L2.
 __device__ __forceinline__ void unit_place(const Schedule& s, int unit, int& tm, int& strip) {
   constexpr int kGroup = 8;
+  if (s.team > 1) {     // a unit is a tile row
+    tm = unit;
+    strip = 0;
+    return;
+  }
   const int per = kGroup * s.strips, g = unit / per, r = unit - g * per;
   const int rows = min(kGroup, s.tiles_m - g * kGroup);
   strip = r / rows;
@@ -103,21 +112,26 @@ struct Item {
   int strip;            // the tile's strip, where the item ends it; else -1 (units dealt in turn)
 };
 struct Items {
-  int pair, unit, tn, tn_end, tm, strip;
-  int64_t at, end;      // left-over (tile, block) yet to do
+  int pair, column;     // column: this pair's of its team
+  int team, unit, tn, tn_end, tm, strip;
+  int64_t at, end;      // left-over (unit, block) yet to do
   bool first;
-  __device__ __forceinline__ Items(const Schedule& s, int p) : pair(p), unit(p), tn(0), tn_end(0), tm(0), strip(0), at(0), end(0), first(true) {
-    if (s.sharers > 0 && p < s.sharers) {
-      at = s.begin[p];
-      end = s.begin[p + 1];
+  __device__ __forceinline__ Items(const Schedule& s, int p) : pair(p), column(0), team(p), unit(p), tn(0), tn_end(0), tm(0), strip(0), at(0), end(0), first(true) {
+    if (s.team > 1) {
+      unit = team = p / s.team;
+      column = p - team * s.team;
+    }
+    if (s.sharers > 0 && team < s.sharers) {
+      at = s.begin[team];
+      end = s.begin[team + 1];
     }
   }
   __device__ __forceinline__ bool next(const Schedule& s, Item& it) {
     if (tn >= tn_end && unit < s.units) {
       unit_place(s, unit, tm, strip);
-      tn = strip * s.strip;
+      tn = strip * s.strip + column;
       tn_end = min(tn + s.strip, s.tiles_n);
-      unit += kPairs;
+      unit += kPairs / s.team;
     }
     if (tn < tn_end) {
       it = Item{tm, tn, 0, s.nkb, -1, tn + 1 == tn_end ? strip : -1};
@@ -128,6 +142,7 @@ struct Items {
     const int t = (int)(at / s.nkb), kb0 = (int)(at - (int64_t)t * s.nkb);
     const int kb1 = (int)min((int64_t)s.nkb, kb0 + (end - at));
     unit_place(s, s.units + t, it.tm, it.tn);
+    it.tn += column;
     it.kb0 = kb0;
     it.kb1 = kb1;
     it.slot = (kb0 == 0 && kb1 == s.nkb) ? -1 : 2 * pair + (first ? 0 : 1);
@@ -155,15 +170,50 @@ __device__ __forceinline__ bool await(uint64_t* bar, uint32_t parity, volatile i
   return true;
 }
 
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+// 32 columns of the warp's lanes; the values are there after tmem_wait, which
+// takes them as its own results so that no use of them moves before it.
+__device__ __forceinline__ void tmem_load(uint32_t taddr, float (&r)[32]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32"
-      " {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
-      "tcgen05.wait::ld.sync.aligned;"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32"
+      " {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15,"
+      " %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]),
+        "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]), "=f"(r[17]),
+        "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]), "=f"(r[24]), "=f"(r[25]), "=f"(r[26]),
+        "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
       : "r"(taddr)
       : "memory");
+}
+__device__ __forceinline__ void tmem_wait(float (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]), "+f"(r[8]),
+                 "+f"(r[9]), "+f"(r[10]), "+f"(r[11]), "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]), "+f"(r[16]), "+f"(r[17]),
+                 "+f"(r[18]), "+f"(r[19]), "+f"(r[20]), "+f"(r[21]), "+f"(r[22]), "+f"(r[23]), "+f"(r[24]), "+f"(r[25]), "+f"(r[26]),
+                 "+f"(r[27]), "+f"(r[28]), "+f"(r[29]), "+f"(r[30]), "+f"(r[31])
+               :
+               : "memory");
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
 }
 
 // Arrive on a barrier of CTA 0.  What the arrival announces is TMEM columns of the
@@ -528,10 +578,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_ke
       at.row = it.tm * kTileM + r0;
       at.col = it.tn * kTileN + at.half * 128;
       float acc[4][32];
-#pragma unroll
-      for (int b = 0; b < 4; ++b)
-#pragma unroll
-        for (int e = 0; e < 32; ++e) acc[b][e] = 0.f;
       for (int kc = it.kb0; kc < it.kb1; kc += kChunk) {
         // one answer for the warp: the TMEM loads below are taken by all lanes or none
         ok = ok && __all_sync(0xFFFFFFFFu, await(&accfull[ab], aph, abort_flag, wait_ns));
@@ -540,25 +586,42 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_ke
           break;
         }
         tc_fence_after();
+        const uint32_t from = tmem_base + (uint32_t)(ab * kTileN + at.half * 128) + lanes;
+        if (kc == it.kb0) {
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
+          for (int b = 0; b < 4; ++b) tmem_load(from + 32 * b, acc[b]);
 #pragma unroll
-          for (int o = 0; o < 32; o += 16) {
-            uint32_t r[16];
-            tmem_ld16(tmem_base + (uint32_t)(ab * kTileN + at.half * 128 + 32 * b + o) + lanes, r);
+          for (int b = 0; b < 4; ++b) tmem_wait(acc[b]);
+        } else {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) acc[b][o + e] += __uint_as_float(r[e]);
+          for (int b = 0; b < 4; b += 2) {
+            float r[2][32];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) tmem_load(from + 32 * (b + k), r[k]);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              tmem_wait(r[k]);
+#pragma unroll
+              for (int e = 0; e < 32; e += 2) {
+                const float2 v = add2(make_float2(acc[b + k][e], acc[b + k][e + 1]), make_float2(r[k][e], r[k][e + 1]));
+                acc[b + k][e] = v.x;
+                acc[b + k][e + 1] = v.y;
+              }
+            }
           }
+        }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) arrive_cta0(&accempty[ab]);
         ab ^= 1;
         if (ab == 0) aph ^= 1u;
       }
+      if (!ok) {
 #pragma unroll
-      for (int b = 0; b < 4; ++b)
+        for (int b = 0; b < 4; ++b)
 #pragma unroll
-        for (int e = 0; e < 32; ++e) acc[b][e] = ok ? acc[b][e] : nan;
+          for (int e = 0; e < 32; ++e) acc[b][e] = nan;
+      }
       epi.tile(p, it, at, acc);
     }
     if (lane == 0) bulk_wait_all();   // stores from the boxes
@@ -588,18 +651,20 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
   if (s.begin[k] <= u0 && s.begin[k + 1] >= u1) return;   // one pair stored it whole
   int tm, tn;
   unit_place(s, s.units + t, tm, tn);
+  const int column = blockIdx.z;
+  tn += column;
   int last = k;   // the last sharer of the tile
   while (last + 1 < s.sharers && s.begin[last + 1] < u1) ++last;
   const int rows = min(kTileM, p.m - tm * kTileM), cols = min(kTileN, p.n - tn * kTileN);
   // the first part may be its pair's second item; every later one is a first
-  const float* part0 = p.parts + (size_t)(2 * k + (s.begin[k] >= u0 ? 0 : 1)) * (kTileM * kTileN);
+  const float* part0 = p.parts + (size_t)(2 * (k * s.team + column) + (s.begin[k] >= u0 ? 0 : 1)) * (kTileM * kTileN);
   const int r = blockIdx.y * 4 + (threadIdx.x >> 6), c = 4 * (threadIdx.x & 63);
   if (r >= rows || c >= cols) return;
   const size_t at = (size_t)r * kTileN + c;
   float4 sum = *reinterpret_cast<const float4*>(part0 + at);
 #pragma unroll 4
   for (int j = k + 1; j <= last; ++j) {
-    const float4 v = *reinterpret_cast<const float4*>(p.parts + (size_t)(2 * j) * (kTileM * kTileN) + at);
+    const float4 v = *reinterpret_cast<const float4*>(p.parts + (size_t)(2 * (j * s.team + column)) * (kTileM * kTileN) + at);
     sum.x += v.x;
     sum.y += v.y;
     sum.z += v.z;
@@ -661,28 +726,35 @@ inline Schedule plain_schedule(int64_t m, int64_t n, int64_t k, int strip) {
   s.tiles_m = (int32_t)((m + kTileM - 1) / kTileM);
   s.tiles_n = (int32_t)((n + kTileN - 1) / kTileN);
   s.nkb = (int32_t)((k + kBlockK - 1) / kBlockK);
+  s.team = 1;
   s.strip = strip;
   s.strips = (s.tiles_n + strip - 1) / strip;
   s.units = s.tiles_m * s.strips;
   return s;
 }
-// Whole waves of tiles, the rest shared by ranges of the sum.
+// Whole waves of units, the rest shared by ranges of the sum.
+constexpr int kMostTeam = 8;      // where more columns would leave many pairs out, each is for itself
 inline Schedule split_schedule(int64_t m, int64_t n, int64_t k) {
   Schedule s = plain_schedule(m, n, k, 1);
-  const int32_t tiles = s.units;
-  s.units = tiles / kPairs * kPairs;
-  s.rest = tiles - s.units;
+  if (s.tiles_n <= kMostTeam && s.tiles_m > 1) {
+    s.team = s.tiles_n;
+    s.strips = 1;
+    s.units = s.tiles_m;
+  }
+  const int32_t all = s.units, teams = kPairs / s.team;
+  s.units = all / teams * teams;
+  s.rest = all - s.units;
   if (s.rest > 0) {
-    // a share of at least kChunk blocks, and never more sharers than pairs
+    // a share of at least kChunk blocks, and never more sharers than teams
     const int64_t most = (int64_t)s.rest * s.nkb / kChunk;
-    s.sharers = (int32_t)(most < s.rest ? s.rest : most < kPairs ? most : kPairs);
+    s.sharers = (int32_t)(most < s.rest ? s.rest : most < teams ? most : teams);
     for (int k2 = 0; k2 <= s.sharers; ++k2) s.begin[k2] = (int64_t)s.rest * s.nkb * k2 / s.sharers;
   }
   return s;
 }
 inline bool has_parts(const Schedule& s) { return s.rest > 0 && s.sharers > s.rest; }
-inline size_t parts_bytes(const Schedule& s) { return has_parts(s) ? 2 * (size_t)s.sharers * kPartBytes : 0; }
-inline int pairs_of(const Schedule& s) { return std::min(kPairs, std::max(s.units, s.sharers)); }
+inline size_t parts_bytes(const Schedule& s) { return has_parts(s) ? 2 * (size_t)s.sharers * s.team * kPartBytes : 0; }
+inline int pairs_of(const Schedule& s) { return std::min(kPairs / s.team, std::max(s.units, s.sharers)) * s.team; }
 
 // A launch whose set-up may overlap the end of the kernel before it (which it
 // waits for itself, griddepcontrol.wait).
@@ -729,7 +801,7 @@ cudaError_t start_store(Params<StoreEpi>& p, cudaStream_t st) {
   }
   if (e == cudaSuccess) e = start<kALie, kBLie, StoreEpi>(p, st);
   if (e != cudaSuccess || !has_parts(p.sch)) return e;
-  return launch_after(join_kernel, dim3(p.sch.rest, kTileM / 4), 256, 0, st, p);
+  return launch_after(join_kernel, dim3(p.sch.rest, kTileM / 4, p.sch.team), 256, 0, st, p);
 }
 
 }  // namespace

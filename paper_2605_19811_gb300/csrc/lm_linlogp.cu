@@ -32,6 +32,7 @@ using namespace gemm;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kGone = -1e4f;      // e^kGone is 0
+constexpr float kOutside = -INFINITY;
 constexpr int kForwardUnits = 16 * kPairs, kLeastStrips = 8;   // of the forward product (forward_strip)
 constexpr int64_t kPieceBytes = (int64_t)512 << 20;   // of the gradient's bf16 values in the workspace
 constexpr int64_t kLeastPiece = 1024;                 // tokens
@@ -78,31 +79,44 @@ struct ForwardEpi {
   template <typename P>
   struct Warp {
     float m, s, t;
-    __device__ __forceinline__ Warp(const P&, const Place&) : m(-INFINITY), s(0.f), t(0.f) {}
+    int tm, y;      // y: the row's target, -1 for none inside the vocabulary
+    __device__ __forceinline__ Warp(const P&, const Place&) : m(-INFINITY), s(0.f), t(0.f), tm(-1), y(-1) {}
     __device__ __forceinline__ void tile(const P& p, const Item& it, const Place& at, float (&acc)[4][32]) {
       const int row = at.row + at.lane;
       const bool in = row < p.m;
-      const int64_t y = in && p.epi.targets != nullptr ? p.epi.targets[row] : -1;
+      if (tm != at.tm) {
+        tm = at.tm;
+        const int64_t target = in && p.epi.targets != nullptr ? p.epi.targets[row] : -1;
+        y = target < p.n ? (int)target : -1;
+        if (target < 0) y = -1;
+      }
       const int left = p.n - at.col;      // columns of the vocabulary from this warp's first
 #pragma unroll
       for (int b = 0; b < 4; ++b)
-        if ((uint64_t)(y - at.col - 32 * b) < 32u && y < p.n) {
+        if ((unsigned)(y - at.col - 32 * b) < 32u && y >= 0) {
           float z = 0.f;
 #pragma unroll
-          for (int e = 0; e < 32; ++e) z = (int)(y - at.col) == 32 * b + e ? acc[b][e] : z;
+          for (int e = 0; e < 32; ++e) z = y - at.col == 32 * b + e ? acc[b][e] : z;
           p.epi.z_target[row] = z;
         }
       if (left < 128) {
 #pragma unroll
         for (int b = 0; b < 4; ++b)
 #pragma unroll
-          for (int e = 0; e < 32; ++e) acc[b][e] = 32 * b + e < left ? acc[b][e] : -INFINITY;
+          for (int e = 0; e < 32; ++e) acc[b][e] = 32 * b + e < left ? acc[b][e] : kOutside;
       }
       float most = m;
+      {
+        float mb[4];
 #pragma unroll
-      for (int b = 0; b < 4; ++b)
+        for (int b = 0; b < 4; ++b) {
+          mb[b] = acc[b][0];
 #pragma unroll
-        for (int e = 0; e < 32; ++e) most = fmaxf(most, acc[b][e]);
+          for (int e = 1; e < 31; e += 2) mb[b] = fmaxf(mb[b], fmaxf(acc[b][e], acc[b][e + 1]));
+          mb[b] = fmaxf(mb[b], acc[b][31]);
+        }
+        most = fmaxf(most, fmaxf(fmaxf(mb[0], mb[1]), fmaxf(mb[2], mb[3])));
+      }
       const float from = reference(most);
       {
         const float d = fmaxf(reference(m) - from, kGone), k = m == -INFINITY ? 0.f : ex2(d * kLog2e);
@@ -113,29 +127,48 @@ struct ForwardEpi {
         if (in) p.epi.from[(int64_t)(2 * at.tn + at.half) * p.epi.rows + row] = from;
         box_free(at.lane);
       }
-      float s4[4], t4[4];
+      float2 s2[2] = {{0.f, 0.f}, {0.f, 0.f}}, t2[2] = {{0.f, 0.f}, {0.f, 0.f}};
+      const float2 minus = make_float2(-from, -from), log2e = make_float2(kLog2e, kLog2e);
+      const float2 steps = make_float2(-kSteps, -kSteps), whole = make_float2(kWhole, kWhole);
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
-        s4[b] = t4[b] = 0.f;
 #pragma unroll
         for (int o = 0; o < 32; o += 8) {
-          float q[8];
+          uint32_t w[4];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float d = acc[b][o + e] - from;
-            const float x = ex2(d * kLog2e);      // NaN for a NaN, and for infinity
-            s4[b] += x;
-            t4[b] += x * fmaxf(d, kGone);
-            if (kKeep) q[e] = fminf(fmaf(d, -kSteps, kWhole), kWhole + 65535.f);
+          for (int e = 0; e < 8; e += 2) {
+            const float2 d = add2(make_float2(acc[b][o + e], acc[b][o + e + 1]), minus);
+            const float2 a = mul2(d, log2e);
+            const float2 x = make_float2(ex2(a.x), ex2(a.y));      // NaN for a NaN, and for infinity
+            const int k = e >> 1 & 1;
+            s2[k] = add2(s2[k], x);
+            t2[k] = fma2(x, d, t2[k]);                              // NaN for -inf too
+            if (kKeep) {
+              const float2 q = fma2(d, steps, whole);
+              w[e >> 1] = two_q(fminf(q.x, kWhole + 65535.f), fminf(q.y, kWhole + 65535.f));
+            }
           }
-          if (kKeep)
-            *box_at(at.box + (b >> 1) * kBoxBytes, at.lane, (b & 1) * 4 + o / 8) = make_uint4(two_q(q[0], q[1]), two_q(q[2], q[3]), two_q(q[4], q[5]), two_q(q[6], q[7]));
+          if (kKeep) *box_at(at.box + (b >> 1) * kBoxBytes, at.lane, (b & 1) * 4 + o / 8) = make_uint4(w[0], w[1], w[2], w[3]);
         }
       }
-      if (kKeep) store_boxes(p, at);
-      s += (s4[0] + s4[1]) + (s4[2] + s4[3]);
-      t += (t4[0] + t4[1]) + (t4[2] + t4[3]);
+      s2[0] = add2(s2[0], s2[1]);
+      t2[0] = add2(t2[0], t2[1]);
+      const float sn = s2[0].x + s2[0].y;
+      float tn = t2[0].x + t2[0].y;
+      if (tn != tn && sn == sn) {      // logits of -inf: nothing is added for them
+        tn = 0.f;
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            const float d = fmaxf(acc[b][e] - from, kGone);
+            tn += ex2(d * kLog2e) * d;
+          }
+      }
+      s += sn;
+      t += tn;
       m = most;
+      if (kKeep) store_boxes(p, at);
       if (it.strip >= 0) {
         if (in) {
           const int64_t o = (int64_t)(2 * it.strip + at.half) * p.epi.rows + row;
@@ -356,7 +389,7 @@ Layout make_layout(const LinLogpParams& q) {
   l.blocks = (q.vocab + 63) / 64;
   l.piece = q.rows;
   if (grad) {
-    const int64_t most = std::max<int64_t>(kLeastPiece, kPieceBytes / 128 / l.blocks);
+    const int64_t most = std::max<int64_t>(kLeastPiece, kPieceBytes / 128 / l.blocks / kTileM * kTileM);
     const int64_t pieces = (q.rows + most - 1) / most;
     l.piece = std::min<int64_t>(((q.rows + pieces - 1) / pieces + kTileM - 1) / kTileM * kTileM, q.rows);
   }
