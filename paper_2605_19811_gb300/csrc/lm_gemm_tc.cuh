@@ -224,8 +224,8 @@ __device__ __forceinline__ void arrive_cta0(uint64_t* bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(peer_addr(bar, 0)) : "memory");
 }
 
-__device__ __forceinline__ void few_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 56;"); }
-__device__ __forceinline__ void many_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 224;"); }
+__device__ __forceinline__ void few_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 96;"); }
+__device__ __forceinline__ void many_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 200;"); }
 
 // Where an epilogue warp stands: lane l holds row `row + l` of D, columns
 // `col` .. `col` + 127 (of them < n inside).
@@ -233,12 +233,32 @@ struct Place {
   int tm, tn;
   int row, col;
   int lane, half;       // half: which 128 columns of the tile
-  uint8_t* box;         // the warp's boxes
+  uint32_t box;         // the warp's boxes (shared address)
 };
 
 // Where 16 bytes of a box lie (chunk 0 .. 7 of a row's 128 bytes).
-__device__ __forceinline__ uint4* box_at(uint8_t* box, int row, int chunk) {
-  return reinterpret_cast<uint4*>(box + row * 128 + ((chunk ^ (row & 7)) << 4));
+__device__ __forceinline__ uint32_t box_at(uint32_t box, int row, int chunk) { return box + row * 128 + ((chunk ^ (row & 7)) << 4); }
+__device__ __forceinline__ void box_put(uint32_t box, int row, int chunk, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box_at(box, row, chunk)), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ void box_put(uint32_t box, int row, int chunk, const float* v) {
+  box_put(box, row, chunk, __float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+}
+__device__ __forceinline__ float4 box_get(uint32_t box, int row, int chunk) {
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(box_at(box, row, chunk)) : "memory");
+  return v;
+}
+__device__ __forceinline__ void box_store(const CUtensorMap* map, uint32_t box, int c0, int c1, int c2) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(box),
+               "r"(c0), "r"(c1), "r"(c2)
+               : "memory");
+}
+// fp32 values added to what is there (one addition an element).
+__device__ __forceinline__ void box_add(const CUtensorMap* map, uint32_t box, int c0, int c1, int c2) {
+  asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(box),
+               "r"(c0), "r"(c1), "r"(c2)
+               : "memory");
 }
 // The TMA has read the warp's boxes: they may be written again.
 __device__ __forceinline__ void box_free(int lane) {
@@ -257,16 +277,9 @@ struct Store {
   int32_t dt;
   int32_t accumulate;   // adds to d
   int32_t vec;          // d takes four elements at a time
-  int32_t tma;          // whole tiles go to d by the TMA (a map of it, nothing added)
-  const float* add;     // NULL, or fp32 values added (may be d itself)
-  int64_t ld_add;
+  int32_t tma;          // whole tiles go to d by the TMA (a map of it; fp32 may be added)
   __device__ __forceinline__ void put(int64_t row, int col, float4 v, int left) const {
     float e[4] = {v.x, v.y, v.z, v.w};
-    if (add != nullptr) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (k < left) e[k] += add[row * ld_add + col + k];
-    }
     const int64_t at = row * d.ld + col;
     if (dt == LM_F32) {
       float* o = static_cast<float*>(d.data) + at;
@@ -320,12 +333,12 @@ __device__ __forceinline__ void put_block(const float (&v)[32], const Place& at,
   const int q = at.lane & 7, r4 = at.lane >> 3;
 #pragma unroll
   for (int e = 0; e < 8; ++e)
-    *box_at(at.box, at.lane, e) = make_uint4(__float_as_uint(v[4 * e]), __float_as_uint(v[4 * e + 1]), __float_as_uint(v[4 * e + 2]), __float_as_uint(v[4 * e + 3]));
+    box_put(at.box, at.lane, e, v + 4 * e);
   __syncwarp();
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     const int r = r4 + 4 * k;
-    if (r < rows) put(r, c + 4 * q, *reinterpret_cast<const float4*>(box_at(at.box, r, q)));
+    if (r < rows) put(r, c + 4 * q, box_get(at.box, r, q));
   }
   __syncwarp();
 }
@@ -348,12 +361,11 @@ struct StoreEpi {
             if (c >= p.n) continue;
             box_free(at.lane);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              *box_at(at.box, at.lane, e) = make_uint4(__float_as_uint(acc[b][4 * e]), __float_as_uint(acc[b][4 * e + 1]), __float_as_uint(acc[b][4 * e + 2]),
-                                                       __float_as_uint(acc[b][4 * e + 3]));
+            for (int e = 0; e < 8; ++e) box_put(at.box, at.lane, e, &acc[b][4 * e]);
             box_ready();
             if (at.lane == 0) {
-              tma_store_3d(&p.out, at.box, c, at.row, 0);
+              if (p.epi.out.accumulate) box_add(&p.out, at.box, c, at.row, 0);
+              else box_store(&p.out, at.box, c, at.row, 0);
               bulk_commit();
             }
           }
@@ -366,11 +378,11 @@ struct StoreEpi {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               const float* v = &acc[b + e / 4][8 * (e % 4)];
-              *box_at(at.box, at.lane, e) = make_uint4(pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3]), pack_bf2(v[4], v[5]), pack_bf2(v[6], v[7]));
+              box_put(at.box, at.lane, e, pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3]), pack_bf2(v[4], v[5]), pack_bf2(v[6], v[7]));
             }
             box_ready();
             if (at.lane == 0) {
-              tma_store_3d(&p.out, at.box, c, at.row, 0);
+              box_store(&p.out, at.box, c, at.row, 0);
               bulk_commit();
             }
           }
@@ -404,19 +416,39 @@ enum Lie { kRowsK = 0, kRowsMn = 1, kBlocksK = 2, kBlocksMn = 3 };
 __host__ __device__ constexpr bool is_mn(int lie) { return (lie & 1) != 0; }
 __host__ __device__ constexpr bool is_blocks(int lie) { return lie >= 2; }
 
+// 3-D tiled TMA load, signalled like tma_load_3d, with an L2 policy.
+__device__ __forceinline__ void load_box(void* dst, const CUtensorMap* map, uint32_t bar_cluster, int c0, int c1, int c2, uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
+      " [%0], [%1, {%3, %4, %5}], [%2], %6;" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar_cluster), "r"(c0), "r"(c1), "r"(c2), "l"(policy)
+      : "memory");
+}
+// What is read once goes from L2 first, what every pair reads last.
+__device__ __forceinline__ uint64_t once_policy() {
+  uint64_t p;
+  asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+  return p;
+}
+__device__ __forceinline__ uint64_t often_policy() {
+  uint64_t p;
+  asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
+  return p;
+}
+
 // One K block (kb) of an operand's half tile from row or column `mn` on.
 template <int kLie>
-__device__ __forceinline__ void load_operand(uint8_t* dst, const CUtensorMap* map, uint32_t bar, int mn, int kb) {
+__device__ __forceinline__ void load_operand(uint8_t* dst, const CUtensorMap* map, uint32_t bar, int mn, int kb, uint64_t policy) {
   constexpr int kBytes = kHalf * kBlockK * 2;
-  if (kLie == kRowsK) tma_load_3d(dst, map, bar, kb * kBlockK, mn, 0);
-  if (kLie == kBlocksK) tma_load_3d(dst, map, bar, 0, mn, kb);
+  if (kLie == kRowsK) load_box(dst, map, bar, kb * kBlockK, mn, 0, policy);
+  if (kLie == kBlocksK) load_box(dst, map, bar, 0, mn, kb, policy);
   if (kLie == kRowsMn) {
-    tma_load_3d(dst, map, bar, mn, kb * kBlockK, 0);
-    tma_load_3d(dst + kBytes / 2, map, bar, mn + 64, kb * kBlockK, 0);
+    load_box(dst, map, bar, mn, kb * kBlockK, 0, policy);
+    load_box(dst + kBytes / 2, map, bar, mn + 64, kb * kBlockK, 0, policy);
   }
   if (kLie == kBlocksMn) {
-    tma_load_3d(dst, map, bar, 0, kb * kBlockK, mn / 64);
-    tma_load_3d(dst + kBytes / 2, map, bar, 0, kb * kBlockK, mn / 64 + 1);
+    load_box(dst, map, bar, 0, kb * kBlockK, mn / 64, policy);
+    load_box(dst + kBytes / 2, map, bar, 0, kb * kBlockK, mn / 64 + 1, policy);
   }
 }
 
@@ -468,7 +500,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_ke
   const uint32_t tmem_base = *tmem_slot;
   const uint64_t wait_ns = p.wait_ns;
 
-  // 384 threads x 168 registers at launch = 128 x 56 + 256 x 224: the epilogue
+  // 384 threads x 168 registers at launch, more than 128 x 96 + 256 x 200: the epilogue
   // holds 128 sums and what it makes of them
   if (warp == 0) {
     // -------------------------------- producer ---------------------------------
@@ -477,6 +509,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_ke
       int stage = 0;
       uint32_t ph = 0;
       bool ok = true;
+      // A in blocks is a passing value (the gradient's d), larger than L2
+      const uint64_t often = often_policy(), a_policy = is_blocks(kALie) ? once_policy() : often;
       Items items(sch, pair);
       Item it;
       while (ok && items.next(sch, it)) {
@@ -495,8 +529,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_ke
           }
           log->bytes[stage] = kStageBytes;
           log->n += 1u;
-          load_operand<kALie>(sa, &p.a, fb, row, kb);
-          load_operand<kBLie>(sb, &p.b, fb, col, kb);
+          load_operand<kALie>(sa, &p.a, fb, row, kb, a_policy);
+          load_operand<kBLie>(sb, &p.b, fb, col, kb, often);
           if (++stage == kStages) {
             stage = 0;
             ph ^= 1u;
@@ -561,7 +595,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_ke
     Place at;
     at.lane = lane;
     at.half = (warp - kFirstEpi) >> 2;
-    at.box = smem + Smem<Epi>::kBoxes + (size_t)(warp - kFirstEpi) * Epi::kBoxes * kBoxBytes;
+    at.box = smem_u32(smem + Smem<Epi>::kBoxes + (size_t)(warp - kFirstEpi) * Epi::kBoxes * kBoxBytes);
     const int q = warp & 3, r0 = (int)rank * kHalf + q * 32;      // the warp's first row of the tile
     const uint32_t lanes = (uint32_t)(q * 32) << 16;
     const float nan = __int_as_float(0x7FC00000);
@@ -594,19 +628,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_ke
           for (int b = 0; b < 4; ++b) tmem_wait(acc[b]);
         } else {
 #pragma unroll
-          for (int b = 0; b < 4; b += 2) {
-            float r[2][32];
+          for (int b = 0; b < 4; ++b) {
+            float r[32];
+            tmem_load(from + 32 * b, r);
+            tmem_wait(r);
 #pragma unroll
-            for (int k = 0; k < 2; ++k) tmem_load(from + 32 * (b + k), r[k]);
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              tmem_wait(r[k]);
-#pragma unroll
-              for (int e = 0; e < 32; e += 2) {
-                const float2 v = add2(make_float2(acc[b + k][e], acc[b + k][e + 1]), make_float2(r[k][e], r[k][e + 1]));
-                acc[b + k][e] = v.x;
-                acc[b + k][e + 1] = v.y;
-              }
+            for (int e = 0; e < 32; e += 2) {
+              const float2 v = add2(make_float2(acc[b][e], acc[b][e + 1]), make_float2(r[e], r[e + 1]));
+              acc[b][e] = v.x;
+              acc[b][e + 1] = v.y;
             }
           }
         }
@@ -795,7 +825,7 @@ cudaError_t start_store(Params<StoreEpi>& p, cudaStream_t st) {
   const int64_t size = o.dt == LM_F32 ? 4 : 2;
   cudaError_t e = cudaSuccess;
   const int64_t ld = p.m > 1 ? o.d.ld : (int64_t)p.n;
-  if (o.add == nullptr && !o.accumulate && reinterpret_cast<uintptr_t>(o.d.data) % 16 == 0 && ld * size % 16 == 0 && ld < ((int64_t)1 << 37) / p.m) {
+  if ((!o.accumulate || o.dt == LM_F32) && reinterpret_cast<uintptr_t>(o.d.data) % 16 == 0 && ld * size % 16 == 0 && ld < ((int64_t)1 << 37) / p.m) {
     e = encode_boxes(&p.out, o.dt, o.d.data, p.n, p.m, 1, ld, ld * p.m, 32);
     p.epi.out.tma = 1;
   }

@@ -55,8 +55,8 @@ template <typename P>
 __device__ __forceinline__ void store_boxes(const P& p, const Place& at) {
   box_ready();
   if (at.lane != 0 || at.row >= p.m) return;
-  if (at.col < p.n) tma_store_3d(&p.out, at.box, 0, at.row, at.col / 64);
-  if (at.col + 64 < p.n) tma_store_3d(&p.out, at.box + kBoxBytes, 0, at.row, at.col / 64 + 1);
+  if (at.col < p.n) box_store(&p.out, at.box, 0, at.row, at.col / 64);
+  if (at.col + 64 < p.n) box_store(&p.out, at.box + kBoxBytes, 0, at.row, at.col / 64 + 1);
   bulk_commit();
 }
 
@@ -148,7 +148,7 @@ struct ForwardEpi {
               w[e >> 1] = two_q(fminf(q.x, kWhole + 65535.f), fminf(q.y, kWhole + 65535.f));
             }
           }
-          if (kKeep) *box_at(at.box + (b >> 1) * kBoxBytes, at.lane, (b & 1) * 4 + o / 8) = make_uint4(w[0], w[1], w[2], w[3]);
+          if (kKeep) box_put(at.box + (b >> 1) * kBoxBytes, at.lane, (b & 1) * 4 + o / 8, w[0], w[1], w[2], w[3]);
         }
       }
       s2[0] = add2(s2[0], s2[1]);
@@ -211,7 +211,7 @@ struct GradEpi {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float* v = &acc[b][8 * e];
-          *box_at(at.box + (b >> 1) * kBoxBytes, at.lane, (b & 1) * 4 + e) = make_uint4(pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3]), pack_bf2(v[4], v[5]), pack_bf2(v[6], v[7]));
+          box_put(at.box + (b >> 1) * kBoxBytes, at.lane, (b & 1) * 4 + e, pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3]), pack_bf2(v[4], v[5]), pack_bf2(v[6], v[7]));
         }
       }
       store_boxes(p, at);
@@ -338,6 +338,19 @@ __global__ void __launch_bounds__(256) linlogp_dz_kernel(uint4* q, const float* 
       o[k] = pack_bf2(d[0], d[1]);
     }
     *at = make_uint4(o[0], o[1], o[2], o[3]);
+  }
+}
+
+// The fp32 sums of dW to its own type.
+__global__ void __launch_bounds__(256) linlogp_round_kernel(const float* sum, int64_t ld, Store out, int64_t rows, int cols) {
+  griddep_wait();
+  griddep_launch_dependents();
+  const int per = (cols + 3) / 4;
+  const int64_t all = rows * per;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / per;
+    const int c = 4 * (int)(i - r * per);
+    out.put(r, c, *reinterpret_cast<const float4*>(sum + r * ld + c), cols - c);
   }
 }
 
@@ -514,15 +527,14 @@ cudaError_t piece(const LinLogpParams& q, const Layout& l, const Mat& h, const M
     s.parts = reinterpret_cast<float*>(ws + l.partial);
     const bool own_sum = !dw_is_sum(q) && l.pieces > 1;
     const Mat sum{ws + l.dw, l.ld};
-    if (own_sum && !last) s.epi.out = make_store(sum, LM_F32, q.vocab, first > 0);
-    else s.epi.out = make_store(q.dw, q.dwdt, q.vocab, q.accumulate != 0 || (!own_sum && first > 0));
-    if (own_sum && last) {
-      s.epi.out.add = static_cast<const float*>(sum.data);
-      s.epi.out.ld_add = l.ld;
-    }
+    if (own_sum) s.epi.out = make_store(sum, LM_F32, q.vocab, first > 0);
+    else s.epi.out = make_store(q.dw, q.dwdt, q.vocab, q.accumulate != 0 || first > 0);
     LM_RUN(encode_blocks(&s.a, ws + l.d, q.vocab, rows, 64));
     LM_RUN(encode_operand(&s.b, h.data, q.width, rows, h.ld, true));
     LM_RUN((start_store<kBlocksMn, kRowsMn>(s, st)));
+    if (own_sum && last)
+      LM_RUN(launch_after(linlogp_round_kernel, dim3((unsigned)std::min<int64_t>(q.vocab, 152 * 16)), 256, 0, st, (const float*)sum.data, l.ld,
+                          make_store(q.dw, q.dwdt, q.vocab, q.accumulate != 0), (int64_t)q.vocab, q.width));
   }
   return cudaSuccess;
 }
