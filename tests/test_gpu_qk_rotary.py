@@ -6,9 +6,11 @@ most 40 additions, a division and a square root, fewer than 64 roundings of
 2^-24.  A result is rotated from two channels of a few products each, fewer
 than 16 roundings of what they add up to in magnitude: together 2^-17 of it,
 then rounded to its type, 2^-8 (bf16) or 2^-24 (fp32) of itself.  The mean of the
-gradient is such a sum of magnitudes itself.  dweight adds tokens x heads
-terms: a warp's own share one after another, then 8 warps, then blocks in
-chains of 20 and 5: fewer than n / 4864 + 40 roundings of what they add up to."""
+gradient is such a sum of magnitudes itself.  dweight adds n = tokens x heads
+terms: a group's own share one after another (at least 4864 groups, or 16 heads
+each), then the block's 2048 / dim groups (or 8 warps), then at most 912 blocks
+in eight chains: fewer than n / 4864 + 16 + 2048 / dim + 130 roundings of what
+they add up to."""
 
 import pytest
 
@@ -143,7 +145,7 @@ def test_against_64_bits(T, tokens, hq, hk, dim, turned, interleaved, norm, lay,
         dx, m, dwant, dm = gradient(d, x, w, cs, c.n, c.inter, c.norm)
         near(got, dx, m, dtype)
         if norm:
-            near(dw, dwant, dm, dtype, E + (x[..., 0].numel() / 4864 + 40) * 2.0 ** -24)
+            near(dw, dwant, dm, dtype, E + (x[..., 0].numel() / 4864 + 146 + 2048 / dim) * 2.0 ** -24)
         else:
             assert dw is None
     assert bool((dout[~mark] == 77).all())
