@@ -20,12 +20,15 @@
 namespace lm {
 namespace {
 
+using gemm::add2;
+using gemm::fma2;
 using gemm::launch_after;
+using gemm::mul2;
 using tc::griddep_launch_dependents;
 using tc::griddep_wait;
 
 constexpr int kWarps = 8, kThreads = 32 * kWarps;
-constexpr int kMostBlocks = 152 * 6;
+constexpr int kMostBlocks = 152 * 2;
 constexpr uint32_t kAll = 0xFFFFFFFFu;
 
 __device__ __forceinline__ float value(const float* p) { return *p; }
@@ -203,34 +206,43 @@ __global__ void __launch_bounds__(kThreads) rotary_join_kernel(const __grid_cons
 
 // --- four pairs a lane ---
 
-// How a part's heads fall to groups of lanes: `lanes` (a power of two) to a
-// head, `chunk` heads of a token one after another.
+// How heads fall to groups of lanes: `lanes` (a power of two) to a head, a part's
+// `chunk` heads of a token to an item, one after another; blocks below q_blocks
+// take the queries' items, the others the keys'.
 struct Deal {
-  int32_t lanes, active;      // active: lanes that hold channels
-  int32_t chunk, chunks[2];   // heads of an item; items a token of each part
+  int32_t lanes;
+  int32_t chunk[2], chunks[2];   // heads of an item; items a token
+  int32_t q_blocks;
 };
-constexpr int kAhead = 4;     // heads loaded at once
 
-__device__ __forceinline__ void load4(const float* p, float (&v)[8], int at) {
-  const float4 x = __ldcs(reinterpret_cast<const float4*>(p));
-  v[at] = x.x; v[at + 1] = x.y; v[at + 2] = x.z; v[at + 3] = x.w;
-}
-__device__ __forceinline__ void load4(const __nv_bfloat16* p, float (&v)[8], int at) {
-  const uint2 x = __ldcs(reinterpret_cast<const uint2*>(p));
-  v[at] = __uint_as_float(x.x << 16);
-  v[at + 1] = __uint_as_float(x.x & 0xFFFF0000u);
-  v[at + 2] = __uint_as_float(x.y << 16);
-  v[at + 3] = __uint_as_float(x.y & 0xFFFF0000u);
-}
-__device__ __forceinline__ void store4(float* p, const float (&v)[8], int at) {
-  __stcs(reinterpret_cast<float4*>(p), make_float4(v[at], v[at + 1], v[at + 2], v[at + 3]));
-}
-__device__ __forceinline__ void store4(__nv_bfloat16* p, const float (&v)[8], int at) {
-  __stcs(reinterpret_cast<uint2*>(p), make_uint2(tc::pack_bf2(v[at], v[at + 1]), tc::pack_bf2(v[at + 2], v[at + 3])));
-}
+// Four channels as they are read.
+template <typename T> struct Piece;
+template <> struct Piece<float> {
+  float4 w;
+  __device__ __forceinline__ void zero() { w = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ __forceinline__ void load(const float* p) { w = __ldcs(reinterpret_cast<const float4*>(p)); }
+  __device__ __forceinline__ void get(float2& a, float2& b) const {
+    a = make_float2(w.x, w.y);
+    b = make_float2(w.z, w.w);
+  }
+  static __device__ __forceinline__ void store(float* p, float2 a, float2 b) { __stcs(reinterpret_cast<float4*>(p), make_float4(a.x, a.y, b.x, b.y)); }
+};
+template <> struct Piece<__nv_bfloat16> {
+  uint2 w;
+  __device__ __forceinline__ void zero() { w = make_uint2(0u, 0u); }
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { w = __ldcs(reinterpret_cast<const uint2*>(p)); }
+  __device__ __forceinline__ void get(float2& a, float2& b) const {
+    a = make_float2(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u));
+    b = make_float2(__uint_as_float(w.y << 16), __uint_as_float(w.y & 0xFFFF0000u));
+  }
+  static __device__ __forceinline__ void store(__nv_bfloat16* p, float2 a, float2 b) {
+    __stcs(reinterpret_cast<uint2*>(p), make_uint2(tc::pack_bf2(a.x, a.y), tc::pack_bf2(b.x, b.y)));
+  }
+};
 
-// A lane's channels: pieces of four from a and b.  Pair k is (v[k], v[4 + k]) of
-// the halves, (v[2 k], v[2 k + 1]) interleaved.
+// A lane's channels: pieces of four from a and b, as v[0], v[1] and v[2], v[3].
+// Its four pairs are (v[0], v[2]) and (v[1], v[3]) element by element (halves),
+// or the two elements of each v (interleaved).
 template <bool kInterleaved>
 struct Lane {
   int a, b, pair;       // pair: the first of its four; -1 where they do not turn
@@ -250,189 +262,304 @@ struct Lane {
       b = a + (p.dim - p.turned) / 2;
       pair = -1;
     }
+    if (!in) pair = -1;
   }
-  // cosines and sines of its pairs at the token's position
-  __device__ __forceinline__ void turns(const RotaryParams& p, int64_t token, float (&c)[4], float (&s)[4]) const {
-    if (pair < 0 || !in) {
+  __device__ __forceinline__ void gains(const void* w, int dt, float2 (&v)[4]) const {
+    const int at[4] = {a, a + 2, b, b + 2};
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        c[k] = 1.f;
-        s[k] = 0.f;
+    for (int k = 0; k < 4; ++k) v[k] = in ? make_float2(gain(w, dt, at[k]), gain(w, dt, at[k] + 1)) : make_float2(1.f, 1.f);
+  }
+};
+// Cosines and sines of a lane's four pairs.
+template <bool kInterleaved>
+struct Turns {
+  float2 c[2], s[2];    // pairs 0, 1 and 2, 3
+  __device__ __forceinline__ void load(const RotaryParams& p, const Lane<kInterleaved>& l, int64_t at) {
+    c[0] = c[1] = make_float2(1.f, 1.f);
+    s[0] = s[1] = make_float2(0.f, 0.f);
+    if (l.pair < 0) return;
+    const bool in = at >= 0 && at < p.table_rows;
+    const float2* t = reinterpret_cast<const float2*>(p.table) + (in ? at : 0) * (p.turned >> 1) + l.pair;
+    const float2 none = make_float2(__int_as_float(0x7FC00000), __int_as_float(0x7FC00000));
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float2 v = in ? __ldg(t + k) : none;
+      (k & 1 ? c[k >> 1].y : c[k >> 1].x) = v.x;
+      (k & 1 ? s[k >> 1].y : s[k >> 1].x) = v.y;
+    }
+  }
+  template <bool kBack>
+  __device__ __forceinline__ void turn(float2 (&v)[4]) const {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      if (kInterleaved) {
+        const float c0[2] = {c[k].x, c[k].y}, s0[2] = {kBack ? -s[k].x : s[k].x, kBack ? -s[k].y : s[k].y};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float2& x = v[2 * k + h];
+          x = fma2(x, make_float2(c0[h], c0[h]), mul2(make_float2(x.y, x.x), make_float2(-s0[h], s0[h])));
+        }
+      } else {
+        const float2 s0 = kBack ? make_float2(-s[k].x, -s[k].y) : s[k], s1 = make_float2(-s0.x, -s0.y), x = v[k], y = v[2 + k];
+        v[k] = fma2(x, c[k], mul2(y, s1));
+        v[2 + k] = fma2(y, c[k], mul2(x, s0));
       }
-      return;
-    }
-    const int64_t at = p.positions[token];
-    if (at < 0 || at >= p.table_rows) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) c[k] = s[k] = __int_as_float(0x7FC00000);
-      return;
-    }
-    const float* t = p.table + (at * (p.turned >> 1) + pair) * 2;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      c[k] = __ldg(t + 2 * k);
-      s[k] = __ldg(t + 2 * k + 1);
-    }
-  }
-  __device__ __forceinline__ void gains(const void* w, int dt, float (&v)[8]) const {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      v[k] = in ? gain(w, dt, a + k) : 1.f;
-      v[4 + k] = in ? gain(w, dt, b + k) : 1.f;
-    }
-  }
-  static __device__ __forceinline__ void turn(float (&v)[8], const float (&c)[4], const float (&s)[4], bool back) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      float &x = v[kInterleaved ? 2 * k : k], &y = v[kInterleaved ? 2 * k + 1 : 4 + k];
-      const float sn = back ? -s[k] : s[k];
-      const float u = x * c[k] - y * sn;
-      y = y * c[k] + x * sn;
-      x = u;
     }
   }
 };
-template <typename T, bool kInterleaved>
-__device__ __forceinline__ void load8(const Heads& h, int64_t token, int head, const Lane<kInterleaved>& l, bool in, float (&v)[8]) {
-  if (in) {
-    const T* p = head_of<const T>(h, token, head);
-    load4(p + l.a, v, 0);
-    load4(p + l.b, v, 4);
-  } else {
+template <int kN>
+__device__ __forceinline__ void group_sums(float (&v)[kN], int lanes) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = 0.f;
+  for (int o = 16; o; o >>= 1) {
+    if (lanes <= o) continue;       // the same for all
+#pragma unroll
+    for (int k = 0; k < kN; ++k) v[k] += __shfl_xor_sync(kAll, v[k], o);
   }
 }
-__device__ __forceinline__ float group_sum(float v, int lanes) {
-  for (int o = lanes >> 1; o; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
-  return v;
+
+// A group's way through its part's items, kAhead heads a step; the groups of a
+// block take the same number of steps (those without heads among them).
+template <int kAhead>
+struct Walk {
+  int64_t item, items, stride, token;
+  int head, end, per, chunk, heads;
+  __device__ __forceinline__ Walk(const RotaryParams& p, const Deal& d, int which, int block, int blocks) {
+    const int groups = kThreads / d.lanes;
+    per = d.chunks[which];
+    chunk = d.chunk[which];
+    heads = p.part[which].heads;
+    items = p.tokens * per;
+    stride = (int64_t)blocks * groups;
+    item = (int64_t)block * groups + threadIdx.x / d.lanes;
+    place();
+  }
+  __device__ __forceinline__ void place() {
+    const int64_t i = min(item, items);
+    token = items <= 0xFFFFFFFFll ? (int64_t)((uint32_t)i / (uint32_t)per) : i / per;
+    head = (int)(i - token * per) * chunk;
+    end = item < items ? min(head + chunk, heads) : head;
+  }
+};
+// Steps of every group of a block.
+__device__ __forceinline__ int64_t steps_of(int64_t items, int64_t stride, int block, int groups, int rounds) {
+  const int64_t first = (int64_t)block * groups;
+  return first < items ? (items - first + stride - 1) / stride * rounds : 0;
 }
 
 template <typename T, bool kInterleaved>
-__global__ void __launch_bounds__(kThreads) rotary8_kernel(const __grid_constant__ RotaryParams p, const __grid_constant__ Deal d) {
+__global__ void __launch_bounds__(kThreads, 2) rotary8_kernel(const __grid_constant__ RotaryParams p, const __grid_constant__ Deal d) {
+  constexpr int kAhead = 4;
   griddep_wait();
   griddep_launch_dependents();
-  const int lane = threadIdx.x % d.lanes, groups = kThreads / d.lanes, per = d.chunks[0] + d.chunks[1];
-  const Lane<kInterleaved> l(p, lane);
-  const int64_t items = p.tokens * per;
-  // whole warps go round together: an item beyond the last has no heads
-  for (int64_t first = (int64_t)blockIdx.x * groups; first < items; first += (int64_t)gridDim.x * groups) {
-    const int64_t item = first + threadIdx.x / d.lanes;
-    const int64_t token = item / per;
-    const int sub = (int)(item - token * per), which = sub >= d.chunks[0] ? 1 : 0;
-    const RotaryPart& part = p.part[which];
-    int head = (sub - (which ? d.chunks[0] : 0)) * d.chunk;
-    const int end = item < items ? min(head + d.chunk, part.heads) : head;
-    float c[4], s[4], w[8];
-    if (head < end) {
-      l.turns(p, token, c, s);
-      if (p.norm) l.gains(part.weight, part.wdt, w);
-    }
-    for (int at = 0; at < d.chunk; at += kAhead) {      // the same number of rounds for every group
-      float v[kAhead][8];
+  const int which = (int)blockIdx.x >= d.q_blocks ? 1 : 0;
+  const RotaryPart& part = p.part[which];
+  const int block = which ? blockIdx.x - d.q_blocks : blockIdx.x, blocks = which ? gridDim.x - d.q_blocks : d.q_blocks;
+  const Lane<kInterleaved> l(p, threadIdx.x % d.lanes);
+  Walk<kAhead> at(p, d, which, block, blocks);
+  const int rounds = (at.chunk + kAhead - 1) / kAhead;
+  const int64_t steps = steps_of(at.items, at.stride, block, kThreads / d.lanes, rounds);
+  const float inv = 1.f / (float)p.dim;
+  const int64_t ldx = part.x.ld_head, ldy = part.y.ld_head;
+  const int gap = l.b - l.a;
+  float2 w[4];
+  if (p.norm) l.gains(part.weight, part.wdt, w);
+  Turns<kInterleaved> t;
+  Piece<T> raw[kAhead][2];
+  int64_t position = 0;
+  auto load = [&]() {
+    const T* x = head_of<const T>(part.x, at.token, at.head) + l.a;
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) load8<T>(part.x, token, head + at + k, l, l.in && head + at + k < end, v[k]);
-      if (p.norm) {
-        float q[kAhead];
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-          q[k] = 0.f;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) q[k] = fmaf(v[k][e], v[k][e], q[k]);
-        }
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-          const float rstd = rsqrtf(group_sum(q[k], d.lanes) / (float)p.dim + p.eps);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[k][e] *= rstd * w[e];
-        }
+    for (int k = 0; k < kAhead; ++k) {
+      raw[k][0].zero();
+      raw[k][1].zero();
+      if (l.in && at.head + k < at.end) {
+        raw[k][0].load(x);
+        raw[k][1].load(x + gap);
       }
+      x += ldx;
+    }
+  };
+  if (steps > 0) {
+    load();
+    if (l.pair >= 0 && at.head < at.end) position = p.positions[at.token];
+  }
+  int round = 0;
+  for (int64_t n = 0; n < steps; ++n) {
+    if (round == 0) t.load(p, l, position);
+    float2 v[kAhead][4];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      raw[k][0].get(v[k][0], v[k][1]);
+      raw[k][1].get(v[k][2], v[k][3]);
+    }
+    T* y = head_of<T>(part.y, at.token, at.head) + l.a;
+    const int left = l.in ? at.end - at.head : 0;
+    // the next step's heads, before this one's are worked on
+    at.head += kAhead;
+    if (++round == rounds) {
+      round = 0;
+      at.item += at.stride;
+      at.place();
+      if (l.pair >= 0 && at.head < at.end) position = p.positions[at.token];
+    }
+    load();
+    if (p.norm) {
+      float q[kAhead];
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
-        if (!l.in || head + at + k >= end) continue;
-        l.turn(v[k], c, s, false);
-        T* y = head_of<T>(part.y, token, head + at + k);
-        store4(y + l.a, v[k], 0);
-        store4(y + l.b, v[k], 4);
+        float2 a = mul2(v[k][0], v[k][0]);
+#pragma unroll
+        for (int e = 1; e < 4; ++e) a = fma2(v[k][e], v[k][e], a);
+        q[k] = a.x + a.y;
       }
+      group_sums(q, d.lanes);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const float rstd = rsqrtf(fmaf(q[k], inv, p.eps));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[k][e] = mul2(mul2(v[k][e], make_float2(rstd, rstd)), w[e]);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      t.template turn<false>(v[k]);
+      if (k < left) {
+        Piece<T>::store(y, v[k][0], v[k][1]);
+        Piece<T>::store(y + gap, v[k][2], v[k][3]);
+      }
+      y += ldy;
     }
   }
 }
 
-// Blocks below q_blocks take the queries' items, the others the keys'.
+// Heads of a step, dy and x of each, and resident blocks: fp32 heads hold twice
+// the registers of bf16 ones (4097 tokens, 40 heads of 80, fp32: 33 us with four
+// and one block, 47 with two and two, which spill; bf16 16384 tokens, 40 heads of
+// 128: 100 us with two and two, 108 with four and one).
+template <typename T> constexpr int kGradAhead = sizeof(T) == 4 ? 4 : 2;
+template <typename T> constexpr int kGradBlocks = sizeof(T) == 4 ? 1 : 2;
 template <typename T, bool kInterleaved>
-__global__ void __launch_bounds__(kThreads) rotary8_grad_kernel(const __grid_constant__ RotaryParams p, const __grid_constant__ Deal d, int q_blocks) {
+__global__ void __launch_bounds__(kThreads, kGradBlocks<T>) rotary8_grad_kernel(const __grid_constant__ RotaryParams p, const __grid_constant__ Deal d) {
   extern __shared__ float sums[];     // groups x dim
+  constexpr int kAhead = kGradAhead<T>;
   griddep_wait();
   griddep_launch_dependents();
-  constexpr int kTogether = 2;        // heads loaded at once: dy and x of each
-  const int lane = threadIdx.x % d.lanes, group = threadIdx.x / d.lanes, groups = kThreads / d.lanes;
-  const int which = (int)blockIdx.x >= q_blocks ? 1 : 0;
+  const int which = (int)blockIdx.x >= d.q_blocks ? 1 : 0, groups = kThreads / d.lanes;
   const RotaryPart& part = p.part[which];
-  const int per = d.chunks[which], block = which ? blockIdx.x - q_blocks : blockIdx.x, blocks = which ? gridDim.x - q_blocks : q_blocks;
-  const Lane<kInterleaved> l(p, lane);
-  const int64_t items = p.tokens * per;
-  float w[8], dw[8];
+  const int block = which ? blockIdx.x - d.q_blocks : blockIdx.x, blocks = which ? gridDim.x - d.q_blocks : d.q_blocks;
+  const Lane<kInterleaved> l(p, threadIdx.x % d.lanes);
+  Walk<kAhead> at(p, d, which, block, blocks);
+  const int rounds = (at.chunk + kAhead - 1) / kAhead;
+  const int64_t steps = steps_of(at.items, at.stride, block, groups, rounds);
+  const float inv = 1.f / (float)p.dim;
+  const int64_t ldx = part.x.ld_head, ldd = part.dy.ld_head, ldo = part.dx.ld_head;
+  const int gap = l.b - l.a;
+  float2 w[4], dw[4];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) dw[e] = 0.f;
+  for (int e = 0; e < 4; ++e) dw[e] = make_float2(0.f, 0.f);
   if (p.norm) l.gains(part.weight, part.wdt, w);
-  for (int64_t first = (int64_t)block * groups; first < items; first += (int64_t)blocks * groups) {
-    const int64_t item = first + group, token = item / per;
-    const int head = (int)(item - token * per) * d.chunk;
-    const int end = item < items ? min(head + d.chunk, part.heads) : head;
-    float c[4], s[4];
-    if (head < end) l.turns(p, token, c, s);
-    for (int at = 0; at < d.chunk; at += kTogether) {
-      float v[kTogether][8], x[kTogether][8];
-      bool in[kTogether];
+  Turns<kInterleaved> t;
+  Piece<T> rawd[kAhead][2], rawx[kAhead][2];
+  int64_t position = 0;
+  auto load = [&]() {
+    const T* dy = head_of<const T>(part.dy, at.token, at.head) + l.a;
+    const T* x = head_of<const T>(part.x, at.token, at.head) + l.a;
 #pragma unroll
-      for (int k = 0; k < kTogether; ++k) {
-        in[k] = l.in && head + at + k < end;
-        load8<T>(part.dy, token, head + at + k, l, in[k], v[k]);
-        if (p.norm) load8<T>(part.x, token, head + at + k, l, in[k], x[k]);
-      }
+    for (int k = 0; k < kAhead; ++k) {
 #pragma unroll
-      for (int k = 0; k < kTogether; ++k) {
-        if (in[k]) l.turn(v[k], c, s, true);
-        if (p.norm) {
-          float q = 0.f, r = 0.f;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            q = fmaf(x[k][e], x[k][e], q);
-            r = fmaf(v[k][e] * w[e], x[k][e], r);
-          }
-          const float rstd = rsqrtf(group_sum(q, d.lanes) / (float)p.dim + p.eps);
-          const float mean = group_sum(r, d.lanes) * rstd / (float)p.dim;
-          if (in[k]) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float xh = x[k][e] * rstd;
-              dw[e] = fmaf(v[k][e], xh, dw[e]);
-              v[k][e] = rstd * (v[k][e] * w[e] - xh * mean);
-            }
-          }
-        }
-        if (in[k]) {
-          T* dx = head_of<T>(part.dx, token, head + at + k);
-          store4(dx + l.a, v[k], 0);
-          store4(dx + l.b, v[k], 4);
+      for (int h = 0; h < 2; ++h) {
+        rawd[k][h].zero();
+        rawx[k][h].zero();
+        if (l.in && at.head + k < at.end) {
+          rawd[k][h].load(dy + h * gap);
+          if (p.norm) rawx[k][h].load(x + h * gap);
         }
       }
+      dy += ldd;
+      x += ldx;
+    }
+  };
+  if (steps > 0) {
+    load();
+    if (l.pair >= 0 && at.head < at.end) position = p.positions[at.token];
+  }
+  int round = 0;
+  for (int64_t n = 0; n < steps; ++n) {
+    if (round == 0) t.load(p, l, position);
+    float2 v[kAhead][4], x[kAhead][4];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      rawd[k][0].get(v[k][0], v[k][1]);
+      rawd[k][1].get(v[k][2], v[k][3]);
+      rawx[k][0].get(x[k][0], x[k][1]);
+      rawx[k][1].get(x[k][2], x[k][3]);
+    }
+    T* dx = head_of<T>(part.dx, at.token, at.head) + l.a;
+    const int left = l.in ? at.end - at.head : 0;
+    at.head += kAhead;
+    const bool turned_on = ++round == rounds;
+    if (turned_on) {
+      round = 0;
+      at.item += at.stride;
+      at.place();
+      if (l.pair >= 0 && at.head < at.end) position = p.positions[at.token];
+    }
+    load();
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) t.template turn<true>(v[k]);
+    if (p.norm) {
+      float q[2 * kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        float2 a = make_float2(0.f, 0.f), b = a;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          a = fma2(x[k][e], x[k][e], a);
+          b = fma2(mul2(v[k][e], w[e]), x[k][e], b);
+        }
+        q[2 * k] = a.x + a.y;
+        q[2 * k + 1] = b.x + b.y;
+      }
+      group_sums(q, d.lanes);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const float rstd = rsqrtf(fmaf(q[2 * k], inv, p.eps)), mean = -q[2 * k + 1] * rstd * inv;
+        const float2 r = make_float2(rstd, rstd), m = make_float2(mean, mean);
+        // a head beyond the item's has v = 0, and x = 0 times a finite rstd unless eps is 0
+        if (k >= left) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 xh = mul2(x[k][e], r);
+          dw[e] = fma2(v[k][e], xh, dw[e]);
+          v[k][e] = mul2(r, fma2(xh, m, mul2(v[k][e], w[e])));
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (k < left) {
+        Piece<T>::store(dx, v[k][0], v[k][1]);
+        Piece<T>::store(dx + gap, v[k][2], v[k][3]);
+      }
+      dx += ldo;
     }
   }
   if (part.dweight == nullptr) return;
   if (l.in) {
+    float* mine = sums + (threadIdx.x / d.lanes) * p.dim;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      sums[group * p.dim + l.a + k] = dw[k];
-      sums[group * p.dim + l.b + k] = dw[4 + k];
+    for (int k = 0; k < 2; ++k) {
+      mine[l.a + 2 * k] = dw[k].x;
+      mine[l.a + 2 * k + 1] = dw[k].y;
+      mine[l.b + 2 * k] = dw[2 + k].x;
+      mine[l.b + 2 * k + 1] = dw[2 + k].y;
     }
   }
   __syncthreads();
   for (int c = threadIdx.x; c < p.dim; c += kThreads) {
-    float t = 0.f;
-    for (int k = 0; k < groups; ++k) t += sums[k * p.dim + c];
-    p.sums[(int64_t)blockIdx.x * p.dim + c] = t;
+    float s = 0.f;
+    for (int k = 0; k < groups; ++k) s += sums[k * p.dim + c];
+    p.sums[(int64_t)blockIdx.x * p.dim + c] = s;
   }
 }
 
@@ -440,24 +567,38 @@ bool pieces_of_four(const Heads& h, int size) {
   return reinterpret_cast<uintptr_t>(h.data) % (4 * size) == 0 && h.ld_token % 4 == 0 && h.ld_head % 4 == 0;
 }
 // Whether eight channels go to a lane, and how.
-bool deal(const RotaryParams& p, lm_dtype dt, bool grad, Deal* d) {
+bool deal(const RotaryParams& p, lm_dtype dt, bool grad, Deal* d, int* k_blocks) {
+  const int64_t most = grad && dt == LM_F32 ? kMostBlocks / 2 : kMostBlocks;     // one wave of blocks
   const int size = dt == LM_F32 ? 4 : 2;
-  if (p.dim % 8 != 0 || p.dim > 256 || p.turned % 8 != 0) return false;
+  if (p.dim % 8 != 0 || p.dim > 256 || p.turned % 8 != 0 || reinterpret_cast<uintptr_t>(p.table) % 8 != 0) return false;
   for (const RotaryPart& r : p.part) {
     if (r.heads == 0) continue;
     if ((!grad || p.norm) && !pieces_of_four(r.x, size)) return false;
     if (!pieces_of_four(grad ? r.dy : r.y, size)) return false;
     if (grad && !pieces_of_four(r.dx, size)) return false;
   }
-  d->active = p.dim / 8;
   d->lanes = 1;
-  while (d->lanes < d->active) d->lanes *= 2;
-  // as many heads to an item as leave every SM 32 warps of items
-  const int64_t groups = (int64_t)152 * 32 * (32 / d->lanes), heads = p.part[0].heads + p.part[1].heads;
-  const int64_t each = p.tokens * heads / groups;
-  d->chunk = (int)std::min<int64_t>(std::max<int64_t>(1, each), 16);
-  if (d->chunk > kAhead) d->chunk = d->chunk / kAhead * kAhead;
-  for (int i = 0; i < 2; ++i) d->chunks[i] = (p.part[i].heads + d->chunk - 1) / d->chunk;
+  while (8 * d->lanes < p.dim) d->lanes *= 2;
+  // as many heads to an item as leave every SM 32 warps of items, 16 at most,
+  // and blocks to each part by the steps of four heads that its items take
+  const int64_t all = (int64_t)152 * 32 * (32 / d->lanes), heads = p.part[0].heads + p.part[1].heads, groups = kThreads / d->lanes;
+  const int64_t chunk = std::min<int64_t>(std::max<int64_t>(1, p.tokens * heads / all), 16);
+  int64_t steps[2] = {0, 0};
+  for (int i = 0; i < 2; ++i) {
+    const int64_t n = p.part[i].heads, items = (n + chunk - 1) / chunk;
+    if (n == 0) continue;
+    d->chunk[i] = (int)((n + items - 1) / items);
+    if (d->chunk[i] > 4) d->chunk[i] = (d->chunk[i] + 3) / 4 * 4;
+    d->chunks[i] = (int)((n + d->chunk[i] - 1) / d->chunk[i]);
+    steps[i] = (int64_t)d->chunks[i] * ((d->chunk[i] + 3) / 4);
+  }
+  int blocks[2];
+  for (int i = 0; i < 2; ++i) {
+    const int64_t want = (p.tokens * d->chunks[i] + groups - 1) / groups, share = std::max<int64_t>(1, most * steps[i] / (steps[0] + steps[1]));
+    blocks[i] = (int)std::min(want, share);
+  }
+  d->q_blocks = blocks[0];
+  *k_blocks = blocks[1];
   return true;
 }
 
@@ -475,13 +616,12 @@ size_t rotary_grad_workspace(int64_t tokens, int64_t heads, int32_t dim) {
 
 cudaError_t launch_rotary(lm_dtype dt, const RotaryParams& p, cudaStream_t st) {
   Deal d{};
-  if (deal(p, dt, false, &d)) {
-    const int64_t items = p.tokens * (d.chunks[0] + d.chunks[1]), groups = kThreads / d.lanes;
-    const dim3 grid((unsigned)std::min<int64_t>((items + groups - 1) / groups, 152 * 32));
+  int k_blocks = 0;
+  if (deal(p, dt, false, &d, &k_blocks)) {
     using Kernel = void (*)(RotaryParams, Deal);
     const Kernel kernels[2][2] = {{rotary8_kernel<float, false>, rotary8_kernel<float, true>},
                                   {rotary8_kernel<__nv_bfloat16, false>, rotary8_kernel<__nv_bfloat16, true>}};
-    return launch_after(kernels[dt == LM_F32 ? 0 : 1][p.interleaved ? 1 : 0], grid, kThreads, 0, st, p, d);
+    return launch_after(kernels[dt == LM_F32 ? 0 : 1][p.interleaved ? 1 : 0], dim3((unsigned)(d.q_blocks + k_blocks)), kThreads, 0, st, p, d);
   }
   const int64_t rows = p.tokens * (p.part[0].heads + p.part[1].heads);
   const dim3 grid((unsigned)std::min<int64_t>((rows + kWarps - 1) / kWarps, 152 * 16));
@@ -494,19 +634,13 @@ cudaError_t launch_rotary_grad(lm_dtype dt, const RotaryParams& p, cudaStream_t 
   Deal d{};
   if (p.tokens > 0 && p.part[0].heads + p.part[1].heads > 0) {
     cudaError_t e;
-    if (deal(p, dt, true, &d)) {
-      const int64_t groups = kThreads / d.lanes, most = kMostBlocks;
-      const int64_t heads = p.part[0].heads + p.part[1].heads;
-      for (int i = 0; i < 2; ++i) {
-        const int64_t want = (p.tokens * d.chunks[i] + groups - 1) / groups, share = std::max<int64_t>(1, most * p.part[i].heads / heads);
-        blocks[i] = (int)std::min(want, share);
-      }
-      first1 = blocks[0];
-      using Kernel = void (*)(RotaryParams, Deal, int);
+    if (deal(p, dt, true, &d, &blocks[1])) {
+      blocks[0] = first1 = d.q_blocks;
+      using Kernel = void (*)(RotaryParams, Deal);
       const Kernel kernels[2][2] = {{rotary8_grad_kernel<float, false>, rotary8_grad_kernel<float, true>},
                                     {rotary8_grad_kernel<__nv_bfloat16, false>, rotary8_grad_kernel<__nv_bfloat16, true>}};
       e = launch_after(kernels[dt == LM_F32 ? 0 : 1][p.interleaved ? 1 : 0], dim3((unsigned)(blocks[0] + blocks[1])), kThreads,
-                       dw ? (size_t)groups * p.dim * sizeof(float) : 0, st, p, d, blocks[0]);
+                       dw ? (size_t)(kThreads / d.lanes) * p.dim * sizeof(float) : 0, st, p, d);
     } else {
       blocks[0] = blocks[1] = first1 = grad_blocks(p.tokens, std::max(p.part[0].heads, p.part[1].heads));
       e = launch_after(dt == LM_F32 ? rotary_grad_kernel<float> : rotary_grad_kernel<__nv_bfloat16>, dim3((unsigned)first1, p.part[1].heads > 0 ? 2 : 1),
