@@ -66,7 +66,6 @@ struct Smem {
   static constexpr size_t kBytes = 1024 + kBars + 512;
   static_assert(kBytes <= 232448, "shared memory of one SM");
 };
-constexpr size_t kPartBytes = (size_t)kTileM * kTileN * 4;
 constexpr int kMostSharers = kPairs;
 
 // How the work falls to the pairs.
@@ -669,7 +668,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_ke
 
 // Left-over tiles that several pairs shared: the parts added in the order of
 // the sum, then stored like a whole tile.
-__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Params<StoreEpi> p) {
+struct JoinParts {
+  Schedule sch;
+  int32_t m, n;
+  const float* parts;
+  Store out;
+};
+template <int kN>
+__global__ void __launch_bounds__(kN) join_kernel(const __grid_constant__ JoinParts p) {
+  constexpr int kRow = kN / 4;      // threads of a row; four rows a block
   const Schedule& s = p.sch;
   const int t = blockIdx.x;
   griddep_wait();
@@ -685,22 +692,22 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Param
   tn += column;
   int last = k;   // the last sharer of the tile
   while (last + 1 < s.sharers && s.begin[last + 1] < u1) ++last;
-  const int rows = min(kTileM, p.m - tm * kTileM), cols = min(kTileN, p.n - tn * kTileN);
+  const int rows = min(kTileM, p.m - tm * kTileM), cols = min(kN, p.n - tn * kN);
   // the first part may be its pair's second item; every later one is a first
-  const float* part0 = p.parts + (size_t)(2 * (k * s.team + column) + (s.begin[k] >= u0 ? 0 : 1)) * (kTileM * kTileN);
-  const int r = blockIdx.y * 4 + (threadIdx.x >> 6), c = 4 * (threadIdx.x & 63);
+  const float* part0 = p.parts + (size_t)(2 * (k * s.team + column) + (s.begin[k] >= u0 ? 0 : 1)) * (kTileM * kN);
+  const int r = blockIdx.y * 4 + (threadIdx.x / kRow), c = 4 * (threadIdx.x % kRow);
   if (r >= rows || c >= cols) return;
-  const size_t at = (size_t)r * kTileN + c;
+  const size_t at = (size_t)r * kN + c;
   float4 sum = *reinterpret_cast<const float4*>(part0 + at);
 #pragma unroll 4
   for (int j = k + 1; j <= last; ++j) {
-    const float4 v = *reinterpret_cast<const float4*>(p.parts + (size_t)(2 * (j * s.team + column)) * (kTileM * kTileN) + at);
+    const float4 v = *reinterpret_cast<const float4*>(p.parts + (size_t)(2 * (j * s.team + column)) * (kTileM * kN) + at);
     sum.x += v.x;
     sum.y += v.y;
     sum.z += v.z;
     sum.w += v.w;
   }
-  p.epi.out.put(tm * kTileM + r, tn * kTileN + c, sum, cols - c);
+  p.out.put(tm * kTileM + r, tn * kN + c, sum, cols - c);
 }
 
 // D of an empty sum.
@@ -751,11 +758,11 @@ inline bool tma_rows(const Mat& m, int64_t rows, int64_t cols) {
 }
 
 // Units of `strip` tiles dealt in turn, no sum split.
-inline Schedule plain_schedule(int64_t m, int64_t n, int64_t k, int strip) {
+inline Schedule plain_schedule(int64_t m, int64_t n, int64_t k, int strip, int tile_n = kTileN, int block_k = kBlockK) {
   Schedule s{};
   s.tiles_m = (int32_t)((m + kTileM - 1) / kTileM);
-  s.tiles_n = (int32_t)((n + kTileN - 1) / kTileN);
-  s.nkb = (int32_t)((k + kBlockK - 1) / kBlockK);
+  s.tiles_n = (int32_t)((n + tile_n - 1) / tile_n);
+  s.nkb = (int32_t)((k + block_k - 1) / block_k);
   s.team = 1;
   s.strip = strip;
   s.strips = (s.tiles_n + strip - 1) / strip;
@@ -764,8 +771,8 @@ inline Schedule plain_schedule(int64_t m, int64_t n, int64_t k, int strip) {
 }
 // Whole waves of units, the rest shared by ranges of the sum.
 constexpr int kMostTeam = 8;      // where more columns would leave many pairs out, each is for itself
-inline Schedule split_schedule(int64_t m, int64_t n, int64_t k) {
-  Schedule s = plain_schedule(m, n, k, 1);
+inline Schedule split_schedule(int64_t m, int64_t n, int64_t k, int tile_n = kTileN, int block_k = kBlockK) {
+  Schedule s = plain_schedule(m, n, k, 1, tile_n, block_k);
   if (s.tiles_n <= kMostTeam && s.tiles_m > 1) {
     s.team = s.tiles_n;
     s.strips = 1;
@@ -783,7 +790,7 @@ inline Schedule split_schedule(int64_t m, int64_t n, int64_t k) {
   return s;
 }
 inline bool has_parts(const Schedule& s) { return s.rest > 0 && s.sharers > s.rest; }
-inline size_t parts_bytes(const Schedule& s) { return has_parts(s) ? 2 * (size_t)s.sharers * s.team * kPartBytes : 0; }
+inline size_t parts_bytes(const Schedule& s, int tile_n = kTileN) { return has_parts(s) ? 2 * (size_t)s.sharers * s.team * kTileM * tile_n * 4 : 0; }
 inline int pairs_of(const Schedule& s) { return std::min(kPairs / s.team, std::max(s.units, s.sharers)) * s.team; }
 
 // A launch whose set-up may overlap the end of the kernel before it (which it
@@ -818,6 +825,11 @@ cudaError_t start(const Params<Epi>& p, cudaStream_t st) {
 inline cudaError_t start_zero(const Mat& d, int dt, int64_t rows, int cols, cudaStream_t st) {
   return launch_after(zero_kernel, dim3((unsigned)std::min<int64_t>(rows, 152 * 8)), 256, 0, st, d, dt, rows, cols);
 }
+template <int kN>
+cudaError_t start_join(const Schedule& s, int32_t m, int32_t n, const float* parts, const Store& out, cudaStream_t st) {
+  const JoinParts j{s, m, n, parts, out};
+  return launch_after(join_kernel<kN>, dim3(s.rest, kTileM / 4, s.team), kN, 0, st, j);
+}
 // A product whose sums may be split: the kernel, and the join where parts are left.
 template <int kALie, int kBLie>
 cudaError_t start_store(Params<StoreEpi>& p, cudaStream_t st) {
@@ -831,7 +843,7 @@ cudaError_t start_store(Params<StoreEpi>& p, cudaStream_t st) {
   }
   if (e == cudaSuccess) e = start<kALie, kBLie, StoreEpi>(p, st);
   if (e != cudaSuccess || !has_parts(p.sch)) return e;
-  return launch_after(join_kernel, dim3(p.sch.rest, kTileM / 4, p.sch.team), 256, 0, st, p);
+  return start_join<kTileN>(p.sch, p.m, p.n, p.parts, p.epi.out, st);
 }
 
 }  // namespace

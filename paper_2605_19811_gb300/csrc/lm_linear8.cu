@@ -2,11 +2,18 @@
 // lionmuon.h):
 //   y = x W^T (tokens x out),  dx = dy W (tokens x in)
 // with activations of one scale for each token's 128 channels and weights of one
-// scale for each block of 128 x 128.
+// scale for each block of 128 x 128, on the tensor cores: tcgen05.mma
+// (kind::mxf8f6f4) on CTA pairs takes the e4m3 codes as they are and multiplies
+// each 32 of the sum by two powers of two, here the same for four such steps.  A
+// power-of-two float's exponent bits are that scale, so a first kernel copies
+// them, a byte a row, in the order in which the tensor memory holds them.
 //
-// A code times its power-of-two scale is a bf16 number: both operands are laid
-// out as bf16 in the workspace without a rounding, and the product of bf16
-// matrices follows.
+// A pair takes a tile of 256 tokens x 192 columns, 128 of the sum at a time: two
+// accumulators of 192 columns leave the tensor memory room for the scales (256
+// would take all of it).  CTA r holds tokens 128 r .. (A) and columns 96 r .. (B);
+// W lies K-major for the product with W^T and MN-major for the one with W, so the
+// same codes serve both.  The sum is cut every 1024 (32 additions) and goes on in
+// fp32 registers, as in lm_gemm_tc.cuh, whose schedules are used here.
 #include <cuda_bf16.h>
 
 #include "lm_code8.cuh"
@@ -77,8 +84,8 @@ __global__ void __launch_bounds__(256) weight8_pack_kernel(Mat w, int64_t rows, 
   }
 }
 
-// Codes back to values, eight a thread: of weights, or (kRows) of activations.
-template <typename T, bool kRows>
+// Codes back to values, eight a thread.
+template <typename T>
 __global__ void __launch_bounds__(256) values_kernel(const uint8_t* codes, int64_t ld, const float* scales, int64_t ld_scales, int64_t nrows, int64_t cols, T* to,
                                                      int64_t ld_to, int vec) {
   griddep_wait();
@@ -87,7 +94,7 @@ __global__ void __launch_bounds__(256) values_kernel(const uint8_t* codes, int64
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / per, c = 8 * (i - r * per);
     const uint2 q = *reinterpret_cast<const uint2*>(codes + r * ld + c);
-    const float s = kRows ? scales[c / kBlock * ld_scales + r] : scales[r / kBlock * ld_scales + c / kBlock];
+    const float s = scales[r / kBlock * ld_scales + c / kBlock];
     const uint32_t two[4] = {q.x, q.x >> 16, q.y, q.y >> 16};
     float v[8];
 #pragma unroll
@@ -112,21 +119,378 @@ unsigned blocks_for(int64_t nrows, int64_t cols) {
   return (unsigned)std::min<int64_t>(b, 152 * 16);
 }
 
+// --- the product ---
+
+constexpr int kN = 192, kHalfN = kN / 2, kK = 128;      // tile columns; of the sum at a time
+constexpr int kChunk8 = 8;                              // most blocks summed in one accumulator: 32 additions
+constexpr int kScaleBytes = 512 + 1024;                 // of a block: the CTA's rows', the tile's columns'
+constexpr int kWarpBytes = 3 * 32 * 64;                 // an epilogue warp's boxes: three of 32 columns in bf16, one in fp32
+template <bool kGrad>
+struct Smem8 {
+  // (an MN-major box is 128 bytes wide: 32 columns of it are the next tile's)
+  static constexpr int kStages = kGrad ? 5 : 6, kB = kGrad ? kK * 128 : kHalfN * kK, kStage = kHalf * kK + kB;
+  static constexpr int kTx = kStage + kScaleBytes;
+  static constexpr size_t kBoxes = (size_t)kStages * kStage, kScales = kBoxes + (size_t)kEpiWarps * kWarpBytes;
+  static constexpr size_t kBars = kScales + (size_t)kStages * kScaleBytes, kBytes = 1024 + kBars + 512;
+  static_assert(kBytes <= 232448, "shared memory of one SM");
+  static_assert(kStage % 1024 == 0 && kWarpBytes % 1024 == 0 && kScaleBytes % 128 == 0, "swizzled boxes repeat every 1024 bytes");
+};
+constexpr int kScaleCol = 2 * kN;                       // TMEM: accumulators, then 16 columns a stage for the scales
+
+struct Params8 {
+  CUtensorMap a, b, sa, sb, y;
+  Schedule sch;
+  int32_t m, n;
+  float* parts;
+  uint64_t wait_ns;
+  Store out;
+};
+
+// Scales as the tensor memory takes them: the 128 of a block of rows as 32 x 16
+// bytes, row 32 j + l at word 4 l + j, in a word's low byte.  Activations: (group,
+// 128 tokens); weights: (group, tile of columns, two blocks of 128).
+struct ScaleParams {
+  const float *x, *w;
+  int64_t ldx, ldw, tokens;
+  int32_t n, groups, row_blocks, tiles_n;
+  bool grad;
+  uint32_t *sa, *sb;
+};
+__device__ __forceinline__ uint32_t exponent(float s) { return __float_as_uint(s) >> 23; }     // 255 for NaN
+__global__ void __launch_bounds__(256) scales_kernel(const ScaleParams p) {
+  griddep_wait();
+  griddep_launch_dependents();
+  const int64_t a = (int64_t)p.groups * p.row_blocks * 128, all = a + (int64_t)p.groups * p.tiles_n * 256;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    if (i < a) {       // threads in the order of the rows
+      const int r = (int)(i & 127);
+      const int64_t block = i >> 7, g = block / p.row_blocks, token = (block - g * p.row_blocks) * 128 + r;
+      p.sa[block * 128 + (r & 31) * 4 + (r >> 5)] = token < p.tokens ? exponent(p.x[g * p.ldx + token]) : 0u;
+    } else {
+      const int64_t k = i - a, block = k >> 7;
+      const int64_t g = block / (2 * p.tiles_n), b = block - g * 2 * p.tiles_n, tile = b >> 1;
+      const int c = (int)(k & 127), w = ((c & 3) * 32 + (c >> 2)) + (int)(b & 1) * 128;     // word c of the block holds this column
+      const int64_t col = tile * kN + w;
+      uint32_t v = 0;
+      if (w < kN && col < p.n) v = exponent(p.grad ? p.w[g * p.ldw + col / kBlock] : p.w[col / kBlock * p.ldw + g]);
+      p.sb[k] = v;
+    }
+  }
+}
+
+// Instruction descriptor, kind::mxf8f6f4: A and B e4m3, scales ue8m0 (bit 23),
+// byte 0 of a scale's word, N >> 3 at bit 17, M >> 7 at bit 27.
+constexpr uint32_t idesc8(bool b_mn_major) {
+  return ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(kN >> 3) << 17) | (1u << 23) | ((uint32_t)(kTileM >> 7) << 27);
+}
+__device__ __forceinline__ void umma_mx8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
+      : "memory");
+}
+// 32 x 16 bytes of shared memory to four columns of every lane quadrant, in both
+// CTAs; MMAs issued after it by the same thread see them.
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint32_t smem) {
+  // no swizzle: eight rows of 16 bytes side by side, 128 bytes apart
+  const uint64_t desc = (uint64_t)((smem >> 4) & 0x3FFFu) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+
+template <bool kGrad>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8_kernel(const __grid_constant__ Params8 p) {
+  using S = Smem8<kGrad>;
+  constexpr int kStages = S::kStages;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kBars);
+  uint64_t* empty = full + kStages;
+  uint64_t* accfull = empty + kStages;
+  uint64_t* accempty = accfull + 2;
+  uint64_t* done = accempty + 2;
+  ProducerLog<kStages>* log = reinterpret_cast<ProducerLog<kStages>*>(done + 1);
+  int* armed = reinterpret_cast<int*>(log + 1);       // last phase CTA 0 armed on each stage, or -1 (producer lane)
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(armed + kStages);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+  const int pair = blockIdx.x >> 1;
+  const Schedule& sch = p.sch;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+      armed[s] = -1;
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&accfull[b], 1);
+      mbar_init(&accempty[b], 2 * kEpiWarps);
+    }
+    mbar_init(done, 1);
+    log->n = 0;
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    tmem_alloc(tmem_slot, kTmemCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  cluster_sync();   // barriers of both CTAs initialised
+  tc_fence_after();
+  griddep_wait();   // the operands are there
+  griddep_launch_dependents();
+  const uint32_t tmem_base = *tmem_slot;
+  const uint64_t wait_ns = p.wait_ns;
+
+  if (warp == 0) {
+    // -------------------------------- producer ---------------------------------
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      Items items(sch, pair);
+      Item it;
+      while (ok && items.next(sch, it)) {
+        const int row = it.tm * kTileM + (int)rank * kHalf, col = it.tn * kN + (int)rank * kHalfN;
+        for (int kb = it.kb0; kb < it.kb1; ++kb) {
+          if (!await(&empty[stage], ph ^ 1u, abort_flag, wait_ns)) {
+            ok = false;
+            break;
+          }
+          uint8_t* sa = smem + (size_t)stage * S::kStage;
+          uint8_t* sb = sa + kHalf * kK;
+          uint8_t* ss = smem + S::kScales + (size_t)stage * kScaleBytes;
+          const uint32_t fb = peer_addr(&full[stage], 0);
+          if (rank == 0) {
+            mbar_arrive_expect_tx(&full[stage], 2u * S::kTx);
+            armed[stage] = (int)ph;
+          }
+          log->bytes[stage] = S::kTx;
+          log->n += 1u;
+          tma_load_3d(sa, &p.a, fb, kb * kK, row, 0);
+          if (kGrad) tma_load_3d(sb, &p.b, fb, col, kb * kK, 0);
+          else tma_load_3d(sb, &p.b, fb, kb * kK, col, 0);
+          tma_load_3d(ss, &p.sa, fb, 0, row / 128, kb);
+          tma_load_3d(ss + 512, &p.sb, fb, 0, it.tn, kb);
+          if (++stage == kStages) {
+            stage = 0;
+            ph ^= 1u;
+          }
+        }
+      }
+      if (!ok) *abort_flag = 1;
+    }
+  } else if (warp == 1) {
+    // -------------------------------- MMA issuer -------------------------------
+    if (lane == 0 && rank == 0) {
+      constexpr uint32_t idesc = idesc8(kGrad);
+      // 32 of the sum: 32 bytes of a row (K-major), 32 rows of 128 bytes (MN-major)
+      constexpr uint64_t a_step = 32 >> 4, b_step = (kGrad ? 4096 : 32) >> 4;
+      int stage = 0, ab = 0;
+      uint32_t ph = 0, aph = 0;
+      bool ok = true;
+      Items items(sch, pair);
+      Item it;
+      while (ok && items.next(sch, it)) {
+        for (int kc = it.kb0; ok && kc < it.kb1;) {
+          const int ke = min(kc + kChunk8, it.kb1);
+          if (!await(&accempty[ab], aph ^ 1u, abort_flag, wait_ns)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t d = tmem_base + (uint32_t)(ab * kN);
+          for (int kb = kc; kb < ke; ++kb) {
+            if (!await(&full[stage], ph, abort_flag, wait_ns)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            const uint32_t sa = smem_u32(smem + (size_t)stage * S::kStage), ss = smem_u32(smem + S::kScales + (size_t)stage * kScaleBytes);
+            const uint64_t a0 = sw128_desc(sa, 16, 1024), b0 = sw128_desc(sa + kHalf * kK, 16, 1024);
+            // a stage's columns are written again once its MMAs are done (its empty barrier)
+            const uint32_t ta = tmem_base + (uint32_t)(kScaleCol + 16 * stage), tb = ta + 4;
+            copy_scales(ta, ss);
+            copy_scales(tb, ss + 512);
+            copy_scales(tb + 4, ss + 1024);
+#pragma unroll
+            for (int kk = 0; kk < kK / 32; ++kk) umma_mx8(d, a0 + kk * a_step, b0 + kk * b_step, idesc, ta, tb, (kb == kc && kk == 0) ? 0u : 1u);
+            umma_commit_pair(&empty[stage]);
+            if (++stage == kStages) {
+              stage = 0;
+              ph ^= 1u;
+            }
+          }
+          if (!ok) break;
+          umma_commit_pair(&accfull[ab]);
+          ab ^= 1;
+          if (ab == 0) aph ^= 1u;
+          kc = ke;
+        }
+      }
+      if (!ok) *abort_flag = 1;
+      umma_commit_local(done);   // all issued MMAs complete before TMEM is released
+      volatile int never = 0;
+      await(done, 0, &never, kCleanupWaitNs);
+    }
+  } else if (warp >= kFirstEpi) {
+    // --------------------------------- epilogue ----------------------------------
+    const int half = (warp - kFirstEpi) >> 2, q = warp & 3, r0 = (int)rank * kHalf + q * 32;
+    const uint32_t box = smem_u32(smem + S::kBoxes + (size_t)(warp - kFirstEpi) * kWarpBytes);
+    const uint32_t lanes = (uint32_t)(q * 32) << 16;
+    const float nan = __int_as_float(0x7FC00000);
+    int ab = 0;
+    uint32_t aph = 0;
+    bool ok = true;
+    Items items(sch, pair);
+    Item it;
+    while (items.next(sch, it)) {
+      const int row0 = it.tm * kTileM + r0, c0 = half * kHalfN, col0 = it.tn * kN + c0, rows = min(32, p.m - row0);
+      float acc[3][32];
+      for (int kc = it.kb0; kc < it.kb1; kc += kChunk8) {
+        // one answer for the warp: the TMEM loads below are taken by all lanes or none
+        ok = ok && __all_sync(0xFFFFFFFFu, await(&accfull[ab], aph, abort_flag, wait_ns));
+        if (!ok) {
+          *abort_flag = 1;
+          break;
+        }
+        tc_fence_after();
+        const uint32_t from = tmem_base + (uint32_t)(ab * kN + c0) + lanes;
+        if (kc == it.kb0) {
+#pragma unroll
+          for (int b = 0; b < 3; ++b) tmem_load(from + 32 * b, acc[b]);
+#pragma unroll
+          for (int b = 0; b < 3; ++b) tmem_wait(acc[b]);
+        } else {
+#pragma unroll
+          for (int b = 0; b < 3; ++b) {
+            float r[32];
+            tmem_load(from + 32 * b, r);
+            tmem_wait(r);
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) {
+              const float2 v = add2(make_float2(acc[b][e], acc[b][e + 1]), make_float2(r[e], r[e + 1]));
+              acc[b][e] = v.x;
+              acc[b][e + 1] = v.y;
+            }
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive_cta0(&accempty[ab]);
+        ab ^= 1;
+        if (ab == 0) aph ^= 1u;
+      }
+      if (!ok) {
+#pragma unroll
+        for (int b = 0; b < 3; ++b)
+#pragma unroll
+          for (int e = 0; e < 32; ++e) acc[b][e] = nan;
+      }
+      if (rows <= 0) continue;
+      box_free(lane);
+      if (it.slot < 0 && p.out.tma && p.out.dt == LM_BF16) {
+        // boxes of 32 x 64 bytes, 64-byte swizzle
+#pragma unroll
+        for (int b = 0; b < 3; ++b)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float* v = &acc[b][8 * e];
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box + b * 2048 + lane * 64 + ((e ^ ((lane >> 1) & 3)) << 4)), "r"(pack_bf2(v[0], v[1])),
+                         "r"(pack_bf2(v[2], v[3])), "r"(pack_bf2(v[4], v[5])), "r"(pack_bf2(v[6], v[7]))
+                         : "memory");
+          }
+        box_ready();
+        if (lane == 0) {
+#pragma unroll
+          for (int b = 0; b < 3; ++b)
+            if (col0 + 32 * b < p.n) box_store(&p.y, box + b * 2048, col0 + 32 * b, row0, 0);
+          bulk_commit();
+        }
+        continue;
+      }
+      Place at;
+      at.lane = lane;
+      at.box = box;
+#pragma unroll
+      for (int b = 0; b < 3; ++b) {
+        const int c = col0 + 32 * b;
+        if (c >= p.n) continue;
+        if (it.slot >= 0) {
+          float* part = p.parts + (size_t)it.slot * (kTileM * kN);
+          put_block(acc[b], at, rows, c0 + 32 * b, [&](int r, int col, float4 v) { *reinterpret_cast<float4*>(part + (size_t)(r0 + r) * kN + col) = v; });
+        } else if (p.out.tma) {
+          box_free(lane);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) box_put(box, lane, e, &acc[b][4 * e]);
+          box_ready();
+          if (lane == 0) {
+            box_store(&p.y, box, c, row0, 0);
+            bulk_commit();
+          }
+        } else {
+          put_block(acc[b], at, rows, c, [&](int r, int col, float4 v) {
+            if (col < p.n) p.out.put(row0 + r, col, v, p.n - col);
+          });
+        }
+      }
+    }
+    if (lane == 0) bulk_wait_all();   // stores from the boxes
+  }
+
+  __syncwarp();
+  pair_finish<kStages>(*log, abort_flag, full, armed, rank);
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, kTmemCols);
+  }
+}
+
+cudaError_t encode(CUtensorMap* m, CUtensorMapDataType type, int size, const void* base, int64_t cols, int64_t rows, int64_t planes, int64_t ld, int64_t plane,
+                   int box_cols, int box_rows, CUtensorMapSwizzle swizzle) {
+  const PFN_cuTensorMapEncodeTiled_v12000 enc = encode_fn();
+  if (enc == nullptr) return cudaErrorNotSupported;
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes}, strides[2] = {(cuuint64_t)(ld * size), (cuuint64_t)(plane * size)};
+  const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1}, estr[3] = {1, 1, 1};
+  return enc(m, type, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+             ? cudaSuccess
+             : cudaErrorInvalidValue;
+}
+
 struct Layout {
-  int64_t ldx, ldw, k, n;
-  size_t x, w, parts, total;
+  int64_t k, n;
+  int32_t groups, row_blocks;
+  Schedule sch;
+  size_t sb, parts, total;     // the activations' scales, the weights', partial sums
 };
 Layout make_layout(const Linear8Params& q) {
   Layout l{};
   l.k = q.grad ? q.out : q.in;
   l.n = q.grad ? q.in : q.out;
-  l.ldx = (l.k + 7) / 8 * 8;
-  l.ldw = ((int64_t)q.in + 7) / 8 * 8;
-  auto up = [](size_t v) { return (v + 255) / 256 * 256; };
-  l.w = up((size_t)q.tokens * l.ldx * 2);
-  l.parts = l.w + up((size_t)q.out * l.ldw * 2);
-  l.total = l.parts + parts_bytes(split_schedule(q.tokens, l.n, l.k));
+  l.groups = (int32_t)((l.k + kBlock - 1) / kBlock);
+  l.row_blocks = (int32_t)((q.tokens + 127) / 128);
+  l.sch = split_schedule(q.tokens, l.n, l.k, kN, kK);
+  l.sb = (size_t)l.groups * l.row_blocks * 512;
+  l.parts = l.sb + (size_t)l.groups * l.sch.tiles_n * 1024;
+  l.total = l.parts + parts_bytes(l.sch, kN);
   return l;
+}
+
+template <bool kGrad>
+cudaError_t start8(const Params8& p, cudaStream_t st) {
+  const int dev = device_slot();
+  static bool ready[kMaxDevices];
+  if (dev < 0 || !ready[dev]) {
+    const cudaError_t e = cudaFuncSetAttribute(linear8_kernel<kGrad>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem8<kGrad>::kBytes);
+    if (e != cudaSuccess) return e;
+    if (dev >= 0) ready[dev] = true;
+  }
+  return launch_after(linear8_kernel<kGrad>, dim3(2 * pairs_of(p.sch)), kThreads, Smem8<kGrad>::kBytes, st, p);
 }
 
 }  // namespace
@@ -142,36 +506,46 @@ cudaError_t launch_weight8_unpack(lm_dtype dt, const Blocks& c, int64_t nrows, i
   const int vec = rows::aligned(w, dt == LM_F32 ? 4 : 2, nrows);
   const dim3 grid(blocks_for(nrows, cols));
   if (dt == LM_F32)
-    return launch_after(values_kernel<float, false>, grid, 256, 0, st, (const uint8_t*)c.data, c.ld, (const float*)c.scales, c.ld_scales, nrows, cols,
+    return launch_after(values_kernel<float>, grid, 256, 0, st, (const uint8_t*)c.data, c.ld, (const float*)c.scales, c.ld_scales, nrows, cols,
                         static_cast<float*>(w.data), w.ld, vec);
-  return launch_after(values_kernel<__nv_bfloat16, false>, grid, 256, 0, st, (const uint8_t*)c.data, c.ld, (const float*)c.scales, c.ld_scales, nrows, cols,
+  return launch_after(values_kernel<__nv_bfloat16>, grid, 256, 0, st, (const uint8_t*)c.data, c.ld, (const float*)c.scales, c.ld_scales, nrows, cols,
                       static_cast<__nv_bfloat16*>(w.data), w.ld, vec);
 }
 
-size_t linear8_workspace(const Linear8Params& q) { return q.tokens <= 0 ? 0 : make_layout(q).total; }
+size_t linear8_workspace(const Linear8Params& q) { return q.tokens <= 0 || q.in <= 0 || q.out <= 0 ? 0 : make_layout(q).total; }
 
 cudaError_t launch_linear8(const Linear8Params& q, cudaStream_t st) {
   if ((q.grad ? q.out : q.in) == 0) return start_zero(q.y, q.ydt, q.tokens, q.grad ? q.in : q.out, st);
   const Layout l = make_layout(q);
   uint8_t* ws = static_cast<uint8_t*>(q.workspace);
-  __nv_bfloat16 *x = reinterpret_cast<__nv_bfloat16*>(ws), *w = reinterpret_cast<__nv_bfloat16*>(ws + l.w);
-  cudaError_t e = launch_after(values_kernel<__nv_bfloat16, true>, dim3(blocks_for(q.tokens, l.k)), 256, 0, st, (const uint8_t*)q.x.data, q.x.ld,
-                               (const float*)q.x.scales, q.x.ld_scales, q.tokens, l.k, x, l.ldx, 1);
+  uint32_t *sa = reinterpret_cast<uint32_t*>(ws), *sb = reinterpret_cast<uint32_t*>(ws + l.sb);
+  const ScaleParams sp{q.x.scales, q.w.scales, q.x.ld_scales, q.w.ld_scales, q.tokens, (int32_t)l.n, l.groups, l.row_blocks, l.sch.tiles_n, q.grad, sa, sb};
+  const int64_t words = (int64_t)l.groups * (l.row_blocks * 128 + (int64_t)l.sch.tiles_n * 256);
+  cudaError_t e = launch_after(scales_kernel, dim3((unsigned)std::min<int64_t>((words + 255) / 256, 152 * 8)), 256, 0, st, sp);
   if (e != cudaSuccess) return e;
-  e = launch_after(values_kernel<__nv_bfloat16, false>, dim3(blocks_for(q.out, q.in)), 256, 0, st, (const uint8_t*)q.w.data, q.w.ld,
-                   (const float*)q.w.scales, q.w.ld_scales, (int64_t)q.out, (int64_t)q.in, w, l.ldw, 1);
-  if (e != cudaSuccess) return e;
-  Params<StoreEpi> s{};
-  s.sch = split_schedule(q.tokens, l.n, l.k);
-  s.m = (int32_t)q.tokens;
-  s.n = (int32_t)l.n;
-  s.wait_ns = env_wait_limit_ns();
-  s.parts = reinterpret_cast<float*>(ws + l.parts);
-  const Mat y{q.y.data, q.y.ld};
-  s.epi.out = make_store(y, q.ydt, q.tokens, false);
-  if ((e = encode_operand(&s.a, x, l.k, q.tokens, l.ldx, false)) != cudaSuccess) return e;
-  if ((e = encode_operand(&s.b, w, q.in, q.out, l.ldw, q.grad)) != cudaSuccess) return e;
-  return q.grad ? start_store<kRowsK, kRowsMn>(s, st) : start_store<kRowsK, kRowsK>(s, st);
+  Params8 p{};
+  p.sch = l.sch;
+  p.m = (int32_t)q.tokens;
+  p.n = (int32_t)l.n;
+  p.wait_ns = env_wait_limit_ns();
+  p.parts = reinterpret_cast<float*>(ws + l.parts);
+  p.out = make_store(q.y, q.ydt, q.tokens, false);
+  const int64_t ld = q.tokens > 1 ? q.y.ld : l.n, size = q.ydt == LM_F32 ? 4 : 2;
+  if (reinterpret_cast<uintptr_t>(q.y.data) % 16 == 0 && ld * size % 16 == 0 && ld < ((int64_t)1 << 37) / q.tokens) {
+    e = q.ydt == LM_F32 ? encode(&p.y, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, q.y.data, l.n, q.tokens, 1, ld, ld * q.tokens, 32, 32, CU_TENSOR_MAP_SWIZZLE_128B)
+                        : encode(&p.y, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, q.y.data, l.n, q.tokens, 1, ld, ld * q.tokens, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+    if (e != cudaSuccess) return e;
+    p.out.tma = 1;
+  }
+  const CUtensorMapDataType u8 = CU_TENSOR_MAP_DATA_TYPE_UINT8, u32 = CU_TENSOR_MAP_DATA_TYPE_UINT32;
+  const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B, none = CU_TENSOR_MAP_SWIZZLE_NONE;
+  if ((e = encode(&p.a, u8, 1, q.x.data, l.k, q.tokens, 1, q.x.ld, q.x.ld * q.tokens, kK, kHalf, sw)) != cudaSuccess) return e;
+  if ((e = encode(&p.b, u8, 1, q.w.data, q.in, q.out, 1, q.w.ld, q.w.ld * q.out, 128, q.grad ? kK : kHalfN, sw)) != cudaSuccess) return e;
+  if ((e = encode(&p.sa, u32, 4, sa, 128, l.row_blocks, l.groups, 128, 128 * (int64_t)l.row_blocks, 128, 1, none)) != cudaSuccess) return e;
+  if ((e = encode(&p.sb, u32, 4, sb, 256, l.sch.tiles_n, l.groups, 256, 256 * (int64_t)l.sch.tiles_n, 256, 1, none)) != cudaSuccess) return e;
+  e = q.grad ? start8<true>(p, st) : start8<false>(p, st);
+  if (e != cudaSuccess || !has_parts(p.sch)) return e;
+  return start_join<kN>(p.sch, p.m, p.n, p.parts, p.out, st);
 }
 
 }  // namespace lm
