@@ -125,17 +125,21 @@ constexpr int kN = 192, kHalfN = kN / 2, kK = 128;      // tile columns; of the 
 constexpr int kChunk8 = 8;                              // most blocks summed in one accumulator: 32 additions
 constexpr int kScaleBytes = 512 + 1024;                 // of a block: the CTA's rows', the tile's columns'
 constexpr int kWarpBytes = 3 * 32 * 64;                 // an epilogue warp's boxes: three of 32 columns in bf16, one in fp32
+constexpr int kScaleCol = 2 * kN;                       // TMEM: accumulators, then 16 columns for each four groups' scales
+constexpr int kScaleSlots = 8;
+static_assert(kScaleCol + 16 * kScaleSlots <= kTmemCols, "tensor memory");
 template <bool kGrad>
 struct Smem8 {
   // (an MN-major box is 128 bytes wide: 32 columns of it are the next tile's)
   static constexpr int kStages = kGrad ? 5 : 6, kB = kGrad ? kK * 128 : kHalfN * kK, kStage = kHalf * kK + kB;
-  static constexpr int kTx = kStage + kScaleBytes;
   static constexpr size_t kBoxes = (size_t)kStages * kStage, kScales = kBoxes + (size_t)kEpiWarps * kWarpBytes;
   static constexpr size_t kBars = kScales + (size_t)kStages * kScaleBytes, kBytes = 1024 + kBars + 512;
   static_assert(kBytes <= 232448, "shared memory of one SM");
+  // scales go where MMAs of a block at least kStages back read theirs: those are
+  // done, since a stage is filled again only then
+  static_assert(kScaleSlots >= kStages, "slots of the scales");
   static_assert(kStage % 1024 == 0 && kWarpBytes % 1024 == 0 && kScaleBytes % 128 == 0, "swizzled boxes repeat every 1024 bytes");
 };
-constexpr int kScaleCol = 2 * kN;                       // TMEM: accumulators, then 16 columns a stage for the scales
 
 struct Params8 {
   CUtensorMap a, b, sa, sb, y;
@@ -147,12 +151,13 @@ struct Params8 {
 };
 
 // Scales as the tensor memory takes them: the 128 of a block of rows as 32 x 16
-// bytes, row 32 j + l at word 4 l + j, in a word's low byte.  Activations: (group,
-// 128 tokens); weights: (group, tile of columns, two blocks of 128).
+// bytes, row 32 j + l at word 4 l + j, four groups of the sum in a word's bytes.
+// Activations: (four groups, 128 tokens); weights: (four groups, tile of columns,
+// two blocks of 128).
 struct ScaleParams {
   const float *x, *w;
   int64_t ldx, ldw, tokens;
-  int32_t n, groups, row_blocks, tiles_n;
+  int32_t n, groups, fours, row_blocks, tiles_n;
   bool grad;
   uint32_t *sa, *sb;
 };
@@ -160,42 +165,62 @@ __device__ __forceinline__ uint32_t exponent(float s) { return __float_as_uint(s
 __global__ void __launch_bounds__(256) scales_kernel(const ScaleParams p) {
   griddep_wait();
   griddep_launch_dependents();
-  const int64_t a = (int64_t)p.groups * p.row_blocks * 128, all = a + (int64_t)p.groups * p.tiles_n * 256;
+  const int64_t a = (int64_t)p.fours * p.row_blocks * 128, all = a + (int64_t)p.fours * p.tiles_n * 256;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    uint32_t v = 0;
     if (i < a) {       // threads in the order of the rows
       const int r = (int)(i & 127);
-      const int64_t block = i >> 7, g = block / p.row_blocks, token = (block - g * p.row_blocks) * 128 + r;
-      p.sa[block * 128 + (r & 31) * 4 + (r >> 5)] = token < p.tokens ? exponent(p.x[g * p.ldx + token]) : 0u;
+      const int64_t block = i >> 7, four = block / p.row_blocks, token = (block - four * p.row_blocks) * 128 + r;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (token < p.tokens && 4 * four + k < p.groups) v |= exponent(p.x[(4 * four + k) * p.ldx + token]) << (8 * k);
+      p.sa[block * 128 + (r & 31) * 4 + (r >> 5)] = v;
     } else {
-      const int64_t k = i - a, block = k >> 7;
-      const int64_t g = block / (2 * p.tiles_n), b = block - g * 2 * p.tiles_n, tile = b >> 1;
-      const int c = (int)(k & 127), w = ((c & 3) * 32 + (c >> 2)) + (int)(b & 1) * 128;     // word c of the block holds this column
+      const int64_t at = i - a, block = at >> 7;
+      const int64_t four = block / (2 * p.tiles_n), b = block - four * 2 * p.tiles_n, tile = b >> 1;
+      const int c = (int)(at & 127), w = ((c & 3) * 32 + (c >> 2)) + (int)(b & 1) * 128;     // word c of the block holds this column
       const int64_t col = tile * kN + w;
-      uint32_t v = 0;
-      if (w < kN && col < p.n) v = exponent(p.grad ? p.w[g * p.ldw + col / kBlock] : p.w[col / kBlock * p.ldw + g]);
-      p.sb[k] = v;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int64_t g = 4 * four + k;
+        if (w < kN && col < p.n && g < p.groups) v |= exponent(p.grad ? p.w[g * p.ldw + col / kBlock] : p.w[col / kBlock * p.ldw + g]) << (8 * k);
+      }
+      p.sb[at] = v;
     }
   }
 }
 
 // Instruction descriptor, kind::mxf8f6f4: A and B e4m3, scales ue8m0 (bit 23),
-// byte 0 of a scale's word, N >> 3 at bit 17, M >> 7 at bit 27.
+// the byte of a scale's word at bits 4 (B) and 29 (A), N >> 3 at bit 17, M >> 7
+// at bit 27.
 constexpr uint32_t idesc8(bool b_mn_major) {
   return ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(kN >> 3) << 17) | (1u << 23) | ((uint32_t)(kTileM >> 7) << 27);
 }
-__device__ __forceinline__ void umma_mx8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
+// The whole warp comes here, so that what the instruction takes is the same in
+// every lane and needs no move from a lane's registers; the leader issues it.
+__device__ __forceinline__ void umma_mx8(uint32_t leader, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-      "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %6, 0;\n\tsetp.ne.b32 q, %7, 0;\n\t"
+      "@q tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate), "r"(leader)
       : "memory");
+}
+// Whether the phase is over, at once.
+__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
 }
 // 32 x 16 bytes of shared memory to four columns of every lane quadrant, in both
 // CTAs; MMAs issued after it by the same thread see them.
-__device__ __forceinline__ void copy_scales(uint32_t tmem, uint32_t smem) {
+__device__ __forceinline__ void copy_scales(uint32_t leader, uint32_t tmem, uint32_t smem) {
   // no swizzle: eight rows of 16 bytes side by side, 128 bytes apart
   const uint64_t desc = (uint64_t)((smem >> 4) & 0x3FFFu) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
-  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(tmem), "l"(desc), "r"(leader) : "memory");
 }
 
 template <bool kGrad>
@@ -214,7 +239,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(armed + kStages);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   const int pair = blockIdx.x >> 1;
   const Schedule& sch = p.sch;
@@ -265,17 +290,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
           uint8_t* sb = sa + kHalf * kK;
           uint8_t* ss = smem + S::kScales + (size_t)stage * kScaleBytes;
           const uint32_t fb = peer_addr(&full[stage], 0);
+          const bool scales = kb == it.kb0 || (kb & 3) == 0;      // the next four groups'
+          const uint32_t tx = S::kStage + (scales ? kScaleBytes : 0);
           if (rank == 0) {
-            mbar_arrive_expect_tx(&full[stage], 2u * S::kTx);
+            mbar_arrive_expect_tx(&full[stage], 2u * tx);
             armed[stage] = (int)ph;
           }
-          log->bytes[stage] = S::kTx;
+          log->bytes[stage] = tx;
           log->n += 1u;
           tma_load_3d(sa, &p.a, fb, kb * kK, row, 0);
           if (kGrad) tma_load_3d(sb, &p.b, fb, col, kb * kK, 0);
           else tma_load_3d(sb, &p.b, fb, kb * kK, col, 0);
-          tma_load_3d(ss, &p.sa, fb, 0, row / 128, kb);
-          tma_load_3d(ss + 512, &p.sb, fb, 0, it.tn, kb);
+          if (scales) {
+            tma_load_3d(ss, &p.sa, fb, 0, row / 128, kb >> 2);
+            tma_load_3d(ss + 512, &p.sb, fb, 0, it.tn, kb >> 2);
+          }
           if (++stage == kStages) {
             stage = 0;
             ph ^= 1u;
@@ -286,56 +315,74 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
     }
   } else if (warp == 1) {
     // -------------------------------- MMA issuer -------------------------------
-    if (lane == 0 && rank == 0) {
+    if (rank == 0) {
       constexpr uint32_t idesc = idesc8(kGrad);
       // 32 of the sum: 32 bytes of a row (K-major), 32 rows of 128 bytes (MN-major)
       constexpr uint64_t a_step = 32 >> 4, b_step = (kGrad ? 4096 : 32) >> 4;
-      int stage = 0, ab = 0;
-      uint32_t ph = 0, aph = 0;
-      bool ok = true;
+      const uint32_t leader = lane == 0 ? 1u : 0u, smem0 = smem_u32(smem), tmem0 = __shfl_sync(0xFFFFFFFFu, tmem_base, 0);
+      int stage = 0, ab = 0, slot = 0;
+      uint32_t ph = 0, aph = 0, ta = 0;
+      bool ok = true, ready = false;
       Items items(sch, pair);
       Item it;
       while (ok && items.next(sch, it)) {
         for (int kc = it.kb0; ok && kc < it.kb1;) {
           const int ke = min(kc + kChunk8, it.kb1);
-          if (!await(&accempty[ab], aph ^ 1u, abort_flag, wait_ns)) {
+          if (!__all_sync(0xFFFFFFFFu, await(&accempty[ab], aph ^ 1u, abort_flag, wait_ns))) {
             ok = false;
             break;
           }
           tc_fence_after();
-          const uint32_t d = tmem_base + (uint32_t)(ab * kN);
+          const uint32_t d = tmem0 + (uint32_t)(ab * kN);
           for (int kb = kc; kb < ke; ++kb) {
-            if (!await(&full[stage], ph, abort_flag, wait_ns)) {
+            if (!ready && !__all_sync(0xFFFFFFFFu, await(&full[stage], ph, abort_flag, wait_ns))) {
               ok = false;
               break;
             }
             tc_fence_after();
-            const uint32_t sa = smem_u32(smem + (size_t)stage * S::kStage), ss = smem_u32(smem + S::kScales + (size_t)stage * kScaleBytes);
+            const uint32_t sa = smem0 + (uint32_t)(stage * S::kStage);
             const uint64_t a0 = sw128_desc(sa, 16, 1024), b0 = sw128_desc(sa + kHalf * kK, 16, 1024);
-            // a stage's columns are written again once its MMAs are done (its empty barrier)
-            const uint32_t ta = tmem_base + (uint32_t)(kScaleCol + 16 * stage), tb = ta + 4;
-            copy_scales(ta, ss);
-            copy_scales(tb, ss + 512);
-            copy_scales(tb + 4, ss + 1024);
-#pragma unroll
-            for (int kk = 0; kk < kK / 32; ++kk) umma_mx8(d, a0 + kk * a_step, b0 + kk * b_step, idesc, ta, tb, (kb == kc && kk == 0) ? 0u : 1u);
-            umma_commit_pair(&empty[stage]);
-            if (++stage == kStages) {
-              stage = 0;
-              ph ^= 1u;
+            if (kb == it.kb0 || (kb & 3) == 0) {
+              const uint32_t ss = smem0 + (uint32_t)(S::kScales + (size_t)stage * kScaleBytes);
+              ta = tmem0 + (uint32_t)(kScaleCol + 16 * slot);
+              slot = (slot + 1) % kScaleSlots;
+              copy_scales(leader, ta, ss);
+              copy_scales(leader, ta + 4, ss + 512);
+              copy_scales(leader, ta + 8, ss + 1024);
             }
+            const uint32_t byte = (uint32_t)(kb & 3), id = idesc | byte << 4 | byte << 29;
+            const uint32_t at = (uint32_t)stage;
+#pragma unroll
+            for (int kk = 0; kk < kK / 32; ++kk) {
+              if (kk == kK / 32 - 1) {
+                // whether the next block is there is asked while MMAs wait in the
+                // queue, which holds few: a wait between two blocks left the tensor
+                // pipe idle for 160 cycles of 550
+                if (++stage == kStages) {
+                  stage = 0;
+                  ph ^= 1u;
+                }
+                ready = __all_sync(0xFFFFFFFFu, mbar_test(&full[stage], ph));
+              }
+              umma_mx8(leader, d, a0 + kk * a_step, b0 + kk * b_step, id, ta, ta + 4, (kb == kc && kk == 0) ? 0u : 1u);
+            }
+            if (leader) umma_commit_pair(&empty[at]);
+            __syncwarp();
           }
           if (!ok) break;
-          umma_commit_pair(&accfull[ab]);
+          if (leader) umma_commit_pair(&accfull[ab]);
+          __syncwarp();
           ab ^= 1;
           if (ab == 0) aph ^= 1u;
           kc = ke;
         }
       }
-      if (!ok) *abort_flag = 1;
-      umma_commit_local(done);   // all issued MMAs complete before TMEM is released
-      volatile int never = 0;
-      await(done, 0, &never, kCleanupWaitNs);
+      if (leader) {
+        if (!ok) *abort_flag = 1;
+        umma_commit_local(done);   // all issued MMAs complete before TMEM is released
+        volatile int never = 0;
+        await(done, 0, &never, kCleanupWaitNs);
+      }
     }
   } else if (warp >= kFirstEpi) {
     // --------------------------------- epilogue ----------------------------------
@@ -464,7 +511,7 @@ cudaError_t encode(CUtensorMap* m, CUtensorMapDataType type, int size, const voi
 
 struct Layout {
   int64_t k, n;
-  int32_t groups, row_blocks;
+  int32_t groups, fours, row_blocks;
   Schedule sch;
   size_t sb, parts, total;     // the activations' scales, the weights', partial sums
 };
@@ -473,10 +520,11 @@ Layout make_layout(const Linear8Params& q) {
   l.k = q.grad ? q.out : q.in;
   l.n = q.grad ? q.in : q.out;
   l.groups = (int32_t)((l.k + kBlock - 1) / kBlock);
+  l.fours = (l.groups + 3) / 4;
   l.row_blocks = (int32_t)((q.tokens + 127) / 128);
   l.sch = split_schedule(q.tokens, l.n, l.k, kN, kK);
-  l.sb = (size_t)l.groups * l.row_blocks * 512;
-  l.parts = l.sb + (size_t)l.groups * l.sch.tiles_n * 1024;
+  l.sb = (size_t)l.fours * l.row_blocks * 512;
+  l.parts = l.sb + (size_t)l.fours * l.sch.tiles_n * 1024;
   l.total = l.parts + parts_bytes(l.sch, kN);
   return l;
 }
@@ -519,8 +567,8 @@ cudaError_t launch_linear8(const Linear8Params& q, cudaStream_t st) {
   const Layout l = make_layout(q);
   uint8_t* ws = static_cast<uint8_t*>(q.workspace);
   uint32_t *sa = reinterpret_cast<uint32_t*>(ws), *sb = reinterpret_cast<uint32_t*>(ws + l.sb);
-  const ScaleParams sp{q.x.scales, q.w.scales, q.x.ld_scales, q.w.ld_scales, q.tokens, (int32_t)l.n, l.groups, l.row_blocks, l.sch.tiles_n, q.grad, sa, sb};
-  const int64_t words = (int64_t)l.groups * (l.row_blocks * 128 + (int64_t)l.sch.tiles_n * 256);
+  const ScaleParams sp{q.x.scales, q.w.scales, q.x.ld_scales, q.w.ld_scales, q.tokens, (int32_t)l.n, l.groups, l.fours, l.row_blocks, l.sch.tiles_n, q.grad, sa, sb};
+  const int64_t words = (int64_t)l.fours * (l.row_blocks * 128 + (int64_t)l.sch.tiles_n * 256);
   cudaError_t e = launch_after(scales_kernel, dim3((unsigned)std::min<int64_t>((words + 255) / 256, 152 * 8)), 256, 0, st, sp);
   if (e != cudaSuccess) return e;
   Params8 p{};
@@ -541,8 +589,8 @@ cudaError_t launch_linear8(const Linear8Params& q, cudaStream_t st) {
   const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B, none = CU_TENSOR_MAP_SWIZZLE_NONE;
   if ((e = encode(&p.a, u8, 1, q.x.data, l.k, q.tokens, 1, q.x.ld, q.x.ld * q.tokens, kK, kHalf, sw)) != cudaSuccess) return e;
   if ((e = encode(&p.b, u8, 1, q.w.data, q.in, q.out, 1, q.w.ld, q.w.ld * q.out, 128, q.grad ? kK : kHalfN, sw)) != cudaSuccess) return e;
-  if ((e = encode(&p.sa, u32, 4, sa, 128, l.row_blocks, l.groups, 128, 128 * (int64_t)l.row_blocks, 128, 1, none)) != cudaSuccess) return e;
-  if ((e = encode(&p.sb, u32, 4, sb, 256, l.sch.tiles_n, l.groups, 256, 256 * (int64_t)l.sch.tiles_n, 256, 1, none)) != cudaSuccess) return e;
+  if ((e = encode(&p.sa, u32, 4, sa, 128, l.row_blocks, l.fours, 128, 128 * (int64_t)l.row_blocks, 128, 1, none)) != cudaSuccess) return e;
+  if ((e = encode(&p.sb, u32, 4, sb, 256, l.sch.tiles_n, l.fours, 256, 256 * (int64_t)l.sch.tiles_n, 256, 1, none)) != cudaSuccess) return e;
   e = q.grad ? start8<true>(p, st) : start8<false>(p, st);
   if (e != cudaSuccess || !has_parts(p.sch)) return e;
   return start_join<kN>(p.sch, p.m, p.n, p.parts, p.out, st);
