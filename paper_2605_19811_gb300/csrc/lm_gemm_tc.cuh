@@ -771,7 +771,7 @@ inline Schedule plain_schedule(int64_t m, int64_t n, int64_t k, int strip, int t
 }
 // Whole waves of units, the rest shared by ranges of the sum.
 constexpr int kMostTeam = 8;      // where more columns would leave many pairs out, each is for itself
-inline Schedule split_schedule(int64_t m, int64_t n, int64_t k, int tile_n = kTileN, int block_k = kBlockK) {
+inline Schedule split_schedule(int64_t m, int64_t n, int64_t k, int tile_n = kTileN, int block_k = kBlockK, int least = kChunk) {
   Schedule s = plain_schedule(m, n, k, 1, tile_n, block_k);
   if (s.tiles_n <= kMostTeam && s.tiles_m > 1) {
     s.team = s.tiles_n;
@@ -782,8 +782,8 @@ inline Schedule split_schedule(int64_t m, int64_t n, int64_t k, int tile_n = kTi
   s.units = all / teams * teams;
   s.rest = all - s.units;
   if (s.rest > 0) {
-    // a share of at least kChunk blocks, and never more sharers than teams
-    const int64_t most = (int64_t)s.rest * s.nkb / kChunk;
+    // a share of at least `least` blocks, and never more sharers than teams
+    const int64_t most = (int64_t)s.rest * s.nkb / least;
     s.sharers = (int32_t)(most < s.rest ? s.rest : most < teams ? most : teams);
     for (int k2 = 0; k2 <= s.sharers; ++k2) s.begin[k2] = (int64_t)s.rest * s.nkb * k2 / s.sharers;
   }

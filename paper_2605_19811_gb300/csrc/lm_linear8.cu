@@ -8,12 +8,18 @@
 // power-of-two float's exponent bits are that scale, so a first kernel copies
 // them, a byte a row, in the order in which the tensor memory holds them.
 //
-// A pair takes a tile of 256 tokens x 192 columns, 128 of the sum at a time: two
-// accumulators of 192 columns leave the tensor memory room for the scales (256
-// would take all of it).  CTA r holds tokens 128 r .. (A) and columns 96 r .. (B);
-// W lies K-major for the product with W^T and MN-major for the one with W, so the
-// same codes serve both.  The sum is cut every 1024 (32 additions) and goes on in
-// fp32 registers, as in lm_gemm_tc.cuh, whose schedules are used here.
+// A pair takes a tile of 256 tokens x 256 columns, 256 of the sum at a time.  CTA r
+// holds tokens 128 r .. (A) and columns 128 r .. (B); W lies K-major for the product
+// with W^T and MN-major for the one with W, so the same codes serve both.  The sum
+// is cut every 1024 (32 additions) and goes on in fp32 registers, as in
+// lm_gemm_tc.cuh, whose schedules are used here.
+//
+// Two accumulators of 256 columns would leave the tensor memory no room for the
+// scales, so they share 32 columns: the second begins where the first has 32 left,
+// and the next 1024 of the sum begin once the epilogue has taken those.  (Tiles of
+// 192 columns, two whole accumulators, 128 of the sum a stage: 16384 x 4096 x 14336
+// 718 us.  What a stage costs the issuing warp beside its MMAs, 250 cycles, is not
+// hidden, as the queue of MMAs is short, so stages are long.)
 #include <cuda_bf16.h>
 
 #include "lm_code8.cuh"
@@ -121,25 +127,20 @@ unsigned blocks_for(int64_t nrows, int64_t cols) {
 
 // --- the product ---
 
-constexpr int kN = 192, kHalfN = kN / 2, kK = 128;      // tile columns; of the sum at a time
-constexpr int kChunk8 = 8;                              // most blocks summed in one accumulator: 32 additions
-constexpr int kScaleBytes = 512 + 1024;                 // of a block: the CTA's rows', the tile's columns'
-constexpr int kWarpBytes = 3 * 32 * 64;                 // an epilogue warp's boxes: three of 32 columns in bf16, one in fp32
-constexpr int kScaleCol = 2 * kN;                       // TMEM: accumulators, then 16 columns for each four groups' scales
-constexpr int kScaleSlots = 8;
+constexpr int kN = 256, kHalfN = kN / 2, kK = 256;      // tile columns; of the sum at a time
+constexpr int kSub = 128, kSubs = kK / kSub;            // of the sum: a swizzled row's bytes, a scale's group
+constexpr int kStages = 3, kSubA = kHalf * kSub, kSubB = kHalfN * kSub, kStage = kSubs * (kSubA + kSubB);
+constexpr int kLeastShare = 2;                          // stages of a split sum's part
+constexpr int kChunk8 = 4;                              // most stages summed in one accumulator: 32 additions
+constexpr int kScaleBytes = 512 + 1024;                 // of two stages: the CTA's rows', the tile's columns'
+constexpr int kWarpBytes = 32 * 64;                     // an epilogue warp's box: 32 columns in bf16, 16 in fp32
+constexpr int kShared = 32, kSecond = kN - kShared;     // TMEM: the second accumulator's first column
+constexpr int kScaleCol = kSecond + kN, kScaleSlots = 2;    // then 16 columns for each two stages' scales
 static_assert(kScaleCol + 16 * kScaleSlots <= kTmemCols, "tensor memory");
-template <bool kGrad>
-struct Smem8 {
-  // (an MN-major box is 128 bytes wide: 32 columns of it are the next tile's)
-  static constexpr int kStages = kGrad ? 5 : 6, kB = kGrad ? kK * 128 : kHalfN * kK, kStage = kHalf * kK + kB;
-  static constexpr size_t kBoxes = (size_t)kStages * kStage, kScales = kBoxes + (size_t)kEpiWarps * kWarpBytes;
-  static constexpr size_t kBars = kScales + (size_t)kStages * kScaleBytes, kBytes = 1024 + kBars + 512;
-  static_assert(kBytes <= 232448, "shared memory of one SM");
-  // scales go where MMAs of a block at least kStages back read theirs: those are
-  // done, since a stage is filled again only then
-  static_assert(kScaleSlots >= kStages, "slots of the scales");
-  static_assert(kStage % 1024 == 0 && kWarpBytes % 1024 == 0 && kScaleBytes % 128 == 0, "swizzled boxes repeat every 1024 bytes");
-};
+constexpr size_t kBoxes8 = (size_t)kStages * kStage, kScales8 = kBoxes8 + (size_t)kEpiWarps * kWarpBytes;
+constexpr size_t kBars8 = kScales8 + (size_t)kStages * kScaleBytes, kBytes8 = 1024 + kBars8 + 512;
+static_assert(kBytes8 <= 232448, "shared memory of one SM");
+static_assert(kSubA % 1024 == 0 && kSubB % 1024 == 0 && kWarpBytes % 512 == 0 && kScaleBytes % 128 == 0, "swizzled boxes");
 
 struct Params8 {
   CUtensorMap a, b, sa, sb, y;
@@ -205,6 +206,14 @@ __device__ __forceinline__ void umma_mx8(uint32_t leader, uint32_t d, uint64_t a
       "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate), "r"(leader)
       : "memory");
 }
+// umma_commit_pair by the leader.
+__device__ __forceinline__ void commit_pair(uint32_t leader, uint64_t* bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t"
+      "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}" ::"r"(smem_u32(bar)),
+      "h"((uint16_t)0x3), "r"(leader)
+      : "memory");
+}
 // Whether the phase is over, at once.
 __device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
   uint32_t ok;
@@ -223,17 +232,42 @@ __device__ __forceinline__ void copy_scales(uint32_t leader, uint32_t tmem, uint
   asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(tmem), "l"(desc), "r"(leader) : "memory");
 }
 
+// 32 rows (one a lane) x 32 columns through a box, 16 columns at a time, then
+// eight rows a step, four columns a lane.
+template <typename Put>
+__device__ __forceinline__ void put16(const float (&v)[32], uint32_t box, int lane, int rows, const Put& put) {
+  const int q = lane & 3, r8 = lane >> 2;
+  auto at = [&](int row, int chunk) { return box + row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4); };
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float* f = v + 16 * h + 4 * e;
+      asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at(lane, e)), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]) : "memory");
+    }
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int r = r8 + 8 * k;
+      if (r >= rows) continue;
+      float4 x;
+      asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(at(r, q)) : "memory");
+      put(r, 16 * h + 4 * q, x);
+    }
+    __syncwarp();
+  }
+}
+
 template <bool kGrad>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8_kernel(const __grid_constant__ Params8 p) {
-  using S = Smem8<kGrad>;
-  constexpr int kStages = S::kStages;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kBars);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + kBars8);
   uint64_t* empty = full + kStages;
   uint64_t* accfull = empty + kStages;
   uint64_t* accempty = accfull + 2;
-  uint64_t* done = accempty + 2;
+  uint64_t* shared = accempty + 2;                    // the columns that both accumulators have are read
+  uint64_t* done = shared + 2;
   ProducerLog<kStages>* log = reinterpret_cast<ProducerLog<kStages>*>(done + 1);
   int* armed = reinterpret_cast<int*>(log + 1);       // last phase CTA 0 armed on each stage, or -1 (producer lane)
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(armed + kStages);
@@ -253,6 +287,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
     for (int b = 0; b < 2; ++b) {
       mbar_init(&accfull[b], 1);
       mbar_init(&accempty[b], 2 * kEpiWarps);
+      mbar_init(&shared[b], kEpiWarps);               // the warps of one half, in both CTAs
     }
     mbar_init(done, 1);
     log->n = 0;
@@ -273,6 +308,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
 
   if (warp == 0) {
     // -------------------------------- producer ---------------------------------
+    few_registers();
     if (lane == 0) {
       int stage = 0;
       uint32_t ph = 0;
@@ -286,24 +322,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
             ok = false;
             break;
           }
-          uint8_t* sa = smem + (size_t)stage * S::kStage;
-          uint8_t* sb = sa + kHalf * kK;
-          uint8_t* ss = smem + S::kScales + (size_t)stage * kScaleBytes;
+          uint8_t* sa = smem + (size_t)stage * kStage;
+          uint8_t* sb = sa + kSubs * kSubA;
+          uint8_t* ss = smem + kScales8 + (size_t)stage * kScaleBytes;
           const uint32_t fb = peer_addr(&full[stage], 0);
-          const bool scales = kb == it.kb0 || (kb & 3) == 0;      // the next four groups'
-          const uint32_t tx = S::kStage + (scales ? kScaleBytes : 0);
+          const bool scales = kb == it.kb0 || (kb & 1) == 0;      // four groups', of two stages
+          const uint32_t tx = kStage + (scales ? kScaleBytes : 0);
           if (rank == 0) {
             mbar_arrive_expect_tx(&full[stage], 2u * tx);
             armed[stage] = (int)ph;
           }
           log->bytes[stage] = tx;
           log->n += 1u;
-          tma_load_3d(sa, &p.a, fb, kb * kK, row, 0);
-          if (kGrad) tma_load_3d(sb, &p.b, fb, col, kb * kK, 0);
-          else tma_load_3d(sb, &p.b, fb, kb * kK, col, 0);
+#pragma unroll
+          for (int k = 0; k < kSubs; ++k) {
+            const int at = (kb * kSubs + k) * kSub;
+            tma_load_3d(sa + k * kSubA, &p.a, fb, at, row, 0);
+            if (kGrad) tma_load_3d(sb + k * kSubB, &p.b, fb, col, at, 0);
+            else tma_load_3d(sb + k * kSubB, &p.b, fb, at, col, 0);
+          }
           if (scales) {
-            tma_load_3d(ss, &p.sa, fb, 0, row / 128, kb >> 2);
-            tma_load_3d(ss + 512, &p.sb, fb, 0, it.tn, kb >> 2);
+            tma_load_3d(ss, &p.sa, fb, 0, row / 128, kb >> 1);
+            tma_load_3d(ss + 512, &p.sb, fb, 0, it.tn, kb >> 1);
           }
           if (++stage == kStages) {
             stage = 0;
@@ -315,63 +355,69 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
     }
   } else if (warp == 1) {
     // -------------------------------- MMA issuer -------------------------------
+    few_registers();
     if (rank == 0) {
       constexpr uint32_t idesc = idesc8(kGrad);
       // 32 of the sum: 32 bytes of a row (K-major), 32 rows of 128 bytes (MN-major)
       constexpr uint64_t a_step = 32 >> 4, b_step = (kGrad ? 4096 : 32) >> 4;
       const uint32_t leader = lane == 0 ? 1u : 0u, smem0 = smem_u32(smem), tmem0 = __shfl_sync(0xFFFFFFFFu, tmem_base, 0);
-      int stage = 0, ab = 0, slot = 0;
-      uint32_t ph = 0, aph = 0, ta = 0;
+      int stage = 0, ab = 0;
+      uint32_t ph = 0, aph = 0, ta = 0, blocks = 0, slot = 0, last_use[kScaleSlots] = {0, 0};   // blocks: issued so far
       bool ok = true, ready = false;
+      auto wait = [&](uint64_t* bar, uint32_t parity) {
+        if (!__all_sync(0xFFFFFFFFu, await(bar, parity, abort_flag, wait_ns))) ok = false;
+        return ok;
+      };
       Items items(sch, pair);
       Item it;
       while (ok && items.next(sch, it)) {
         for (int kc = it.kb0; ok && kc < it.kb1;) {
           const int ke = min(kc + kChunk8, it.kb1);
-          if (!__all_sync(0xFFFFFFFFu, await(&accempty[ab], aph ^ 1u, abort_flag, wait_ns))) {
-            ok = false;
-            break;
-          }
+          // this accumulator read to its end, and the other one's columns that it shares
+          // (the one before the first has none: that wait passes)
+          if (!wait(&accempty[ab], aph ^ 1u) || !wait(&shared[ab ^ 1], ab ? aph : aph ^ 1u)) break;
           tc_fence_after();
-          const uint32_t d = tmem0 + (uint32_t)(ab * kN);
+          const uint32_t d = tmem0 + (uint32_t)(ab * kSecond);
           for (int kb = kc; kb < ke; ++kb) {
-            if (!ready && !__all_sync(0xFFFFFFFFu, await(&full[stage], ph, abort_flag, wait_ns))) {
-              ok = false;
-              break;
-            }
+            if (!ready && !wait(&full[stage], ph)) break;
             tc_fence_after();
-            const uint32_t sa = smem0 + (uint32_t)(stage * S::kStage);
-            const uint64_t a0 = sw128_desc(sa, 16, 1024), b0 = sw128_desc(sa + kHalf * kK, 16, 1024);
-            if (kb == it.kb0 || (kb & 3) == 0) {
-              const uint32_t ss = smem0 + (uint32_t)(S::kScales + (size_t)stage * kScaleBytes);
-              ta = tmem0 + (uint32_t)(kScaleCol + 16 * slot);
-              slot = (slot + 1) % kScaleSlots;
+            if (kb == it.kb0 || (kb & 1) == 0) {
+              // MMAs of kStages blocks ago are done, as their stage is filled again; of
+              // later ones (an item that began or ended between two) the slot's are waited for
+              slot ^= 1u;
+              if (last_use[slot] > 0 && blocks + 1 - last_use[slot] < (uint32_t)kStages &&
+                  !wait(&empty[(last_use[slot] - 1) % kStages], ((last_use[slot] - 1) / kStages) & 1u))
+                break;
+              const uint32_t ss = smem0 + (uint32_t)(kScales8 + (size_t)stage * kScaleBytes);
+              ta = tmem0 + (uint32_t)kScaleCol + 16u * slot;
               copy_scales(leader, ta, ss);
               copy_scales(leader, ta + 4, ss + 512);
               copy_scales(leader, ta + 8, ss + 1024);
             }
-            const uint32_t byte = (uint32_t)(kb & 3), id = idesc | byte << 4 | byte << 29;
-            const uint32_t at = (uint32_t)stage;
-#pragma unroll
-            for (int kk = 0; kk < kK / 32; ++kk) {
-              if (kk == kK / 32 - 1) {
-                // whether the next block is there is asked while MMAs wait in the
-                // queue, which holds few: a wait between two blocks left the tensor
-                // pipe idle for 160 cycles of 550
-                if (++stage == kStages) {
-                  stage = 0;
-                  ph ^= 1u;
-                }
-                ready = __all_sync(0xFFFFFFFFu, mbar_test(&full[stage], ph));
-              }
-              umma_mx8(leader, d, a0 + kk * a_step, b0 + kk * b_step, id, ta, ta + 4, (kb == kc && kk == 0) ? 0u : 1u);
+            last_use[slot] = ++blocks;
+            const uint32_t sa = smem0 + (uint32_t)(stage * kStage);
+            uint64_t* const free = &empty[stage];
+            // Whether the next block is there is asked now and known after this
+            // block's MMAs: the answer comes late, behind what they read of shared
+            // memory.
+            if (++stage == kStages) {
+              stage = 0;
+              ph ^= 1u;
             }
-            if (leader) umma_commit_pair(&empty[at]);
-            __syncwarp();
+            const bool there = mbar_test(&full[stage], ph);
+#pragma unroll
+            for (int k = 0; k < kSubs; ++k) {
+              const uint64_t a0 = sw128_desc(sa + k * kSubA, 16, 1024), b0 = sw128_desc(sa + kSubs * kSubA + k * kSubB, 16, 1024);
+              const uint32_t byte = (uint32_t)((kb & 1) * kSubs + k), id = idesc | byte << 4 | byte << 29;
+#pragma unroll
+              for (int kk = 0; kk < kSub / 32; ++kk)
+                umma_mx8(leader, d, a0 + kk * a_step, b0 + kk * b_step, id, ta, ta + 4, (kb == kc && k == 0 && kk == 0) ? 0u : 1u);
+            }
+            commit_pair(leader, free);
+            ready = __all_sync(0xFFFFFFFFu, there);
           }
           if (!ok) break;
-          if (leader) umma_commit_pair(&accfull[ab]);
-          __syncwarp();
+          commit_pair(leader, &accfull[ab]);
           ab ^= 1;
           if (ab == 0) aph ^= 1u;
           kc = ke;
@@ -386,8 +432,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
     }
   } else if (warp >= kFirstEpi) {
     // --------------------------------- epilogue ----------------------------------
+    many_registers();
     const int half = (warp - kFirstEpi) >> 2, q = warp & 3, r0 = (int)rank * kHalf + q * 32;
-    const uint32_t box = smem_u32(smem + S::kBoxes + (size_t)(warp - kFirstEpi) * kWarpBytes);
+    const uint32_t box = smem_u32(smem + kBoxes8 + (size_t)(warp - kFirstEpi) * kWarpBytes);
     const uint32_t lanes = (uint32_t)(q * 32) << 16;
     const float nan = __int_as_float(0x7FC00000);
     int ab = 0;
@@ -397,7 +444,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
     Item it;
     while (items.next(sch, it)) {
       const int row0 = it.tm * kTileM + r0, c0 = half * kHalfN, col0 = it.tn * kN + c0, rows = min(32, p.m - row0);
-      float acc[3][32];
+      float acc[4][32];
       for (int kc = it.kb0; kc < it.kb1; kc += kChunk8) {
         // one answer for the warp: the TMEM loads below are taken by all lanes or none
         ok = ok && __all_sync(0xFFFFFFFFu, await(&accfull[ab], aph, abort_flag, wait_ns));
@@ -406,87 +453,86 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
           break;
         }
         tc_fence_after();
-        const uint32_t from = tmem_base + (uint32_t)(ab * kN + c0) + lanes;
-        if (kc == it.kb0) {
+        const uint32_t from = tmem_base + (uint32_t)(ab * kSecond + c0) + lanes;
+        const bool fresh = kc == it.kb0;
+        auto take = [&](float (&a)[32], int b) {
+          float r[32];
+          tmem_load(from + 32 * b, r);
+          tmem_wait(r);
 #pragma unroll
-          for (int b = 0; b < 3; ++b) tmem_load(from + 32 * b, acc[b]);
-#pragma unroll
-          for (int b = 0; b < 3; ++b) tmem_wait(acc[b]);
-        } else {
-#pragma unroll
-          for (int b = 0; b < 3; ++b) {
-            float r[32];
-            tmem_load(from + 32 * b, r);
-            tmem_wait(r);
-#pragma unroll
-            for (int e = 0; e < 32; e += 2) {
-              const float2 v = add2(make_float2(acc[b][e], acc[b][e + 1]), make_float2(r[e], r[e + 1]));
-              acc[b][e] = v.x;
-              acc[b][e + 1] = v.y;
-            }
+          for (int e = 0; e < 32; e += 2) {
+            const float2 v = add2(fresh ? make_float2(0.f, 0.f) : make_float2(a[e], a[e + 1]), make_float2(r[e], r[e + 1]));
+            a[e] = v.x;
+            a[e + 1] = v.y;
           }
+        };
+        auto arrive = [&](uint64_t* bar) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) arrive_cta0(bar);
+        };
+        // the first accumulator's last 32 columns are the second one's first
+        const bool last_first = ab == 0 && half == 1;
+        if (last_first) {
+          take(acc[3], 3);
+          arrive(&shared[0]);
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) arrive_cta0(&accempty[ab]);
+        take(acc[0], 0);
+        if (ab == 1 && half == 0) arrive(&shared[1]);
+        take(acc[1], 1);
+        take(acc[2], 2);
+        if (!last_first) take(acc[3], 3);
+        arrive(&accempty[ab]);
         ab ^= 1;
         if (ab == 0) aph ^= 1u;
       }
       if (!ok) {
 #pragma unroll
-        for (int b = 0; b < 3; ++b)
+        for (int b = 0; b < 4; ++b)
 #pragma unroll
           for (int e = 0; e < 32; ++e) acc[b][e] = nan;
       }
       if (rows <= 0) continue;
-      box_free(lane);
-      if (it.slot < 0 && p.out.tma && p.out.dt == LM_BF16) {
-        // boxes of 32 x 64 bytes, 64-byte swizzle
+      const bool whole = it.slot < 0 && p.out.tma;
 #pragma unroll
-        for (int b = 0; b < 3; ++b)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float* v = &acc[b][8 * e];
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box + b * 2048 + lane * 64 + ((e ^ ((lane >> 1) & 3)) << 4)), "r"(pack_bf2(v[0], v[1])),
-                         "r"(pack_bf2(v[2], v[3])), "r"(pack_bf2(v[4], v[5])), "r"(pack_bf2(v[6], v[7]))
-                         : "memory");
-          }
-        box_ready();
-        if (lane == 0) {
-#pragma unroll
-          for (int b = 0; b < 3; ++b)
-            if (col0 + 32 * b < p.n) box_store(&p.y, box + b * 2048, col0 + 32 * b, row0, 0);
-          bulk_commit();
-        }
-        continue;
-      }
-      Place at;
-      at.lane = lane;
-      at.box = box;
-#pragma unroll
-      for (int b = 0; b < 3; ++b) {
+      for (int b = 0; b < 4; ++b) {
         const int c = col0 + 32 * b;
         if (c >= p.n) continue;
-        if (it.slot >= 0) {
-          float* part = p.parts + (size_t)it.slot * (kTileM * kN);
-          put_block(acc[b], at, rows, c0 + 32 * b, [&](int r, int col, float4 v) { *reinterpret_cast<float4*>(part + (size_t)(r0 + r) * kN + col) = v; });
-        } else if (p.out.tma) {
-          box_free(lane);
+        if (whole) {
+          // boxes of 32 rows x 64 bytes, 64-byte swizzle: 32 columns in bf16, 16 in fp32
+          const int boxes = p.out.dt == LM_BF16 ? 1 : 2;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) box_put(box, lane, e, &acc[b][4 * e]);
-          box_ready();
-          if (lane == 0) {
-            box_store(&p.y, box, c, row0, 0);
-            bulk_commit();
+          for (int h = 0; h < 2; ++h) {
+            if (h >= boxes || c + 16 * h >= p.n) continue;
+            box_free(lane);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float *v = &acc[b][8 * e], *f = &acc[b][16 * h + 4 * e];
+              const bool two = boxes == 1;
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box + lane * 64 + ((e ^ ((lane >> 1) & 3)) << 4)),
+                           "r"(two ? pack_bf2(v[0], v[1]) : __float_as_uint(f[0])), "r"(two ? pack_bf2(v[2], v[3]) : __float_as_uint(f[1])),
+                           "r"(two ? pack_bf2(v[4], v[5]) : __float_as_uint(f[2])), "r"(two ? pack_bf2(v[6], v[7]) : __float_as_uint(f[3]))
+                           : "memory");
+            }
+            box_ready();
+            if (lane == 0) {
+              box_store(&p.y, box, c + 16 * h, row0, 0);
+              bulk_commit();
+            }
           }
         } else {
-          put_block(acc[b], at, rows, c, [&](int r, int col, float4 v) {
-            if (col < p.n) p.out.put(row0 + r, col, v, p.n - col);
+          box_free(lane);
+          put16(acc[b], box, lane, rows, [&](int r, int e, float4 v) {
+            const int col = c + e;
+            if (it.slot >= 0) *reinterpret_cast<float4*>(p.parts + (size_t)it.slot * (kTileM * kN) + (size_t)(r0 + r) * kN + (c0 + 32 * b + e)) = v;
+            else if (col < p.n) p.out.put(row0 + r, col, v, p.n - col);
           });
         }
       }
     }
     if (lane == 0) bulk_wait_all();   // stores from the boxes
+  } else {
+    few_registers();
   }
 
   __syncwarp();
@@ -522,7 +568,7 @@ Layout make_layout(const Linear8Params& q) {
   l.groups = (int32_t)((l.k + kBlock - 1) / kBlock);
   l.fours = (l.groups + 3) / 4;
   l.row_blocks = (int32_t)((q.tokens + 127) / 128);
-  l.sch = split_schedule(q.tokens, l.n, l.k, kN, kK);
+  l.sch = split_schedule(q.tokens, l.n, l.k, kN, kK, kLeastShare);
   l.sb = (size_t)l.fours * l.row_blocks * 512;
   l.parts = l.sb + (size_t)l.fours * l.sch.tiles_n * 1024;
   l.total = l.parts + parts_bytes(l.sch, kN);
@@ -534,11 +580,11 @@ cudaError_t start8(const Params8& p, cudaStream_t st) {
   const int dev = device_slot();
   static bool ready[kMaxDevices];
   if (dev < 0 || !ready[dev]) {
-    const cudaError_t e = cudaFuncSetAttribute(linear8_kernel<kGrad>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem8<kGrad>::kBytes);
+    const cudaError_t e = cudaFuncSetAttribute(linear8_kernel<kGrad>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBytes8);
     if (e != cudaSuccess) return e;
     if (dev >= 0) ready[dev] = true;
   }
-  return launch_after(linear8_kernel<kGrad>, dim3(2 * pairs_of(p.sch)), kThreads, Smem8<kGrad>::kBytes, st, p);
+  return launch_after(linear8_kernel<kGrad>, dim3(2 * pairs_of(p.sch)), kThreads, kBytes8, st, p);
 }
 
 }  // namespace
@@ -580,15 +626,15 @@ cudaError_t launch_linear8(const Linear8Params& q, cudaStream_t st) {
   p.out = make_store(q.y, q.ydt, q.tokens, false);
   const int64_t ld = q.tokens > 1 ? q.y.ld : l.n, size = q.ydt == LM_F32 ? 4 : 2;
   if (reinterpret_cast<uintptr_t>(q.y.data) % 16 == 0 && ld * size % 16 == 0 && ld < ((int64_t)1 << 37) / q.tokens) {
-    e = q.ydt == LM_F32 ? encode(&p.y, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, q.y.data, l.n, q.tokens, 1, ld, ld * q.tokens, 32, 32, CU_TENSOR_MAP_SWIZZLE_128B)
+    e = q.ydt == LM_F32 ? encode(&p.y, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, q.y.data, l.n, q.tokens, 1, ld, ld * q.tokens, 16, 32, CU_TENSOR_MAP_SWIZZLE_64B)
                         : encode(&p.y, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, q.y.data, l.n, q.tokens, 1, ld, ld * q.tokens, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
     if (e != cudaSuccess) return e;
     p.out.tma = 1;
   }
   const CUtensorMapDataType u8 = CU_TENSOR_MAP_DATA_TYPE_UINT8, u32 = CU_TENSOR_MAP_DATA_TYPE_UINT32;
   const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B, none = CU_TENSOR_MAP_SWIZZLE_NONE;
-  if ((e = encode(&p.a, u8, 1, q.x.data, l.k, q.tokens, 1, q.x.ld, q.x.ld * q.tokens, kK, kHalf, sw)) != cudaSuccess) return e;
-  if ((e = encode(&p.b, u8, 1, q.w.data, q.in, q.out, 1, q.w.ld, q.w.ld * q.out, 128, q.grad ? kK : kHalfN, sw)) != cudaSuccess) return e;
+  if ((e = encode(&p.a, u8, 1, q.x.data, l.k, q.tokens, 1, q.x.ld, q.x.ld * q.tokens, kSub, kHalf, sw)) != cudaSuccess) return e;
+  if ((e = encode(&p.b, u8, 1, q.w.data, q.in, q.out, 1, q.w.ld, q.w.ld * q.out, 128, q.grad ? kSub : kHalfN, sw)) != cudaSuccess) return e;
   if ((e = encode(&p.sa, u32, 4, sa, 128, l.row_blocks, l.fours, 128, 128 * (int64_t)l.row_blocks, 128, 1, none)) != cudaSuccess) return e;
   if ((e = encode(&p.sb, u32, 4, sb, 256, l.sch.tiles_n, l.fours, 256, 256 * (int64_t)l.sch.tiles_n, 256, 1, none)) != cudaSuccess) return e;
   e = q.grad ? start8<true>(p, st) : start8<false>(p, st);
