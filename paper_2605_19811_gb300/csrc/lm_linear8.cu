@@ -11,12 +11,13 @@
 // A pair takes a tile of 256 tokens x 256 columns, 256 of the sum at a time.  CTA r
 // holds tokens 128 r .. (A) and columns 128 r .. (B); W lies K-major for the product
 // with W^T and MN-major for the one with W, so the same codes serve both.  The sum
-// is cut every 1024 (32 additions) and goes on in fp32 registers, as in
-// lm_gemm_tc.cuh, whose schedules are used here.
+// is cut every 2048 (64 additions, each of which may drop 2^-23 of what is there)
+// and goes on in fp32 registers, as in lm_gemm_tc.cuh, whose schedules are used
+// here.  (Cut every 1024: 631 us where 597 are taken; not cut: 584.)
 //
 // Two accumulators of 256 columns would leave the tensor memory no room for the
 // scales, so they share 32 columns: the second begins where the first has 32 left,
-// and the next 1024 of the sum begin once the epilogue has taken those.  (Tiles of
+// and the next 2048 of the sum begin once the epilogue has taken those.  (Tiles of
 // 192 columns, two whole accumulators, 128 of the sum a stage: 16384 x 4096 x 14336
 // 718 us.  What a stage costs the issuing warp beside its MMAs, 250 cycles, is not
 // hidden, as the queue of MMAs is short, so stages are long.)
@@ -131,7 +132,7 @@ constexpr int kN = 256, kHalfN = kN / 2, kK = 256;      // tile columns; of the 
 constexpr int kSub = 128, kSubs = kK / kSub;            // of the sum: a swizzled row's bytes, a scale's group
 constexpr int kStages = 3, kSubA = kHalf * kSub, kSubB = kHalfN * kSub, kStage = kSubs * (kSubA + kSubB);
 constexpr int kLeastShare = 2;                          // stages of a split sum's part
-constexpr int kChunk8 = 4;                              // most stages summed in one accumulator: 32 additions
+constexpr int kChunk8 = 8;                              // most stages summed in one accumulator: 64 additions
 constexpr int kScaleBytes = 512 + 1024;                 // of two stages: the CTA's rows', the tile's columns'
 constexpr int kWarpBytes = 32 * 64;                     // an epilogue warp's box: 32 columns in bf16, 16 in fp32
 constexpr int kShared = 32, kSecond = kN - kShared;     // TMEM: the second accumulator's first column

@@ -2,9 +2,10 @@
 
 Codes and scales are compared bit by bit with the definition in 64 bits.  A
 product of two codes is exact.  The tensor cores drop up to 2^-23 of what they
-have at each addition, at most 32 additions in a row, then fp32 additions
-(2^-24) of such sums; nothing they have is above S = sum |x w|: together at most
-S (2^-18 + k / 512 2^-24).  The result is rounded once, 2^-8 (bf16) or 2^-24
+have at each addition of 32 products, at most 64 additions in a row, then fp32
+additions (2^-24) of such sums; nothing they have is above S = sum |x w|: together
+at most S (2^-17 + k / 512 2^-24).  Of a sum of one sign they have half on
+average, so that half as much is dropped.  The result is rounded once, 2^-8 (bf16) or 2^-24
 (fp32) of itself."""
 
 import numpy as np
@@ -114,7 +115,7 @@ def test_products(T, rows, cols, out, grad, to):
     n = cols if grad else out
     y = Held(rows, n, to, pad=rows % 3 * 4, offset=rows % 5)
     (T.linear8_grad if grad else T.linear8)(x, w, out=y.t)
-    bound = most * (2.0 ** -18 + (out if grad else cols) / 512 * 2.0 ** -24) + HALF[to] * want.abs()
+    bound = most * (2.0 ** -17 + (out if grad else cols) / 512 * 2.0 ** -24) + HALF[to] * want.abs()
     off = (y.t.double() - want).abs()
     assert bool((off <= bound).all()), float((off / bound).max())
     assert y.untouched()
@@ -150,7 +151,7 @@ def test_wide_scales_and_nan(T, rows, grad):
     want, most = product(cx, cw, grad)
     f = T.linear8_grad if grad else T.linear8
     y = f(cx, cw, dtype=torch.float32)
-    assert bool(((y.double() - want).abs() <= most * 2.0 ** -17.9).all())
+    assert bool(((y.double() - want).abs() <= most * 2.0 ** -16.9).all())
     x[rows - 1, 300] = float("nan")
     cx = T.checkpoint8(x, "e4m3")
     z = f(cx, cw, dtype=torch.float32)
@@ -167,10 +168,10 @@ def test_views_empty_and_refused(T):
     x, w = layer(T, 40, 256, 384, False, 1)
     one = T.Checkpoint8(x.codes[3:4], x.scales[:, 3:4], 256, "e4m3")
     assert float((T.linear8(one, w, dtype=torch.float32) - T.linear8(x, w, dtype=torch.float32)[3:4]).abs().max()) <= \
-        2.0 ** -17 * float(product(one, w, False)[1].max())
+        2.0 ** -16 * float(product(one, w, False)[1].max())
     part = T.Weight8(w.codes[128:], w.scales[1:], 256)        # rows of the weights from the second block on
     off = (T.linear8(x, part, dtype=torch.float32).double() - product(x, w, False)[0][:, 128:]).abs()
-    assert bool((off <= 2.0 ** -17.9 * product(x, w, False)[1][:, 128:]).all())
+    assert bool((off <= 2.0 ** -16.9 * product(x, w, False)[1][:, 128:]).all())
     none = T.Checkpoint8(x.codes[:0], x.scales[:, :0], 256, "e4m3")
     assert T.linear8(none, w).shape == (0, 384)
     empty = T.Weight8.empty(384, 0)
