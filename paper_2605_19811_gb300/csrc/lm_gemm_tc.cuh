@@ -785,9 +785,12 @@ inline Schedule split_schedule(int64_t m, int64_t n, int64_t k, int tile_n = kTi
     // a share of at least `least` blocks, and never more sharers than teams
     const int64_t most = (int64_t)s.rest * s.nkb / least;
     s.sharers = (int32_t)(most < s.rest ? s.rest : most < teams ? most : teams);
-    for (int k2 = 0; k2 <= s.sharers; ++k2) s.begin[k2] = (int64_t)s.rest * s.nkb * k2 / s.sharers;
   }
   return s;
+}
+// Where the sharers' ranges begin (for the launch alone).
+inline void share(Schedule& s) {
+  for (int k = 0; s.sharers > 0 && k <= s.sharers; ++k) s.begin[k] = (int64_t)s.rest * s.nkb * k / s.sharers;
 }
 inline bool has_parts(const Schedule& s) { return s.rest > 0 && s.sharers > s.rest; }
 inline size_t parts_bytes(const Schedule& s, int tile_n = kTileN) { return has_parts(s) ? 2 * (size_t)s.sharers * s.team * kTileM * tile_n * 4 : 0; }
@@ -833,6 +836,7 @@ cudaError_t start_join(const Schedule& s, int32_t m, int32_t n, const float* par
 // A product whose sums may be split: the kernel, and the join where parts are left.
 template <int kALie, int kBLie>
 cudaError_t start_store(Params<StoreEpi>& p, cudaStream_t st) {
+  share(p.sch);
   const Store& o = p.epi.out;
   const int64_t size = o.dt == LM_F32 ? 4 : 2;
   cudaError_t e = cudaSuccess;

@@ -130,7 +130,7 @@ unsigned blocks_for(int64_t nrows, int64_t cols) {
 
 constexpr int kN = 256, kHalfN = kN / 2, kK = 256;      // tile columns; of the sum at a time
 constexpr int kSub = 128, kSubs = kK / kSub;            // of the sum: a swizzled row's bytes, a scale's group
-constexpr int kStages = 3, kSubA = kHalf * kSub, kSubB = kHalfN * kSub, kStage = kSubs * (kSubA + kSubB);
+constexpr int kFewTokens = 32;
 constexpr int kLeastShare = 2;                          // stages of a split sum's part
 constexpr int kChunk8 = 8;                              // most stages summed in one accumulator: 64 additions
 constexpr int kScaleBytes = 512 + 1024;                 // of two stages: the CTA's rows', the tile's columns'
@@ -138,10 +138,20 @@ constexpr int kWarpBytes = 32 * 64;                     // an epilogue warp's bo
 constexpr int kShared = 32, kSecond = kN - kShared;     // TMEM: the second accumulator's first column
 constexpr int kScaleCol = kSecond + kN, kScaleSlots = 2;    // then 16 columns for each two stages' scales
 static_assert(kScaleCol + 16 * kScaleSlots <= kTmemCols, "tensor memory");
-constexpr size_t kBoxes8 = (size_t)kStages * kStage, kScales8 = kBoxes8 + (size_t)kEpiWarps * kWarpBytes;
-constexpr size_t kBars8 = kScales8 + (size_t)kStages * kScaleBytes, kBytes8 = 1024 + kBars8 + 512;
-static_assert(kBytes8 <= 232448, "shared memory of one SM");
-static_assert(kSubA % 1024 == 0 && kSubB % 1024 == 0 && kWarpBytes % 512 == 0 && kScaleBytes % 128 == 0, "swizzled boxes");
+// Shared memory.  kFew: at most kFewTokens tokens.  Then the weights' bytes are all
+// that counts, and more of them are under way: A is loaded, and has room, for those
+// rows alone.  The MMA reads 128 rows from A's place all the same; the others are
+// bytes of B, and the rows of the result that they reach are never stored.
+template <bool kFew>
+struct Ring {
+  static constexpr int kStages = kFew ? 5 : 3, kRowsA = kFew ? kFewTokens : kHalf, kSubA = kRowsA * kSub, kSubB = kHalfN * kSub;
+  static constexpr int kStage = kSubs * (kSubA + kSubB);
+  static constexpr size_t kBoxes = (size_t)kStages * kStage, kScales = kBoxes + (size_t)kEpiWarps * kWarpBytes;
+  static constexpr size_t kBars = kScales + (size_t)kStages * kScaleBytes, kBytes = 1024 + kBars + 512;
+  static_assert(kBytes <= 232448, "shared memory of one SM");
+  static_assert(kSubA % 1024 == 0 && kSubB % 1024 == 0 && kWarpBytes % 512 == 0 && kScaleBytes % 128 == 0, "swizzled boxes");
+  static_assert(kSubs * kSubA + kSubs * kSubB >= (kSubs - 1) * kSubA + kHalf * kSub, "128 rows from A's last place on are inside the stage");
+};
 
 struct Params8 {
   CUtensorMap a, b, sa, sb, y;
@@ -259,11 +269,13 @@ __device__ __forceinline__ void put16(const float (&v)[32], uint32_t box, int la
   }
 }
 
-template <bool kGrad>
+template <bool kGrad, bool kFew>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8_kernel(const __grid_constant__ Params8 p) {
+  using R = Ring<kFew>;
+  constexpr int kStages = R::kStages, kStage = R::kStage, kSubA = R::kSubA, kSubB = R::kSubB;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + kBars8);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + R::kBars);
   uint64_t* empty = full + kStages;
   uint64_t* accfull = empty + kStages;
   uint64_t* accempty = accfull + 2;
@@ -325,7 +337,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
           }
           uint8_t* sa = smem + (size_t)stage * kStage;
           uint8_t* sb = sa + kSubs * kSubA;
-          uint8_t* ss = smem + kScales8 + (size_t)stage * kScaleBytes;
+          uint8_t* ss = smem + R::kScales + (size_t)stage * kScaleBytes;
           const uint32_t fb = peer_addr(&full[stage], 0);
           const bool scales = kb == it.kb0 || (kb & 1) == 0;      // four groups', of two stages
           const uint32_t tx = kStage + (scales ? kScaleBytes : 0);
@@ -389,7 +401,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
               if (last_use[slot] > 0 && blocks + 1 - last_use[slot] < (uint32_t)kStages &&
                   !wait(&empty[(last_use[slot] - 1) % kStages], ((last_use[slot] - 1) / kStages) & 1u))
                 break;
-              const uint32_t ss = smem0 + (uint32_t)(kScales8 + (size_t)stage * kScaleBytes);
+              const uint32_t ss = smem0 + (uint32_t)(R::kScales + (size_t)stage * kScaleBytes);
               ta = tmem0 + (uint32_t)kScaleCol + 16u * slot;
               copy_scales(leader, ta, ss);
               copy_scales(leader, ta + 4, ss + 512);
@@ -435,7 +447,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
     // --------------------------------- epilogue ----------------------------------
     many_registers();
     const int half = (warp - kFirstEpi) >> 2, q = warp & 3, r0 = (int)rank * kHalf + q * 32;
-    const uint32_t box = smem_u32(smem + kBoxes8 + (size_t)(warp - kFirstEpi) * kWarpBytes);
+    const uint32_t box = smem_u32(smem + R::kBoxes + (size_t)(warp - kFirstEpi) * kWarpBytes);
     const uint32_t lanes = (uint32_t)(q * 32) << 16;
     const float nan = __int_as_float(0x7FC00000);
     int ab = 0;
@@ -569,23 +581,26 @@ Layout make_layout(const Linear8Params& q) {
   l.groups = (int32_t)((l.k + kBlock - 1) / kBlock);
   l.fours = (l.groups + 3) / 4;
   l.row_blocks = (int32_t)((q.tokens + 127) / 128);
-  l.sch = split_schedule(q.tokens, l.n, l.k, kN, kK, kLeastShare);
+  // few tokens: half of the pairs draw the weights as fast as all, and a sum that is
+  // not split needs no second kernel
+  l.sch = plain_schedule(q.tokens, l.n, l.k, 1, kN, kK);
+  if (q.tokens > kFewTokens || l.sch.units < kPairs / 2) l.sch = split_schedule(q.tokens, l.n, l.k, kN, kK, kLeastShare);
   l.sb = (size_t)l.fours * l.row_blocks * 512;
   l.parts = l.sb + (size_t)l.fours * l.sch.tiles_n * 1024;
   l.total = l.parts + parts_bytes(l.sch, kN);
   return l;
 }
 
-template <bool kGrad>
+template <bool kGrad, bool kFew>
 cudaError_t start8(const Params8& p, cudaStream_t st) {
   const int dev = device_slot();
   static bool ready[kMaxDevices];
   if (dev < 0 || !ready[dev]) {
-    const cudaError_t e = cudaFuncSetAttribute(linear8_kernel<kGrad>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBytes8);
+    const cudaError_t e = cudaFuncSetAttribute(linear8_kernel<kGrad, kFew>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Ring<kFew>::kBytes);
     if (e != cudaSuccess) return e;
     if (dev >= 0) ready[dev] = true;
   }
-  return launch_after(linear8_kernel<kGrad>, dim3(2 * pairs_of(p.sch)), kThreads, kBytes8, st, p);
+  return launch_after(linear8_kernel<kGrad, kFew>, dim3(2 * pairs_of(p.sch)), kThreads, Ring<kFew>::kBytes, st, p);
 }
 
 }  // namespace
@@ -620,6 +635,7 @@ cudaError_t launch_linear8(const Linear8Params& q, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   Params8 p{};
   p.sch = l.sch;
+  share(p.sch);
   p.m = (int32_t)q.tokens;
   p.n = (int32_t)l.n;
   p.wait_ns = env_wait_limit_ns();
@@ -632,13 +648,14 @@ cudaError_t launch_linear8(const Linear8Params& q, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     p.out.tma = 1;
   }
+  const bool few = q.tokens <= kFewTokens;
   const CUtensorMapDataType u8 = CU_TENSOR_MAP_DATA_TYPE_UINT8, u32 = CU_TENSOR_MAP_DATA_TYPE_UINT32;
   const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B, none = CU_TENSOR_MAP_SWIZZLE_NONE;
-  if ((e = encode(&p.a, u8, 1, q.x.data, l.k, q.tokens, 1, q.x.ld, q.x.ld * q.tokens, kSub, kHalf, sw)) != cudaSuccess) return e;
+  if ((e = encode(&p.a, u8, 1, q.x.data, l.k, q.tokens, 1, q.x.ld, q.x.ld * q.tokens, kSub, few ? kFewTokens : kHalf, sw)) != cudaSuccess) return e;
   if ((e = encode(&p.b, u8, 1, q.w.data, q.in, q.out, 1, q.w.ld, q.w.ld * q.out, 128, q.grad ? kSub : kHalfN, sw)) != cudaSuccess) return e;
   if ((e = encode(&p.sa, u32, 4, sa, 128, l.row_blocks, l.fours, 128, 128 * (int64_t)l.row_blocks, 128, 1, none)) != cudaSuccess) return e;
   if ((e = encode(&p.sb, u32, 4, sb, 256, l.sch.tiles_n, l.fours, 256, 256 * (int64_t)l.sch.tiles_n, 256, 1, none)) != cudaSuccess) return e;
-  e = q.grad ? start8<true>(p, st) : start8<false>(p, st);
+  e = q.grad ? (few ? start8<true, true>(p, st) : start8<true, false>(p, st)) : (few ? start8<false, true>(p, st) : start8<false, false>(p, st));
   if (e != cudaSuccess || !has_parts(p.sch)) return e;
   return start_join<kN>(p.sch, p.m, p.n, p.parts, p.out, st);
 }

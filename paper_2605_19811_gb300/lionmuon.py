@@ -216,24 +216,24 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.lm_linear_wgrad8.restype = c_int
     size = ctypes.c_size_t
     for fn in ("lm_linear_logprob", "lm_linear_logprob_grad"):
-        getattr(lib, fn).argtypes = [P(LmLinearLogprobArgs), c_void_p, size, c_void_p]
+        getattr(lib, fn).argtypes = [c_void_p, c_void_p, size, c_void_p]     # (a struct by reference, or its bytes)
         getattr(lib, fn).restype = c_int
-    lib.lm_linear_logprob_workspace.argtypes = [P(LmLinearLogprobArgs)]
+    lib.lm_linear_logprob_workspace.argtypes = [c_void_p]
     lib.lm_linear_logprob_workspace.restype = size
     lib.lm_weight8_pack.argtypes = [P(LmMatrix), P(LmWeight8), c_void_p]
     lib.lm_weight8_pack.restype = c_int
     lib.lm_weight8_unpack.argtypes = [P(LmWeight8), P(LmMatrix), c_void_p]
     lib.lm_weight8_unpack.restype = c_int
     for fn in ("lm_linear8", "lm_linear8_grad"):
-        getattr(lib, fn).argtypes = [P(LmCheckpoint8), P(LmWeight8), P(LmMatrix), c_void_p, size, c_void_p]
+        getattr(lib, fn).argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, size, c_void_p]
         getattr(lib, fn).restype = c_int
-    lib.lm_linear8_workspace.argtypes = [P(LmCheckpoint8), P(LmWeight8), c_int]
+    lib.lm_linear8_workspace.argtypes = [c_void_p, c_void_p, c_int]
     lib.lm_linear8_workspace.restype = size
-    lib.lm_qk_rotary.argtypes = [P(LmQkRotaryArgs), c_void_p]
+    lib.lm_qk_rotary.argtypes = [c_void_p, c_void_p]
     lib.lm_qk_rotary.restype = c_int
-    lib.lm_qk_rotary_grad.argtypes = [P(LmQkRotaryArgs), c_void_p, size, c_void_p]
+    lib.lm_qk_rotary_grad.argtypes = [c_void_p, c_void_p, size, c_void_p]
     lib.lm_qk_rotary_grad.restype = c_int
-    lib.lm_qk_rotary_grad_workspace.argtypes = [P(LmQkRotaryArgs)]
+    lib.lm_qk_rotary_grad_workspace.argtypes = [c_void_p]
     lib.lm_qk_rotary_grad_workspace.restype = size
     if path is None:
         _LIB = lib

@@ -18,13 +18,13 @@ freed early.
 from __future__ import annotations
 
 import math
+import struct
 from typing import NamedTuple, Optional
 
 import torch
 
 from . import lionmuon as _L
-from .lionmuon import (LM_BF16, LM_F32, LmCheckpoint8, LmHeads, LmLinearLogprobArgs, LmMatrix, LmQkRotaryArgs,
-                       LmTensor, LmTokenLogprobArgs, LmWeight8)
+from .lionmuon import LM_BF16, LM_F32, LmCheckpoint8, LmMatrix, LmTensor, LmTokenLogprobArgs, LmWeight8
 
 GROUP = 128                                   # channels that share one scale (LM_CODE_GROUP)
 FORMATS = {"i8": 0, "e4m3": 1}                # lm_code_format
@@ -39,8 +39,8 @@ def _dtype(t) -> int:
     return code
 
 
-def _matrix(t, what: str) -> LmMatrix:
-    """lm_matrix of a tensor (a vector is one row)."""
+def _matrix_fields(t, what: str):
+    """lm_matrix's fields of a tensor (a vector is one row)."""
     code = _DTYPES.get(t.dtype)
     if code is None:
         raise TypeError(f"{what}: unsupported dtype {t.dtype}")
@@ -59,13 +59,34 @@ def _matrix(t, what: str) -> LmMatrix:
     ld, one = t.stride()
     if one != 1 and cols > 1 and rows > 0:
         raise ValueError(f"{what}: the last dimension must have stride 1")
-    return LmMatrix(t.data_ptr(), rows, cols, ld if rows > 1 else cols, code)
+    return t.data_ptr(), rows, cols, ld if rows > 1 else cols, code
+
+
+def _matrix(t, what: str) -> LmMatrix:
+    return LmMatrix(*_matrix_fields(t, what))
+
+
+# Structs as their bytes, field by field: cheaper to make than ctypes objects.
+_MATRIX = "QqqqI4x"
+_NO_MATRIX = (0, 0, 0, 0, 0)
+_pack_matrix = struct.Struct("=" + _MATRIX).pack
+_pack_checkpoint8 = struct.Struct("=QQqqqqI4x").pack
+_pack_weight8 = struct.Struct("=QQqqqq").pack
+_pack_linear_logprob = struct.Struct("=" + 2 * _MATRIX + "7Q" + 2 * _MATRIX + "i4x").pack
+_HEADS, _TENSOR = "Qqqqqqi4x", "Qqqi4x"
+_NO_HEADS, _NO_TENSOR = (0,) * 7, (0,) * 4
+_NO_PART = 3 * _NO_HEADS + 2 * _NO_TENSOR
+_pack_qk_rotary = struct.Struct("=" + 2 * (3 * _HEADS + 2 * _TENSOR) + "QQqiii4xd").pack
+
+
+def _vector_fields(t, what: str):
+    if t.dim() != 1 or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous vector")
+    return t.data_ptr(), 1, t.shape[0], _dtype(t)
 
 
 def _vector(t, what: str) -> LmTensor:
-    if t.dim() != 1 or not t.is_contiguous():
-        raise ValueError(f"{what}: expected a contiguous vector")
-    return LmTensor(t.data_ptr(), 1, t.shape[0], _dtype(t))
+    return LmTensor(*_vector_fields(t, what))
 
 
 def _array(t, n: int, dtype, what: str):
@@ -124,13 +145,17 @@ class Checkpoint8:
     def nbytes(self) -> int:
         return self.codes.numel() + 4 * self.scales.numel()
 
-    def desc(self) -> LmCheckpoint8:
+    def fields(self):
+        """lm_checkpoint8's."""
         codes, scales = self.codes, self.scales
         rows, pitch = codes.shape
         groups, lds = scales.shape
         # (one row of a wider buffer keeps its buffer's pitch, as several do)
-        return LmCheckpoint8(codes.data_ptr(), scales.data_ptr(), rows, self.cols, codes.stride(0) if rows > 1 else max(codes.stride(0), pitch),
-                             scales.stride(0) if groups > 1 else lds, FORMATS[self.format])
+        return (codes.data_ptr(), scales.data_ptr(), rows, self.cols, codes.stride(0) if rows > 1 else max(codes.stride(0), pitch),
+                scales.stride(0) if groups > 1 else lds, FORMATS[self.format])
+
+    def desc(self) -> LmCheckpoint8:
+        return LmCheckpoint8(*self.fields())
 
     def unpack(self, dtype=torch.bfloat16, out=None, stream=None):
         """The values the checkpoint stands for (exact in bf16 and in fp32)."""
@@ -215,12 +240,16 @@ class Weight8:
     def nbytes(self) -> int:
         return self.codes.numel() + 4 * self.scales.numel()
 
-    def desc(self) -> LmWeight8:
+    def fields(self):
+        """lm_weight8's."""
         codes, scales = self.codes, self.scales
         rows, pitch = codes.shape
         down, across = scales.shape
-        return LmWeight8(codes.data_ptr(), scales.data_ptr(), rows, self.cols, codes.stride(0) if rows > 1 else max(codes.stride(0), pitch),
-                         scales.stride(0) if down > 1 else across)
+        return (codes.data_ptr(), scales.data_ptr(), rows, self.cols, codes.stride(0) if rows > 1 else max(codes.stride(0), pitch),
+                scales.stride(0) if down > 1 else across)
+
+    def desc(self) -> LmWeight8:
+        return LmWeight8(*self.fields())
 
     def unpack(self, dtype=torch.bfloat16, out=None, stream=None):
         """The values the codes stand for (exact in bf16 and in fp32)."""
@@ -254,10 +283,10 @@ def weight8(w, out: Optional[Weight8] = None, stream=None) -> Weight8:
 
 def _linear8(fn: str, x: Checkpoint8, w: Weight8, cols: int, out, dtype, grad: int):
     lib = _L.load_library()
-    cx, cw = x.desc(), w.desc()
+    cx, cw = _pack_checkpoint8(*x.fields()), _pack_weight8(*w.fields())
     if out is None:
-        out = torch.empty((x.rows, cols), dtype=dtype, device=x.codes.device)
-    m = _matrix(out, "out")
+        out = torch.empty((x.codes.shape[0], cols), dtype=dtype, device=x.codes.device)
+    m = _pack_matrix(*_matrix_fields(out, "out"))
     need = lib.lm_linear8_workspace(cx, cw, grad)
     ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
     st = getattr(lib, fn)(cx, cw, m, ws.data_ptr() if need else None, need, _stream_of(x.codes))
@@ -433,21 +462,19 @@ class LinearLogprob(NamedTuple):
     dweight: Optional[torch.Tensor]
 
 
-def _linear_logprob_args(h, weight, targets, g_logp, g_entropy, g_lse, dh, dweight, accumulate):
-    m = _matrix(h, "h")
-    a = LmLinearLogprobArgs()
-    a.h = m
-    a.weight = _matrix(weight, "weight")
-    a.targets = _array(targets, m.rows, torch.int64, "targets")
-    a.g_logp = _array(g_logp, m.rows, torch.float32, "g_logp")
-    a.g_entropy = _array(g_entropy, m.rows, torch.float32, "g_entropy")
-    a.g_lse = _array(g_lse, m.rows, torch.float32, "g_lse")
-    if dh is not None:
-        a.dh = _matrix(dh, "dh")
-    if dweight is not None:
-        a.dweight = _matrix(dweight, "dweight")
-    a.accumulate = 1 if accumulate else 0
-    return a, m.rows
+def _linear_logprob(fn, lib, h, weight, targets, logp, entropy, lse, g_logp, g_entropy, g_lse, dh, dweight, accumulate):
+    mh = _matrix_fields(h, "h")
+    n = mh[1]
+    floats = [_array(t, n, torch.float32, what) or 0 if t is not None else 0
+              for t, what in ((logp, "logp"), (entropy, "entropy"), (lse, "lse"), (g_logp, "g_logp"), (g_entropy, "g_entropy"), (g_lse, "g_lse"))]
+    a = _pack_linear_logprob(*mh, *_matrix_fields(weight, "weight"), _array(targets, n, torch.int64, "targets") or 0, *floats,
+                             *(_matrix_fields(dh, "dh") if dh is not None else _NO_MATRIX),
+                             *(_matrix_fields(dweight, "dweight") if dweight is not None else _NO_MATRIX), 1 if accumulate else 0)
+    need = lib.lm_linear_logprob_workspace(a)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
+    st = getattr(lib, fn)(a, ws.data_ptr() if need else None, need, _stream_of(h))
+    if st:
+        _L._check(lib, st, fn)
 
 
 def _gradients(h, weight, dh, dweight, accumulate, none):
@@ -456,14 +483,6 @@ def _gradients(h, weight, dh, dweight, accumulate, none):
         raise ValueError("accumulate adds to dweight: give it")
     made = lambda t, like: None if t is False or (none and t is None) else torch.empty(like.shape, dtype=like.dtype, device=like.device) if t is None else t  # noqa: E731
     return made(dh, h), made(dweight, weight)
-
-
-def _linear_logprob(fn, lib, a, device_of):
-    need = lib.lm_linear_logprob_workspace(a)
-    ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
-    st = getattr(lib, fn)(a, ws.data_ptr() if need else None, need, _stream_of(device_of))
-    if st:
-        _L._check(lib, st, fn)
 
 
 def linear_logprob(h, weight, targets=None, g_logp=None, g_entropy=None, g_lse=None, dh=None, dweight=None,
@@ -479,15 +498,10 @@ def linear_logprob(h, weight, targets=None, g_logp=None, g_entropy=None, g_lse=N
             return linear_logprob(h, weight, targets, g_logp, g_entropy, g_lse, dh, dweight, accumulate)
     lib = _L.load_library()
     dh, dweight = _gradients(h, weight, dh, dweight, accumulate, g_logp is None and g_entropy is None and g_lse is None)
-    a, _ = _linear_logprob_args(h, weight, targets, g_logp, g_entropy, g_lse, dh, dweight, accumulate)
     lead, device = h.shape[:-1], h.device
     entropy, lse = torch.empty(lead, dtype=torch.float32, device=device), torch.empty(lead, dtype=torch.float32, device=device)
-    a.entropy, a.lse = entropy.data_ptr(), lse.data_ptr()
-    logp = None
-    if targets is not None:
-        logp = torch.empty(lead, dtype=torch.float32, device=device)
-        a.logp = logp.data_ptr()
-    _linear_logprob("lm_linear_logprob", lib, a, h)
+    logp = torch.empty(lead, dtype=torch.float32, device=device) if targets is not None else None
+    _linear_logprob("lm_linear_logprob", lib, h, weight, targets, logp, entropy, lse, g_logp, g_entropy, g_lse, dh, dweight, accumulate)
     return LinearLogprob(logp, entropy, lse, dh, dweight)
 
 
@@ -501,10 +515,7 @@ def linear_logprob_grad(h, weight, targets, lse, entropy, g_logp, g_entropy=None
             return linear_logprob_grad(h, weight, targets, lse, entropy, g_logp, g_entropy, g_lse, dh, dweight, accumulate)
     lib = _L.load_library()
     dh, dweight = _gradients(h, weight, dh, dweight, accumulate, False)
-    a, n = _linear_logprob_args(h, weight, targets, g_logp, g_entropy, g_lse, dh, dweight, accumulate)
-    a.lse = _array(lse, n, torch.float32, "lse")
-    a.entropy = _array(entropy, n, torch.float32, "entropy")
-    _linear_logprob("lm_linear_logprob_grad", lib, a, h)
+    _linear_logprob("lm_linear_logprob_grad", lib, h, weight, targets, None, entropy, lse, g_logp, g_entropy, g_lse, dh, dweight, accumulate)
     return dh, dweight
 
 
@@ -550,27 +561,31 @@ class QkRotaryGrad(NamedTuple):
     dk_weight: Optional[torch.Tensor]
 
 
-def _heads(t, what: str) -> LmHeads:
-    """lm_heads of a tensor (.., heads, dim): the leading dimensions fold into
-    tokens of one pitch."""
+def _heads(t, what: str):
+    """lm_heads' fields of a tensor (.., heads, dim): the leading dimensions fold
+    into tokens of one pitch."""
     code = _DTYPES.get(t.dtype)
     if code is None:
         raise TypeError(f"{what}: unsupported dtype {t.dtype}")
-    if t.dim() < 2:
-        raise ValueError(f"{what}: expected (.., heads, dim)")
-    if t.dim() != 3:
+    shape = t.shape
+    if len(shape) != 3:
+        if len(shape) < 2:
+            raise ValueError(f"{what}: expected (.., heads, dim)")
         try:
-            t = t.view(math.prod(t.shape[:-2]), *t.shape[-2:])
+            t = t.view(math.prod(shape[:-2]), *shape[-2:])
         except RuntimeError:
             raise ValueError(f"{what}: the leading dimensions do not fold into tokens of one pitch") from None
-    tokens, heads, dim = t.shape
-    if t.stride(2) != 1 and dim > 1 and tokens > 0 and heads > 0:
+        shape = t.shape
+    tokens, heads, dim = shape
+    by_token, by_head, one = t.stride()
+    if one != 1 and dim > 1 and tokens > 0 and heads > 0:
         raise ValueError(f"{what}: the last dimension must have stride 1")
-    return LmHeads(t.data_ptr(), tokens, heads, dim, t.stride(0), t.stride(1), code)
+    return t.data_ptr(), tokens, heads, dim, by_token, by_head, code
 
 
-def _rotary_args(tokens: int, positions, table, norm, eps, interleaved) -> LmQkRotaryArgs:
-    a = LmQkRotaryArgs()
+def _rotary_tail(tokens: int, positions, table, norm, eps, interleaved):
+    """The fields of lm_qk_rotary_args after its parts."""
+    at = rows = turned = where = 0
     if table is not None:
         if table.dtype != torch.float32:
             raise TypeError(f"table: expected float32, got {table.dtype}")
@@ -578,10 +593,10 @@ def _rotary_args(tokens: int, positions, table, norm, eps, interleaved) -> LmQkR
             raise ValueError("table: expected positions x dims / 2 x 2, contiguous")
         if positions is None:
             raise ValueError("a table goes with positions")
-        a.positions = _array(positions, tokens, torch.int64, "positions")
-        a.table, a.table_rows, a.turned = table.data_ptr(), table.shape[0], 2 * table.shape[1]
-    a.norm, a.eps, a.interleaved = (1 if norm else 0), eps, (1 if interleaved else 0)
-    return a
+        at = _array(positions, tokens, torch.int64, "positions")
+        rows, pairs, _ = table.shape
+        where, turned = table.data_ptr(), 2 * pairs
+    return at, where, rows, turned, 1 if norm else 0, 1 if interleaved else 0, eps
 
 
 def qk_rotary(q, k, positions, table, q_weight=None, k_weight=None, norm: bool = True, eps: float = 1e-6,
@@ -596,19 +611,17 @@ def qk_rotary(q, k, positions, table, q_weight=None, k_weight=None, norm: bool =
             return qk_rotary(q, k, positions, table, q_weight, k_weight, norm, eps, interleaved, q_out, k_out)
     lib = _L.load_library()
     hq = _heads(q, "q")
-    a = _rotary_args(hq.tokens, positions, table, norm, eps, interleaved)
     q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
-    a.q.x, a.q.y = hq, _heads(q_out, "q_out")
-    if q_weight is not None:
-        a.q.weight = _vector(q_weight, "q_weight")
+    fields = [*hq, *_heads(q_out, "q_out"), *_NO_HEADS, *(_vector_fields(q_weight, "q_weight") if q_weight is not None else _NO_TENSOR), *_NO_TENSOR]
     if k is not None:
         k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out
-        a.k.x, a.k.y = _heads(k, "k"), _heads(k_out, "k_out")
-        if k_weight is not None:
-            a.k.weight = _vector(k_weight, "k_weight")
+        fields += [*_heads(k, "k"), *_heads(k_out, "k_out"), *_NO_HEADS, *(_vector_fields(k_weight, "k_weight") if k_weight is not None else _NO_TENSOR),
+                   *_NO_TENSOR]
     elif k_weight is not None or k_out is not None:
         raise ValueError("k_weight or k_out without k")
-    st = lib.lm_qk_rotary(a, _stream_of(q))
+    else:
+        fields += _NO_PART
+    st = lib.lm_qk_rotary(_pack_qk_rotary(*fields, *_rotary_tail(hq[1], positions, table, norm, eps, interleaved)), _stream_of(q))
     if st:
         _L._check(lib, st, "lm_qk_rotary")
     return QkRotary(q_out, k_out)
@@ -626,27 +639,28 @@ def qk_rotary_grad(dq, dk, positions, table, q=None, k=None, q_weight=None, k_we
             return qk_rotary_grad(dq, dk, positions, table, q, k, q_weight, k_weight, norm, eps, interleaved, dq_out,
                                   dk_out, dweight)
     lib = _L.load_library()
-    hq = _heads(dq, "dq")
-    a = _rotary_args(hq.tokens, positions, table, norm, eps, interleaved)
+    tokens = _heads(dq, "dq")[1]
     gains = [None, None]
     outs = [dq_out, dk_out]
-    for i, (part, d, x, w) in enumerate(((a.q, dq, q, q_weight), (a.k, dk, k, k_weight))):
+    fields = []
+    for i, (d, x, w) in enumerate(((dq, q, q_weight), (dk, k, k_weight))):
         if d is None:
             if w is not None or outs[i] is not None or x is not None:
                 raise ValueError("keys, their gain or gradient without dk")
+            fields += _NO_PART
             continue
         if outs[i] is None:
             outs[i] = torch.empty(d.shape, dtype=d.dtype, device=d.device)
-        part.y, part.dx = _heads(d, "dq" if i == 0 else "dk"), _heads(outs[i], "dq_out" if i == 0 else "dk_out")
         if norm:
             if x is None:
                 raise ValueError("the gradient of the norm reads q and k")
-            part.x = _heads(x, "q" if i == 0 else "k")
             if dweight:
-                gains[i] = torch.empty(part.y.dim, dtype=w.dtype if w is not None else torch.float32, device=d.device)
-                part.dweight = _vector(gains[i], "dweight")
-        if w is not None:
-            part.weight = _vector(w, "q_weight" if i == 0 else "k_weight")
+                gains[i] = torch.empty(d.shape[-1], dtype=w.dtype if w is not None else torch.float32, device=d.device)
+        fields += [*(_heads(x, "q" if i == 0 else "k") if norm else _NO_HEADS), *_heads(d, "dq" if i == 0 else "dk"),
+                   *_heads(outs[i], "dq_out" if i == 0 else "dk_out"),
+                   *(_vector_fields(w, "q_weight" if i == 0 else "k_weight") if w is not None else _NO_TENSOR),
+                   *(_vector_fields(gains[i], "dweight") if gains[i] is not None else _NO_TENSOR)]
+    a = _pack_qk_rotary(*fields, *_rotary_tail(tokens, positions, table, norm, eps, interleaved))
     need = lib.lm_qk_rotary_grad_workspace(a) if norm and dweight else 0
     ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
     st = lib.lm_qk_rotary_grad(a, ws.data_ptr() if need else None, need, _stream_of(dq))

@@ -186,6 +186,36 @@ def test_rotary_refusals(L):
     assert call(q=none) == 0 and call(True, q=none) == 0
 
 
+def test_packed_structs_are_the_header_s(L):
+    """The binding's packed bytes are the ctypes structs' (and so the header's)."""
+    from paper_2605_19811_gb300 import training as T
+    n = iter(range(1, 1000))
+    take = lambda k: [next(n) for _ in range(k)]  # noqa: E731
+
+    def tensor():
+        return L.LmTensor(*take(3), 1)
+
+    m = [L.LmMatrix(*take(4), 1) for _ in range(4)]
+    flat = lambda x: [getattr(x, f) or 0 for f, _ in x._fields_]  # noqa: E731
+    assert T._pack_matrix(*flat(m[0])) == bytes(m[0])
+    c = L.LmCheckpoint8(*take(6), 1)
+    assert T._pack_checkpoint8(*flat(c)) == bytes(c)
+    w = L.LmWeight8(*take(6))
+    assert T._pack_weight8(*flat(w)) == bytes(w)
+    pointers = take(7)
+    a = L.LmLinearLogprobArgs(m[0], m[1], *pointers, m[2], m[3], 1)
+    assert T._pack_linear_logprob(*flat(m[0]), *flat(m[1]), *pointers, *flat(m[2]), *flat(m[3]), 1) == bytes(a)
+    parts, fields = [], []
+    for _ in range(2):
+        heads = [L.LmHeads(*take(6), 1) for _ in range(3)]
+        tensors = [tensor(), tensor()]
+        parts.append(L.LmRotaryPart(*heads, *tensors))
+        for x in heads + tensors:
+            fields += flat(x)
+    tail = (*take(3), 64, 1, 0, 1e-6)
+    assert T._pack_qk_rotary(*fields, *tail) == bytes(L.LmQkRotaryArgs(*parts, *tail))
+
+
 def test_binding_refusals(L):
     from paper_2605_19811_gb300 import training as T
     codes, scales = torch.zeros(130, 32, dtype=torch.uint8), torch.ones(2, 1)
@@ -206,13 +236,12 @@ def test_binding_refusals(L):
         T._heads(x.half(), "q")
     with pytest.raises(ValueError):
         T._heads(torch.zeros(8), "q")
-    h = T._heads(torch.zeros(3, 4, 50)[..., :16].unflatten(-1, (2, 8)), "q")
-    assert (h.tokens, h.heads, h.dim, h.ld_token, h.ld_head) == (12, 2, 8, 50, 8)
+    assert T._heads(torch.zeros(3, 4, 50)[..., :16].unflatten(-1, (2, 8)), "q")[1:] == (12, 2, 8, 50, 8, 0)
     table = torch.zeros(10, 4, 2)
     for p, t, e in ((torch.zeros(4, dtype=torch.int32), table, TypeError), (torch.zeros(5, dtype=torch.int64), table, ValueError), (None, table, ValueError),
                     (torch.zeros(4, dtype=torch.int64), table.double(), TypeError), (torch.zeros(4, dtype=torch.int64), torch.zeros(10, 8), ValueError)):
         with pytest.raises(e):
-            T._rotary_args(4, p, t, True, 1e-6, False)
+            T._rotary_tail(4, p, t, True, 1e-6, False)
     with pytest.raises(ValueError):
         T.qk_rotary_grad(x, None, None, None)                     # the norm's gradient reads q
     for kw in (dict(dims=7), dict(dims=8, base=0.0), dict(dims=8, factor=-1.0), dict(dims=8, original=100, low=4.0, high=1.0)):
