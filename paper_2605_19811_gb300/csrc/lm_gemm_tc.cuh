@@ -50,8 +50,6 @@ using tcs::kCleanupWaitNs;
 
 constexpr int kTileM = 256, kTileN = 256, kBlockK = 64;
 constexpr int kHalf = 128;
-constexpr int kABytes = kHalf * kBlockK * 2, kBBytes = kHalf * kBlockK * 2;
-constexpr int kStageBytes = kABytes + kBBytes;
 constexpr int kFirstEpi = 4, kEpiWarps = 8;            // whole warpgroups: a warp reads the TMEM lanes of its number mod 4
 constexpr int kThreads = 32 * (kFirstEpi + kEpiWarps);
 constexpr int kChunk = 8;                              // most blocks summed in one accumulator
@@ -59,9 +57,14 @@ constexpr int kPairs = 76;                             // CTA pairs of the GPU (
 constexpr int kTmemCols = 512;
 constexpr int kBoxBytes = 32 * 128;                    // an epilogue warp's 32 rows of 128 bytes (128-byte swizzle), as the TMA stores them
 // Shared memory of a CTA: stages, the epilogue warps' boxes, barriers.
+// Epi::kRowsA rows of A are loaded and have room: kHalf, or fewer where D has no
+// more rows.  The MMA then reads kHalf rows from A's place all the same; the others
+// are bytes of B, and the rows of D that they reach are left alone.
 template <typename Epi>
 struct Smem {
-  static constexpr size_t kBoxes = (size_t)Epi::kStages * kStageBytes;
+  static constexpr int kA = Epi::kRowsA * kBlockK * 2, kB = kHalf * kBlockK * 2, kStage = kA + kB;
+  static_assert(kStage >= kHalf * kBlockK * 2, "what the MMA reads as A is inside the stage");
+  static constexpr size_t kBoxes = (size_t)Epi::kStages * kStage;
   static constexpr size_t kBars = kBoxes + (size_t)kEpiWarps * Epi::kBoxes * kBoxBytes;
   static constexpr size_t kBytes = 1024 + kBars + 512;
   static_assert(kBytes <= 232448, "shared memory of one SM");
@@ -344,7 +347,7 @@ __device__ __forceinline__ void put_block(const float (&v)[32], const Place& at,
 
 // Epilogue that stores D.
 struct StoreEpi {
-  static constexpr int kStages = 6, kBoxes = 1;
+  static constexpr int kStages = 6, kBoxes = 1, kRowsA = kHalf;
   Store out;
   template <typename P>
   struct Warp {
@@ -453,7 +456,8 @@ __device__ __forceinline__ void load_operand(uint8_t* dst, const CUtensorMap* ma
 
 template <int kALie, int kBLie, typename Epi>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_kernel(const __grid_constant__ Params<Epi> p) {
-  constexpr int kStages = Epi::kStages;
+  constexpr int kStages = Epi::kStages, kABytes = Smem<Epi>::kA, kBBytes = Smem<Epi>::kB, kStageBytes = Smem<Epi>::kStage;
+  static_assert(Epi::kRowsA == kHalf || kALie == kRowsK, "fewer rows are rows of a box");
   constexpr bool kAMn = is_mn(kALie), kBMn = is_mn(kBLie);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -745,8 +749,8 @@ inline cudaError_t encode_boxes(CUtensorMap* m, int dt, const void* base, int64_
              : cudaErrorInvalidValue;
 }
 // The rows of a bf16 matrix as an operand, and its 64-column blocks (block, row, 64).
-inline cudaError_t encode_operand(CUtensorMap* m, const void* base, int64_t cols, int64_t rows, int64_t ld, bool mn_major) {
-  return encode_boxes(m, LM_BF16, base, cols, rows, 1, ld, ld * rows, mn_major ? 64 : 128);
+inline cudaError_t encode_operand(CUtensorMap* m, const void* base, int64_t cols, int64_t rows, int64_t ld, bool mn_major, int box_rows = kHalf) {
+  return encode_boxes(m, LM_BF16, base, cols, rows, 1, ld, ld * rows, mn_major ? 64 : box_rows);
 }
 inline cudaError_t encode_blocks(CUtensorMap* m, const void* base, int64_t cols, int64_t rows, int box_rows) {
   return encode_boxes(m, LM_BF16, base, 64, rows, (cols + 63) / 64, 64, 64 * rows, box_rows);

@@ -24,6 +24,7 @@
 #include <math.h>
 
 #include "lm_gemm_tc.cuh"
+#include "lm_rows.cuh"
 
 namespace lm {
 namespace {
@@ -67,10 +68,13 @@ struct RowTerms {
   int32_t* target;    // -1 in a row without one
 };
 
-// kKeep: the logits are kept in 16 bits for the gradient.
-template <bool kKeep>
+// kKeep: the logits are kept in 16 bits for the gradient.  kFew: at most kFewRows
+// rows, without it; W's bytes are then all that counts, and more of them are under
+// way.
+constexpr int kFewRows = 32;
+template <bool kKeep, bool kFew>
 struct ForwardEpi {
-  static constexpr int kStages = kKeep ? 5 : 6, kBoxes = kKeep ? 2 : 0;
+  static constexpr int kStages = kKeep ? 5 : kFew ? 10 : 6, kBoxes = kKeep ? 2 : 0, kRowsA = kFew ? kFewRows : kHalf;
   float* from;          // kKeep: r of each half tile's rows, (2 tiles_n) x rows
   const int64_t* targets;
   float *m, *s, *t;     // (2 strips) x rows
@@ -188,7 +192,7 @@ __device__ __forceinline__ float gradient(float lp, const float4& w) {
 }
 
 struct GradEpi {
-  static constexpr int kStages = 5, kBoxes = 2;
+  static constexpr int kStages = 5, kBoxes = 2, kRowsA = kHalf;
   RowTerms rows;
   template <typename P>
   struct Warp {
@@ -253,26 +257,37 @@ __global__ void __launch_bounds__(32 * kJoinParts) linlogp_join_kernel(const Joi
   const int lane = threadIdx.x & 31, k = threadIdx.x >> 5;
   const int64_t row = (int64_t)blockIdx.x * 32 + lane;
   const bool in = row < p.rows;
+  // the row's maximum first, so that the sums that follow do not wait for one another
   float m = -INFINITY, s = 0.f, t = 0.f;
-  auto add = [&](float m2, float s2, float t2) {
-    const float most = fmaxf(m, m2), from = reference(most);
-    const float d1 = fmaxf(reference(m) - from, kGone), d2 = fmaxf(reference(m2) - from, kGone);
-    const float k1 = m == -INFINITY ? 0.f : ex2(d1 * kLog2e), k2 = m2 == -INFINITY ? 0.f : ex2(d2 * kLog2e);
-    // a part that holds NaN or infinity has s NaN, whatever its maximum
-    t = k1 * (t + d1 * s) + k2 * (t2 + d2 * s2);
-    s = k1 * s + k2 * s2;
-    m = most;
-  };
   if (in) {
-#pragma unroll 4
-    for (int i = k; i < p.parts; i += kJoinParts) add(p.m[i * p.rows + row], p.s[i * p.rows + row], p.t[i * p.rows + row]);
+#pragma unroll 8
+    for (int i = k; i < p.parts; i += kJoinParts) m = fmaxf(m, p.m[i * p.rows + row]);
   }
   sm[k][lane] = m;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kJoinParts; ++i) m = fmaxf(m, sm[i][lane]);
+  const float from = reference(m);
+  if (in) {
+#pragma unroll 4
+    for (int i = k; i < p.parts; i += kJoinParts) {
+      const float mi = p.m[i * p.rows + row], si = p.s[i * p.rows + row], ti = p.t[i * p.rows + row];
+      const float d = fmaxf(reference(mi) - from, kGone), f = mi == -INFINITY ? 0.f : ex2(d * kLog2e);
+      // a part that holds NaN or infinity has s NaN, whatever its maximum
+      s = fmaf(f, si, s);
+      t = fmaf(f, fmaf(d, si, ti), t);
+    }
+  }
   ss[k][lane] = s;
   st[k][lane] = t;
   __syncthreads();
   if (k != 0 || !in) return;
-  for (int i = 1; i < kJoinParts; ++i) add(sm[i][lane], ss[i][lane], st[i][lane]);
+  s = t = 0.f;
+#pragma unroll
+  for (int i = 0; i < kJoinParts; ++i) {
+    s += ss[i][lane];
+    t += st[i][lane];
+  }
   const int64_t y = p.targets != nullptr ? p.targets[row] : -1;
   float lse, h, logp;
   if (m == -INFINITY && s == 0.f) {
@@ -354,13 +369,33 @@ __global__ void __launch_bounds__(256) linlogp_round_kernel(const float* sum, in
   }
 }
 
-// A matrix laid out anew with rows that the TMA takes.
-__global__ void __launch_bounds__(256) linlogp_copy_kernel(Mat from, int64_t rows, int cols, __nv_bfloat16* to, int64_t ld) {
+// A matrix laid out anew with rows that the TMA takes: a warp takes 256 columns of
+// a row, eight a lane, four such pieces at once (50257 x 1285 of 1280: element by
+// element 125 us).
+__global__ void __launch_bounds__(256) linlogp_copy_kernel(Mat from, int64_t nrows, int cols, __nv_bfloat16* to, int64_t ld) {
+  constexpr int kAhead = 4;
   griddep_wait();
   griddep_launch_dependents();
-  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-    const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(from.data) + r * from.ld;
-    for (int c = threadIdx.x; c < cols; c += 256) to[r * ld + c] = src[c];
+  const int per = (cols + 255) / 256, lane = threadIdx.x & 31;
+  const int64_t all = nrows * per, step = (int64_t)gridDim.x * 8;
+  for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < all; i += kAhead * step) {
+    rows::Raw<__nv_bfloat16> raw[kAhead];
+    int64_t row[kAhead];
+    int c[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int64_t at = i + k * step;
+      row[k] = at < all ? at / per : -1;
+      c[k] = (int)(at - row[k] * per) * 256 + 8 * lane;
+      raw[k].load<false>(rows::Row<const __nv_bfloat16>(from, row[k] < 0 ? 0 : row[k], nrows), c[k], row[k] < 0 ? rows::kNoRow : cols - c[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (row[k] < 0) break;
+      raw[k].settle<false>(rows::Row<const __nv_bfloat16>(from, row[k], nrows), c[k], cols - c[k]);
+      // (ld is a multiple of eight: eight are inside the row wherever one is)
+      if (c[k] < cols) *reinterpret_cast<uint4*>(to + row[k] * ld + c[k]) = make_uint4(raw[k].w[0], raw[k].w[1], raw[k].w[2], raw[k].w[3]);
+    }
   }
 }
 
@@ -457,12 +492,13 @@ cudaError_t piece(const LinLogpParams& q, const Layout& l, const Mat& h, const M
   j.g_entropy = from_row(q.g_entropy, first);
   j.g_lse = from_row(q.g_lse, first);
   if (grad) j.out = RowTerms{reinterpret_cast<float4*>(ws + l.terms), reinterpret_cast<float*>(ws + l.gl), reinterpret_cast<int32_t*>(ws + l.target)};
+  const bool few = !grad && rows <= kFewRows;
   // the operands of the logits' product, and the blocks that its epilogue fills
   auto logits = [&](auto& p) {
     p.m = (int32_t)rows;
     p.n = q.vocab;
     p.wait_ns = wait_ns;
-    cudaError_t e = encode_operand(&p.a, h.data, q.width, rows, h.ld, false);
+    cudaError_t e = encode_operand(&p.a, h.data, q.width, rows, h.ld, false, few ? kFewRows : kHalf);
     if (e == cudaSuccess) e = encode_operand(&p.b, w.data, q.width, q.vocab, w.ld, false);
     if (e == cudaSuccess && grad) e = encode_blocks(&p.out, ws + l.d, q.vocab, rows, 32);
     return e;
@@ -493,13 +529,17 @@ cudaError_t piece(const LinLogpParams& q, const Layout& l, const Mat& h, const M
       return logits(f);
     };
     if (grad) {
-      Params<ForwardEpi<true>> f{};
+      Params<ForwardEpi<true, false>> f{};
       LM_RUN(forward(f));
-      LM_RUN((start<kRowsK, kRowsK, ForwardEpi<true>>(f, st)));
+      LM_RUN((start<kRowsK, kRowsK, ForwardEpi<true, false>>(f, st)));
+    } else if (few) {
+      Params<ForwardEpi<false, true>> f{};
+      LM_RUN(forward(f));
+      LM_RUN((start<kRowsK, kRowsK, ForwardEpi<false, true>>(f, st)));
     } else {
-      Params<ForwardEpi<false>> f{};
+      Params<ForwardEpi<false, false>> f{};
       LM_RUN(forward(f));
-      LM_RUN((start<kRowsK, kRowsK, ForwardEpi<false>>(f, st)));
+      LM_RUN((start<kRowsK, kRowsK, ForwardEpi<false, false>>(f, st)));
     }
     LM_RUN(launch_after(linlogp_join_kernel, dim3((unsigned)((rows + 31) / 32)), 32 * kJoinParts, 0, st, j));
     if (grad)
@@ -540,7 +580,8 @@ cudaError_t piece(const LinLogpParams& q, const Layout& l, const Mat& h, const M
 }
 
 cudaError_t copy_rows(const Mat& from, int64_t rows, int cols, void* to, int64_t ld, cudaStream_t st) {
-  return launch_after(linlogp_copy_kernel, dim3((unsigned)std::min<int64_t>(rows, 152 * 8)), 256, 0, st, from, rows, cols,
+  const int64_t blocks = (rows * ((cols + 255) / 256) + 31) / 32;
+  return launch_after(linlogp_copy_kernel, dim3((unsigned)std::min<int64_t>(blocks, 152 * 8)), 256, 0, st, from, rows, cols,
                       static_cast<__nv_bfloat16*>(to), ld);
 }
 
