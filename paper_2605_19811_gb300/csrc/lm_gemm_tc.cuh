@@ -218,6 +218,33 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
   return d;
 }
 
+// The issuing warp comes to these as a whole, so that what they take is the same in
+// every lane; its leader acts.
+__device__ __forceinline__ void umma_by(uint32_t leader, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(leader)
+      : "memory");
+}
+__device__ __forceinline__ void commit_pair(uint32_t leader, uint64_t* bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t"
+      "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}" ::"r"(smem_u32(bar)),
+      "h"((uint16_t)0x3), "r"(leader)
+      : "memory");
+}
+// Whether the phase is over, at once.
+__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+
 // Arrive on a barrier of CTA 0.  What the arrival announces is TMEM columns of the
 // arriving CTA read to the end (tcgen05.wait::ld, fence before_thread_sync).
 // Nothing in global memory hangs on it, so the arrival needs no fence of cluster
@@ -471,7 +498,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_ke
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(armed + kStages);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   const int pair = blockIdx.x >> 1;
   const Schedule& sch = p.sch;
@@ -545,52 +572,59 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_ke
   } else if (warp == 1) {
     // -------------------------------- MMA issuer -------------------------------
     few_registers();
-    if (lane == 0 && rank == 0) {
-      const uint32_t idesc = make_idesc(kTileM, kTileN, kAMn, kBMn);
+    if (rank == 0) {
+      constexpr uint32_t idesc = make_idesc(kTileM, kTileN, kAMn, kBMn);
       // 16 of the sum: 16 rows of 128 bytes (MN-major), 32 bytes of a row (K-major)
       constexpr uint64_t a_step = (kAMn ? 2048 : 32) >> 4, b_step = (kBMn ? 2048 : 32) >> 4;
+      const uint32_t leader = lane == 0 ? 1u : 0u, smem0 = smem_u32(smem), tmem0 = __shfl_sync(0xFFFFFFFFu, tmem_base, 0);
       int stage = 0, ab = 0;
       uint32_t ph = 0, aph = 0;
-      bool ok = true;
+      bool ok = true, ready = false;
+      auto wait = [&](uint64_t* bar, uint32_t parity) {
+        if (!__all_sync(0xFFFFFFFFu, await(bar, parity, abort_flag, wait_ns))) ok = false;
+        return ok;
+      };
       Items items(sch, pair);
       Item it;
       while (ok && items.next(sch, it)) {
         for (int kc = it.kb0; ok && kc < it.kb1;) {
           const int ke = min(kc + kChunk, it.kb1);
-          if (!await(&accempty[ab], aph ^ 1u, abort_flag, wait_ns)) {
-            ok = false;
-            break;
-          }
+          if (!wait(&accempty[ab], aph ^ 1u)) break;
           tc_fence_after();
-          const uint32_t d = tmem_base + (uint32_t)(ab * kTileN);
+          const uint32_t d = tmem0 + (uint32_t)(ab * kTileN);
           for (int kb = kc; kb < ke; ++kb) {
-            if (!await(&full[stage], ph, abort_flag, wait_ns)) {
-              ok = false;
-              break;
-            }
+            if (!ready && !wait(&full[stage], ph)) break;
             tc_fence_after();
-            const uint32_t sa = smem_u32(smem + (size_t)stage * kStageBytes);
+            const uint32_t sa = smem0 + (uint32_t)(stage * kStageBytes);
             const uint64_t a0 = sw128_desc(sa, kAMn ? kABytes / 2 : 16, 1024), b0 = sw128_desc(sa + kABytes, kBMn ? kBBytes / 2 : 16, 1024);
-#pragma unroll
-            for (int kk = 0; kk < kBlockK / 16; ++kk)
-              umma_bf16(d, a0 + kk * a_step, b0 + kk * b_step, idesc, (kb == kc && kk == 0) ? 0u : 1u);
-            umma_commit_pair(&empty[stage]);
+            uint64_t* const free = &empty[stage];
+            // Whether the next block is there is asked now and known after this
+            // block's MMAs: the answer comes late, behind what they read of shared
+            // memory, and their queue is short.
             if (++stage == kStages) {
               stage = 0;
               ph ^= 1u;
             }
+            const bool there = mbar_test(&full[stage], ph);
+#pragma unroll
+            for (int kk = 0; kk < kBlockK / 16; ++kk)
+              umma_by(leader, d, a0 + kk * a_step, b0 + kk * b_step, idesc, (kb == kc && kk == 0) ? 0u : 1u);
+            commit_pair(leader, free);
+            ready = __all_sync(0xFFFFFFFFu, there);
           }
           if (!ok) break;
-          umma_commit_pair(&accfull[ab]);
+          commit_pair(leader, &accfull[ab]);
           ab ^= 1;
           if (ab == 0) aph ^= 1u;
           kc = ke;
         }
       }
-      if (!ok) *abort_flag = 1;
-      umma_commit_local(done);   // all issued MMAs complete before TMEM is released
-      volatile int never = 0;
-      await(done, 0, &never, kCleanupWaitNs);
+      if (leader) {
+        if (!ok) *abort_flag = 1;
+        umma_commit_local(done);   // all issued MMAs complete before TMEM is released
+        volatile int never = 0;
+        await(done, 0, &never, kCleanupWaitNs);
+      }
     }
   } else if (warp >= kFirstEpi) {
     // --------------------------------- epilogue ----------------------------------

@@ -217,24 +217,6 @@ __device__ __forceinline__ void umma_mx8(uint32_t leader, uint32_t d, uint64_t a
       "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate), "r"(leader)
       : "memory");
 }
-// umma_commit_pair by the leader.
-__device__ __forceinline__ void commit_pair(uint32_t leader, uint64_t* bar) {
-  asm volatile(
-      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t"
-      "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}" ::"r"(smem_u32(bar)),
-      "h"((uint16_t)0x3), "r"(leader)
-      : "memory");
-}
-// Whether the phase is over, at once.
-__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(smem_u32(bar)), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
 // 32 x 16 bytes of shared memory to four columns of every lane quadrant, in both
 // CTAs; MMAs issued after it by the same thread see them.
 __device__ __forceinline__ void copy_scales(uint32_t leader, uint32_t tmem, uint32_t smem) {
