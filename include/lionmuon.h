@@ -655,7 +655,9 @@ lm_status lm_weight8_unpack(const lm_weight8* c, const lm_matrix* w, void* cuda_
  * x and dy are checkpoints in LM_CODE_E4M3 (lm_checkpoint8_pack, or kept by
  * lm_rmsnorm), w the layer's weights (out x in); y and dx are bf16 or fp32.
  * Products of codes are exact and the sums fp32, in a fixed order: the same
- * inputs give the same bits.  The weight gradient is lm_linear_wgrad8's.
+ * inputs give the same bits.  The tensor cores add at most 2048 products (each
+ * addition of 32 may drop 2^-23 of what it has); their sums are added in fp32.
+ * The weight gradient is lm_linear_wgrad8's.
  * workspace: lm_linear8_workspace(x, w, grad) bytes of device memory, 256-byte
  * aligned, free again when the work is done.
  * Should a device-side wait give up (LM_WAIT_LIMIT_NS), what was not computed

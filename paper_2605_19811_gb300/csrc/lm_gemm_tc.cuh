@@ -53,6 +53,7 @@ constexpr int kHalf = 128;
 constexpr int kFirstEpi = 4, kEpiWarps = 8;            // whole warpgroups: a warp reads the TMEM lanes of its number mod 4
 constexpr int kThreads = 32 * (kFirstEpi + kEpiWarps);
 constexpr int kChunk = 8;                              // most blocks summed in one accumulator
+constexpr int kLeast = 16;                             // blocks of a split sum's part: the parts and their join cost as much
 constexpr int kPairs = 76;                             // CTA pairs of the GPU (152 SMs)
 constexpr int kTmemCols = 512;
 constexpr int kBoxBytes = 32 * 128;                    // an epilogue warp's 32 rows of 128 bytes (128-byte swizzle), as the TMA stores them
@@ -809,7 +810,7 @@ inline Schedule plain_schedule(int64_t m, int64_t n, int64_t k, int strip, int t
 }
 // Whole waves of units, the rest shared by ranges of the sum.
 constexpr int kMostTeam = 8;      // where more columns would leave many pairs out, each is for itself
-inline Schedule split_schedule(int64_t m, int64_t n, int64_t k, int tile_n = kTileN, int block_k = kBlockK, int least = kChunk) {
+inline Schedule split_schedule(int64_t m, int64_t n, int64_t k, int tile_n = kTileN, int block_k = kBlockK, int least = kLeast) {
   Schedule s = plain_schedule(m, n, k, 1, tile_n, block_k);
   if (s.tiles_n <= kMostTeam && s.tiles_m > 1) {
     s.team = s.tiles_n;

@@ -76,6 +76,8 @@ __global__ void __launch_bounds__(256) weight8_pack_kernel(Mat w, int64_t rows, 
     for (int k = 0; k < 8; ++k) most = max(most, part[k]);
     const float scale = code8::group_scale<LM_CODE_E4M3>(most), inv = code8::inverse_scale(scale);
     if (threadIdx.x == 0) out.scales[block * out.ld_scales + blockIdx.x] = scale;
+    // code8::encode2's two exceptions are the block's: a NaN scale, and the largest
+    const bool plain = inv != 0.f && inv != __uint_as_float(7u << 23);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const int64_t r = r0 + 2 * k;
@@ -83,47 +85,56 @@ __global__ void __launch_bounds__(256) weight8_pack_kernel(Mat w, int64_t rows, 
       float v[8];
       raw[k].get(v);
       uint32_t q[4];
+      if (plain) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) q[i] = code8::encode2<LM_CODE_E4M3>(v[2 * i], v[2 * i + 1], inv);
+        for (int i = 0; i < 4; ++i)
+          q[i] = (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(v[2 * i] * inv, v[2 * i + 1] * inv), __NV_SATFINITE, __NV_E4M3);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = code8::encode2<LM_CODE_E4M3>(v[2 * i], v[2 * i + 1], inv);
+      }
       // the pitch is a multiple of 16: eight codes are inside the row wherever one is
-      *reinterpret_cast<uint2*>(out.data + r * out.ld + c) = make_uint2(q[0] | q[1] << 16, q[2] | q[3] << 16);
+      __stcs(reinterpret_cast<uint2*>(out.data + r * out.ld + c), make_uint2(q[0] | q[1] << 16, q[2] | q[3] << 16));
     }
   }
 }
 
-// Codes back to values, eight a thread.
-template <typename T>
-__global__ void __launch_bounds__(256) values_kernel(const uint8_t* codes, int64_t ld, const float* scales, int64_t ld_scales, int64_t nrows, int64_t cols, T* to,
-                                                     int64_t ld_to, int vec) {
+// Codes back to values: a warp takes 256 columns of a row, eight a lane, kAhead rows
+// at once.
+template <typename T, bool kVec>
+__global__ void __launch_bounds__(256) values_kernel(Blocks w, int64_t nrows, int64_t cols, Mat to) {
+  constexpr int kAhead = 4;
   griddep_wait();
   griddep_launch_dependents();
-  const int64_t per = (cols + 7) / 8, all = nrows * per;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / per, c = 8 * (i - r * per);
-    const uint2 q = *reinterpret_cast<const uint2*>(codes + r * ld + c);
-    const float s = scales[r / kBlock * ld_scales + c / kBlock];
-    const uint32_t two[4] = {q.x, q.x >> 16, q.y, q.y >> 16};
-    float v[8];
+  const int64_t c = (int64_t)blockIdx.x * 256 + 8 * (threadIdx.x & 31);
+  const int left = (int)max((int64_t)0, min((int64_t)8, cols - c));
+  for (int64_t r0 = ((int64_t)blockIdx.y * 8 + (threadIdx.x >> 5)) * kAhead; r0 < nrows; r0 += (int64_t)gridDim.y * 8 * kAhead) {
+    uint2 q[kAhead];
+    float s[kAhead];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float2 d = code8::decode2<LM_CODE_E4M3>(two[k]);
-      v[2 * k] = d.x * s;
-      v[2 * k + 1] = d.y * s;
+    for (int k = 0; k < kAhead; ++k) {
+      q[k] = make_uint2(0u, 0u);
+      s[k] = 0.f;
+      if (r0 + k >= nrows || left == 0) continue;
+      q[k] = __ldcs(reinterpret_cast<const uint2*>(w.data + (r0 + k) * w.ld + c));
+      s[k] = w.scales[(r0 + k) / kBlock * w.ld_scales + c / kBlock];
     }
-    rows::Raw<T> o;
-    o.set(v);
-    T* p = to + r * ld_to + c;
-    if (vec && cols - c >= 8) {
 #pragma unroll
-      for (int k = 0; k < rows::Raw<T>::kPieces; ++k) reinterpret_cast<uint4*>(p)[k] = make_uint4(o.w[4 * k], o.w[4 * k + 1], o.w[4 * k + 2], o.w[4 * k + 3]);
-    } else {
-      o.put_single(p, 0, (int)min((int64_t)8, cols - c));
+    for (int k = 0; k < kAhead; ++k) {
+      if (r0 + k >= nrows) break;
+      const uint32_t two[4] = {q[k].x, q[k].x >> 16, q[k].y, q[k].y >> 16};
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2 d = code8::decode2<LM_CODE_E4M3>(two[i]);
+        v[2 * i] = d.x * s[k];
+        v[2 * i + 1] = d.y * s[k];
+      }
+      rows::Raw<T> o;
+      o.set(v);
+      o.template store<kVec>(static_cast<T*>(to.data) + (r0 + k) * to.ld + c, left);
     }
   }
-}
-unsigned blocks_for(int64_t nrows, int64_t cols) {
-  const int64_t b = (nrows * ((cols + 7) / 8) + 255) / 256;
-  return (unsigned)std::min<int64_t>(b, 152 * 16);
 }
 
 // --- the product ---
@@ -131,7 +142,7 @@ unsigned blocks_for(int64_t nrows, int64_t cols) {
 constexpr int kN = 256, kHalfN = kN / 2, kK = 256;      // tile columns; of the sum at a time
 constexpr int kSub = 128, kSubs = kK / kSub;            // of the sum: a swizzled row's bytes, a scale's group
 constexpr int kFewTokens = 32;
-constexpr int kLeastShare = 2;                          // stages of a split sum's part
+constexpr int kLeastShare = 8;                          // stages of a split sum's part: the parts and their join cost as much as ten
 constexpr int kChunk8 = 8;                              // most stages summed in one accumulator: 64 additions
 constexpr int kScaleBytes = 512 + 1024;                 // of two stages: the CTA's rows', the tile's columns'
 constexpr int kWarpBytes = 32 * 64;                     // an epilogue warp's box: 32 columns in bf16, 16 in fp32
@@ -174,33 +185,33 @@ struct ScaleParams {
   uint32_t *sa, *sb;
 };
 __device__ __forceinline__ uint32_t exponent(float s) { return __float_as_uint(s) >> 23; }     // 255 for NaN
-__global__ void __launch_bounds__(256) scales_kernel(const ScaleParams p) {
+__global__ void __launch_bounds__(128) scales_kernel(const ScaleParams p) {
   griddep_wait();
   griddep_launch_dependents();
-  const int64_t a = (int64_t)p.fours * p.row_blocks * 128, all = a + (int64_t)p.fours * p.tiles_n * 256;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+  const int t = threadIdx.x;
+  const uint32_t a = (uint32_t)p.fours * (uint32_t)p.row_blocks, all = a + (uint32_t)p.fours * 2u * (uint32_t)p.tiles_n;
+  for (uint32_t block = blockIdx.x; block < all; block += gridDim.x) {     // 128 words each
     uint32_t v = 0;
-    if (i < a) {       // threads in the order of the rows
-      const int r = (int)(i & 127);
-      const int64_t block = i >> 7, four = block / p.row_blocks, token = (block - four * p.row_blocks) * 128 + r;
+    if (block < a) {       // threads in the order of the rows
+      const int four = (int)(block / (uint32_t)p.row_blocks);
+      const int64_t token = (int64_t)(block - (uint32_t)four * (uint32_t)p.row_blocks) * 128 + t;
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        if (token < p.tokens && 4 * four + k < p.groups) v |= exponent(p.x[(4 * four + k) * p.ldx + token]) << (8 * k);
-      p.sa[block * 128 + (r & 31) * 4 + (r >> 5)] = v;
-    } else {
-      const int64_t at = i - a, block = at >> 7;
-      const int64_t four = block / (2 * p.tiles_n), b = block - four * 2 * p.tiles_n, tile = b >> 1;
-      const int c = (int)(at & 127), w = ((c & 3) * 32 + (c >> 2)) + (int)(b & 1) * 128;     // word c of the block holds this column
-      const int64_t col = tile * kN + w;
+        if (token < p.tokens && 4 * four + k < p.groups) v |= exponent(p.x[(int64_t)(4 * four + k) * p.ldx + token]) << (8 * k);
+      p.sa[(size_t)block * 128 + (t & 31) * 4 + (t >> 5)] = v;
+    } else {               // in the order of the words: word t holds this column
+      const uint32_t b = block - a, four = b / (2u * (uint32_t)p.tiles_n), tile = b - four * 2u * (uint32_t)p.tiles_n;
+      const int64_t col = (int64_t)tile * 128 + (t & 3) * 32 + (t >> 2);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const int64_t g = 4 * four + k;
-        if (w < kN && col < p.n && g < p.groups) v |= exponent(p.grad ? p.w[g * p.ldw + col / kBlock] : p.w[col / kBlock * p.ldw + g]) << (8 * k);
+        const int64_t g = 4 * (int64_t)four + k;
+        if (col < p.n && g < p.groups) v |= exponent(p.grad ? p.w[g * p.ldw + col / kBlock] : p.w[col / kBlock * p.ldw + g]) << (8 * k);
       }
-      p.sb[at] = v;
+      p.sb[(size_t)b * 128 + t] = v;
     }
   }
 }
+static_assert(kN == 256, "two blocks of scales a tile");
 
 // Instruction descriptor, kind::mxf8f6f4: A and B e4m3, scales ue8m0 (bit 23),
 // the byte of a scale's word at bits 4 (B) and 29 (A), N >> 3 at bit 17, M >> 7
@@ -595,13 +606,10 @@ cudaError_t launch_weight8_pack(lm_dtype dt, const Mat& w, int64_t nrows, int64_
 }
 
 cudaError_t launch_weight8_unpack(lm_dtype dt, const Blocks& c, int64_t nrows, int64_t cols, const Mat& w, cudaStream_t st) {
-  const int vec = rows::aligned(w, dt == LM_F32 ? 4 : 2, nrows);
-  const dim3 grid(blocks_for(nrows, cols));
-  if (dt == LM_F32)
-    return launch_after(values_kernel<float>, grid, 256, 0, st, (const uint8_t*)c.data, c.ld, (const float*)c.scales, c.ld_scales, nrows, cols,
-                        static_cast<float*>(w.data), w.ld, vec);
-  return launch_after(values_kernel<__nv_bfloat16>, grid, 256, 0, st, (const uint8_t*)c.data, c.ld, (const float*)c.scales, c.ld_scales, nrows, cols,
-                      static_cast<__nv_bfloat16*>(w.data), w.ld, vec);
+  const bool vec = rows::aligned(w, dt == LM_F32 ? 4 : 2, nrows);
+  const dim3 grid((unsigned)((cols + 255) / 256), (unsigned)std::min<int64_t>((nrows + 31) / 32, 65535));
+  if (dt == LM_F32) return launch_after(vec ? values_kernel<float, true> : values_kernel<float, false>, grid, 256, 0, st, c, nrows, cols, w);
+  return launch_after(vec ? values_kernel<__nv_bfloat16, true> : values_kernel<__nv_bfloat16, false>, grid, 256, 0, st, c, nrows, cols, w);
 }
 
 size_t linear8_workspace(const Linear8Params& q) { return q.tokens <= 0 || q.in <= 0 || q.out <= 0 ? 0 : make_layout(q).total; }
@@ -612,8 +620,8 @@ cudaError_t launch_linear8(const Linear8Params& q, cudaStream_t st) {
   uint8_t* ws = static_cast<uint8_t*>(q.workspace);
   uint32_t *sa = reinterpret_cast<uint32_t*>(ws), *sb = reinterpret_cast<uint32_t*>(ws + l.sb);
   const ScaleParams sp{q.x.scales, q.w.scales, q.x.ld_scales, q.w.ld_scales, q.tokens, (int32_t)l.n, l.groups, l.fours, l.row_blocks, l.sch.tiles_n, q.grad, sa, sb};
-  const int64_t words = (int64_t)l.fours * (l.row_blocks * 128 + (int64_t)l.sch.tiles_n * 256);
-  cudaError_t e = launch_after(scales_kernel, dim3((unsigned)std::min<int64_t>((words + 255) / 256, 152 * 8)), 256, 0, st, sp);
+  const int64_t words = (int64_t)l.fours * (l.row_blocks + 2 * (int64_t)l.sch.tiles_n);      // blocks of 128
+  cudaError_t e = launch_after(scales_kernel, dim3((unsigned)std::min<int64_t>(words, 152 * 32)), 128, 0, st, sp);
   if (e != cudaSuccess) return e;
   Params8 p{};
   p.sch = l.sch;
