@@ -301,13 +301,23 @@ __device__ __forceinline__ void box_ready() {
   __syncwarp();
 }
 
-// Four elements of a row, `left` of them inside.
+// Where a result goes: one element, or four of a row, `left` of them inside.
 struct Store {
   Mat d;
   int32_t dt;
   int32_t accumulate;   // adds to d
   int32_t vec;          // d takes four elements at a time
   int32_t tma;          // whole tiles go to d by the TMA (a map of it; fp32 may be added)
+  __device__ __forceinline__ void one(int64_t row, int col, float v) const {
+    const int64_t at = row * d.ld + col;
+    if (dt == LM_F32) {
+      float* o = static_cast<float*>(d.data) + at;
+      *o = accumulate ? *o + v : v;
+    } else {
+      __nv_bfloat16* o = static_cast<__nv_bfloat16*>(d.data) + at;
+      *o = __float2bfloat16_rn(accumulate ? __bfloat162float(*o) + v : v);
+    }
+  }
   __device__ __forceinline__ void put(int64_t row, int col, float4 v, int left) const {
     float e[4] = {v.x, v.y, v.z, v.w};
     const int64_t at = row * d.ld + col;
@@ -373,6 +383,21 @@ __device__ __forceinline__ void put_block(const float (&v)[32], const Place& at,
   __syncwarp();
 }
 
+// The same where D's rows do not take four at a time: a row a step, a column a
+// lane, so that a row's elements still go out side by side.
+__device__ __forceinline__ void put_rows(const float (&v)[32], const Place& at, int rows, int c, int n, const Store& out) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) box_put(at.box, at.lane, e, v + 4 * e);
+  __syncwarp();
+#pragma unroll 8
+  for (int r = 0; r < rows; ++r) {
+    float x;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(box_at(at.box, r, at.lane >> 2) + 4 * (at.lane & 3)) : "memory");
+    if (c + at.lane < n) out.one(at.row + r, c + at.lane, x);
+  }
+  __syncwarp();
+}
+
 // Epilogue that stores D.
 struct StoreEpi {
   static constexpr int kStages = 6, kBoxes = 1, kRowsA = kHalf;
@@ -430,10 +455,12 @@ struct StoreEpi {
           put_block(acc[b], at, rows, c, [&](int r, int col, float4 v) {
             *reinterpret_cast<float4*>(part + (size_t)(r0 + r) * kTileN + (col - c0)) = v;
           });
-        } else {
+        } else if (p.epi.out.vec) {
           put_block(acc[b], at, rows, c, [&](int r, int col, float4 v) {
             if (col < p.n) p.epi.out.put(at.row + r, col, v, p.n - col);
           });
+        } else {
+          put_rows(acc[b], at, rows, c, p.n, p.epi.out);
         }
       }
     }

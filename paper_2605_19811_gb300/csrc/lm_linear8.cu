@@ -262,6 +262,29 @@ __device__ __forceinline__ void put16(const float (&v)[32], uint32_t box, int la
   }
 }
 
+// The same where y's rows do not take four at a time: two rows a step, 16 columns
+// of each, a column a lane.
+__device__ __forceinline__ void put16_rows(const float (&v)[32], uint32_t box, int lane, int row0, int rows, int c, int n, const Store& out) {
+  auto at = [&](int row, int chunk) { return box + row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4); };
+  const int e = lane & 15;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float* f = v + 16 * h + 4 * k;
+      asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at(lane, k)), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]) : "memory");
+    }
+    __syncwarp();
+#pragma unroll 8
+    for (int r = lane >> 4; r < rows; r += 2) {
+      float x;
+      asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(at(r, e >> 2) + 4 * (e & 3)) : "memory");
+      if (c + 16 * h + e < n) out.one(row0 + r, c + 16 * h + e, x);
+    }
+    __syncwarp();
+  }
+}
+
 template <bool kGrad, bool kFew>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8_kernel(const __grid_constant__ Params8 p) {
   using R = Ring<kFew>;
@@ -526,6 +549,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
               bulk_commit();
             }
           }
+        } else if (it.slot < 0 && !p.out.vec) {
+          put16_rows(acc[b], box, lane, row0, rows, c, p.n, p.out);
         } else {
           box_free(lane);
           put16(acc[b], box, lane, rows, [&](int r, int e, float4 v) {
