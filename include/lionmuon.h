@@ -584,7 +584,9 @@ lm_status lm_linear_wgrad8(const lm_matrix* dy, const lm_checkpoint8* x, const l
  * add at most 512 products (each addition of 16 may drop 2^-23 of what it has);
  * their sums are added in fp32.  Sums are taken in a fixed order: the same
  * inputs give the same bits.
- * dh has the dtype of h; dweight is bf16 or fp32, accumulate != 0 adds to it. */
+ * dh has the dtype of h; dweight is bf16 or fp32, accumulate != 0 adds to it (to
+ * fp32 values, and between pieces of the tokens, sums below 2^-126 may count as
+ * zero). */
 typedef struct {
   lm_matrix h;
   lm_matrix weight;

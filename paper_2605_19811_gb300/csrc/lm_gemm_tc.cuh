@@ -15,7 +15,7 @@
 //
 // Accumulation: the tensor cores drop up to a unit of the last place of the
 // accumulator at each addition (16 of the sum), always towards zero, so a sum of
-// more than kChunk blocks (512) is cut: the epilogue adds the accumulator, in
+// more than Epi::kChunk blocks (64 each) is cut: the epilogue adds the accumulator, in
 // fp32, to sums that it holds in registers while the MMA fills the other one.
 //
 // Schedule: units of `strip` tiles of one tile row, dealt to the pairs in turn.
@@ -52,7 +52,6 @@ constexpr int kTileM = 256, kTileN = 256, kBlockK = 64;
 constexpr int kHalf = 128;
 constexpr int kFirstEpi = 4, kEpiWarps = 8;            // whole warpgroups: a warp reads the TMEM lanes of its number mod 4
 constexpr int kThreads = 32 * (kFirstEpi + kEpiWarps);
-constexpr int kChunk = 8;                              // most blocks summed in one accumulator
 constexpr int kLeast = 16;                             // blocks of a split sum's part: the parts and their join cost as much
 constexpr int kPairs = 76;                             // CTA pairs of the GPU (152 SMs)
 constexpr int kTmemCols = 512;
@@ -400,7 +399,7 @@ __device__ __forceinline__ void put_rows(const float (&v)[32], const Place& at, 
 
 // Epilogue that stores D.
 struct StoreEpi {
-  static constexpr int kStages = 6, kBoxes = 1, kRowsA = kHalf;
+  static constexpr int kStages = 6, kBoxes = 1, kRowsA = kHalf, kChunk = 8;
   Store out;
   template <typename P>
   struct Warp {
@@ -511,6 +510,7 @@ __device__ __forceinline__ void load_operand(uint8_t* dst, const CUtensorMap* ma
 
 template <int kALie, int kBLie, typename Epi>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_kernel(const __grid_constant__ Params<Epi> p) {
+  constexpr int kChunk = Epi::kChunk;
   constexpr int kStages = Epi::kStages, kABytes = Smem<Epi>::kA, kBBytes = Smem<Epi>::kB, kStageBytes = Smem<Epi>::kStage;
   static_assert(Epi::kRowsA == kHalf || kALie == kRowsK, "fewer rows are rows of a box");
   constexpr bool kAMn = is_mn(kALie), kBMn = is_mn(kBLie);

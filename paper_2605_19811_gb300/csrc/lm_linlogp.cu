@@ -75,6 +75,7 @@ constexpr int kFewRows = 32;
 template <bool kKeep, bool kFew>
 struct ForwardEpi {
   static constexpr int kStages = kKeep ? 5 : kFew ? 10 : 6, kBoxes = kKeep ? 2 : 0, kRowsA = kFew ? kFewRows : kHalf;
+  static constexpr int kChunk = kFew ? 2 : 4;      // blocks of a logit's sum in one accumulator: 128 products, or 256
   float* from;          // kKeep: r of each half tile's rows, (2 tiles_n) x rows
   const int64_t* targets;
   float *m, *s, *t;     // (2 strips) x rows
@@ -192,7 +193,7 @@ __device__ __forceinline__ float gradient(float lp, const float4& w) {
 }
 
 struct GradEpi {
-  static constexpr int kStages = 5, kBoxes = 2, kRowsA = kHalf;
+  static constexpr int kStages = 5, kBoxes = 2, kRowsA = kHalf, kChunk = 8;
   RowTerms rows;
   template <typename P>
   struct Warp {
@@ -329,30 +330,31 @@ __global__ void __launch_bounds__(256) linlogp_dz_kernel(uint4* q, const float* 
   const int part = threadIdx.x & 7;
   const float4 w = t.terms[row];
   const int y = t.target[row];
-  const int b1 = min((int)(blockIdx.y + 1) * kDzBlocks, blocks);
+  for (int b0 = (int)blockIdx.y * kDzBlocks; b0 < blocks; b0 += (int)gridDim.y * kDzBlocks) {
 #pragma unroll 4
-  for (int b = blockIdx.y * kDzBlocks; b < b1; ++b) {
-    uint4* at = q + ((int64_t)b * rows + row) * 8 + part;
-    const uint4 v = __ldcs(at);
-    const float ref = from[(int64_t)(b >> 1) * rows + row] - w.x;
-    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-    uint32_t o[4];
-    const int c = y - 64 * b - 8 * part;
-    float gl = 0.f;
-    if ((unsigned)c < 8u) gl = t.g_logp[row];
+    for (int b = b0; b < min(b0 + kDzBlocks, blocks); ++b) {
+      uint4* at = q + ((int64_t)b * rows + row) * 8 + part;
+      const uint4 v = __ldcs(at);
+      const float ref = from[(int64_t)(b >> 1) * rows + row] - w.x;
+      const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+      uint32_t o[4];
+      const int c = y - 64 * b - 8 * part;
+      float gl = 0.f;
+      if ((unsigned)c < 8u) gl = t.g_logp[row];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      float d[2];
+      for (int k = 0; k < 4; ++k) {
+        float d[2];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint32_t x = h ? u[k] >> 16 : u[k] & 0xFFFFu;
-        const float whole = __uint_as_float(x | 0x4B000000u) - kWhole;
-        d[h] = gradient(x == 0xFFFFu ? -INFINITY : fmaf(whole, -1.f / kSteps, ref), w);
-        if (c == 2 * k + h) d[h] += gl;
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t x = h ? u[k] >> 16 : u[k] & 0xFFFFu;
+          const float whole = __uint_as_float(x | 0x4B000000u) - kWhole;
+          d[h] = gradient(x == 0xFFFFu ? -INFINITY : fmaf(whole, -1.f / kSteps, ref), w);
+          if (c == 2 * k + h) d[h] += gl;
+        }
+        o[k] = pack_bf2(d[0], d[1]);
       }
-      o[k] = pack_bf2(d[0], d[1]);
+      *at = make_uint4(o[0], o[1], o[2], o[3]);
     }
-    *at = make_uint4(o[0], o[1], o[2], o[3]);
   }
 }
 
@@ -543,7 +545,7 @@ cudaError_t piece(const LinLogpParams& q, const Layout& l, const Mat& h, const M
     }
     LM_RUN(launch_after(linlogp_join_kernel, dim3((unsigned)((rows + 31) / 32)), 32 * kJoinParts, 0, st, j));
     if (grad)
-      LM_RUN(launch_after(linlogp_dz_kernel, dim3((unsigned)((rows + 31) / 32), (unsigned)((l.blocks + kDzBlocks - 1) / kDzBlocks)), 256, 0, st,
+      LM_RUN(launch_after(linlogp_dz_kernel, dim3((unsigned)((rows + 31) / 32), (unsigned)std::min((l.blocks + kDzBlocks - 1) / kDzBlocks, 65535)), 256, 0, st,
                           reinterpret_cast<uint4*>(ws + l.d), (const float*)(ws + l.from), j.out, rows, (int)l.blocks));
   }
   if (q.dh.data != nullptr) {

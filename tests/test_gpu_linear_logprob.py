@@ -137,8 +137,16 @@ def test_several_pieces_of_the_tokens(T, rows, vocab, width):
     T.linear_logprob(h.t, w.t, y, gl, gh, gz, dh=False, dweight=dw, accumulate=True)
     ref["dweight"] = ref["dweight"] + 1.0
     near(dw, ref, "dweight", 2.0 ** -22)       # four pieces' additions and the first value's
-    again = T.linear_logprob_grad(h.t, w.t, y, o.lse, o.entropy, gl, gh, gz)
+    ref["dweight"] = ref["dweight"] - 1.0
+    _, dw = T.linear_logprob_grad(h.t, w.t, y, o.lse, o.entropy, gl, gh, gz, dh=False, dweight=torch.empty_like(w.t, dtype=torch.float32))
+    near(dw, ref, "dweight", 2.0 ** -22)
+    # added to a bf16 sum
+    before = (torch.randn(w.t.shape, device="cuda") * o.dweight.float().std()).bfloat16()
+    added = before.clone()
+    again = T.linear_logprob_grad(h.t, w.t, y, o.lse, o.entropy, gl, gh, gz, dweight=added, accumulate=True)
     near(again[0], ref, "dh")
+    ref["dweight"] = ref["dweight"] + before.double()
+    near(added, ref, "dweight", U)
 
 
 @pytest.mark.parametrize("to", [torch.bfloat16, torch.float32])
