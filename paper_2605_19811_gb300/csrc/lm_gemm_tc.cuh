@@ -258,8 +258,18 @@ __device__ __forceinline__ void arrive_cta0(uint64_t* bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(peer_addr(bar, 0)) : "memory");
 }
 
-__device__ __forceinline__ void few_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 96;"); }
-__device__ __forceinline__ void many_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 200;"); }
+// 384 threads have 168 registers each at launch; the first warpgroup leaves some
+// to the epilogue's two.
+template <int kFew>
+__device__ __forceinline__ void few_registers() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFew));
+}
+template <int kFew>
+__device__ __forceinline__ void many_registers() {
+  constexpr int kMany = (168 * 3 - kFew) / 2 / 8 * 8;
+  static_assert(kFew % 8 == 0 && kFew + 2 * kMany <= 168 * 3, "registers of the launch");
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kMany));
+}
 
 // Where an epilogue warp stands: lane l holds row `row + l` of D, columns
 // `col` .. `col` + 127 (of them < n inside).
@@ -405,6 +415,9 @@ __device__ __forceinline__ void put_rows(const float (&v)[32], const Place& at, 
 // Epilogue that stores D.
 struct StoreEpi {
   static constexpr int kStages = 6, kBoxes = 1, kRowsA = kHalf, kChunk = 8;
+  // registers a thread of the first warpgroup: with 136 (and 184) ptxas spills none,
+  // with 96 (and 200) 212 bytes (dh of 4096 x 4096 over 50257: 1006 us, 968 so)
+  static constexpr int kFewRegs = 136;
   Store out;
   template <typename P>
   struct Warp {
@@ -563,11 +576,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_ke
   const uint32_t tmem_base = *tmem_slot;
   const uint64_t wait_ns = p.wait_ns;
 
-  // 384 threads x 168 registers at launch, more than 128 x 96 + 256 x 200: the epilogue
-  // holds 128 sums and what it makes of them
   if (warp == 0) {
     // -------------------------------- producer ---------------------------------
-    few_registers();
+    few_registers<Epi::kFewRegs>();
     if (lane == 0) {
       int stage = 0;
       uint32_t ph = 0;
@@ -604,7 +615,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_ke
     }
   } else if (warp == 1) {
     // -------------------------------- MMA issuer -------------------------------
-    few_registers();
+    few_registers<Epi::kFewRegs>();
     if (rank == 0) {
       constexpr uint32_t idesc = make_idesc(kTileM, kTileN, kAMn, kBMn);
       // 16 of the sum: 16 rows of 128 bytes (MN-major), 32 bytes of a row (K-major)
@@ -661,7 +672,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_ke
     }
   } else if (warp >= kFirstEpi) {
     // --------------------------------- epilogue ----------------------------------
-    many_registers();
+    many_registers<Epi::kFewRegs>();
     Place at;
     at.lane = lane;
     at.half = (warp - kFirstEpi) >> 2;
@@ -726,7 +737,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) gemm_ke
     }
     if (lane == 0) bulk_wait_all();   // stores from the boxes
   } else {
-    few_registers();
+    few_registers<Epi::kFewRegs>();
   }
 
   __syncwarp();

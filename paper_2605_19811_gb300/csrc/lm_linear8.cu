@@ -344,7 +344,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
 
   if (warp == 0) {
     // -------------------------------- producer ---------------------------------
-    few_registers();
+    few_registers<96>();
     if (lane == 0) {
       int stage = 0;
       uint32_t ph = 0;
@@ -391,7 +391,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
     }
   } else if (warp == 1) {
     // -------------------------------- MMA issuer -------------------------------
-    few_registers();
+    few_registers<96>();
     if (rank == 0) {
       constexpr uint32_t idesc = idesc8(kGrad);
       // 32 of the sum: 32 bytes of a row (K-major), 32 rows of 128 bytes (MN-major)
@@ -468,7 +468,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
     }
   } else if (warp >= kFirstEpi) {
     // --------------------------------- epilogue ----------------------------------
-    many_registers();
+    many_registers<96>();
     const int half = (warp - kFirstEpi) >> 2, q = warp & 3, r0 = (int)rank * kHalf + q * 32;
     const uint32_t box = smem_u32(smem + R::kBoxes + (size_t)(warp - kFirstEpi) * kWarpBytes);
     const uint32_t lanes = (uint32_t)(q * 32) << 16;
@@ -570,7 +570,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
     }
     if (lane == 0) bulk_wait_all();   // stores from the boxes
   } else {
-    few_registers();
+    few_registers<96>();
   }
 
   __syncwarp();

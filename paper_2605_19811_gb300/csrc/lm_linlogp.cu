@@ -97,6 +97,7 @@ constexpr int kFewRows = 32;
 template <bool kKeep, bool kFew>
 struct ForwardEpi {
   static constexpr int kStages = kKeep ? 5 : kFew ? 10 : 6, kBoxes = kKeep ? 2 : 0, kRowsA = kFew ? kFewRows : kHalf;
+  static constexpr int kFewRegs = 120;             // (fewest spills)
   static constexpr int kChunk = kFew ? 2 : 4;      // blocks of a logit's sum in one accumulator: 128 products, or 256
   float* from;          // kKeep: r of each half tile's rows, (2 tiles_n) x rows
   const int64_t* targets;
@@ -215,7 +216,7 @@ __device__ __forceinline__ float gradient(float lp, const float4& w) {
 }
 
 struct GradEpi {
-  static constexpr int kStages = 5, kBoxes = 2, kRowsA = kHalf, kChunk = 8;
+  static constexpr int kStages = 5, kBoxes = 2, kRowsA = kHalf, kChunk = 8, kFewRegs = 120;
   RowTerms rows;
   template <typename P>
   struct Warp {
