@@ -103,7 +103,8 @@ def product(x, w, grad):
 
 
 SIZES = [(1, 1, 1), (1, 64, 7), (1, 4096, 2304), (3, 129, 130), (8, 1024, 300), (16, 512, 4097), (17, 517, 128), (31, 16, 1000), (33, 2049, 640),
-         (64, 96, 256), (65, 300, 511), (127, 128, 128), (128, 1024, 512), (129, 640, 257), (256, 256, 256), (257, 1283, 517), (1000, 4096, 768), (2049, 64, 130)]
+         (64, 96, 256), (65, 300, 511), (127, 128, 128), (128, 1024, 512), (129, 640, 257), (256, 256, 256), (257, 1283, 517), (1000, 4096, 768), (2049, 64, 130),
+         (5, 300, 10000), (32, 1030, 19999), (33, 1030, 9999)]
 
 
 @pytest.mark.parametrize("to", [torch.bfloat16, torch.float32])
@@ -182,6 +183,19 @@ def test_views_empty_and_refused(T):
         T.linear8(x, part, out=torch.empty(40, 384, device="cuda"))
     with pytest.raises(RuntimeError):
         T.linear8_grad(x, w)
+
+
+def test_results_beyond_31_bits(T):
+    """2.2 G elements of y: the last tokens' are those of a call with them alone."""
+    tokens, cols, out = 270001, 128, 8192
+    g = torch.Generator(device="cuda").manual_seed(9)
+    x = T.checkpoint8(torch.randn(tokens, cols, device="cuda", generator=g), "e4m3")
+    w = T.weight8(torch.randn(out, cols, device="cuda", generator=g))
+    y = T.linear8(x, w)
+    for at in (0, 135000, tokens - 500):
+        part = T.Checkpoint8(x.codes[at:at + 500], x.scales[:, at:at + 500], cols, "e4m3")
+        want, most = product(part, w, False)
+        assert bool(((y[at:at + 500].double() - want).abs() <= most * 2.0 ** -17 + 2.0 ** -8 * want.abs()).all())
 
 
 def test_streams_and_graphs(T):

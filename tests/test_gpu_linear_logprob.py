@@ -94,7 +94,7 @@ def near(got, ref, name, more=0.0):
 
 SIZES = [(1, 1, 1, 0, 0), (1, 7, 8, 0, 0), (1, 1000, 64, 0, 0), (2, 129, 65, 3, 1), (31, 257, 63, 0, 0), (256, 256, 512, 0, 0),
          (257, 255, 513, 8, 0), (255, 5003, 200, 0, 0), (300, 128, 1283, 5, 3), (1000, 1000, 768, 0, 8), (3, 50257, 128, 0, 0),
-         (513, 2049, 1024, 0, 0), (40, 20000, 1100, 8, 8)]
+         (513, 2049, 1024, 0, 0), (40, 20000, 1100, 8, 8), (32, 5000, 96, 0, 0), (33, 5000, 96, 8, 0)]
 
 
 @pytest.mark.parametrize("rows,vocab,width,pad,offset", SIZES)

@@ -202,6 +202,22 @@ def test_rows_of_zeros_infinity_and_nan(T):
     assert bool((o.k[3, 0][~o.k[3, 0].isnan()] == 0).all())
 
 
+def test_offsets_beyond_31_bits(T):
+    """2.6 G elements: the last tokens' results, forward and gradient, are those of a call with them alone."""
+    tokens, heads, dim = 500001, 40, 128
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q = torch.empty(tokens, heads, dim, device="cuda", dtype=torch.bfloat16).normal_(generator=g)
+    pos = torch.arange(tokens, device="cuda") % 1000
+    table = T.rotary_table(1000, T.rotary_frequencies(dim))
+    w = torch.rand(dim, device="cuda", generator=g)
+    o = T.qk_rotary(q, None, pos, table, w)
+    r = T.qk_rotary_grad(q, None, pos, table, q, None, w)
+    for at in (0, tokens - 300):
+        e = slice(at, at + 300)
+        assert torch.equal(o.q[e], T.qk_rotary(q[e], None, pos[e], table, w).q)
+        assert torch.equal(r.dq[e], T.qk_rotary_grad(q[e], None, pos[e], table, q[e], None, w).dq)
+
+
 def test_no_tokens(T):
     c = Case(3, 2, 2, 64, 64, False, True, torch.float32, "packed")
     o = T.qk_rotary(c.q[:0], c.k[:0], c.pos[:0], c.table, c.qw, c.kw, **c.args())
