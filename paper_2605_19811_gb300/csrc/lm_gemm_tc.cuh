@@ -19,13 +19,14 @@
 // fp32, to sums that it holds in registers while the MMA fills the other one.
 //
 // Schedule: units of `strip` tiles of one tile row, dealt to the pairs in turn.
-// With split sums, as many tiles as fill whole waves go one to a pair, and the
-// tiles left over are one line of (tile, block) work cut into equal ranges; a
-// tile that falls to several pairs is summed from their fp32 parts, in order,
-// by a second kernel.  Where D has few tile columns, as many pairs walk a tile
-// row together, one a column, and the line is of (tile row, block): they read
-// the same blocks of A at the same time, from L2 (each column for itself, A came
-// from memory once for each: 4096 x 768 over 50304, 284 us).
+// With split sums, as many tiles as fill whole waves go one to a pair; the tiles
+// left over are shared, each cut into equal ranges of its sum where that leaves few
+// pairs out, else as one line of (tile, block) work cut into equal ranges.  A tile
+// that falls to several pairs is summed from their fp32 parts, in order, by a second
+// kernel.  Where D has few tile columns, as many pairs walk a tile row together, one
+// a column, and what is dealt and cut is tile rows: they read the same blocks of A
+// at the same time, from L2 (each column for itself, A came from memory once for
+// each: 4096 x 768 over 50304, 284 us).
 //
 // The whole issuing warp goes through the MMAs' loop, so that what they take is
 // uniform, and asks for the next block before this one's: their queue is short, and
@@ -86,6 +87,7 @@ struct Schedule {
   int32_t units;        // units dealt to the teams in turn (tile row, strip)
   int32_t rest;         // units left over, shared by range (strip 1)
   int32_t sharers;      // teams that share them; 0: none left over
+  int32_t cuts;         // as many to each unit, over equal ranges of its sum; 0: equal ranges of the line
   int64_t begin[kMostSharers + 1];   // sharer k's first (tile, block) in the line of left-over work
 };
 template <typename Epi>
@@ -315,23 +317,13 @@ __device__ __forceinline__ void box_ready() {
   __syncwarp();
 }
 
-// Where a result goes: one element, or four of a row, `left` of them inside.
+// Four elements of a row, `left` of them inside.
 struct Store {
   Mat d;
   int32_t dt;
   int32_t accumulate;   // adds to d
   int32_t vec;          // d takes four elements at a time
   int32_t tma;          // whole tiles go to d by the TMA (a map of it; fp32 may be added)
-  __device__ __forceinline__ void one(int64_t row, int col, float v) const {
-    const int64_t at = row * d.ld + col;
-    if (dt == LM_F32) {
-      float* o = static_cast<float*>(d.data) + at;
-      *o = accumulate ? *o + v : v;
-    } else {
-      __nv_bfloat16* o = static_cast<__nv_bfloat16*>(d.data) + at;
-      *o = __float2bfloat16_rn(accumulate ? __bfloat162float(*o) + v : v);
-    }
-  }
   __device__ __forceinline__ void put(int64_t row, int col, float4 v, int left) const {
     float e[4] = {v.x, v.y, v.z, v.w};
     const int64_t at = row * d.ld + col;
@@ -397,17 +389,40 @@ __device__ __forceinline__ void put_block(const float (&v)[32], const Place& at,
   __syncwarp();
 }
 
-// The same where D's rows do not take four at a time: a row a step, a column a
-// lane, so that a row's elements still go out side by side.
-__device__ __forceinline__ void put_rows(const float (&v)[32], const Place& at, int rows, int c, int n, const Store& out) {
+// 32 rows (one a lane) x 32 columns from column c, stored and not added: four
+// columns a lane where D's rows take them, else a row a step and a column a lane,
+// so that a row's elements still go out side by side.  One way through the rows,
+// without a question an element (dW of 150000 x 2500 over 700 tokens, rows of 5000
+// bytes: 909 us with Store::put).
+__device__ __forceinline__ void put_plain4(float* o, float4 v) { *reinterpret_cast<float4*>(o) = v; }
+__device__ __forceinline__ void put_plain4(__nv_bfloat16* o, float4 v) { *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf2(v.x, v.y), pack_bf2(v.z, v.w)); }
+__device__ __forceinline__ void put_plain(float* o, float v) { *o = v; }
+__device__ __forceinline__ void put_plain(__nv_bfloat16* o, float v) { *o = __float2bfloat16_rn(v); }
+template <typename T>
+__device__ __forceinline__ void put_plain_block(const float (&v)[32], const Place& at, int rows, int c, int n, const Store& out) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) box_put(at.box, at.lane, e, v + 4 * e);
   __syncwarp();
+  T* o = static_cast<T*>(out.d.data) + (int64_t)at.row * out.d.ld + c;
+  if (out.vec && c + 32 <= n) {
+    const int q = at.lane & 7, r4 = at.lane >> 3;
+    o += r4 * out.d.ld + 4 * q;
+    const int64_t step = 4 * out.d.ld;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (r4 + 4 * k < rows) put_plain4(o, box_get(at.box, r4 + 4 * k, q));
+      o += step;
+    }
+  } else {
+    o += at.lane;
+    const bool in = c + at.lane < n;
 #pragma unroll 8
-  for (int r = 0; r < rows; ++r) {
-    float x;
-    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(box_at(at.box, r, at.lane >> 2) + 4 * (at.lane & 3)) : "memory");
-    if (c + at.lane < n) out.one(at.row + r, c + at.lane, x);
+    for (int r = 0; r < rows; ++r) {
+      float x;
+      asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(box_at(at.box, r, at.lane >> 2) + 4 * (at.lane & 3)) : "memory");
+      if (in) put_plain(o, x);
+      o += out.d.ld;
+    }
   }
   __syncwarp();
 }
@@ -472,12 +487,13 @@ struct StoreEpi {
           put_block(acc[b], at, rows, c, [&](int r, int col, float4 v) {
             *reinterpret_cast<float4*>(part + (size_t)(r0 + r) * kTileN + (col - c0)) = v;
           });
-        } else if (p.epi.out.vec) {
+        } else if (!p.epi.out.accumulate) {
+          if (p.epi.out.dt == LM_F32) put_plain_block<float>(acc[b], at, rows, c, p.n, p.epi.out);
+          else put_plain_block<__nv_bfloat16>(acc[b], at, rows, c, p.n, p.epi.out);
+        } else {
           put_block(acc[b], at, rows, c, [&](int r, int col, float4 v) {
             if (col < p.n) p.epi.out.put(at.row + r, col, v, p.n - col);
           });
-        } else {
-          put_rows(acc[b], at, rows, c, p.n, p.epi.out);
         }
       }
     }
@@ -867,12 +883,22 @@ inline Schedule split_schedule(int64_t m, int64_t n, int64_t k, int tile_n = kTi
     // a share of at least `least` blocks, and never more sharers than teams
     const int64_t most = (int64_t)s.rest * s.nkb / least;
     s.sharers = (int32_t)(most < s.rest ? s.rest : most < teams ? most : teams);
+    // Equal cuts of every unit, where they leave few teams out: those of one range of
+    // the sum then read the same blocks of A and B at the same time, from L2 (dh of
+    // 700 x 2500 over 150000: 723 us with equal ranges of the line, each operand from
+    // memory several times).
+    const int32_t cuts = (int32_t)std::min<int64_t>(teams / s.rest, std::max<int64_t>(1, s.nkb / least));
+    if (4 * s.rest * cuts >= 3 * s.sharers) {
+      s.cuts = cuts;
+      s.sharers = s.rest * cuts;
+    }
   }
   return s;
 }
 // Where the sharers' ranges begin (for the launch alone).
 inline void share(Schedule& s) {
-  for (int k = 0; s.sharers > 0 && k <= s.sharers; ++k) s.begin[k] = (int64_t)s.rest * s.nkb * k / s.sharers;
+  for (int k = 0; s.sharers > 0 && k <= s.sharers; ++k)
+    s.begin[k] = s.cuts > 0 ? (int64_t)(k / s.cuts) * s.nkb + (int64_t)s.nkb * (k % s.cuts) / s.cuts : (int64_t)s.rest * s.nkb * k / s.sharers;
 }
 inline bool has_parts(const Schedule& s) { return s.rest > 0 && s.sharers > s.rest; }
 inline size_t parts_bytes(const Schedule& s, int tile_n = kTileN) { return has_parts(s) ? 2 * (size_t)s.sharers * s.team * kTileM * tile_n * 4 : 0; }

@@ -269,11 +269,11 @@ __device__ __forceinline__ void put16(const float (&v)[32], uint32_t box, int la
   }
 }
 
-// The same where y's rows do not take four at a time: two rows a step, 16 columns
-// of each, a column a lane.
-__device__ __forceinline__ void put16_rows(const float (&v)[32], uint32_t box, int lane, int row0, int rows, int c, int n, const Store& out) {
+// The same straight to y, as gemm::put_plain_block: eight rows a step and four
+// columns a lane, or two rows and a column.
+template <typename T>
+__device__ __forceinline__ void put16_plain(const float (&v)[32], uint32_t box, int lane, int row0, int rows, int c, int n, const Store& out) {
   auto at = [&](int row, int chunk) { return box + row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4); };
-  const int e = lane & 15;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -282,11 +282,28 @@ __device__ __forceinline__ void put16_rows(const float (&v)[32], uint32_t box, i
       asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at(lane, k)), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]) : "memory");
     }
     __syncwarp();
+    T* o = static_cast<T*>(out.d.data) + (int64_t)row0 * out.d.ld + c + 16 * h;
+    if (out.vec && c + 16 * h + 16 <= n) {
+      const int q = lane & 3, r8 = lane >> 2;
+      o += r8 * out.d.ld + 4 * q;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float4 x;
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(at(r8 + 8 * k, q)) : "memory");
+        if (r8 + 8 * k < rows) put_plain4(o, x);
+        o += 8 * out.d.ld;
+      }
+    } else {
+      const int e = lane & 15;
+      const bool in = c + 16 * h + e < n;
+      o += (lane >> 4) * out.d.ld + e;
 #pragma unroll 8
-    for (int r = lane >> 4; r < rows; r += 2) {
-      float x;
-      asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(at(r, e >> 2) + 4 * (e & 3)) : "memory");
-      if (c + 16 * h + e < n) out.one(row0 + r, c + 16 * h + e, x);
+      for (int r = lane >> 4; r < rows; r += 2) {
+        float x;
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(at(r, e >> 2) + 4 * (e & 3)) : "memory");
+        if (in) put_plain(o, x);
+        o += 2 * out.d.ld;
+      }
     }
     __syncwarp();
   }
@@ -556,15 +573,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
               bulk_commit();
             }
           }
-        } else if (it.slot < 0 && !p.out.vec) {
-          put16_rows(acc[b], box, lane, row0, rows, c, p.n, p.out);
+        } else if (it.slot < 0) {
+          if (p.out.dt == LM_F32) put16_plain<float>(acc[b], box, lane, row0, rows, c, p.n, p.out);
+          else put16_plain<__nv_bfloat16>(acc[b], box, lane, row0, rows, c, p.n, p.out);
         } else {
           box_free(lane);
-          put16(acc[b], box, lane, rows, [&](int r, int e, float4 v) {
-            const int col = c + e;
-            if (it.slot >= 0) *reinterpret_cast<float4*>(p.parts + (size_t)it.slot * (kTileM * kN) + (size_t)(r0 + r) * kN + (c0 + 32 * b + e)) = v;
-            else if (col < p.n) p.out.put(row0 + r, col, v, p.n - col);
-          });
+          float* part = p.parts + (size_t)it.slot * (kTileM * kN) + (size_t)r0 * kN + c0 + 32 * b;
+          put16(acc[b], box, lane, rows, [&](int r, int e, float4 v) { *reinterpret_cast<float4*>(part + r * kN + e) = v; });
         }
       }
     }

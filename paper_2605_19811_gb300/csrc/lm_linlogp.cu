@@ -411,24 +411,33 @@ __global__ void __launch_bounds__(256) linlogp_copy_kernel(Mat from, int64_t nro
   griddep_wait();
   griddep_launch_dependents();
   const int per = (cols + 255) / 256, lane = threadIdx.x & 31;
-  const int64_t all = nrows * per, step = (int64_t)gridDim.x * 8;
-  for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < all; i += kAhead * step) {
+  // a warp's way over the pieces, `step` apart
+  const int64_t first = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), step = (int64_t)gridDim.x * 8, drow = step / per;
+  int64_t row = first / per;
+  int piece = (int)(first - row * per);
+  const int dpiece = (int)(step - drow * per);
+  while (row < nrows) {
     rows::Raw<__nv_bfloat16> raw[kAhead];
-    int64_t row[kAhead];
+    int64_t r[kAhead];
     int c[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      const int64_t at = i + k * step;
-      row[k] = at < all ? at / per : -1;
-      c[k] = (int)(at - row[k] * per) * 256 + 8 * lane;
-      raw[k].load<false>(rows::Row<const __nv_bfloat16>(from, row[k] < 0 ? 0 : row[k], nrows), c[k], row[k] < 0 ? rows::kNoRow : cols - c[k]);
+      r[k] = row;
+      c[k] = piece * 256 + 8 * lane;
+      raw[k].load<false>(rows::Row<const __nv_bfloat16>(from, row < nrows ? row : 0, nrows), c[k], row < nrows ? cols - c[k] : rows::kNoRow);
+      row += drow;
+      piece += dpiece;
+      if (piece >= per) {
+        piece -= per;
+        ++row;
+      }
     }
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      if (row[k] < 0) break;
-      raw[k].settle<false>(rows::Row<const __nv_bfloat16>(from, row[k], nrows), c[k], cols - c[k]);
+      if (r[k] >= nrows) break;
+      raw[k].settle<false>(rows::Row<const __nv_bfloat16>(from, r[k], nrows), c[k], cols - c[k]);
       // (ld is a multiple of eight: eight are inside the row wherever one is)
-      if (c[k] < cols) *reinterpret_cast<uint4*>(to + row[k] * ld + c[k]) = make_uint4(raw[k].w[0], raw[k].w[1], raw[k].w[2], raw[k].w[3]);
+      if (c[k] < cols) *reinterpret_cast<uint4*>(to + r[k] * ld + c[k]) = make_uint4(raw[k].w[0], raw[k].w[1], raw[k].w[2], raw[k].w[3]);
     }
   }
 }
