@@ -5,8 +5,10 @@
 // scale for each block of 128 x 128, on the tensor cores: tcgen05.mma
 // (kind::mxf8f6f4) on CTA pairs takes the e4m3 codes as they are and multiplies
 // each 32 of the sum by two powers of two, here the same for four such steps.  A
-// power-of-two float's exponent bits are that scale, so a first kernel copies
-// them, a byte a row, in the order in which the tensor memory holds them.
+// power-of-two float's exponent bits are that scale; they are put, a byte a row, into
+// the order in which the tensor memory holds them: by a first kernel, from which they
+// are loaded like the codes, or, where there is little work, by two warps of each CTA
+// (kMake).
 //
 // A pair takes a tile of 256 tokens x 256 columns, 256 of the sum at a time.  CTA r
 // holds tokens 128 r .. (A) and columns 128 r .. (B); W lies K-major for the product
@@ -17,9 +19,9 @@
 //
 // Measured: 16384 x 4096 x 14336 580 us (3.3 PFLOP/s), by itself; bound by what the
 // SMs take from L2 (473 us without the TMA's loads) and by the copies of the scales
-// (15 us) and the accumulators' turns (13).  16384 x 1280 x 5120 by W 82 us.  One
-// token by 14336 x 4096 17 us (59 MB, 3.5 TB/s): 2 us until the first bytes are there,
-// 3 us at the end.  Packing 14336 x 4096 bf16 42 us (4.2 TB/s, instructions), back 31 us
+// (15 us) and the accumulators' turns (13).  16384 x 5120 by W of 5120 x 1280 76 us.
+// One token by 14336 x 4096 19.5 us (59 MB, 3 TB/s): 2 us until the first bytes are
+// there, 3 us at the end, and the scales' way.  Packing 14336 x 4096 bf16 42 us (4.2 TB/s, instructions), back 31 us
 // (5.7 TB/s).
 //
 // Two accumulators of 256 columns would leave the tensor memory no room for the
@@ -152,6 +154,13 @@ constexpr int kFewTokens = 32;
 constexpr int kLeastShare = 8;                          // stages of a split sum's part: the parts and their join cost as much as ten
 constexpr int kChunk8 = 8;                              // most stages summed in one accumulator: 64 additions
 constexpr int kScaleBytes = 512 + 1024;                 // of two stages: the CTA's rows', the tile's columns'
+constexpr int kScaleRing = 4;                           // kMake: how many are under way
+// The kernel makes the scales itself where a pair takes at most so many stages.  One
+// launch less: one token by 14336 x 4096 20.4 us a call instead of 22 to 31 (the kernel
+// 19.5 instead of 17.1 and 1.8); 1021 x 517 by 1283 the kernel 17.1 us instead of 15.3
+// and 1.7, calls one after another 4 us less.  But these warps' loads cost 6% of the
+// rate: 16384 x 5120 by 1280 83 us instead of 76 and 3.7.
+constexpr int kMakeStages = 32;
 constexpr int kWarpBytes = 32 * 64;                     // an epilogue warp's box: 32 columns in bf16, 16 in fp32
 constexpr int kShared = 32, kSecond = kN - kShared;     // TMEM: the second accumulator's first column
 constexpr int kScaleCol = kSecond + kN, kScaleSlots = 2;    // then 16 columns for each two stages' scales
@@ -160,38 +169,62 @@ static_assert(kScaleCol + 16 * kScaleSlots <= kTmemCols, "tensor memory");
 // that counts, and more of them are under way: A is loaded, and has room, for those
 // rows alone.  The MMA reads 128 rows from A's place all the same; the others are
 // bytes of B, and the rows of the result that they reach are never stored.
-template <bool kFew>
+template <bool kFew, bool kMake>
 struct Ring {
   static constexpr int kStages = kFew ? 5 : 3, kRowsA = kFew ? kFewTokens : kHalf, kSubA = kRowsA * kSub, kSubB = kHalfN * kSub;
   static constexpr int kStage = kSubs * (kSubA + kSubB);
   static constexpr size_t kBoxes = (size_t)kStages * kStage, kScales = kBoxes + (size_t)kEpiWarps * kWarpBytes;
-  static constexpr size_t kBars = kScales + (size_t)kStages * kScaleBytes, kBytes = 1024 + kBars + 512;
+  static constexpr size_t kBars = kScales + (size_t)(kMake ? kScaleRing : kStages) * kScaleBytes, kBytes = 1024 + kBars + 512;
   static_assert(kBytes <= 232448, "shared memory of one SM");
   static_assert(kSubA % 1024 == 0 && kSubB % 1024 == 0 && kWarpBytes % 512 == 0 && kScaleBytes % 128 == 0, "swizzled boxes");
   static_assert(kSubs * kSubA + kSubs * kSubB >= (kSubs - 1) * kSubA + kHalf * kSub, "128 rows from A's last place on are inside the stage");
 };
 
-struct Params8 {
-  CUtensorMap a, b, sa, sb, y;
-  Schedule sch;
-  int32_t m, n;
-  float* parts;
-  uint64_t wait_ns;
-  Store out;
-};
 
-// Scales as the tensor memory takes them: the 128 of a block of rows as 32 x 16
-// bytes, row 32 j + l at word 4 l + j, four groups of the sum in a word's bytes.
-// Activations: (four groups, 128 tokens); weights: (four groups, tile of columns,
-// two blocks of 128).
-struct ScaleParams {
+// The scales' source.
+struct Scales {
   const float *x, *w;
   int64_t ldx, ldw, tokens;
-  int32_t n, groups, fours, row_blocks, tiles_n;
+  int32_t n, groups;
+};
+__device__ __forceinline__ uint32_t exponent(float s) { return __float_as_uint(s) >> 23; }     // 255 for NaN
+// As the tensor memory takes them: the 128 of a block of rows as 32 x 16 bytes,
+// row 32 j + l at word 4 l + j, four groups of the sum in a word's bytes.  kMake: lane l
+// reads those of rows l, 32 + l, 64 + l, 96 + l of its CTA's tokens, and those of the
+// tile's two blocks of 128 columns, from group 4 `four` on; 0 where there are none.
+struct FourScales {
+  float x[4][4], w[2][4];
+  template <bool kGrad>
+  __device__ __forceinline__ void load(const Scales& p, int four, int64_t row, int64_t col, int lane) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int64_t g = 4 * (int64_t)four + k;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int64_t token = row + 32 * j + lane;
+        x[j][k] = g < p.groups && token < p.tokens ? p.x[g * p.ldx + token] : 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int64_t block = col / kBlock + j;
+        w[j][k] = g < p.groups && block * kBlock < p.n ? (kGrad ? p.w[g * p.ldw + block] : p.w[block * p.ldw + g]) : 0.f;
+      }
+    }
+  }
+  static __device__ __forceinline__ uint32_t word(const float (&v)[4]) {
+    return exponent(v[0]) | exponent(v[1]) << 8 | exponent(v[2]) << 16 | exponent(v[3]) << 24;
+  }
+};
+static_assert(kN == 2 * kBlock, "two blocks of the weights' scales a tile");
+
+// The first kernel's: activations (four groups, 128 tokens), weights (four groups,
+// tile of columns, two blocks of 128).
+struct ScaleParams {
+  Scales from;
+  int32_t fours, row_blocks, tiles_n;
   bool grad;
   uint32_t *sa, *sb;
 };
-__device__ __forceinline__ uint32_t exponent(float s) { return __float_as_uint(s) >> 23; }     // 255 for NaN
 __global__ void __launch_bounds__(128) scales_kernel(const ScaleParams p) {
   griddep_wait();
   griddep_launch_dependents();
@@ -204,7 +237,7 @@ __global__ void __launch_bounds__(128) scales_kernel(const ScaleParams p) {
       const int64_t token = (int64_t)(block - (uint32_t)four * (uint32_t)p.row_blocks) * 128 + t;
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        if (token < p.tokens && 4 * four + k < p.groups) v |= exponent(p.x[(int64_t)(4 * four + k) * p.ldx + token]) << (8 * k);
+        if (token < p.from.tokens && 4 * four + k < p.from.groups) v |= exponent(p.from.x[(int64_t)(4 * four + k) * p.from.ldx + token]) << (8 * k);
       p.sa[(size_t)block * 128 + (t & 31) * 4 + (t >> 5)] = v;
     } else {               // in the order of the words: word t holds this column
       const uint32_t b = block - a, four = b / (2u * (uint32_t)p.tiles_n), tile = b - four * 2u * (uint32_t)p.tiles_n;
@@ -212,13 +245,22 @@ __global__ void __launch_bounds__(128) scales_kernel(const ScaleParams p) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const int64_t g = 4 * (int64_t)four + k;
-        if (col < p.n && g < p.groups) v |= exponent(p.grad ? p.w[g * p.ldw + col / kBlock] : p.w[col / kBlock * p.ldw + g]) << (8 * k);
+        if (col < p.from.n && g < p.from.groups) v |= exponent(p.grad ? p.from.w[g * p.from.ldw + col / kBlock] : p.from.w[col / kBlock * p.from.ldw + g]) << (8 * k);
       }
       p.sb[(size_t)b * 128 + t] = v;
     }
   }
 }
-static_assert(kN == 256, "two blocks of scales a tile");
+
+struct Params8 {
+  CUtensorMap a, b, sa, sb, y;                        // sa, sb: from the first kernel
+  Schedule sch;
+  Scales scales;                                      // kMake
+  int32_t m, n;
+  float* parts;
+  uint64_t wait_ns;
+  Store out;
+};
 
 // Instruction descriptor, kind::mxf8f6f4: A and B e4m3, scales ue8m0 (bit 23),
 // the byte of a scale's word at bits 4 (B) and 29 (A), N >> 3 at bit 17, M >> 7
@@ -234,6 +276,20 @@ __device__ __forceinline__ void umma_mx8(uint32_t leader, uint32_t d, uint64_t a
       "@q tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
       "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate), "r"(leader)
       : "memory");
+}
+// await and mbar_test for a barrier on which the other CTA's scales arrive: what
+// that CTA wrote before is visible too.
+__device__ __forceinline__ bool mbar_test_cluster(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ bool await_cluster(uint64_t* bar, uint32_t parity, volatile int* abort_flag, uint64_t limit_ns) {
+  return await(bar, parity, abort_flag, limit_ns) && mbar_test_cluster(bar, parity);
 }
 // 32 x 16 bytes of shared memory to four columns of every lane quadrant, in both
 // CTAs; MMAs issued after it by the same thread see them.
@@ -309,9 +365,9 @@ __device__ __forceinline__ void put16_plain(const float (&v)[32], uint32_t box, 
   }
 }
 
-template <bool kGrad, bool kFew>
+template <bool kGrad, bool kFew, bool kMake>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8_kernel(const __grid_constant__ Params8 p) {
-  using R = Ring<kFew>;
+  using R = Ring<kFew, kMake>;
   constexpr int kStages = R::kStages, kStage = R::kStage, kSubA = R::kSubA, kSubB = R::kSubB;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -320,7 +376,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
   uint64_t* accfull = empty + kStages;
   uint64_t* accempty = accfull + 2;
   uint64_t* shared = accempty + 2;                    // the columns that both accumulators have are read
-  uint64_t* done = shared + 2;
+  uint64_t* sfull = shared + 2;                       // kMake: both CTAs' scales are there, and copied
+  uint64_t* sempty = sfull + kScaleRing;
+  uint64_t* done = sempty + kScaleRing;
   ProducerLog<kStages>* log = reinterpret_cast<ProducerLog<kStages>*>(done + 1);
   int* armed = reinterpret_cast<int*>(log + 1);       // last phase CTA 0 armed on each stage, or -1 (producer lane)
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(armed + kStages);
@@ -341,6 +399,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
       mbar_init(&accfull[b], 1);
       mbar_init(&accempty[b], 2 * kEpiWarps);
       mbar_init(&shared[b], kEpiWarps);               // the warps of one half, in both CTAs
+    }
+    for (int b = 0; b < kScaleRing; ++b) {
+      mbar_init(&sfull[b], 2);
+      mbar_init(&sempty[b], 1);
     }
     mbar_init(done, 1);
     log->n = 0;
@@ -377,9 +439,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
           }
           uint8_t* sa = smem + (size_t)stage * kStage;
           uint8_t* sb = sa + kSubs * kSubA;
-          uint8_t* ss = smem + R::kScales + (size_t)stage * kScaleBytes;
           const uint32_t fb = peer_addr(&full[stage], 0);
-          const bool scales = kb == it.kb0 || (kb & 1) == 0;      // four groups', of two stages
+          const bool scales = !kMake && (kb == it.kb0 || (kb & 1) == 0);      // four groups', of two stages
           const uint32_t tx = kStage + (scales ? kScaleBytes : 0);
           if (rank == 0) {
             mbar_arrive_expect_tx(&full[stage], 2u * tx);
@@ -395,6 +456,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
             else tma_load_3d(sb + k * kSubB, &p.b, fb, at, col, 0);
           }
           if (scales) {
+            uint8_t* ss = smem + R::kScales + (size_t)stage * kScaleBytes;
             tma_load_3d(ss, &p.sa, fb, 0, row / 128, kb >> 1);
             tma_load_3d(ss + 512, &p.sb, fb, 0, it.tn, kb >> 1);
           }
@@ -416,7 +478,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
       const uint32_t leader = lane == 0 ? 1u : 0u, smem0 = smem_u32(smem), tmem0 = __shfl_sync(0xFFFFFFFFu, tmem_base, 0);
       int stage = 0, ab = 0;
       uint32_t ph = 0, aph = 0, ta = 0, blocks = 0, slot = 0, last_use[kScaleSlots] = {0, 0};   // blocks: issued so far
-      bool ok = true, ready = false;
+      int sslot = 0;
+      uint32_t sph = 0;
+      bool ok = true, ready = false, sready = false;
       auto wait = [&](uint64_t* bar, uint32_t parity) {
         if (!__all_sync(0xFFFFFFFFu, await(bar, parity, abort_flag, wait_ns))) ok = false;
         return ok;
@@ -441,11 +505,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
               if (last_use[slot] > 0 && blocks + 1 - last_use[slot] < (uint32_t)kStages &&
                   !wait(&empty[(last_use[slot] - 1) % kStages], ((last_use[slot] - 1) / kStages) & 1u))
                 break;
-              const uint32_t ss = smem0 + (uint32_t)(R::kScales + (size_t)stage * kScaleBytes);
+              if (kMake && !sready && !__all_sync(0xFFFFFFFFu, await_cluster(&sfull[sslot], sph, abort_flag, wait_ns))) {
+                ok = false;
+                break;
+              }
+              const uint32_t ss = smem0 + (uint32_t)(R::kScales + (size_t)(kMake ? sslot : stage) * kScaleBytes);
               ta = tmem0 + (uint32_t)kScaleCol + 16u * slot;
               copy_scales(leader, ta, ss);
               copy_scales(leader, ta + 4, ss + 512);
               copy_scales(leader, ta + 8, ss + 1024);
+              if (kMake) {
+                commit_pair(leader, &sempty[sslot]);
+                if (++sslot == kScaleRing) {
+                  sslot = 0;
+                  sph ^= 1u;
+                }
+              }
             }
             last_use[slot] = ++blocks;
             const uint32_t sa = smem0 + (uint32_t)(stage * kStage);
@@ -457,7 +532,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
               stage = 0;
               ph ^= 1u;
             }
-            const bool there = mbar_test(&full[stage], ph);
+            const bool there = mbar_test(&full[stage], ph), sthere = kMake && mbar_test_cluster(&sfull[sslot], sph);
 #pragma unroll
             for (int k = 0; k < kSubs; ++k) {
               const uint64_t a0 = sw128_desc(sa + k * kSubA, 16, 1024), b0 = sw128_desc(sa + kSubs * kSubA + k * kSubB, 16, 1024);
@@ -468,6 +543,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
             }
             commit_pair(leader, free);
             ready = __all_sync(0xFFFFFFFFu, there);
+            if (kMake) sready = __all_sync(0xFFFFFFFFu, sthere);
           }
           if (!ok) break;
           commit_pair(leader, &accfull[ab]);
@@ -584,8 +660,47 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear8
       }
     }
     if (lane == 0) bulk_wait_all();   // stores from the boxes
-  } else {
+  } else if constexpr (!kMake) {
     few_registers<96>();
+  } else {
+    // ---------------------------------- scales -----------------------------------
+    // In the order in which the MMA issuer takes them: an item's first stage's, then
+    // each even stage's.  The two warps take turns, and load a turn's before they
+    // wait for the room of the last one's: a load's time is that of two stages.
+    few_registers<96>();
+    Items items(sch, pair);
+    Item it{};
+    int kb = 0;
+    auto step = [&]() {
+      kb = (kb | 1) + 1;
+      if (kb < it.kb1) return true;
+      if (!items.next(sch, it)) return false;
+      kb = it.kb0;
+      return true;
+    };
+    FourScales now;
+    auto load = [&]() { now.load<kGrad>(p.scales, kb >> 1, (int64_t)it.tm * kTileM + (int)rank * kHalf, (int64_t)it.tn * kN, lane); };
+    bool more = step() && (warp == 2 || step()), ok = true;
+    if (more) load();
+    for (uint32_t turn = warp - 2; more; turn += 2) {
+      const uint32_t x0 = now.word(now.x[0]), x1 = now.word(now.x[1]), x2 = now.word(now.x[2]), x3 = now.word(now.x[3]);
+      const uint32_t w[2] = {now.word(now.w[0]), now.word(now.w[1])};
+      more = step() && step();
+      if (more) load();
+      const uint32_t slot = turn % kScaleRing, ph = turn / kScaleRing & 1u;
+      if (!__all_sync(0xFFFFFFFFu, await(&sempty[slot], ph ^ 1u, abort_flag, wait_ns))) {
+        ok = false;
+        break;
+      }
+      const uint32_t to = smem_u32(smem + R::kScales + (size_t)slot * kScaleBytes) + 16 * lane;
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(x0), "r"(x1), "r"(x2), "r"(x3) : "memory");
+#pragma unroll
+      for (int j = 0; j < 2; ++j) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(to + 512 * (j + 1)), "r"(w[j]) : "memory");
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(peer_addr(&sfull[slot], 0));
+    }
+    if (!ok && lane == 0) *abort_flag = 1;
   }
 
   __syncwarp();
@@ -612,6 +727,7 @@ struct Layout {
   int64_t k, n;
   int32_t groups, fours, row_blocks;
   Schedule sch;
+  bool few, make;
   size_t sb, parts, total;     // the activations' scales, the weights', partial sums
 };
 Layout make_layout(const Linear8Params& q) {
@@ -621,26 +737,28 @@ Layout make_layout(const Linear8Params& q) {
   l.groups = (int32_t)((l.k + kBlock - 1) / kBlock);
   l.fours = (l.groups + 3) / 4;
   l.row_blocks = (int32_t)((q.tokens + 127) / 128);
+  l.few = q.tokens <= kFewTokens;
   // few tokens: half of the pairs draw the weights as fast as all, and a sum that is
   // not split needs no second kernel
   l.sch = plain_schedule(q.tokens, l.n, l.k, 1, kN, kK);
-  if (q.tokens > kFewTokens || l.sch.units < kPairs / 2) l.sch = split_schedule(q.tokens, l.n, l.k, kN, kK, kLeastShare);
-  l.sb = (size_t)l.fours * l.row_blocks * 512;
-  l.parts = l.sb + (size_t)l.fours * l.sch.tiles_n * 1024;
+  if (!l.few || l.sch.units < kPairs / 2) l.sch = split_schedule(q.tokens, l.n, l.k, kN, kK, kLeastShare);
+  l.make = l.few || (int64_t)l.sch.tiles_m * l.sch.tiles_n * ((l.k + kK - 1) / kK) <= (int64_t)kPairs * kMakeStages;
+  l.sb = l.make ? 0 : (size_t)l.fours * l.row_blocks * 512;
+  l.parts = l.make ? 0 : l.sb + (size_t)l.fours * l.sch.tiles_n * 1024;
   l.total = l.parts + parts_bytes(l.sch, kN);
   return l;
 }
 
-template <bool kGrad, bool kFew>
+template <bool kGrad, bool kFew, bool kMake>
 cudaError_t start8(const Params8& p, cudaStream_t st) {
   const int dev = device_slot();
   static bool ready[kMaxDevices];
   if (dev < 0 || !ready[dev]) {
-    const cudaError_t e = cudaFuncSetAttribute(linear8_kernel<kGrad, kFew>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Ring<kFew>::kBytes);
+    const cudaError_t e = cudaFuncSetAttribute(linear8_kernel<kGrad, kFew, kMake>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Ring<kFew, kMake>::kBytes);
     if (e != cudaSuccess) return e;
     if (dev >= 0) ready[dev] = true;
   }
-  return launch_after(linear8_kernel<kGrad, kFew>, dim3(2 * pairs_of(p.sch)), kThreads, Ring<kFew>::kBytes, st, p);
+  return launch_after(linear8_kernel<kGrad, kFew, kMake>, dim3(2 * pairs_of(p.sch)), kThreads, Ring<kFew, kMake>::kBytes, st, p);
 }
 
 }  // namespace
@@ -666,11 +784,14 @@ cudaError_t launch_linear8(const Linear8Params& q, cudaStream_t st) {
   const Layout l = make_layout(q);
   uint8_t* ws = static_cast<uint8_t*>(q.workspace);
   uint32_t *sa = reinterpret_cast<uint32_t*>(ws), *sb = reinterpret_cast<uint32_t*>(ws + l.sb);
-  const ScaleParams sp{q.x.scales, q.w.scales, q.x.ld_scales, q.w.ld_scales, q.tokens, (int32_t)l.n, l.groups, l.fours, l.row_blocks, l.sch.tiles_n, q.grad, sa, sb};
-  const int64_t words = (int64_t)l.fours * (l.row_blocks + 2 * (int64_t)l.sch.tiles_n);      // blocks of 128
-  cudaError_t e = launch_after(scales_kernel, dim3((unsigned)std::min<int64_t>(words, 152 * 32)), 128, 0, st, sp);
-  if (e != cudaSuccess) return e;
   Params8 p{};
+  p.scales = Scales{q.x.scales, q.w.scales, q.x.ld_scales, q.w.ld_scales, q.tokens, (int32_t)l.n, l.groups};
+  cudaError_t e;
+  if (!l.make) {
+    const ScaleParams sp{p.scales, l.fours, l.row_blocks, l.sch.tiles_n, q.grad, sa, sb};
+    const int64_t words = (int64_t)l.fours * (l.row_blocks + 2 * (int64_t)l.sch.tiles_n);      // blocks of 128
+    if ((e = launch_after(scales_kernel, dim3((unsigned)std::min<int64_t>(words, 152 * 32)), 128, 0, st, sp)) != cudaSuccess) return e;
+  }
   p.sch = l.sch;
   share(p.sch);
   p.m = (int32_t)q.tokens;
@@ -685,14 +806,15 @@ cudaError_t launch_linear8(const Linear8Params& q, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     p.out.tma = 1;
   }
-  const bool few = q.tokens <= kFewTokens;
   const CUtensorMapDataType u8 = CU_TENSOR_MAP_DATA_TYPE_UINT8, u32 = CU_TENSOR_MAP_DATA_TYPE_UINT32;
   const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B, none = CU_TENSOR_MAP_SWIZZLE_NONE;
-  if ((e = encode(&p.a, u8, 1, q.x.data, l.k, q.tokens, 1, q.x.ld, q.x.ld * q.tokens, kSub, few ? kFewTokens : kHalf, sw)) != cudaSuccess) return e;
+  if ((e = encode(&p.a, u8, 1, q.x.data, l.k, q.tokens, 1, q.x.ld, q.x.ld * q.tokens, kSub, l.few ? kFewTokens : kHalf, sw)) != cudaSuccess) return e;
   if ((e = encode(&p.b, u8, 1, q.w.data, q.in, q.out, 1, q.w.ld, q.w.ld * q.out, 128, q.grad ? kSub : kHalfN, sw)) != cudaSuccess) return e;
-  if ((e = encode(&p.sa, u32, 4, sa, 128, l.row_blocks, l.fours, 128, 128 * (int64_t)l.row_blocks, 128, 1, none)) != cudaSuccess) return e;
-  if ((e = encode(&p.sb, u32, 4, sb, 256, l.sch.tiles_n, l.fours, 256, 256 * (int64_t)l.sch.tiles_n, 256, 1, none)) != cudaSuccess) return e;
-  e = q.grad ? (few ? start8<true, true>(p, st) : start8<true, false>(p, st)) : (few ? start8<false, true>(p, st) : start8<false, false>(p, st));
+  if (!l.make && (e = encode(&p.sa, u32, 4, sa, 128, l.row_blocks, l.fours, 128, 128 * (int64_t)l.row_blocks, 128, 1, none)) != cudaSuccess) return e;
+  if (!l.make && (e = encode(&p.sb, u32, 4, sb, 256, l.sch.tiles_n, l.fours, 256, 256 * (int64_t)l.sch.tiles_n, 256, 1, none)) != cudaSuccess) return e;
+  if (l.few) e = q.grad ? start8<true, true, true>(p, st) : start8<false, true, true>(p, st);
+  else if (l.make) e = q.grad ? start8<true, false, true>(p, st) : start8<false, false, true>(p, st);
+  else e = q.grad ? start8<true, false, false>(p, st) : start8<false, false, false>(p, st);
   if (e != cudaSuccess || !has_parts(p.sch)) return e;
   return start_join<kN>(p.sch, p.m, p.n, p.parts, p.out, st);
 }

@@ -230,3 +230,36 @@ def test_waits_that_run_out_leave_nan(T, rows, cols, out, monkeypatch):
     assert bool((y.isnan() | (y == right)).all())
     monkeypatch.delenv("LM_WAIT_LIMIT_NS")
     assert torch.equal(T.linear8(x, w), right)
+
+
+@pytest.mark.parametrize("to", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("rows,cols,out", [(2048, 4096, 4864), (2048, 4096, 4865), (2750, 4001, 4100), (33, 40001, 5100), (5001, 1029, 9999)])
+def test_products_of_more_work(T, rows, cols, out, grad, to):
+    """From 2433 tiles of 256 x 256 x 256 on, the scales are laid out before the product."""
+    test_products(T, rows, cols, out, grad, to)
+
+
+def test_more_work_wide_scales_nan_and_waits(T, monkeypatch):
+    rows, cols, out = 3000, 4000, 4100
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    x = torch.randn(rows, cols, device="cuda", generator=g)
+    x[:, :128] *= 2.0 ** 40
+    x[2999, 3840:3968] = float("nan")
+    w = torch.randn(out, cols, device="cuda", generator=g)
+    w[:, :128] *= 2.0 ** -40
+    w[4097, 3999] = float("inf")
+    cx, cw = T.checkpoint8(x, "e4m3"), T.weight8(w)
+    y = T.linear8(cx, cw, dtype=torch.float32)
+    want, most = product(cx, cw, False)
+    assert torch.equal(y.isnan(), want.isnan()) and bool(y[:2999, :4096].isfinite().all())
+    fine = ~want.isnan()
+    bound = most * (2.0 ** -17 + cols / 512 * 2.0 ** -24) + HALF[torch.float32] * want.abs()
+    assert bool(((y.double() - want).abs() <= bound)[fine].all())
+    torch.cuda.synchronize()
+    monkeypatch.setenv("LM_WAIT_LIMIT_NS", "1")
+    z = T.linear8(cx, cw, dtype=torch.float32)
+    torch.cuda.synchronize()
+    assert bool((z.isnan() | (z == y)).all())
+    monkeypatch.delenv("LM_WAIT_LIMIT_NS")
+    assert torch.equal(T.linear8(cx, cw, dtype=torch.float32).nan_to_num(), y.nan_to_num())
