@@ -586,7 +586,7 @@ lm_status lm_linear_wgrad8(const lm_matrix* dy, const lm_checkpoint8* x, const l
  * inputs give the same bits.
  * dh has the dtype of h; dweight is bf16 or fp32, accumulate != 0 adds to it (to
  * fp32 values, and between pieces of the tokens, sums below 2^-126 may count as
- * zero). */
+ * zero).  Neither gradient may be written over h, weight or the other. */
 typedef struct {
   lm_matrix h;
   lm_matrix weight;
@@ -705,7 +705,7 @@ typedef struct {
 typedef struct {
   lm_heads x;               /* forward: read; gradient: the forward call's, read with norm (else ignored) */
   lm_heads y;               /* forward: written, may be x itself (same strides); gradient: dy, read */
-  lm_heads dx;              /* gradient: written, may be dy itself (same strides) */
+  lm_heads dx;              /* gradient: written, may be dy or x itself (same strides) */
   lm_tensor weight;         /* dim elements, bf16 or fp32; data NULL for ones; with norm only */
   lm_tensor dweight;        /* gradient: dim elements, bf16 or fp32, or data NULL; with norm only */
 } lm_rotary_part;
@@ -722,7 +722,8 @@ typedef struct {
 } lm_qk_rotary_args;
 
 /* All tensors of a call have one dtype (bf16 or fp32), one number of tokens and
- * one dim, at most 1024.  dweight is summed in a fixed order: the same inputs
+ * one dim, at most 1024.  What is written for the queries is neither the keys'
+ * nor read for them, and the other way about.  dweight is summed in a fixed order: the same inputs
  * give the same bits.  workspace: lm_qk_rotary_grad_workspace(args) bytes of
  * device memory, 16-byte aligned, free again when the work is done (not read
  * when no dweight is wanted).

@@ -238,6 +238,10 @@ lm_status linlogp_call(const lm_linear_logprob_args* a, bool gradient_only, void
     if (a->dh.dtype != LM_BF16) return fail(LM_ERR_DTYPE, "dh and h differ in dtype");
   }
   if (dw) LM_TRY(check_matrix(a->dweight, v, c, "dweight"));
+  // (each gradient reads what the other is written over)
+  if (dh && n > 0 && (a->dh.data == a->h.data || a->dh.data == a->weight.data)) return fail(LM_ERR_INVALID_ARG, "dh written over an input");
+  if (dw && n > 0 && (a->dweight.data == a->h.data || a->dweight.data == a->weight.data)) return fail(LM_ERR_INVALID_ARG, "dweight written over an input");
+  if (dh && dw && n > 0 && a->dh.data == a->dweight.data) return fail(LM_ERR_INVALID_ARG, "dh and dweight share places");
   if (gradient_only && !dh && !dw && n > 0) return fail(LM_ERR_INVALID_ARG, "dh and dweight are both NULL");
   if ((dh || dw) && !g && n > 0) return fail(LM_ERR_INVALID_ARG, "dh or dweight without any of g_logp, g_entropy, g_lse");
   if (g && !dh && !dw && n > 0) return fail(LM_ERR_INVALID_ARG, "g_logp, g_entropy or g_lse without dh or dweight");
@@ -380,12 +384,15 @@ lm_status rotary_call(const lm_qk_rotary_args* a, bool grad, void* workspace, si
     if (reads_x) LM_TRY(check_heads(r.x, tokens, n, dim, dt, xn));
     if (grad) LM_TRY(check_heads(r.dx, tokens, n, dim, dt, dn));
     const lm_heads &out = grad ? r.dx : r.y, &in = grad ? r.y : r.x;
-    if (out.data == in.data && tokens > 0 && n > 0 && ((tokens > 1 && out.ld_token != in.ld_token) || (n > 1 && out.ld_head != in.ld_head)))
-      return fail(LM_ERR_INVALID_ARG, "%s written over its input needs the same strides", grad ? dn : yn);
+    for (const lm_heads* from : {&in, &r.x})
+      if ((from == &in || reads_x) && out.data == from->data && tokens > 0 && n > 0 &&
+          ((tokens > 1 && out.ld_token != from->ld_token) || (n > 1 && out.ld_head != from->ld_head)))
+        return fail(LM_ERR_INVALID_ARG, "%s written over its input needs the same strides", grad ? dn : yn);
     if (a->norm == 0 && (r.weight.data != nullptr || (grad && r.dweight.data != nullptr))) return fail(LM_ERR_INVALID_ARG, "a weight without the norm");
     if (r.weight.data != nullptr) LM_TRY(check_vector(r.weight, dim, "weight"));
     if (grad && r.dweight.data != nullptr) {
       LM_TRY(check_vector(r.dweight, dim, "dweight"));
+      if (any_dw && r.dweight.data == a->q.dweight.data) return fail(LM_ERR_INVALID_ARG, "one dweight for queries and keys");
       any_dw = true;
     }
     RotaryPart& o = p.part[i];
@@ -411,6 +418,13 @@ lm_status rotary_call(const lm_qk_rotary_args* a, bool grad, void* workspace, si
     LM_TRY(check_aligned(a->table, 4, "table"));
   }
   if (a->norm != 0 && (!(a->eps >= 0.0) || !isfinite(a->eps))) return fail(LM_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  if (tokens > 0 && dim > 0 && p.part[0].heads > 0 && p.part[1].heads > 0)
+    for (int i = 0; i < 2; ++i) {
+      const lm_rotary_part &r = *parts[i], &other = *parts[1 - i];
+      const void* const out = grad ? r.dx.data : r.y.data;
+      if (out == (grad ? other.dx.data : other.y.data) || out == (grad ? other.y.data : other.x.data) || (reads_x && out == other.x.data))
+        return fail(LM_ERR_INVALID_ARG, "the %s result is written over the %s", i ? "keys'" : "queries'", i ? "queries" : "keys");
+    }
   const bool rows = tokens > 0 && p.part[0].heads + p.part[1].heads > 0;
   if (dim == 0 || (!rows && !any_dw)) return LM_OK;
   if (any_dw) LM_TRY(check_workspace(workspace, workspace_bytes, lm_qk_rotary_grad_workspace(a), 16));

@@ -277,3 +277,16 @@ def test_tables(T, dims, factor, original):
     want = 1.5 * torch.stack((a.cos(), a.sin()), dim=-1)
     # the two machines' 64-bit cosines of angles up to 2^18 agree to 2^-33
     assert t.shape == (200000, dims // 2, 2) and float((t.cpu()[at].double() - want).abs().max()) <= 1.5 * (2.0 ** -24 + 2.0 ** -33)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("tokens,hq,hk,dim,turned,interleaved,norm,lay", [case for case in CASES if case[6]])
+def test_gradient_over_an_input(T, tokens, hq, hk, dim, turned, interleaved, norm, lay, dtype):
+    """Over dy, or over the forward call's queries and keys: the same bits."""
+    c = Case(tokens, hq, hk, dim, turned, interleaved, norm, dtype, lay)
+    want = T.qk_rotary_grad(c.dq, c.dk, c.pos, c.table, c.q, c.k, c.qw, c.kw, **c.args())
+    for over in ("x", "dy"):
+        d = Case(tokens, hq, hk, dim, turned, interleaved, norm, dtype, lay)
+        to = (d.q, d.k) if over == "x" else (d.dq, d.dk)
+        got = T.qk_rotary_grad(d.dq, d.dk, d.pos, d.table, d.q, d.k, d.qw, d.kw, **d.args(), dq_out=to[0], dk_out=to[1])
+        assert all(torch.equal(a, b) for a, b in zip(got, want))

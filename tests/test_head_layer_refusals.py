@@ -249,3 +249,39 @@ def test_binding_refusals(L):
             T.rotary_frequencies(**kw)
     with pytest.raises(ValueError):
         T.linear_logprob(torch.zeros(2, 4), torch.zeros(3, 4), accumulate=True)
+
+
+def test_results_over_each_other_are_refused(L):
+    lib = L.load_library()
+
+    def head(dh=mat(L, data=2 * BASE), dweight=mat(L, rows=10, data=3 * BASE)):
+        a = L.LmLinearLogprobArgs()
+        a.h, a.weight, a.targets, a.lse, a.g_logp, a.dh, a.dweight = mat(L, data=4 * BASE), mat(L, rows=10, data=5 * BASE), BASE, BASE, BASE, dh, dweight
+        codes = set()
+        for f in (lib.lm_linear_logprob, lib.lm_linear_logprob_grad):
+            codes.add(f(ctypes.byref(a), BASE + 128, 1 << 40, None))
+        return codes
+
+    assert head() == {ALIGN}                                       # the workspace, after all else
+    for at in (4, 5, 3):
+        assert head(dh=mat(L, data=at * BASE)) == {INVALID}
+    for at in (4, 5):
+        assert head(dweight=mat(L, rows=10, data=at * BASE)) == {INVALID}
+
+    def rotary(grad, at, dweight=(0, 0)):
+        a = L.LmQkRotaryArgs()
+        for part, first, w in ((a.q, 0, dweight[0]), (a.k, 3, dweight[1])):
+            for i, name in enumerate(("x", "y", "dx")):
+                setattr(part, name, L.LmHeads(at[first + i] * BASE, 4, 2, 8, 32 if i == 0 else 16, 8, 1))
+            part.dweight = L.LmTensor(w * BASE, 1, 8, 1) if w else L.LmTensor()
+        a.turned, a.norm, a.eps = 0, 1, 1e-6
+        return lib.lm_qk_rotary_grad(ctypes.byref(a), BASE + 8, 1 << 40, None) if grad else lib.lm_qk_rotary(ctypes.byref(a), None)
+
+    assert rotary(True, (1, 2, 3, 4, 5, 6), (7, 8)) == ALIGN       # the workspace
+    assert rotary(True, (1, 2, 2, 4, 5, 5), (7, 8)) == ALIGN       # over dy
+    assert rotary(True, (1, 2, 3, 4, 5, 6), (7, 7)) == INVALID
+    assert rotary(True, (1, 2, 1, 4, 5, 6), (7, 8)) == INVALID     # over x, other strides
+    for at in ((1, 2, 3, 4, 5, 3), (1, 2, 5, 4, 5, 6), (1, 2, 4, 4, 5, 6), (1, 2, 3, 4, 5, 2), (1, 2, 3, 4, 5, 1)):
+        assert rotary(True, at, (7, 8)) == INVALID
+    for at in ((1, 2, 3, 4, 2, 6), (1, 4, 3, 4, 5, 6), (1, 2, 3, 4, 1, 6)):
+        assert rotary(False, at) == INVALID
