@@ -220,10 +220,9 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
         getattr(lib, fn).restype = c_int
     lib.lm_linear_logprob_workspace.argtypes = [c_void_p]
     lib.lm_linear_logprob_workspace.restype = size
-    lib.lm_weight8_pack.argtypes = [P(LmMatrix), P(LmWeight8), c_void_p]
-    lib.lm_weight8_pack.restype = c_int
-    lib.lm_weight8_unpack.argtypes = [P(LmWeight8), P(LmMatrix), c_void_p]
-    lib.lm_weight8_unpack.restype = c_int
+    for fn in ("lm_weight8_pack", "lm_weight8_unpack"):
+        getattr(lib, fn).argtypes = [c_void_p, c_void_p, c_void_p]
+        getattr(lib, fn).restype = c_int
     for fn in ("lm_linear8", "lm_linear8_grad"):
         getattr(lib, fn).argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, size, c_void_p]
         getattr(lib, fn).restype = c_int

@@ -24,7 +24,7 @@ from typing import NamedTuple, Optional
 import torch
 
 from . import lionmuon as _L
-from .lionmuon import LM_BF16, LM_F32, LmCheckpoint8, LmMatrix, LmTensor, LmTokenLogprobArgs, LmWeight8
+from .lionmuon import LM_BF16, LM_F32, LmCheckpoint8, LmMatrix, LmTensor, LmTokenLogprobArgs
 
 GROUP = 128                                   # channels that share one scale (LM_CODE_GROUP)
 FORMATS = {"i8": 0, "e4m3": 1}                # lm_code_format
@@ -248,9 +248,6 @@ class Weight8:
         return (codes.data_ptr(), scales.data_ptr(), rows, self.cols, codes.stride(0) if rows > 1 else max(codes.stride(0), pitch),
                 scales.stride(0) if down > 1 else across)
 
-    def desc(self) -> LmWeight8:
-        return LmWeight8(*self.fields())
-
     def unpack(self, dtype=torch.bfloat16, out=None, stream=None):
         """The values the codes stand for (exact in bf16 and in fp32)."""
         if stream is not None:
@@ -260,7 +257,7 @@ class Weight8:
         codes = self.codes
         if out is None:
             out = torch.empty((codes.shape[0], self.cols), dtype=dtype, device=codes.device)
-        st = lib.lm_weight8_unpack(self.desc(), _matrix(out, "out"), _stream_of(codes))
+        st = lib.lm_weight8_unpack(_pack_weight8(*self.fields()), _pack_matrix(*_matrix_fields(out, "out")), _stream_of(codes))
         if st:
             _L._check(lib, st, "lm_weight8_unpack")
         return out
@@ -272,10 +269,10 @@ def weight8(w, out: Optional[Weight8] = None, stream=None) -> Weight8:
         with torch.cuda.stream(stream):
             return weight8(w, out)
     lib = _L.load_library()
-    m = _matrix(w, "w")
+    m = _matrix_fields(w, "w")
     if out is None:
-        out = Weight8.empty(m.rows, m.cols, w.device)
-    st = lib.lm_weight8_pack(m, out.desc(), _stream_of(w))
+        out = Weight8.empty(m[1], m[2], w.device)
+    st = lib.lm_weight8_pack(_pack_matrix(*m), _pack_weight8(*out.fields()), _stream_of(w))
     if st:
         _L._check(lib, st, "lm_weight8_pack")
     return out
