@@ -579,11 +579,12 @@ lm_status lm_linear_wgrad8(const lm_matrix* dy, const lm_checkpoint8* x, const l
  *   dh = dz weight,   dweight (+)= dz^T h
  * z is summed in fp32; for the gradients of one call with the forward results it
  * is kept in 16 bits, in steps of 2^-10 below the row's maximum (p is off by
- * 2^-11 of itself at most, and 0 where the logit is 64 below).  dz is rounded to
- * bf16, as the tensor cores take it, and both products are summed in fp32.  The tensor cores
- * add at most 512 products (each addition of 16 may drop 2^-23 of what it has);
- * their sums are added in fp32.  Sums are taken in a fixed order: the same
- * inputs give the same bits.
+ * 2^-11 of itself at most, and 0 where the logit is 64 below).  dz, times one
+ * factor for a piece of the tokens, is rounded to bf16, as the tensor cores take
+ * it, and both products are summed in fp32.  The tensor cores add at most 512
+ * products (each addition of 16 may drop 2^-23 of what it has); their sums are
+ * added in fp32.  Sums are taken in a fixed order: the same inputs give the same
+ * bits.
  * dh has the dtype of h; dweight is bf16 or fp32, accumulate != 0 adds to it (to
  * fp32 values, and between pieces of the tokens, sums below 2^-126 may count as
  * zero).  Neither gradient may be written over h, weight or the other. */
@@ -723,10 +724,10 @@ typedef struct {
 
 /* All tensors of a call have one dtype (bf16 or fp32), one number of tokens and
  * one dim, at most 1024.  What is written for the queries is neither the keys'
- * nor read for them, and the other way about.  dweight is summed in a fixed order: the same inputs
- * give the same bits.  workspace: lm_qk_rotary_grad_workspace(args) bytes of
- * device memory, 16-byte aligned, free again when the work is done (not read
- * when no dweight is wanted).
+ * nor read for them, and the other way about.  dweight is summed in a fixed
+ * order: the same inputs give the same bits.  workspace:
+ * lm_qk_rotary_grad_workspace(args) bytes of device memory, 16-byte aligned, free
+ * again when the work is done (not read when no dweight is wanted).
  * Errors: LM_ERR_INVALID_ARG (also a workspace that is too small),
  * LM_ERR_DTYPE, LM_ERR_ALIGN, LM_ERR_UNSUPPORTED, LM_ERR_CUDA. */
 lm_status lm_qk_rotary(const lm_qk_rotary_args* a, void* cuda_stream);

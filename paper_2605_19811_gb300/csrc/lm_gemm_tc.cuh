@@ -434,11 +434,21 @@ struct StoreEpi {
   // with 96 (and 200) 212 bytes (dh of 4096 x 4096 over 50257: 1006 us, 968 so)
   static constexpr int kFewRegs = 136;
   Store out;
+  const float* factor;        // of the product, in device memory
   template <typename P>
   struct Warp {
     __device__ __forceinline__ Warp(const P&, const Place&) {}
     __device__ __forceinline__ void tile(const P& p, const Item& it, const Place& at, float (&acc)[4][32]) {
       const int rows = min(32, p.m - at.row);
+      const float f = *p.epi.factor;
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+          const float2 v = mul2(make_float2(acc[b][e], acc[b][e + 1]), make_float2(f, f));
+          acc[b][e] = v.x;
+          acc[b][e + 1] = v.y;
+        }
       if (it.slot < 0 && p.epi.out.tma) {
         if (rows <= 0) return;
         if (p.epi.out.dt == LM_F32) {

@@ -19,8 +19,8 @@
 // (p is then off by 2^-11 of itself at most, a quarter of the bf16 rounding that
 // follows).  Once lse is known, a kernel makes of q, in its place,
 //   d = p (a - g_H (log p + H)) (+ g_logp at the target),  a = g_lse - g_logp
-// as bf16 (the rounding that the tensor cores ask for), and two products of it
-// follow, dh = d W and dW = d^T h.  Where lse comes from an earlier call the
+// as bf16 (the rounding that the tensor cores ask for; times a scale, see put_scale),
+// and two products of it follow, dh = d W and dW = d^T h.  Where lse comes from an earlier call the
 // logits' product writes d itself.  Over several pieces dW is summed in fp32, each
 // piece's tiles added by the TMA.
 //
@@ -88,7 +88,25 @@ struct RowTerms {
   float4* terms;
   float* g_logp;      // 0 in a row without a target
   int32_t* target;    // -1 in a row without one
+  float* scale;       // d = scale[0] dz is rounded, and scale[1] = 1 / scale[0] times the products
 };
+
+// The rounding of d to bf16 costs 2^-8 of values just above a power of two, half of
+// that just below the next one.  Where the tokens count alike, the targets' dz, which
+// carry most of the gradient, are g_logp times what is left to 1, and lie together:
+// the scale puts the largest g_logp of the piece's first 32 tokens (`g`: one a lane of
+// `lanes`) on 127/64 of a power of two.  Weights of -1 / tokens, 1000 tokens: both
+// gradients are 1.17 times as far off as by their own rounding alone instead of 1.33
+// (100 tokens: 1.17 instead of 1.46).  It takes nothing of the logits, so that one
+// token's never change another's gradient.
+__device__ __forceinline__ void put_scale(float* scale, unsigned lanes, float g) {
+  const uint32_t most = __reduce_max_sync(lanes, __float_as_uint(fabsf(g)));
+  if ((threadIdx.x & 31) != 0) return;
+  float s = 1.f;
+  if (most >= 0x00800000u && most < 0x7F800000u) s = (127.f / 64.f) / __uint_as_float((most & 0x007FFFFFu) | 0x3F800000u);
+  scale[0] = s;
+  scale[1] = 1.f / s;
+}
 
 // kKeep: the logits are kept in 16 bits for the gradient.  kFew: at most kFewRows
 // rows, without it; W's bytes are then all that counts, and more of them are under
@@ -224,7 +242,10 @@ struct GradEpi {
     __device__ __forceinline__ void tile(const P& p, const Item&, const Place& at, float (&acc)[4][32]) {
       const int row = at.row + at.lane;
       const bool in = row < p.m;
-      const float4 w = in ? p.epi.rows.terms[row] : make_float4(0.f, 0.f, 0.f, 0.f);
+      float4 w = in ? p.epi.rows.terms[row] : make_float4(0.f, 0.f, 0.f, 0.f);
+      const float scale = p.epi.rows.scale[0];
+      w.y *= scale;
+      w.z *= scale;
       const int y = in ? p.epi.rows.target[row] - at.col : -1;
       box_free(at.lane);
 #pragma unroll
@@ -232,7 +253,7 @@ struct GradEpi {
 #pragma unroll
         for (int e = 0; e < 32; ++e) acc[b][e] = gradient(acc[b][e] - w.x, w);
         if ((unsigned)(y - 32 * b) < 32u) {
-          const float gl = p.epi.rows.g_logp[row];
+          const float gl = p.epi.rows.g_logp[row] * scale;
 #pragma unroll
           for (int e = 0; e < 32; ++e) acc[b][e] += y == 32 * b + e ? gl : 0.f;
         }
@@ -305,6 +326,7 @@ __global__ void __launch_bounds__(32 * kJoinParts) linlogp_join_kernel(const Joi
   ss[k][lane] = s;
   st[k][lane] = t;
   __syncthreads();
+  const unsigned lanes = __ballot_sync(0xFFFFFFFFu, in);
   if (k != 0 || !in) return;
   s = t = 0.f;
 #pragma unroll
@@ -329,7 +351,9 @@ __global__ void __launch_bounds__(32 * kJoinParts) linlogp_join_kernel(const Joi
   if (p.logp != nullptr) p.logp[row] = logp;
   if (p.entropy != nullptr) p.entropy[row] = h;
   if (p.lse != nullptr) p.lse[row] = lse;
-  if (p.out.terms != nullptr) put_terms(p.out, row, lse, h, y, p.vocab, p.g_logp, p.g_entropy, p.g_lse);
+  if (p.out.terms == nullptr) return;
+  put_terms(p.out, row, lse, h, y, p.vocab, p.g_logp, p.g_entropy, p.g_lse);
+  if (row < 32) put_scale(p.out.scale, lanes, p.g_logp != nullptr ? p.g_logp[row] : 0.f);
 }
 
 // The gradient's terms from lse and entropy of an earlier call.
@@ -337,9 +361,11 @@ __global__ void __launch_bounds__(256) linlogp_terms_kernel(const JoinParams p) 
   griddep_wait();
   griddep_launch_dependents();
   const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const unsigned lanes = __ballot_sync(0xFFFFFFFFu, row < p.rows);
   if (row >= p.rows) return;
   put_terms(p.out, row, p.lse[row], p.entropy != nullptr && p.g_entropy != nullptr ? p.entropy[row] : 0.f,
             p.targets != nullptr ? p.targets[row] : -1, p.vocab, p.g_logp, p.g_entropy, p.g_lse);
+  if (row < 32) put_scale(p.out.scale, lanes, p.g_logp != nullptr ? p.g_logp[row] : 0.f);
 }
 
 // d in the place of q: eight lanes to a row of a block (64 columns), a block of
@@ -351,7 +377,10 @@ __global__ void __launch_bounds__(256) linlogp_dz_kernel(uint4* q, const float* 
   const int64_t row = (int64_t)blockIdx.x * 32 + (threadIdx.x >> 3);
   if (row >= rows) return;
   const int part = threadIdx.x & 7;
-  const float4 w = t.terms[row];
+  float4 w = t.terms[row];
+  const float scale = t.scale[0];
+  w.y *= scale;
+  w.z *= scale;
   const int y = t.target[row];
   for (int b0 = (int)blockIdx.y * kDzBlocks; b0 < blocks; b0 += (int)gridDim.y * kDzBlocks) {
 #pragma unroll 4
@@ -375,7 +404,7 @@ __global__ void __launch_bounds__(256) linlogp_dz_kernel(uint4* q, const float* 
       }
       const int c = y - 64 * b - 8 * part;
       if ((unsigned)c < 8u) {
-        const float gl = t.g_logp[row];
+        const float gl = t.g_logp[row] * scale;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           d[k].x += c == 2 * k ? gl : 0.f;
@@ -460,7 +489,7 @@ struct Layout {
   int32_t strip;                     // of the forward product
   int32_t parts;                     // of a row's statistics
   // offsets in the workspace
-  size_t h, w, z, terms, gl, target, stats, from, d, dw, partial, total;
+  size_t h, w, z, terms, gl, target, scale, stats, from, d, dw, partial, total;
 };
 bool dw_is_sum(const LinLogpParams& q) { return q.dwdt == LM_F32; }   // several pieces are summed in dW itself
 Layout make_layout(const LinLogpParams& q) {
@@ -494,6 +523,7 @@ Layout make_layout(const LinLogpParams& q) {
     l.terms = take(n * 16);
     l.gl = take(n * 4);
     l.target = take(n * 4);
+    l.scale = take(8);
     l.from = take(q.gradient_only ? 0 : n * (2 * (((size_t)q.vocab + kTileN - 1) / kTileN)) * 4);
     l.d = take(n * l.blocks * 128);
     if (q.dw.data != nullptr && l.pieces > 1 && !dw_is_sum(q)) l.dw = take((size_t)q.vocab * l.ld * 4);
@@ -534,7 +564,7 @@ cudaError_t piece(const LinLogpParams& q, const Layout& l, const Mat& h, const M
   j.g_logp = from_row(q.g_logp, first);
   j.g_entropy = from_row(q.g_entropy, first);
   j.g_lse = from_row(q.g_lse, first);
-  if (grad) j.out = RowTerms{reinterpret_cast<float4*>(ws + l.terms), reinterpret_cast<float*>(ws + l.gl), reinterpret_cast<int32_t*>(ws + l.target)};
+  if (grad) j.out = RowTerms{reinterpret_cast<float4*>(ws + l.terms), reinterpret_cast<float*>(ws + l.gl), reinterpret_cast<int32_t*>(ws + l.target), reinterpret_cast<float*>(ws + l.scale)};
   const bool few = !grad && rows <= kFewRows;
   // the operands of the logits' product, and the blocks that its epilogue fills
   auto logits = [&](auto& p) {
@@ -596,6 +626,7 @@ cudaError_t piece(const LinLogpParams& q, const Layout& l, const Mat& h, const M
     s.n = q.width;
     s.wait_ns = wait_ns;
     s.parts = reinterpret_cast<float*>(ws + l.partial);
+    s.epi.factor = j.out.scale + 1;
     s.epi.out = make_store(Mat{static_cast<__nv_bfloat16*>(q.dh.data) + first * q.dh.ld, q.dh.ld}, LM_BF16, rows, false);
     LM_RUN(encode_blocks(&s.a, ws + l.d, q.vocab, rows, 128));
     LM_RUN(encode_operand(&s.b, w.data, q.width, q.vocab, w.ld, true));
@@ -608,6 +639,7 @@ cudaError_t piece(const LinLogpParams& q, const Layout& l, const Mat& h, const M
     s.n = q.width;
     s.wait_ns = wait_ns;
     s.parts = reinterpret_cast<float*>(ws + l.partial);
+    s.epi.factor = j.out.scale + 1;
     const bool own_sum = !dw_is_sum(q) && l.pieces > 1;
     const Mat sum{ws + l.dw, l.ld};
     if (own_sum) s.epi.out = make_store(sum, LM_F32, q.vocab, first > 0);

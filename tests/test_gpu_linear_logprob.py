@@ -324,3 +324,51 @@ def test_waits_that_run_out_leave_nan(T, rows, vocab, width, monkeypatch):
     monkeypatch.delenv("LM_WAIT_LIMIT_NS")
     again = T.linear_logprob(h.t, w.t, y, gl, gh, gz)
     assert torch.equal(again.dh, right.dh) and torch.equal(again.dweight, right.dweight)
+
+
+@pytest.mark.parametrize("later", [False, True])
+@pytest.mark.parametrize("g", [-1.0, -1.02, -1 / 3, -0.9, 1.7, -1e-30])
+def test_the_targets_gradients_are_rounded_finely(T, g, later):
+    """Tokens that count alike have their weight scaled to 127/64 of a power of two
+    before dz is rounded.  |z| <= 1 over 300 tokens: p <= e^2 / 300 < 2^-5, so that the
+    targets' dz are at least 1.92 there and rounded by 2^-8 / 1.92; p is off by
+    2^-11 + 2^-17 of itself; 1 - p, the scale, its inverse and the products by 2^-19
+    at most.  (A rounding without the scale is up to 2^-8 off.)"""
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    w = (torch.rand(300, 64, device="cuda", generator=gen) / 4 - 1 / 8).bfloat16()
+    h = (torch.rand(40, 64, device="cuda", generator=gen) / 4 - 1 / 8).bfloat16()
+    y = torch.arange(0, 280, 7, device="cuda")
+    weight = torch.full((40,), g, device="cuda")
+    p = torch.softmax(h.double() @ w.double().t(), dim=1)
+    # one token's at a time, the others without a target: dW's row is that token's alone but for their zeros
+    for i in (0, 17, 39):
+        t = torch.full_like(y, -1)
+        t[i] = y[i]
+        dw = torch.empty(300, 64, device="cuda")
+        if later:
+            o = T.linear_logprob(h, w, t)
+            T.linear_logprob_grad(h, w, t, o.lse, o.entropy, weight, dh=False, dweight=dw)
+        else:
+            T.linear_logprob(h, w, t, weight, dh=False, dweight=dw)
+        want = float(weight[0]) * (1 - p[i, y[i]]) * h[i].double()
+        assert bool(((dw[y[i]].double() - want).abs() <= (2.0 ** -8 / 1.92 + 2.0 ** -15) * want.abs()).all())
+
+
+def test_scale_with_weights_that_are_none(T):
+    """Zero, infinite, NaN and the smallest weights among the first tokens: no scale, the rest as ever."""
+    h, w, y, gl, gh, gz = inputs(70, 300, 96, 4)
+    ref = reference(h.t, w.t, y, torch.zeros_like(gl), gh, gz)
+    o = T.linear_logprob(h.t, w.t, y, torch.zeros_like(gl), gh, gz)
+    near(o.dh, ref, "dh")
+    near(o.dweight, ref, "dweight", U)
+    y[:] = 5
+    for bad in (float("inf"), float("nan")):
+        for f in (0, 1):
+            g = gl.clone()
+            g[3] = bad
+            a = T.linear_logprob(h.t, w.t, y, g, gh, gz)
+            dh = a.dh if f == 0 else T.linear_logprob_grad(h.t, w.t, y, a.lse, a.entropy, g, gh, gz)[0]
+            ref = reference(h.t, w.t, y, gl, gh, gz)
+            rest = torch.arange(70, device="cuda") != 3
+            off = (dh.double() - ref["dh"]).abs()
+            assert bool((off <= ref["dh_b"])[rest].all()) and bool(dh[3].isnan().all())
