@@ -34,14 +34,14 @@
 // (16384 x 768 x 50304: 5554 us with the product twice and d written element by
 // element, 4035 us so.)
 //
-// Measured: 16384 x 768 x 50304 with both gradients 3.39 ms (each product of 0.32
-// TFLOP a piece: logits 233 us, dh 203, dW 203; d 143 us at 5.8 TB/s), 4096 x 4096 x
-// 50257 3.38 ms (logits 899 us, 1.88 PFLOP/s; dh 937, dW 930, 1.8), the latter under
+// Measured: 16384 x 768 x 50304 with both gradients 3.42 ms (each product of 0.32
+// TFLOP a piece: logits 233 us, dh 205, dW 205; d 145 us at 5.7 TB/s), 4096 x 4096 x
+// 50257 3.47 ms (logits 941 us, 1.79 PFLOP/s; dh 968, dW 974, 1.74), the latter under
 // the power limit (by itself 3.05).  The products are bound by what the SMs take from
 // L2 (64 bytes a cycle for each: 512 cycles of MMAs for 64 of the sum take 640); the
 // logits' at a width of 768 also by their epilogue and the 16-bit logits' way out
-// (181 us without either).  One token, 768 x 50304: 20 us of kernels (77 MB), 26 us a
-// call: host time.
+// (181 us without either).  One token, 768 x 50304: 20 us of kernels (77 MB), 27
+// to 29 us a call: host time.
 #include <cuda_bf16.h>
 #include <math.h>
 

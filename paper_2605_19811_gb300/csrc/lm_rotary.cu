@@ -16,7 +16,7 @@
 // warp a head): no shuffles for the pairs and a token's angles in registers (134 us);
 // the next heads' loads under way while these are worked on, packed fp32, and one wave
 // of blocks shared between queries and keys by the steps that they take (61 us).  One
-// token: 3 us, a call 19 us: host time.
+// token: 3 us, a call 20 us: host time.
 // Heads of other sizes or alignments take a warp each, a pair or a channel a lane.
 #include <cuda_bf16.h>
 #include <math.h>
