@@ -247,6 +247,15 @@ struct GradEpi {
       w.y *= scale;
       w.z *= scale;
       const int y = in ? p.epi.rows.target[row] - at.col : -1;
+      // The blocks go on to a multiple of 64 columns, and dh's product takes them whole
+      // (times rows of 0 beyond W): a logit of 0 there, as the product leaves it, would
+      // count e^(0 - lse), which is infinite below lse = -88.7.
+      if (p.n - at.col < 128) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+          for (int e = 0; e < 32; ++e) acc[b][e] = 32 * b + e < p.n - at.col ? acc[b][e] : kOutside;
+      }
       box_free(at.lane);
 #pragma unroll
       for (int b = 0; b < 4; ++b) {

@@ -372,3 +372,80 @@ def test_scale_with_weights_that_are_none(T):
             rest = torch.arange(70, device="cuda") != 3
             off = (dh.double() - ref["dh"]).abs()
             assert bool((off <= ref["dh_b"])[rest].all()) and bool(dh[3].isnan().all())
+
+
+def later_reference(h, w, y, gl, gh, gz):
+    """dh, dW and their bounds for lse and entropy of an earlier call: both the logits and
+    that lse are off by E, lse by its sum and rounding too (2^-16 + 2^-23 |lse|), the
+    exponential by 2^-18, so that p is off by their sum of itself; H of the earlier
+    call by at most 1 + ln V times that.  The rest as above."""
+    x, m = h.double(), w.double()
+    v, c = m.shape
+    z = x @ m.t()
+    e = (x.abs() @ m.abs().t()).amax(dim=1, keepdim=True) * (2.0 ** -18 + c / 512 * 2.0 ** -24)
+    lse = torch.logsumexp(z, dim=1, keepdim=True)
+    lp = z - lse
+    p = lp.exp()
+    ent = -(p * lp).sum(dim=1, keepdim=True)
+    a, b, k = (q[:, None].double() for q in (gl, gh, gz))
+    a = torch.where((y >= 0)[:, None], a, 0.0)
+    d = p * ((k - a) - b * (lp + ent))
+    db = (2 * e + 2.0 ** -16 + 2.0 ** -23 * lse.abs() + 2.0 ** -18) * p * ((k - a).abs() + b.abs() * ((lp + ent).abs() + 1 + 2 * math.log(v)))
+    d.scatter_add_(1, y.clamp(min=0)[:, None], a)
+    db += (U + 2.0 ** -18) * (d.abs() + db)
+    dh, dw = d @ m, d.t() @ x
+    return {"dh": dh, "dh_b": db @ m.abs() + U * dh.abs() + 1e-38, "dweight": dw, "dweight_b": db.t() @ x.abs()}
+
+
+@pytest.mark.parametrize("shift", [-20000.0, -100.0, 100.0, 20000.0])
+@pytest.mark.parametrize("rows,vocab,width", [(33, 900, 128), (300, 64, 128), (70, 50257, 64), (5, 129, 128)])
+def test_large_logits_and_weights_known_later(T, rows, vocab, width, shift):
+    """All logits of a token far below or above 0: what lies between the vocabulary and
+    the next multiple of 64 has logits of 0 in the products and counts for nothing, also
+    where a token has no weights at all."""
+    h, w, y, gl, gh, gz = inputs(rows, vocab, width, 6)
+    h.t[:, 0] = 128.0
+    w.t[:, 0] = shift / 128.0
+    for g in (gl, gh, gz):
+        g[2::5] = 0.0
+    o = T.linear_logprob(h.t, w.t, y)
+    dw = torch.empty(vocab, width, device="cuda")
+    dh, _ = T.linear_logprob_grad(h.t, w.t, y, o.lse, o.entropy, gl, gh, gz, dweight=dw)
+    ref = later_reference(h.t, w.t, y, gl, gh, gz)
+    near(dh, ref, "dh")
+    near(dw, ref, "dweight", 2.0 ** -23)
+    assert bool((dh[2::5] == 0).all())
+
+
+def test_masked_and_non_finite_logits_and_weights_known_later(T):
+    """From lse and entropy of an earlier call: logits of -inf have no gradient, nor has a row
+    of them; a row with NaN or +inf is NaN, and no other is."""
+    rows, vocab, width = 40, 700, 64
+    h, w, y, gl, gh, gz = inputs(rows, vocab, width, 4)
+    h.t.abs_().clamp_(min=0.01)
+    masked = torch.arange(vocab, device="cuda") % 3 == 0
+    w.t[masked, 7] = float("-inf")
+    y.clamp_(min=1)
+    y[y % 3 == 0] -= 1
+    o = T.linear_logprob(h.t, w.t, y)
+    dw = torch.empty(vocab, width, device="cuda")
+    T.linear_logprob_grad(h.t, w.t, y, o.lse, o.entropy, gl, gh, gz, dh=False, dweight=dw)
+    assert bool((dw[masked] == 0).all())
+    index = torch.cumsum((~masked).long(), 0) - 1              # of the words that are left
+    ref = later_reference(h.t, w.t[~masked], index[y], gl, gh, gz)
+    near(dw[~masked], ref, "dweight", 2.0 ** -23)
+    w.t[:, 7] = float("-inf")
+    o = T.linear_logprob(h.t, w.t, y)
+    T.linear_logprob_grad(h.t, w.t, y, o.lse, o.entropy, gl, gh, gz, dh=False, dweight=dw)
+    assert bool((o.lse == float("-inf")).all()) and bool((dw == 0).all())
+    h, w, y, gl, gh, gz = inputs(rows, vocab, width, 4)
+    clean = T.linear_logprob(h.t, w.t, y)
+    want, _ = T.linear_logprob_grad(h.t, w.t, y, clean.lse, clean.entropy, gl, gh, gz, dweight=False)
+    h.t[3, 5] = float("nan")
+    h.t[8] = 0.0
+    h.t[8, 0] = float("inf")
+    o = T.linear_logprob(h.t, w.t, y)
+    dh, _ = T.linear_logprob_grad(h.t, w.t, y, o.lse, o.entropy, gl, gh, gz, dweight=False)
+    bad = torch.zeros(rows, dtype=torch.bool, device="cuda")
+    bad[3] = bad[8] = True
+    assert torch.equal(dh.isnan().all(dim=1), bad) and torch.equal(dh[~bad], want[~bad])
