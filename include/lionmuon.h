@@ -657,6 +657,8 @@ lm_status lm_weight8_unpack(const lm_weight8* c, const lm_matrix* w, void* cuda_
  *   lm_linear8_grad:  dx = dy W     dy: T x out, dx: T x in
  * x and dy are checkpoints in LM_CODE_E4M3 (lm_checkpoint8_pack, or kept by
  * lm_rmsnorm), w the layer's weights (out x in); y and dx are bf16 or fp32.
+ * The tensor cores multiply by the scales as powers of two: any other scale (a
+ * negative one, an infinity) counts as NaN, and 0 as 2^-127.
  * Products of codes are exact and the sums fp32, in a fixed order: the same
  * inputs give the same bits.  The tensor cores add at most 2048 products (each
  * addition of 32 may drop 2^-23 of what it has); their sums are added in fp32.

@@ -187,7 +187,13 @@ struct Scales {
   int64_t ldx, ldw, tokens;
   int32_t n, groups;
 };
-__device__ __forceinline__ uint32_t exponent(float s) { return __float_as_uint(s) >> 23; }     // 255 for NaN
+// The byte that the tensor cores multiply by 2^(byte - 127) for, 255 being NaN: of NaN, and
+// of whatever is no power of two (its fraction would be lost, and a sign's bit would reach
+// the next group's byte).
+__device__ __forceinline__ uint32_t exponent(float s) {
+  const uint32_t bits = __float_as_uint(s);
+  return (bits & 0x807FFFFFu) != 0 ? 255u : bits >> 23;
+}
 // As the tensor memory takes them: the 128 of a block of rows as 32 x 16 bytes,
 // row 32 j + l at word 4 l + j, four groups of the sum in a word's bytes.  kMake: lane l
 // reads those of rows l, 32 + l, 64 + l, 96 + l of its CTA's tokens, and those of the

@@ -112,7 +112,8 @@ def _stream_of(t) -> int:
 class Checkpoint8:
     """An 8-bit checkpoint (``lm_checkpoint8``): ``codes``, uint8, rows x pitch
     with the pitch a multiple of 16; ``scales``, float32, groups of 128 channels
-    x (at least) rows; ``cols`` channels; ``format`` "i8" or "e4m3"."""
+    x (at least) rows, powers of two as ``checkpoint8`` writes them; ``cols``
+    channels; ``format`` "i8" or "e4m3"."""
 
     __slots__ = ("codes", "scales", "cols", "format")
 
@@ -211,7 +212,8 @@ def linear_wgrad8(dy, x: Checkpoint8, out=None, accumulate: bool = False, dtype=
 class Weight8:
     """8-bit weights of a linear layer (``lm_weight8``): ``codes``, uint8 (e4m3),
     out x pitch with the pitch a multiple of 16; ``scales``, float32, one for each
-    block of 128 x 128; ``cols`` input channels."""
+    block of 128 x 128, powers of two as ``weight8`` writes them (``linear8`` and
+    ``linear8_grad`` take any other for NaN, 0 for 2^-127); ``cols`` input channels."""
 
     __slots__ = ("codes", "scales", "cols")
 

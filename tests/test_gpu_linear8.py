@@ -263,3 +263,35 @@ def test_more_work_wide_scales_nan_and_waits(T, monkeypatch):
     assert bool((z.isnan() | (z == y)).all())
     monkeypatch.delenv("LM_WAIT_LIMIT_NS")
     assert torch.equal(T.linear8(cx, cw, dtype=torch.float32).nan_to_num(), y.nan_to_num())
+
+
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("rows,cols,out", [(1, 1100, 700), (40, 1100, 700), (2050, 4100, 5000)])
+def test_scales_that_are_no_powers_of_two(T, rows, cols, out, grad):
+    """The products multiply by powers of two: with any other scale what it counts for is
+    NaN, and nothing else is; a scale of 0 counts as 2^-127."""
+    x, w = layer(T, rows, cols, out, grad, 7)
+    f = T.linear8_grad if grad else T.linear8
+    y = f(x, w, dtype=torch.float32)
+    n, k = (cols, out) if grad else (out, cols)
+    block = -(-n // 128) // 2                                  # of y's columns
+    where = (lambda g: (g, block)) if grad else (lambda g: (block, g))
+    inside = torch.zeros(rows, n, dtype=torch.bool, device="cuda")
+    inside[:, 128 * block:128 * block + 128] = True
+    for bad in (1.5, -1.0, -2.0 ** -60, 2.0 ** -128, float("inf"), float("-inf"), 1.0 + 2.0 ** -23):
+        for g in (0, 3, -(-k // 128) - 1):
+            s = w.scales.clone()
+            s[where(g)] = bad
+            z = f(x, T.Weight8(w.codes, s, cols), dtype=torch.float32)
+            assert torch.equal(z.isnan(), inside) and torch.equal(z[~inside], y[~inside]), (bad, g)
+            s = x.scales.clone()
+            s[g, rows // 2] = bad
+            z = f(T.Checkpoint8(x.codes, s, k, "e4m3"), w, dtype=torch.float32)
+            here = torch.arange(rows, device="cuda") == rows // 2
+            assert bool(z[here].isnan().all()) and torch.equal(z[~here], y[~here]), (bad, g)
+    # a group of zeros with scale 0, as another packing may leave it
+    codes, s = x.codes.clone(), x.scales.clone()
+    codes[rows // 2, 128:256] = 0
+    want = f(T.Checkpoint8(codes, s, k, "e4m3"), w, dtype=torch.float32)
+    s[1, rows // 2] = 0.0
+    assert torch.equal(f(T.Checkpoint8(codes, s, k, "e4m3"), w, dtype=torch.float32), want)
