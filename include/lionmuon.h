@@ -647,8 +647,8 @@ typedef struct {
 } lm_weight8;
 
 /* c <- w, and w <- c (w in bf16 or fp32; the values are bf16 numbers, so both
- * are exact).  Errors: LM_ERR_INVALID_ARG, LM_ERR_DTYPE, LM_ERR_ALIGN,
- * LM_ERR_UNSUPPORTED, LM_ERR_CUDA. */
+ * are exact).  Neither is written over the other.  Errors: LM_ERR_INVALID_ARG,
+ * LM_ERR_DTYPE, LM_ERR_ALIGN, LM_ERR_UNSUPPORTED, LM_ERR_CUDA. */
 lm_status lm_weight8_pack(const lm_matrix* w, const lm_weight8* c, void* cuda_stream);
 lm_status lm_weight8_unpack(const lm_weight8* c, const lm_matrix* w, void* cuda_stream);
 
@@ -662,7 +662,8 @@ lm_status lm_weight8_unpack(const lm_weight8* c, const lm_matrix* w, void* cuda_
  * Products of codes are exact and the sums fp32, in a fixed order: the same
  * inputs give the same bits.  The tensor cores add at most 2048 products (each
  * addition of 32 may drop 2^-23 of what it has); their sums are added in fp32.
- * The weight gradient is lm_linear_wgrad8's.
+ * The weight gradient is lm_linear_wgrad8's.  The result is not written over
+ * codes or scales of either operand.
  * workspace: lm_linear8_workspace(x, w, grad) bytes of device memory, 256-byte
  * aligned, free again when the work is done.
  * Should a device-side wait give up (LM_WAIT_LIMIT_NS), what was not computed

@@ -296,6 +296,8 @@ lm_status weight8_call(const lm_matrix* w, const lm_weight8* c, bool pack, void*
   LM_TRY(check_matrix(*w, w->rows, w->cols, "w"));
   LM_TRY(check_weight8(*c, w->rows, w->cols, "c"));
   if (w->rows == 0 || w->cols == 0) return LM_OK;
+  // (a block is written while others are still read)
+  if (w->data == c->codes || w->data == c->scales) return fail(LM_ERR_INVALID_ARG, "%s written over its input", pack ? "c" : "w");
   int dev = 0;
   LM_TRY(current_device(&dev));
   LM_TRY(check_memory(w->data, dev, "w"));
@@ -321,6 +323,9 @@ lm_status linear8_call(const lm_checkpoint8* x, const lm_weight8* w, const lm_ma
     return fail(LM_ERR_UNSUPPORTED, "%s or w of 2^38 elements or more", xn);
   const size_t need = lm_linear8_workspace(x, w, grad);
   LM_TRY(check_workspace(workspace, workspace_bytes, need, 256));
+  // (a tile is stored while others' operands are still read)
+  if (k > 0 && (y->data == x->codes || y->data == x->scales || y->data == w->codes || y->data == w->scales))
+    return fail(LM_ERR_INVALID_ARG, "%s written over %s or w", yn, xn);
   int dev = 0;
   LM_TRY(current_device(&dev));
   if (k > 0) {

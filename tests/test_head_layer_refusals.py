@@ -285,3 +285,26 @@ def test_results_over_each_other_are_refused(L):
         assert rotary(True, at, (7, 8)) == INVALID
     for at in ((1, 2, 3, 4, 2, 6), (1, 4, 3, 4, 5, 6), (1, 2, 3, 4, 1, 6)):
         assert rotary(False, at) == INVALID
+
+
+def test_8_bit_results_over_inputs_are_refused(L):
+    """Tiles are stored while others' operands are still read, blocks packed while others are."""
+    lib = L.load_library()
+    over = lambda st: st == INVALID and b"written over" in lib.lm_last_error()  # noqa: E731
+    for grad in (False, True):
+        f = lib.lm_linear8_grad if grad else lib.lm_linear8
+        cols = 6 if grad else 8
+
+        def call(y, rows=4):
+            m = mat(L, rows=rows, cols=14 - cols, data=y * BASE)
+            return f(ref(code(L, rows=rows, cols=cols, codes=2 * BASE, scales=3 * BASE)), ref(weight(L, codes=4 * BASE, scales=5 * BASE)), ref(m), BASE, 1 << 40, None)
+
+        for at in (2, 3, 4, 5):
+            assert over(call(at))
+        assert not over(call(6)) and call(2, rows=0) == 0
+    # an empty sum reads neither operand
+    assert not over(lib.lm_linear8(ref(code(L, cols=0, codes=BASE, scales=BASE)), ref(weight(L, cols=0)), ref(mat(L, cols=6)), BASE, 1 << 40, None))
+    for fn in (lambda w, c: lib.lm_weight8_pack(ref(w), ref(c), None), lambda w, c: lib.lm_weight8_unpack(ref(c), ref(w), None)):
+        c = weight(L, codes=2 * BASE, scales=3 * BASE)
+        assert over(fn(mat(L, rows=6, data=2 * BASE), c)) and over(fn(mat(L, rows=6, data=3 * BASE), c))
+        assert not over(fn(mat(L, rows=6, data=4 * BASE), c))
