@@ -449,3 +449,62 @@ def test_masked_and_non_finite_logits_and_weights_known_later(T):
     bad = torch.zeros(rows, dtype=torch.bool, device="cuda")
     bad[3] = bad[8] = True
     assert torch.equal(dh.isnan().all(dim=1), bad) and torch.equal(dh[~bad], want[~bad])
+
+
+FEW = [(1, 50304, 768, 0, 0), (7, 5003, 1283, 5, 3), (32, 20000, 4096, 8, 8), (31, 513, 2049, 0, 0), (2, 1000, 8192, 0, 0), (17, 50257, 1280, 5, 0),
+       (1, 100000, 130, 0, 0)]
+
+
+@pytest.mark.parametrize("rows,vocab,width,pad,offset", FEW)
+def test_few_tokens_of_wide_models(T, rows, vocab, width, pad, offset):
+    """At most 32 tokens without gradients: sums are cut every 128 products (8 additions of
+    the tensor cores, 2^-20 of S) and width / 128 such sums are added in fp32, which is
+    below the E above up to a width of 8192: 2^-20 + width / 128 2^-24 <= 2^-18 + width /
+    512 2^-24.  The same bits from call to call, and from a captured one."""
+    h, w, y, _, _, _ = inputs(rows, vocab, width, rows + vocab + width, pad, offset)
+    ref = reference(h.t, w.t, y)
+    o = T.linear_logprob(h.t, w.t, y)
+    for k in ("lse", "entropy", "logp"):
+        near(getattr(o, k), ref, k)
+    assert h.untouched() and w.untouched()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c = T.linear_logprob(h.t, w.t, y)
+    for _ in range(2):
+        graph.replay()
+        again = T.linear_logprob(h.t, w.t, y)
+        for k in ("lse", "entropy", "logp"):
+            assert torch.equal(getattr(c, k), getattr(o, k)) and torch.equal(getattr(again, k), getattr(o, k)), k
+    # the gradients' call cuts its sums elsewhere
+    if rows * vocab <= 1 << 20:
+        o2 = T.linear_logprob(h.t, w.t, y, g_lse=torch.ones(rows, device="cuda") / rows, dweight=False)
+        for k in ("lse", "entropy", "logp"):
+            near(getattr(o2, k), ref, k)
+
+
+def test_few_tokens_waits_that_run_out_leave_nan(T, monkeypatch):
+    h, w, y, _, _, _ = inputs(5, 60000, 2048, 11)
+    right = T.linear_logprob(h.t, w.t, y)
+    torch.cuda.synchronize()
+    monkeypatch.setenv("LM_WAIT_LIMIT_NS", "1")
+    o = T.linear_logprob(h.t, w.t, y)
+    torch.cuda.synchronize()
+    for k in ("lse", "entropy"):
+        got, want = getattr(o, k), getattr(right, k)
+        assert bool((got.isnan() | (got == want)).all()), k
+    monkeypatch.delenv("LM_WAIT_LIMIT_NS")
+    assert torch.equal(T.linear_logprob(h.t, w.t, y).lse, right.lse)
+
+
+@pytest.mark.parametrize("rows,vocab,width", [(16384, 50304, 768), (4096, 50257, 1024)])
+def test_large_steps_repeat_their_bits(T, rows, vocab, width):
+    """Several pieces, teams and split sums: every output of a whole step is the same, call after call."""
+    h, w, y, gl, gh, gz = inputs(rows, vocab, width, 12)
+    first = T.linear_logprob(h.t, w.t, y, gl, gh, gz)
+    for _ in range(8):
+        o = T.linear_logprob(h.t, w.t, y, gl, gh, gz)
+        assert all(torch.equal(a, b) for a, b in zip(o, first))
+    later = T.linear_logprob_grad(h.t, w.t, y, first.lse, first.entropy, gl, gh, gz)
+    for _ in range(4):
+        o = T.linear_logprob_grad(h.t, w.t, y, first.lse, first.entropy, gl, gh, gz)
+        assert all(torch.equal(a, b) for a, b in zip(o, later))
