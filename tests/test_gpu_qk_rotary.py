@@ -290,3 +290,57 @@ def test_gradient_over_an_input(T, tokens, hq, hk, dim, turned, interleaved, nor
         to = (d.q, d.k) if over == "x" else (d.dq, d.dk)
         got = T.qk_rotary_grad(d.dq, d.dk, d.pos, d.table, d.q, d.k, d.qw, d.kw, **d.args(), dq_out=to[0], dk_out=to[1])
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def longest_chain(tokens, hq, hk, dim, fp32):
+    """Of the roundings that one term of each dweight goes through: eight channels a lane,
+    in one wave of 304 blocks (fp32: 152), which the two parts share by their steps of four
+    heads; a group of lanes adds up its items' heads, a block its groups, the join
+    the blocks in eight chains."""
+    lanes = 1
+    while 8 * lanes < dim:
+        lanes *= 2
+    groups, most = 256 // lanes, 152 if fp32 else 304
+    size = min(max(1, tokens * (hq + hk) // (152 * 32 * (32 // lanes))), 16)
+    parts = []
+    for n in (hq, hk):
+        a = -(-n // -(-n // size)) if n else 0
+        a = -(-a // 4) * 4 if a > 4 else a
+        parts.append((a, -(-n // a) if n else 0))
+    steps = [items * -(-a // 4) for a, items in parts]
+    out = []
+    for (a, items), mine in zip(parts, steps):
+        if not items:
+            continue
+        blocks = min(-(-tokens * items // groups), max(1, most * mine // sum(steps)))
+        out.append(a * -(-tokens * items // (blocks * groups)) + groups + -(-blocks // 8) + 8)
+    return out
+
+
+MANY = [(8193, 20, 5, 80, 32, True, "packed"), (8193, 20, 5, 256, 256, False, "packed"), (9001, 9, 9, 128, 64, False, "packed"),
+        (4097, 33, 3, 64, 64, True, "apart"), (20011, 13, 0, 48, 48, False, "packed"), (8193, 17, 7, 50, 50, False, "packed"), (8193, 11, 6, 80, 80, False, "odd")]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("tokens,hq,hk,dim,turned,interleaved,lay", MANY)
+def test_many_heads_an_item(T, tokens, hq, hk, dim, turned, interleaved, lay, dtype):
+    """Items of 8 to 16 heads, several steps each, and numbers of heads that they do not
+    divide; heads of other sizes and alignments one after another.  Both gains' gradients
+    of up to 260000 heads."""
+    c = Case(tokens, hq, hk, dim, turned, interleaved, True, dtype, lay)
+    cs = c.cs()
+    k, dk, kw = (c.k, c.dk, c.kw) if hk else (None, None, None)
+    o = T.qk_rotary(c.q, k, c.pos, c.table, c.qw, kw, **c.args())
+    r = T.qk_rotary_grad(c.dq, dk, c.pos, c.table, c.q, k, c.qw, kw, **c.args())
+    eight = dim % 8 == 0 and lay != "odd"
+    # a warp's own terms, 8 warps, and 304 blocks in eight chains, or as above
+    chains = longest_chain(tokens, hq, hk, dim, dtype == torch.float32) if eight else \
+        [-(-tokens * n // (8 * 304)) + 8 + 38 + 8 for n in (hq, hk)]
+    for (x, d, w), got, dx, dw, chain in zip(c.pairs()[:2 if hk else 1], (o.q, o.k), (r.dq, r.dk), (r.dq_weight, r.dk_weight), chains):
+        near(got, *forward(x, w, cs, c.n, interleaved, True), dtype)
+        want, m, dwant, dm = gradient(d, x, w, cs, c.n, interleaved, True)
+        near(dx, want, m, dtype)
+        near(dw, dwant, dm, dtype, E + chain * 2.0 ** -24)
+        del want, m
+    r2 = T.qk_rotary_grad(c.dq, dk, c.pos, c.table, c.q, k, c.qw, kw, **c.args())
+    assert all(torch.equal(a, b) for a, b in zip(r, r2) if a is not None)
