@@ -579,7 +579,8 @@ lm_status lm_linear_wgrad8(const lm_matrix* dy, const lm_checkpoint8* x, const l
  *   dh = dz weight,   dweight (+)= dz^T h
  * z is summed in fp32; for the gradients of one call with the forward results it
  * is kept in 16 bits, in steps of 2^-10 below the row's maximum (p is off by
- * 2^-11 of itself at most, and 0 where the logit is 64 below).  dz, times one
+ * 2^-11 of itself at most, and 0 where the logit is 64 below).  A later call has
+ * only lse as it was rounded: its p is off by 2^-24 |lse| of itself.  dz, times one
  * factor for a piece of the tokens, is rounded to bf16, as the tensor cores take
  * it, and both products are summed in fp32.  The tensor cores add at most 512
  * products (each addition of 16 may drop 2^-23 of what it has); their sums are

@@ -17,7 +17,7 @@
 // its distance below the row's running maximum r in steps of 2^-10,
 //   q = rint((r - z) 2^10),  65535 and more (64 below): p = 0
 // (p is then off by 2^-11 of itself at most, a quarter of the bf16 rounding that
-// follows).  Once lse is known, a kernel makes of q, in its place,
+// follows).  Once M and S are known, a kernel makes of q, in its place,
 //   d = p (a - g_H (log p + H)) (+ g_logp at the target),  a = g_lse - g_logp
 // as bf16 (the rounding that the tensor cores ask for; times a scale, see put_scale),
 // and two products of it follow, dh = d W and dW = d^T h.  Where lse comes from an earlier call the
@@ -83,9 +83,13 @@ __device__ __forceinline__ void store_boxes(const P& p, const Place& at) {
   bulk_commit();
 }
 
-// What a row's gradient takes: lse, a = g_lse - g_logp, g_H, H.
+// What a row's gradient takes: lse, a = g_lse - g_logp, g_H, H.  In the call that computes
+// them, M in the place of lse, and log S beside it: log p = (z - M) - log S then lacks
+// lse's rounding at its own size, which is all that is left of the dz of a target with p
+// near 1 (1 - p = 2e-5 with lse = 52: such a token's dh 6% off, 0.6% so).
 struct RowTerms {
   float4* terms;
+  float* log_s;       // NULL: terms hold lse
   float* g_logp;      // 0 in a row without a target
   int32_t* target;    // -1 in a row without one
   float* scale;       // d = scale[0] dz is rounded, and scale[1] = 1 / scale[0] times the products
@@ -277,18 +281,20 @@ struct GradEpi {
   };
 };
 
-__device__ __forceinline__ void put_terms(const RowTerms& o, int64_t row, float lse, float h, int64_t y, int64_t vocab, const float* g_logp,
-                                          const float* g_entropy, const float* g_lse) {
+// from: what log p counts from, lse, or M with log_s.
+__device__ __forceinline__ void put_terms(const RowTerms& o, int64_t row, float from, float log_s, bool empty, float h, int64_t y, int64_t vocab,
+                                          const float* g_logp, const float* g_entropy, const float* g_lse) {
   const bool has = y >= 0 && g_logp != nullptr;
   float gl = has ? g_logp[row] : 0.f;
   float a = (g_lse != nullptr ? g_lse[row] : 0.f) - gl;
   const float gh = g_entropy != nullptr ? g_entropy[row] : 0.f;
   if (has && y >= vocab) a = __int_as_float(0x7FC00000);
-  if (lse == -INFINITY) {       // every logit -inf: no gradient
-    lse = INFINITY;
+  if (empty) {       // every logit -inf: no gradient
+    from = log_s = INFINITY;
     gl = 0.f;
   }
-  o.terms[row] = make_float4(lse, a, gh, h);
+  o.terms[row] = make_float4(from, a, gh, h);
+  if (o.log_s != nullptr) o.log_s[row] = log_s;
   o.g_logp[row] = gl;
   o.target[row] = has && y < vocab ? (int32_t)y : -1;
 }
@@ -344,13 +350,14 @@ __global__ void __launch_bounds__(32 * kJoinParts) linlogp_join_kernel(const Joi
     t += st[i][lane];
   }
   const int64_t y = p.targets != nullptr ? p.targets[row] : -1;
-  float lse, h, logp;
-  if (m == -INFINITY && s == 0.f) {
+  float lse, h, logp, log_s = 0.f;
+  const bool empty = m == -INFINITY && s == 0.f;
+  if (empty) {
     lse = -INFINITY;
     h = 0.f;
     logp = y < 0 ? 0.f : -INFINITY;
   } else {
-    const float log_s = logf(s);      // NaN where the row holds NaN or infinity
+    log_s = logf(s);      // NaN where the row holds NaN or infinity
     lse = m + log_s;
     h = log_s - t / s;
     logp = y >= 0 && y < p.vocab ? (p.z_target[row] - m) - log_s : 0.f;
@@ -361,7 +368,7 @@ __global__ void __launch_bounds__(32 * kJoinParts) linlogp_join_kernel(const Joi
   if (p.entropy != nullptr) p.entropy[row] = h;
   if (p.lse != nullptr) p.lse[row] = lse;
   if (p.out.terms == nullptr) return;
-  put_terms(p.out, row, lse, h, y, p.vocab, p.g_logp, p.g_entropy, p.g_lse);
+  put_terms(p.out, row, from, log_s, empty, h, y, p.vocab, p.g_logp, p.g_entropy, p.g_lse);
   if (row < 32) put_scale(p.out.scale, lanes, p.g_logp != nullptr ? p.g_logp[row] : 0.f);
 }
 
@@ -372,7 +379,7 @@ __global__ void __launch_bounds__(256) linlogp_terms_kernel(const JoinParams p) 
   const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const unsigned lanes = __ballot_sync(0xFFFFFFFFu, row < p.rows);
   if (row >= p.rows) return;
-  put_terms(p.out, row, p.lse[row], p.entropy != nullptr && p.g_entropy != nullptr ? p.entropy[row] : 0.f,
+  put_terms(p.out, row, p.lse[row], 0.f, p.lse[row] == -INFINITY, p.entropy != nullptr && p.g_entropy != nullptr ? p.entropy[row] : 0.f,
             p.targets != nullptr ? p.targets[row] : -1, p.vocab, p.g_logp, p.g_entropy, p.g_lse);
   if (row < 32) put_scale(p.out.scale, lanes, p.g_logp != nullptr ? p.g_logp[row] : 0.f);
 }
@@ -387,7 +394,7 @@ __global__ void __launch_bounds__(256) linlogp_dz_kernel(uint4* q, const float* 
   if (row >= rows) return;
   const int part = threadIdx.x & 7;
   float4 w = t.terms[row];
-  const float scale = t.scale[0];
+  const float scale = t.scale[0], log_s = t.log_s[row];
   w.y *= scale;
   w.z *= scale;
   const int y = t.target[row];
@@ -396,7 +403,7 @@ __global__ void __launch_bounds__(256) linlogp_dz_kernel(uint4* q, const float* 
     for (int b = b0; b < min(b0 + kDzBlocks, blocks); ++b) {
       uint4* at = q + ((int64_t)b * rows + row) * 8 + part;
       const uint4 v = __ldcs(at);
-      const float ref = from[(int64_t)(b >> 1) * rows + row] - w.x;
+      const float ref = (from[(int64_t)(b >> 1) * rows + row] - w.x) - log_s;
       const uint32_t u[4] = {v.x, v.y, v.z, v.w};
       float2 d[4];
 #pragma unroll
@@ -498,7 +505,7 @@ struct Layout {
   int32_t strip;                     // of the forward product
   int32_t parts;                     // of a row's statistics
   // offsets in the workspace
-  size_t h, w, z, terms, gl, target, scale, stats, from, d, dw, partial, total;
+  size_t h, w, z, terms, log_s, gl, target, scale, stats, from, d, dw, partial, total;
 };
 bool dw_is_sum(const LinLogpParams& q) { return q.dwdt == LM_F32; }   // several pieces are summed in dW itself
 Layout make_layout(const LinLogpParams& q) {
@@ -530,6 +537,7 @@ Layout make_layout(const LinLogpParams& q) {
   l.stats = take(q.gradient_only ? 0 : n * l.parts * 12);
   if (grad) {
     l.terms = take(n * 16);
+    l.log_s = take(q.gradient_only ? 0 : n * 4);
     l.gl = take(n * 4);
     l.target = take(n * 4);
     l.scale = take(8);
@@ -573,7 +581,9 @@ cudaError_t piece(const LinLogpParams& q, const Layout& l, const Mat& h, const M
   j.g_logp = from_row(q.g_logp, first);
   j.g_entropy = from_row(q.g_entropy, first);
   j.g_lse = from_row(q.g_lse, first);
-  if (grad) j.out = RowTerms{reinterpret_cast<float4*>(ws + l.terms), reinterpret_cast<float*>(ws + l.gl), reinterpret_cast<int32_t*>(ws + l.target), reinterpret_cast<float*>(ws + l.scale)};
+  if (grad)
+    j.out = RowTerms{reinterpret_cast<float4*>(ws + l.terms), q.gradient_only ? nullptr : reinterpret_cast<float*>(ws + l.log_s),
+                     reinterpret_cast<float*>(ws + l.gl), reinterpret_cast<int32_t*>(ws + l.target), reinterpret_cast<float*>(ws + l.scale)};
   const bool few = !grad && rows <= kFewRows;
   // the operands of the logits' product, and the blocks that its epilogue fills
   auto logits = [&](auto& p) {

@@ -508,3 +508,39 @@ def test_large_steps_repeat_their_bits(T, rows, vocab, width):
     for _ in range(4):
         o = T.linear_logprob_grad(h.t, w.t, y, first.lse, first.entropy, gl, gh, gz)
         assert all(torch.equal(a, b) for a, b in zip(o, later))
+
+
+@pytest.mark.parametrize("shift", [-4096.0, -512.0, 0.0, 512.0, 4096.0])
+@pytest.mark.parametrize("rows,vocab", [(64, 900), (40, 20000)])
+def test_gradients_of_tokens_that_are_almost_certain(T, rows, vocab, shift):
+    """1 - p of 1e-6 to 1e-2, all logits far from 0: in the one call lse's rounding at its own
+    size (2^-24 |lse|, 2^-12 here) does not reach dz.  1 - p is the others' sum, off by 2 E +
+    2^-18 of itself, and by what numbers near 1 lose: the sum's additions (32 of a
+    chain in a tile, fewer than 96 after it), 2^-24 each, the logarithm and the
+    exponential, 2^-22 each.  The others' p are off by 2 E + 2^-11 + 2^-18 of
+    themselves; then dz is rounded, and the products' sums, as above."""
+    width = 64
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    w = torch.randn(vocab, width, device="cuda", generator=g)
+    h = torch.randn(rows, width, device="cuda", generator=g) / 8
+    y = torch.randint(0, vocab, (rows,), device="cuda", generator=g)
+    h += torch.linspace(12, 24, rows, device="cuda")[:, None] * w[y] / w[y].square().sum(dim=1, keepdim=True)
+    h[:, 0] = 128.0
+    w[:, 0] = shift / 128.0
+    h, w = h.bfloat16(), w.bfloat16()
+    gl = torch.full((rows,), -1.0 / rows, device="cuda")
+    o = T.linear_logprob(h, w, y, gl, dweight=False)
+    x, m = h.double(), w.double()
+    z = x @ m.t()
+    e = (x.abs() @ m.abs().t()).amax(dim=1, keepdim=True) * (2.0 ** -18 + 2.0 ** -27)
+    p = torch.softmax(z, dim=1)
+    at = y[:, None]
+    others = p.scatter(1, at, 0.0)
+    rest = others.sum(dim=1, keepdim=True)                     # 1 - p of the target
+    assert float(rest.min()) < 1e-4
+    d = others.scatter(1, at, -rest) / rows
+    db = ((2 * e + 2.0 ** -11 + 2.0 ** -18) * others).scatter(1, at, (2 * e + 2.0 ** -18) * rest + 128 * 2.0 ** -24 + 2.0 ** -21) / rows
+    db = db + (U + 2.0 ** -18) * (d.abs() + db)
+    want = d @ m
+    off, bound = (o.dh.double() - want).abs(), db @ m.abs() + U * want.abs() + 1e-38
+    assert bool((off <= bound).all()), float((off / bound).max())
