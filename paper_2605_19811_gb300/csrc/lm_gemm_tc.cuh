@@ -951,6 +951,11 @@ cudaError_t start_join(const Schedule& s, int32_t m, int32_t n, const float* par
   const JoinParts j{s, m, n, parts, out};
   return launch_after(join_kernel<kN>, dim3(s.rest, kTileM / 4, s.team), kN, 0, st, j);
 }
+// Whether the TMA may store a result's tiles: it stores rows in whole 16 bytes, past
+// the last column of a row that ends between them, over what a wider buffer has there.
+inline bool tma_stores(const void* data, int64_t rows, int64_t cols, int64_t ld, int64_t size) {
+  return reinterpret_cast<uintptr_t>(data) % 16 == 0 && ld * size % 16 == 0 && cols * size % 16 == 0 && ld < ((int64_t)1 << 37) / rows;
+}
 // A product whose sums may be split: the kernel, and the join where parts are left.
 template <int kALie, int kBLie>
 cudaError_t start_store(Params<StoreEpi>& p, cudaStream_t st) {
@@ -959,7 +964,7 @@ cudaError_t start_store(Params<StoreEpi>& p, cudaStream_t st) {
   const int64_t size = o.dt == LM_F32 ? 4 : 2;
   cudaError_t e = cudaSuccess;
   const int64_t ld = p.m > 1 ? o.d.ld : (int64_t)p.n;
-  if ((!o.accumulate || o.dt == LM_F32) && reinterpret_cast<uintptr_t>(o.d.data) % 16 == 0 && ld * size % 16 == 0 && ld < ((int64_t)1 << 37) / p.m) {
+  if ((!o.accumulate || o.dt == LM_F32) && tma_stores(o.d.data, p.m, p.n, ld, size)) {
     e = encode_boxes(&p.out, o.dt, o.d.data, p.n, p.m, 1, ld, ld * p.m, 32);
     p.epi.out.tma = 1;
   }

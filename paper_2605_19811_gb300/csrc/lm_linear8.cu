@@ -806,7 +806,7 @@ cudaError_t launch_linear8(const Linear8Params& q, cudaStream_t st) {
   p.parts = reinterpret_cast<float*>(ws + l.parts);
   p.out = make_store(q.y, q.ydt, q.tokens, false);
   const int64_t ld = q.tokens > 1 ? q.y.ld : l.n, size = q.ydt == LM_F32 ? 4 : 2;
-  if (reinterpret_cast<uintptr_t>(q.y.data) % 16 == 0 && ld * size % 16 == 0 && ld < ((int64_t)1 << 37) / q.tokens) {
+  if (tma_stores(q.y.data, q.tokens, l.n, ld, size)) {
     e = q.ydt == LM_F32 ? encode(&p.y, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, q.y.data, l.n, q.tokens, 1, ld, ld * q.tokens, 16, 32, CU_TENSOR_MAP_SWIZZLE_64B)
                         : encode(&p.y, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, q.y.data, l.n, q.tokens, 1, ld, ld * q.tokens, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
     if (e != cudaSuccess) return e;

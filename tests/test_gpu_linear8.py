@@ -295,3 +295,19 @@ def test_scales_that_are_no_powers_of_two(T, rows, cols, out, grad):
     want = f(T.Checkpoint8(codes, s, k, "e4m3"), w, dtype=torch.float32)
     s[1, rows // 2] = 0.0
     assert torch.equal(f(T.Checkpoint8(codes, s, k, "e4m3"), w, dtype=torch.float32), want)
+
+
+@pytest.mark.parametrize("to", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("rows,k,n", [(1, 300, 517), (2, 300, 29), (40, 130, 4), (300, 1024, 260), (257, 640, 5), (128, 128, 127), (3000, 4096, 5001), (5000, 128, 1254)])
+def test_results_beside_other_columns(T, rows, k, n, grad, to):
+    """Rows that end between 16-byte boundaries, of a pitch that is a multiple of 16 bytes:
+    what lies behind them stays as it was."""
+    x, w = layer(T, rows, n if grad else k, k if grad else n, grad, rows + n)
+    want, most = product(x, w, grad)
+    for more in (0, 64):
+        y = Held(rows, n, to, pad=-n % 8 + more)
+        (T.linear8_grad if grad else T.linear8)(x, w, out=y.t)
+        assert y.untouched()
+        bound = most * (2.0 ** -17 + k / 512 * 2.0 ** -24) + HALF[to] * want.abs()
+        assert bool(((y.t.double() - want).abs() <= bound).all())

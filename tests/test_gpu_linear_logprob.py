@@ -544,3 +544,36 @@ def test_gradients_of_tokens_that_are_almost_certain(T, rows, vocab, shift):
     want = d @ m
     off, bound = (o.dh.double() - want).abs(), db @ m.abs() + U * want.abs() + 1e-38
     assert bool((off <= bound).all()), float((off / bound).max())
+
+
+@pytest.mark.parametrize("to", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,vocab,width", [(1, 575, 5), (5, 1, 29), (2, 129, 29), (129, 2003, 437), (40, 3000, 4), (300, 700, 255), (1344, 183, 1181), (2043, 134, 5), (600, 3000, 260)])
+def test_gradients_beside_other_columns(T, rows, vocab, width, to):
+    """Rows that end between 16-byte boundaries, of a pitch that is a multiple of 16 bytes:
+    what lies behind them stays as it was, written or added to."""
+    h, w, y, gl, gh, gz = inputs(rows, vocab, width, rows + vocab + width)
+    ref = reference(h.t, w.t, y, gl, gh, gz)
+    dh, dw = Held(rows, width, torch.bfloat16, -width % 8), Held(vocab, width, to, -width % 8 + 8)
+    o = T.linear_logprob(h.t, w.t, y, gl, gh, gz, dh=dh.t, dweight=dw.t)
+    assert dh.untouched() and dw.untouched()
+    near(dh.t, ref, "dh")
+    near(dw.t, ref, "dweight", U)
+    first = dw.t.clone()
+    T.linear_logprob_grad(h.t, w.t, y, o.lse, o.entropy, gl, gh, gz, dh=dh.t, dweight=dw.t, accumulate=True)
+    assert dh.untouched() and dw.untouched()
+    near(dh.t, ref, "dh")
+    ref["dweight"] = ref["dweight"] + first.double()
+    near(dw.t, ref, "dweight", U)
+
+
+def test_several_pieces_beside_other_columns(T):
+    """The same where dW's sums go on from piece to piece."""
+    rows, vocab, width = 2500, 270001, 21
+    h, w, y, gl, gh, gz = inputs(rows, vocab, width, 5)
+    ref = reference(h.t, w.t, y, gl, gh, gz)
+    for to in (torch.bfloat16, torch.float32):
+        dh, dw = Held(rows, width, torch.bfloat16, 3), Held(vocab, width, to, 3)
+        T.linear_logprob(h.t, w.t, y, gl, gh, gz, dh=dh.t, dweight=dw.t)
+        assert dh.untouched() and dw.untouched()
+        near(dh.t, ref, "dh")
+        near(dw.t, ref, "dweight", U)
