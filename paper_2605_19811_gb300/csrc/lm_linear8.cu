@@ -156,7 +156,7 @@ constexpr int kChunk8 = 8;                              // most stages summed in
 constexpr int kScaleBytes = 512 + 1024;                 // of two stages: the CTA's rows', the tile's columns'
 constexpr int kScaleRing = 4;                           // kMake: how many are under way
 // The kernel makes the scales itself where a pair takes at most so many stages.  One
-// launch less: one token by 14336 x 4096 20.4 us a call instead of 22 to 31 (the kernel
+// launch less: one token by 14336 x 4096 20.4 us a call instead of 25 (the kernel
 // 19.5 instead of 17.1 and 1.8); 1021 x 517 by 1283 the kernel 17.1 us instead of 15.3
 // and 1.7, calls one after another 4 us less.  But these warps' loads cost 6% of the
 // rate: 16384 x 5120 by 1280 83 us instead of 76 and 3.7.

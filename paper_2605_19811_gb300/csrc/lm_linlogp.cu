@@ -10,7 +10,7 @@
 // The tensor cores sum 256 products of a logit at a time (128 for few rows), half as
 // many as elsewhere: the epilogue has the time, and log p is then as exact as plain
 // fp32's (rows of 4096: 9e-8 off, 1.8e-7 with 512; one token of 768, whose target's
-// products have one sign: 1e-7 and 2e-6).
+// products have one sign: 7e-8 in the median of 40, 6e-7 at most, and 2e-6).
 //
 // Gradients, for a piece of the tokens at a time.  In the forward call the
 // product's epilogue also leaves every logit in the workspace in 16 bits, as
